@@ -406,6 +406,141 @@ crvq_status crvq_dequant_gemv(int64_t M, int64_t N, int64_t n_crit, const uint8_
                               const int32_t* ext_dtypes, const int64_t* K_ext, const int32_t* perm, const void* x,
                               int x_dtype, float* y, void* workspace, size_t ws_bytes, void* stream);
 
+/* ===========================================================================
+ * The attention block of a decoder on quantized data: projections in 4 bits
+ * (crvq_w4_*) and a paged cache of keys and values in 8 bits (crvq_kv_*).
+ *
+ * The cache.  Pages of `page` tokens (16, 32, 64, 128 or 256) of Hkv heads of
+ * D elements (a multiple of 16 up to 256), n_pages of them:
+ *   k_cache  int8 [n_pages][Hkv][page][D]      key of slot s:   k_scale * k_cache[.][h][s][:]
+ *   v_cache  int8 [n_pages][Hkv][D][page]      value of slot s: v_scale * v_cache[.][h][:][s]
+ *   k_scale, v_scale  float [n_pages][Hkv]     one scale for a head's tokens in a page
+ * (values are stored transposed, so that both products of attention read
+ * their operand along the contracted index).  Both arrays 16-byte aligned.
+ * Token t of sequence b is in slot t % page of page block_table[b * ld_table +
+ * t / page].  A page may belong to several sequences as long as no call
+ * appends to it.
+ *
+ * A batch of B sequences with new tokens: rows start[b] .. start[b+1] - 1 of
+ * the n_tokens rows of q, k, v are sequence b's new tokens (start: int32[B+1],
+ * device), and kv_len[b] (int32, device) is its number of tokens in the cache
+ * with the new ones included: they are the last ones, token i of n being at
+ * place kv_len[b] - n + i.  max_new and max_kv (host) are upper bounds of the
+ * rows and of kv_len over the batch.  q is n_tokens x Hq x D, k and v n_tokens x
+ * Hkv x D with strides (in elements) between tokens and between heads, the D
+ * elements of a head contiguous; Hq is a multiple of Hkv, and query heads
+ * h * Hq/Hkv .. share key head h.  Element type CRVQ_F32 or CRVQ_BF16.
+ * ------------------------------------------------------------------------- */
+#define CRVQ_KV_MAX_D 256
+
+/* crvq_kv_append -- rotates, quantizes and stores the new keys and values, and
+ * rotates the queries, in one launch.
+ *
+ * Rotation (cos != NULL; rot even, 0 < rot <= D): pair j < rot/2 is elements
+ * (j, j + rot/2), or (2j, 2j+1) when interleaved, and becomes (a c - b s,
+ * b c + a s) with c = cos[p*rot/2 + j], s = sin[..] (float, n_angles rows) of
+ * row p = the token's place in its sequence, or positions[row] (int32, device)
+ * when given; fp32, every operation rounded on its own.  The other elements
+ * stay.  A place outside the table makes the rotated elements NaN.  q (may be
+ * NULL) goes to q_out the same way, rounded to dtype; q_out may be q itself.
+ * Quantization of a head's tokens in a page, for k and v alike: with m the
+ * largest magnitude among its new tokens, s = max(m / 127, 2^-100).  If the
+ * page holds tokens from before the call, the larger of s and its old scale
+ * becomes the scale, and if that is s the old codes c become
+ * rint(c * (old / s)) (a growth costs an old code up to half a step); otherwise
+ * the scale is s.  A new element x becomes min(max(rint(x / scale), -127), 127).
+ * A NaN or infinity among the new tokens makes the scale NaN (and the page's
+ * head NaN for every reader) with new codes 0.
+ * A sequence whose rows are not within [0, n_tokens], that has more than
+ * max_new of them or more than kv_len[b], or whose kv_len[b] exceeds ld_table *
+ * page, is left out; so are tokens whose page is outside [0, n_pages).
+ * Results depend on how tokens are grouped into calls only through the scales'
+ * growth. */
+crvq_status crvq_kv_append(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages, int8_t* k_cache,
+                           int8_t* v_cache, float* k_scale, float* v_scale, const int32_t* block_table,
+                           int64_t ld_table, const int32_t* start, const int32_t* kv_len, int32_t max_new,
+                           int64_t n_tokens, int dtype, const void* k, int64_t k_tok, int64_t k_head, const void* v,
+                           int64_t v_tok, int64_t v_head, const void* q, int64_t q_tok, int64_t q_head, void* q_out,
+                           int64_t qo_tok, int64_t qo_head, const float* cos, const float* sin, int64_t n_angles,
+                           int32_t rot, const int32_t* positions, int interleaved, void* stream);
+
+/* crvq_kv_read -- the values the cache holds for the last start[b+1] - start[b]
+ * tokens of every sequence (all of them when that is kv_len[b]): k_out and
+ * v_out (either may be NULL), n_tokens x Hkv x D of dtype, each element
+ * scale * code rounded once.  Sequences that crvq_kv_append would leave out
+ * leave their rows unwritten; tokens whose page is outside [0, n_pages) read
+ * NaN. */
+crvq_status crvq_kv_read(int32_t B, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages, const int8_t* k_cache,
+                         const int8_t* v_cache, const float* k_scale, const float* v_scale, const int32_t* block_table,
+                         int64_t ld_table, const int32_t* start, const int32_t* kv_len, int32_t max_new,
+                         int64_t n_tokens, int dtype, void* k_out, int64_t k_tok, int64_t k_head, void* v_out,
+                         int64_t v_tok, int64_t v_head, void* stream);
+
+/* crvq_kv_attention -- attention of the new tokens over the cache:
+ *
+ *   out_i = sum_t p_t V_t,  p = softmax over the visible t < kv_len[b] of scale * q_i . K_t
+ *
+ * with token i of n at place P_i = kv_len[b] - n + i.  causal != 0: t <= P_i is
+ * visible, and with window > 0 only t > P_i - window; causal == 0: every t (window must
+ * be 0).  n may exceed kv_len[b] (places then start below 0).  A row that sees nothing is
+ * 0.  lse (float [n_tokens][Hq] or NULL) = log sum_t exp(scale q_i . K_t), -inf
+ * for a row that sees nothing.  out: n_tokens x Hq x D of q's type, its own
+ * strides; it may be q itself (same strides), and may not overlap it otherwise.
+ * Arithmetic: a query row is held as fixed-point digits (16 bits below its
+ * largest element for CRVQ_BF16, 24 for CRVQ_F32) whose products with the key
+ * codes are exact; softmax statistics and sums are fp32; weights enter the
+ * product with the values rounded to fp16 (CRVQ_BF16) or to a pair of fp16 (CRVQ_F32).
+ * A row with a NaN or infinite query element is NaN, as is a row that sees a
+ * page outside [0, n_pages) or a page whose scale is not finite.  Rows of a sequence
+ * with kv_len[b] < 0 or > ld_table * page are NaN, as are the first max_new rows of one
+ * with more than max_new; a sequence whose rows are not within [0, n_tokens] is
+ * left out.  Deterministic.
+ * workspace: crvq_kv_attention_workspace_size(...) bytes. */
+size_t crvq_kv_attention_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new, int32_t max_kv);
+crvq_status crvq_kv_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages,
+                              const int8_t* k_cache, const int8_t* v_cache, const float* k_scale, const float* v_scale,
+                              const int32_t* block_table, int64_t ld_table, const int32_t* start, const int32_t* kv_len,
+                              int32_t max_new, int32_t max_kv, int64_t n_tokens, int dtype, const void* q, int64_t q_tok,
+                              int64_t q_head, void* out, int64_t o_tok, int64_t o_head, float scale, int causal,
+                              int32_t window, float* lse, void* workspace, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * 4-bit matrices.  An M x N matrix as codes c in 0 .. 15 with a scale s and a
+ * zero point z for every `group` (32, 64, 128 or 256) consecutive columns of a row:
+ *   W[r][j] = s[r][j/group] * (c[r][j] - z[r][j/group]),   z = 8 when zeros is NULL.
+ * codes: uint8, column 2i in the low and 2i+1 in the high half of byte i of
+ * its row; 16-byte aligned, row stride ld bytes, a multiple of 16 with 2 ld >= N.
+ * scales: CRVQ_F32 or CRVQ_BF16, row stride ld_s >= ceil(N / group).  zeros:
+ * uint8, row stride ld_z, or NULL.  The last group of a row may be shorter.
+ * ------------------------------------------------------------------------- */
+
+/* crvq_w4_quantize -- the codes, scales (and zero points) of W (M x N of dtype,
+ * row stride ldw) rounded to nearest, group by group.  zeros NULL: s = max|w| / 7,
+ * z = 8.  Otherwise lo = min(0, min w), hi = max(0, max w), s = (hi - lo) / 15,
+ * z = min(max(rint(-lo / s), 0), 15).  s is at least 2^-100 and is rounded to its stored type
+ * first; c = min(max(rint(w / s) + z, 0), 15).  A NaN or infinity in a group makes its
+ * scale NaN (codes 0, zero point 0 or 8).  The last bytes of a row up to a multiple of 16 bytes get zero
+ * codes past column N. */
+crvq_status crvq_w4_quantize(int64_t M, int64_t N, int32_t group, const void* W, int64_t ldw, int dtype, uint8_t* codes,
+                             int64_t ld, void* scales, int scale_dtype, int64_t ld_s, uint8_t* zeros, int64_t ld_z,
+                             void* stream);
+
+/* crvq_w4_dequant -- out (M x N of dtype, row stride ldo) = the values, rounded once. */
+crvq_status crvq_w4_dequant(int64_t M, int64_t N, int32_t group, const uint8_t* codes, int64_t ld, const void* scales,
+                            int scale_dtype, int64_t ld_s, const uint8_t* zeros, int64_t ld_z, void* out, int64_t ldo,
+                            int dtype, void* stream);
+
+/* crvq_w4_gemv -- y[t] = W x[t] for T >= 0 vectors: x is T x N of x_dtype (row
+ * stride ldx), y is T x M of y_dtype (row stride ldy).  Products are exact
+ * (bf16 x as it is, fp32 x as the sum of three bf16 terms), sums fp32 per group and across groups, rounded
+ * once.  An infinite or NaN element of x[t] makes y[t] NaN.  y may not overlap x.  Deterministic.
+ * workspace: crvq_w4_gemv_workspace_size(M, N, T) bytes. */
+size_t crvq_w4_gemv_workspace_size(int64_t M, int64_t N, int64_t T);
+crvq_status crvq_w4_gemv(int64_t M, int64_t N, int64_t T, int32_t group, const uint8_t* codes, int64_t ld,
+                         const void* scales, int scale_dtype, int64_t ld_s, const uint8_t* zeros, int64_t ld_z,
+                         const void* x, int64_t ldx, int x_dtype, void* y, int64_t ldy, int y_dtype, void* workspace,
+                         size_t ws_bytes, void* stream);
+
 /* ---------------------------------------------------------------------------
  * crvq_workspace_size -- one entry for every call's workspace size: the value
  * the per-call *_workspace_size function above returns for the same shape.
@@ -421,6 +556,9 @@ crvq_status crvq_dequant_gemv(int64_t M, int64_t N, int64_t n_crit, const uint8_
  *   CRVQ_OP_REFINE      M, N, n_cols                 (crvq_refine_codes)
  *   CRVQ_OP_GEMV        M, N, K = K_base             (crvq_dequant_gemv)
  *   CRVQ_OP_HINV        N                            (crvq_hessian_inverse_diagonal)
+ *   CRVQ_OP_KV_ATTENTION  n_vectors = B, d = D, M = Hq, N = Hkv, K = max_new,
+ *                       n_cols = max_kv              (crvq_kv_attention)
+ *   CRVQ_OP_W4_GEMV     M, N, K = T                  (crvq_w4_gemv)
  * Returns 0 for an unknown op or a shape the call rejects (and for calls that
  * need no workspace at that shape).  Ks is a host array of n_books entries.
  */
@@ -434,7 +572,9 @@ typedef enum {
   CRVQ_OP_CODE_SUMS = 6,
   CRVQ_OP_REFINE = 7,
   CRVQ_OP_GEMV = 8,
-  CRVQ_OP_HINV = 9
+  CRVQ_OP_HINV = 9,
+  CRVQ_OP_KV_ATTENTION = 10,
+  CRVQ_OP_W4_GEMV = 11
 } crvq_op;
 size_t crvq_workspace_size(int op, int64_t n_vectors, int64_t K, int32_t beam, int32_t n_books, int32_t d,
                            const int64_t* Ks, int64_t M, int64_t N, int64_t n_cols);

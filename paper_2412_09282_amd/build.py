@@ -34,6 +34,9 @@ SOURCES = {
     "k_gemm.hip": [],
     "k_refine.hip": [],
     "k_hinv.hip": [],
+    "k_kv.hip": [],
+    "k_attn.hip": [],
+    "k_w4.hip": [],
 }
 
 COMMON = [

@@ -89,6 +89,20 @@ def lib(build_if_missing: bool = True):
                 "crvq_dequant_gemv": ([I64, I64, I64, P, I64, P, ctypes.c_int, I64, I32, PP, I64, PP, P, P, P, P,
                                        ctypes.c_int, P, P, SZ, P], ctypes.c_int),
                 "crvq_pack_codes_u8": ([P, I64, P, P], ctypes.c_int),
+                "crvq_kv_append": ([I32] * 5 + [I64] + [P] * 5 + [I64, P, P, I32, I64, ctypes.c_int] + [P, I64, I64] * 4 +
+                                   [P, P, I64, I32, P, ctypes.c_int, P], ctypes.c_int),
+                "crvq_kv_read": ([I32] * 4 + [I64] + [P] * 5 + [I64, P, P, I32, I64, ctypes.c_int] + [P, I64, I64] * 2 +
+                                 [P], ctypes.c_int),
+                "crvq_kv_attention_workspace_size": ([I32] * 6, SZ),
+                "crvq_kv_attention": ([I32] * 5 + [I64] + [P] * 5 + [I64, P, P, I32, I32, I64, ctypes.c_int] +
+                                      [P, I64, I64] * 2 + [ctypes.c_float, ctypes.c_int, I32, P, P, SZ, P], ctypes.c_int),
+                "crvq_w4_quantize": ([I64, I64, I32, P, I64, ctypes.c_int, P, I64, P, ctypes.c_int, I64, P, I64, P],
+                                     ctypes.c_int),
+                "crvq_w4_dequant": ([I64, I64, I32, P, I64, P, ctypes.c_int, I64, P, I64, P, I64, ctypes.c_int, P],
+                                    ctypes.c_int),
+                "crvq_w4_gemv_workspace_size": ([I64, I64, I64], SZ),
+                "crvq_w4_gemv": ([I64, I64, I64, I32, P, I64, P, ctypes.c_int, I64, P, I64, P, I64, ctypes.c_int, P, I64,
+                                  ctypes.c_int, P, SZ, P], ctypes.c_int),
             }
             for name, (args, res) in sigs.items():
                 f = getattr(L, name)
@@ -339,7 +353,7 @@ def crvq_hessian_product(R: torch.Tensor, H: torch.Tensor, G: torch.Tensor, row_
 
 
 CRVQ_OP = {"importance": 0, "reorder": 1, "assign": 2, "beam": 3, "kmeans": 4, "dequant": 5, "code_sums": 6,
-           "refine": 7, "gemv": 8, "hinv": 9}
+           "refine": 7, "gemv": 8, "hinv": 9, "kv_attention": 10, "w4_gemv": 11}
 
 
 def crvq_workspace_size(op: str, n_vectors: int = 0, K: int = 0, beam: int = 0, Ks: Sequence[int] = (), d: int = 0,
@@ -411,3 +425,121 @@ def crvq_dequant_gemv(M: int, N: int, q_base: torch.Tensor, ldq_base: int, C_bas
         ctypes.cast(_ptr_array(C_ext), ctypes.POINTER(ctypes.c_void_p)) if ne else None,
         ctypes.cast(dts, ctypes.c_void_p) if ne else None, ctypes.cast(Ks, ctypes.c_void_p) if ne else None,
         _ptr(perm), _ptr(x), dtype_code(x), _ptr(y), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+
+
+# ---- the attention block on quantized data: 8-bit paged cache, 4-bit matrices ---------------------
+def _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len):
+    """The cache's and batch's arguments, with the shapes and types the C call cannot see checked."""
+    n_pages, Hkv, page, D = k_cache.shape
+    assert v_cache.shape == (n_pages, Hkv, D, page) and k_cache.dtype == v_cache.dtype == torch.int8
+    assert k_scale.shape == v_scale.shape == (n_pages, Hkv) and k_scale.dtype == v_scale.dtype == torch.float32
+    assert k_cache.is_contiguous() and v_cache.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()
+    B = kv_len.numel()
+    assert start.dtype == kv_len.dtype == block_table.dtype == torch.int32 and start.numel() == B + 1
+    assert start.is_contiguous() and kv_len.is_contiguous()
+    assert block_table.dim() == 2 and block_table.shape[0] == B and (B == 0 or block_table.is_contiguous())
+    return B, Hkv, D, page, (n_pages, k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                             block_table.data_ptr(), block_table.shape[1], start.data_ptr(), kv_len.data_ptr())
+
+
+def _row_args(t, n_tokens, heads, D, dtype):
+    assert t.shape == (n_tokens, heads, D) and t.dtype == dtype and (D == 1 or t.stride(2) == 1)
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def crvq_kv_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                   k_scale: torch.Tensor, v_scale: torch.Tensor, block_table: torch.Tensor, start: torch.Tensor,
+                   kv_len: torch.Tensor, max_new: int, cos: Optional[torch.Tensor] = None,
+                   sin: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                   interleaved: bool = False, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                   stream=None) -> None:
+    """Rotates, quantizes and stores the new keys and values k, v (tokens x Hkv x D) in the paged 8-bit cache, and
+    rotates the queries q into q_out (which may be q); see include/crvq.h for the cache and the batch."""
+    B, Hkv, D, page, cache = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len)
+    n, dt = k.shape[0], k.dtype
+    Hq = 0 if q is None else q.shape[1]
+    rows = (None, 0, 0, None, 0, 0) if q is None else _row_args(q, n, Hq, D, dt) + _row_args(q_out, n, Hq, D, dt)
+    angles = (None, None, 0, 0)
+    if cos is not None:
+        assert cos.dtype == sin.dtype == torch.float32 and cos.shape == sin.shape and cos.dim() == 2
+        assert cos.is_contiguous() and sin.is_contiguous()
+        angles = (cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1])
+    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == n)
+    _check("crvq_kv_append", lib().crvq_kv_append(
+        B, Hq, Hkv, D, page, *cache, max_new, n, dtype_code(k), *_row_args(k, n, Hkv, D, dt),
+        *_row_args(v, n, Hkv, D, dt), *rows, *angles, _ptr(positions), int(interleaved), _stream(stream)))
+
+
+def crvq_kv_read(k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor], k_cache: torch.Tensor,
+                 v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, block_table: torch.Tensor,
+                 start: torch.Tensor, kv_len: torch.Tensor, max_tokens: int, stream=None) -> None:
+    """The values that the cache holds for the last start[b+1] - start[b] tokens of every sequence."""
+    B, Hkv, D, page, cache = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len)
+    one = k_out if k_out is not None else v_out
+    if one is None:
+        return
+    n, none = one.shape[0], (None, 0, 0)
+    _check("crvq_kv_read", lib().crvq_kv_read(
+        B, Hkv, D, page, *cache, max_tokens, n, dtype_code(one),
+        *(none if k_out is None else _row_args(k_out, n, Hkv, D, one.dtype)),
+        *(none if v_out is None else _row_args(v_out, n, Hkv, D, one.dtype)), _stream(stream)))
+
+
+def crvq_kv_attention(q: torch.Tensor, out: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                      k_scale: torch.Tensor, v_scale: torch.Tensor, block_table: torch.Tensor, start: torch.Tensor,
+                      kv_len: torch.Tensor, max_new: int, max_kv: int, scale: Optional[float] = None,
+                      causal: bool = True, window: int = 0, lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of the new tokens' queries q (tokens x Hq x D) over the paged 8-bit cache; scale: D ** -0.5."""
+    L = lib()
+    B, Hkv, D, page, cache = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len)
+    n, Hq = q.shape[0], q.shape[1]
+    assert lse is None or (lse.dtype == torch.float32 and lse.shape == (n, Hq) and lse.is_contiguous())
+    ws = _workspace(L.crvq_kv_attention_workspace_size(B, Hq, Hkv, D, max_new, max_kv), q.device)
+    _check("crvq_kv_attention", L.crvq_kv_attention(
+        B, Hq, Hkv, D, page, *cache, max_new, max_kv, n, dtype_code(q), *_row_args(q, n, Hq, D, q.dtype),
+        *_row_args(out, n, Hq, D, q.dtype), D ** -0.5 if scale is None else scale, int(causal), window, _ptr(lse),
+        _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def _w4_args(codes, scales, zeros):
+    assert codes.dim() == 2 and codes.dtype == torch.uint8 and codes.stride(1) == 1
+    assert scales.dim() == 2 and scales.shape[0] == codes.shape[0] and scales.stride(1) == 1
+    assert zeros is None or (zeros.dtype == torch.uint8 and zeros.shape == scales.shape and zeros.stride(1) == 1)
+    return (codes.data_ptr(), codes.stride(0), scales.data_ptr(), dtype_code(scales), scales.stride(0), _ptr(zeros),
+            0 if zeros is None else zeros.stride(0))
+
+
+def _w4_holds(codes, scales, group, N):
+    return codes.shape[1] * 2 >= N and group > 0 and scales.shape[1] * group >= N
+
+
+def crvq_w4_quantize(W: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, group: int,
+                     zeros: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The 4-bit codes (two a byte), group scales and (if given) zero points of W; see include/crvq.h."""
+    M, N = W.shape
+    assert W.stride(1) == 1 and codes.shape[0] == M and _w4_holds(codes, scales, group, N)
+    c, ld, s, st, ld_s, z, ld_z = _w4_args(codes, scales, zeros)
+    _check("crvq_w4_quantize", lib().crvq_w4_quantize(M, N, group, _ptr(W), W.stride(0), dtype_code(W), c, ld, s, st,
+                                                      ld_s, z, ld_z, _stream(stream)))
+
+
+def crvq_w4_dequant(codes: torch.Tensor, scales: torch.Tensor, group: int, out: torch.Tensor,
+                    zeros: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out (M x N) = the values of a 4-bit matrix."""
+    M, N = out.shape
+    assert out.stride(1) == 1 and codes.shape[0] == M and _w4_holds(codes, scales, group, N)
+    _check("crvq_w4_dequant", lib().crvq_w4_dequant(M, N, group, *_w4_args(codes, scales, zeros), _ptr(out),
+                                                    out.stride(0), dtype_code(out), _stream(stream)))
+
+
+def crvq_w4_gemv(codes: torch.Tensor, scales: torch.Tensor, group: int, x: torch.Tensor, y: torch.Tensor,
+                 zeros: Optional[torch.Tensor] = None, stream=None) -> None:
+    """y[t] = W x[t] for the rows of x (T x N) and a 4-bit matrix W (M x N); y is T x M."""
+    L = lib()
+    T, N = x.shape
+    M = codes.shape[0]
+    assert y.shape == (T, M) and x.stride(1) == 1 and y.stride(1) == 1 and _w4_holds(codes, scales, group, N)
+    ws = _workspace(L.crvq_w4_gemv_workspace_size(M, N, T), y.device)
+    _check("crvq_w4_gemv", L.crvq_w4_gemv(M, N, T, group, *_w4_args(codes, scales, zeros), _ptr(x), x.stride(0),
+                                          dtype_code(x), _ptr(y), y.stride(0), dtype_code(y), _ptr(ws),
+                                          0 if ws is None else ws.numel(), _stream(stream)))

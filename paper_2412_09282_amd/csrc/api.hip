@@ -747,6 +747,14 @@ size_t crvq_workspace_size(int op, int64_t n_vectors, int64_t K, int32_t beam, i
     case CRVQ_OP_REFINE: return crvq_refine_workspace_size(M, N, n_cols);
     case CRVQ_OP_GEMV: return crvq_gemv_workspace_size(M, N, K);
     case CRVQ_OP_HINV: return crvq_hessian_inverse_workspace_size(N);
+    case CRVQ_OP_KV_ATTENTION:
+      if (n_vectors > 0x7fffffff || M > 0x7fffffff || N > 0x7fffffff || K > 0x7fffffff || n_cols > 0x7fffffff ||
+          n_vectors < 0 || M < 0 || N < 0 || K < 0 || n_cols < 0)
+        return 0;
+      return crvq_kv_attention_workspace_size(static_cast<int32_t>(n_vectors), static_cast<int32_t>(M),
+                                              static_cast<int32_t>(N), d, static_cast<int32_t>(K),
+                                              static_cast<int32_t>(n_cols));
+    case CRVQ_OP_W4_GEMV: return crvq_w4_gemv_workspace_size(M, N, K);
     default: return 0;
   }
 }
@@ -804,4 +812,267 @@ crvq_status crvq_pack_codes_u8(const int32_t* codes, int64_t n, uint8_t* out, vo
   if (n == 0) return CRVQ_OK;
   if (!codes || !out) return fail(CRVQ_ERR_INVALID, "%s: codes and out must not be NULL", fn);
   return hip_status(launch_pack_codes_u8(codes, n, out, static_cast<hipStream_t>(stream)), fn);
+}
+
+// ---- the attention block on quantized data ---------------------------------------------------------
+namespace {
+
+// Bytes from an array's first to its last element (rows x heads x D with strides, or rows x columns).
+size_t extent(int64_t rows, int64_t ld, int64_t heads, int64_t ld_head, int64_t d, int es) {
+  if (rows < 1 || heads < 1) return 0;
+  return static_cast<size_t>((rows - 1) * ld + (heads - 1) * ld_head + d) * es;
+}
+
+crvq_status check_cache(int32_t B, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages, const int8_t* k_cache,
+                        const int8_t* v_cache, const float* k_scale, const float* v_scale, const int32_t* table,
+                        int64_t ld_table, const int32_t* start, const int32_t* kv_len, int32_t max_new, int64_t n_tokens,
+                        int dtype, const char* fn, KvCache* c, KvBatch* bt) {
+  if (B < 0 || max_new < 0 || n_tokens < 0) return fail(CRVQ_ERR_INVALID, "%s: negative B, max_new or n_tokens", fn);
+  if (!dtype_ok(dtype)) return fail(CRVQ_ERR_INVALID, "%s: dtype %d is not CRVQ_F32 or CRVQ_BF16", fn, dtype);
+  if (Hkv < 1) return fail(CRVQ_ERR_INVALID, "%s: Hkv = %d", fn, Hkv);
+  if (D < 16 || D > CRVQ_KV_MAX_D || D % 16)
+    return fail(CRVQ_ERR_UNSUPPORTED, "%s: D = %d is not a multiple of 16 in [16, %d]", fn, D, CRVQ_KV_MAX_D);
+  int log2 = 4;
+  while (log2 < 8 && (1 << log2) != page) ++log2;
+  if ((1 << log2) != page) return fail(CRVQ_ERR_UNSUPPORTED, "%s: page = %d is not 16, 32, 64, 128 or 256", fn, page);
+  if (n_pages < 0 || ld_table < 0) return fail(CRVQ_ERR_INVALID, "%s: negative n_pages or ld_table", fn);
+  if (n_tokens > 0x7fffffffLL) return fail(CRVQ_ERR_UNSUPPORTED, "%s: %lld rows exceed 2^31 - 1", fn, (long long)n_tokens);
+  if (n_pages > 0x7fffffffLL) return fail(CRVQ_ERR_UNSUPPORTED, "%s: %lld pages exceed 2^31 - 1", fn, (long long)n_pages);
+  *c = {const_cast<int8_t*>(k_cache), const_cast<int8_t*>(v_cache), const_cast<float*>(k_scale),
+        const_cast<float*>(v_scale), n_pages, Hkv, D, log2};
+  *bt = {table, ld_table, start, kv_len, n_tokens, B, max_new};
+  if (B == 0 || max_new == 0 || n_tokens == 0) return CRVQ_OK;
+  if (!start || !kv_len) return fail(CRVQ_ERR_INVALID, "%s: start and kv_len must not be NULL", fn);
+  if (ld_table > 0 && !table) return fail(CRVQ_ERR_INVALID, "%s: block_table must not be NULL", fn);
+  if (n_pages > 0 && (!k_cache || !v_cache || !k_scale || !v_scale))
+    return fail(CRVQ_ERR_INVALID, "%s: the cache's arrays must not be NULL", fn);
+  if ((reinterpret_cast<uintptr_t>(k_cache) & 15) || (reinterpret_cast<uintptr_t>(v_cache) & 15))
+    return fail(CRVQ_ERR_INVALID, "%s: k_cache and v_cache must be 16-byte aligned", fn);
+  return CRVQ_OK;
+}
+
+crvq_status check_rows(const char* what, const void* p, int64_t tok, int64_t head, int32_t heads, int32_t D, int dtype,
+                       const char* fn) {
+  if (!p) return fail(CRVQ_ERR_INVALID, "%s: %s must not be NULL", fn, what);
+  if (tok < 0 || head < 0) return fail(CRVQ_ERR_INVALID, "%s: negative stride of %s", fn, what);
+  if (reinterpret_cast<uintptr_t>(p) % esize(dtype)) return fail(CRVQ_ERR_INVALID, "%s: %s is not aligned to its type", fn, what);
+  return CRVQ_OK;
+}
+
+// Outputs: no two (token, head) rows may share elements.
+crvq_status check_out_rows(const char* what, const void* p, int64_t tok, int64_t head, int64_t rows, int32_t heads,
+                           int32_t D, int dtype, const char* fn) {
+  const crvq_status s = check_rows(what, p, tok, head, heads, D, dtype, fn);
+  if (s) return s;
+  const bool token_major = (heads == 1 || head >= D) && (rows == 1 || tok >= (heads - 1) * head + D);
+  const bool head_major = (rows == 1 || tok >= D) && (heads == 1 || head >= (rows - 1) * tok + D);
+  if (!token_major && !head_major) return fail(CRVQ_ERR_INVALID, "%s: rows of %s overlap", fn, what);
+  return CRVQ_OK;
+}
+
+}  // namespace
+
+crvq_status crvq_kv_append(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages, int8_t* k_cache,
+                           int8_t* v_cache, float* k_scale, float* v_scale, const int32_t* block_table,
+                           int64_t ld_table, const int32_t* start, const int32_t* kv_len, int32_t max_new,
+                           int64_t n_tokens, int dtype, const void* k, int64_t k_tok, int64_t k_head, const void* v,
+                           int64_t v_tok, int64_t v_head, const void* q, int64_t q_tok, int64_t q_head, void* q_out,
+                           int64_t qo_tok, int64_t qo_head, const float* cos, const float* sin, int64_t n_angles,
+                           int32_t rot, const int32_t* positions, int interleaved, void* stream) {
+  const ApiRange range("crvq_kv_append");
+  static const char* fn = "crvq_kv_append";
+  g_err.clear();
+  KvCache c;
+  KvBatch bt;
+  crvq_status s = check_cache(B, Hkv, D, page, n_pages, k_cache, v_cache, k_scale, v_scale, block_table, ld_table, start,
+                              kv_len, max_new, n_tokens, dtype, fn, &c, &bt);
+  if (s) return s;
+  if (q && (Hq < 1 || Hq % Hkv)) return fail(CRVQ_ERR_INVALID, "%s: Hq = %d is not a multiple of Hkv = %d", fn, Hq, Hkv);
+  if (!q != !q_out) return fail(CRVQ_ERR_INVALID, "%s: q and q_out go together", fn);
+  if (!cos != !sin) return fail(CRVQ_ERR_INVALID, "%s: cos and sin go together", fn);
+  if (cos && (rot < 2 || rot > D || rot % 2 || n_angles < 0))
+    return fail(CRVQ_ERR_INVALID, "%s: rot = %d is not even in [2, D], or n_angles < 0", fn, rot);
+  if (B == 0 || max_new == 0 || n_tokens == 0) return CRVQ_OK;
+  if ((s = check_rows("k", k, k_tok, k_head, Hkv, D, dtype, fn))) return s;
+  if ((s = check_rows("v", v, v_tok, v_head, Hkv, D, dtype, fn))) return s;
+  const int es = esize(dtype);
+  if (q) {
+    if ((s = check_rows("q", q, q_tok, q_head, Hq, D, dtype, fn))) return s;
+    if ((s = check_out_rows("q_out", q_out, qo_tok, qo_head, n_tokens, Hq, D, dtype, fn))) return s;
+    const size_t out_n = extent(n_tokens, qo_tok, Hq, qo_head, D, es);
+    if (overlaps(q_out, out_n, q, extent(n_tokens, q_tok, Hq, q_head, D, es)) &&
+        !(q_out == q && qo_tok == q_tok && qo_head == q_head))
+      return fail(CRVQ_ERR_INVALID, "%s: q_out overlaps q without being q", fn);
+  }
+  const size_t page_bytes = static_cast<size_t>(n_pages) * Hkv * D * page, scales = static_cast<size_t>(n_pages) * Hkv * 4;
+  if (overlaps(k_cache, page_bytes, v_cache, page_bytes) || overlaps(k_scale, scales, v_scale, scales))
+    return fail(CRVQ_ERR_INVALID, "%s: the cache's arrays overlap", fn);
+  const KvRotation rt = {cos, sin, n_angles, positions, rot, interleaved ? 1 : 0};
+  return hip_status(launch_kv_append(c, bt, dtype, {const_cast<void*>(k), k_tok, k_head}, {const_cast<void*>(v), v_tok, v_head},
+                                     Hq, {const_cast<void*>(q), q_tok, q_head}, {q_out, qo_tok, qo_head}, rt,
+                                     static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+crvq_status crvq_kv_read(int32_t B, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages, const int8_t* k_cache,
+                         const int8_t* v_cache, const float* k_scale, const float* v_scale, const int32_t* block_table,
+                         int64_t ld_table, const int32_t* start, const int32_t* kv_len, int32_t max_new,
+                         int64_t n_tokens, int dtype, void* k_out, int64_t k_tok, int64_t k_head, void* v_out,
+                         int64_t v_tok, int64_t v_head, void* stream) {
+  const ApiRange range("crvq_kv_read");
+  static const char* fn = "crvq_kv_read";
+  g_err.clear();
+  KvCache c;
+  KvBatch bt;
+  crvq_status s = check_cache(B, Hkv, D, page, n_pages, k_cache, v_cache, k_scale, v_scale, block_table, ld_table, start,
+                              kv_len, max_new, n_tokens, dtype, fn, &c, &bt);
+  if (s) return s;
+  if (B == 0 || max_new == 0 || n_tokens == 0 || (!k_out && !v_out)) return CRVQ_OK;
+  if (k_out && (s = check_out_rows("k_out", k_out, k_tok, k_head, n_tokens, Hkv, D, dtype, fn))) return s;
+  if (v_out && (s = check_out_rows("v_out", v_out, v_tok, v_head, n_tokens, Hkv, D, dtype, fn))) return s;
+  return hip_status(launch_kv_read(c, bt, dtype, {k_out, k_tok, k_head}, {v_out, v_tok, v_head},
+                                   static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+size_t crvq_kv_attention_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new, int32_t max_kv) {
+  if (B < 1 || Hkv < 1 || Hq < Hkv || Hq % Hkv || D < 16 || D > CRVQ_KV_MAX_D || D % 16 || max_new < 1 || max_kv < 0) return 0;
+  return kv_attention_ws_bytes(B, Hq, Hkv, D, max_new, max_kv);
+}
+
+crvq_status crvq_kv_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages,
+                              const int8_t* k_cache, const int8_t* v_cache, const float* k_scale, const float* v_scale,
+                              const int32_t* block_table, int64_t ld_table, const int32_t* start, const int32_t* kv_len,
+                              int32_t max_new, int32_t max_kv, int64_t n_tokens, int dtype, const void* q, int64_t q_tok,
+                              int64_t q_head, void* out, int64_t o_tok, int64_t o_head, float scale, int causal,
+                              int32_t window, float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  const ApiRange range("crvq_kv_attention");
+  static const char* fn = "crvq_kv_attention";
+  g_err.clear();
+  KvCache c;
+  KvBatch bt;
+  crvq_status s = check_cache(B, Hkv, D, page, n_pages, k_cache, v_cache, k_scale, v_scale, block_table, ld_table, start,
+                              kv_len, max_new, n_tokens, dtype, fn, &c, &bt);
+  if (s) return s;
+  if (Hq < 1 || Hq % Hkv) return fail(CRVQ_ERR_INVALID, "%s: Hq = %d is not a multiple of Hkv = %d", fn, Hq, Hkv);
+  if (max_kv < 0) return fail(CRVQ_ERR_INVALID, "%s: max_kv < 0", fn);
+  if (!std::isfinite(scale)) return fail(CRVQ_ERR_INVALID, "%s: scale is not finite", fn);
+  if (window < 0 || (window && !causal)) return fail(CRVQ_ERR_INVALID, "%s: window < 0, or a window without causal", fn);
+  if (B == 0 || max_new == 0 || n_tokens == 0) return CRVQ_OK;
+  if ((s = check_rows("q", q, q_tok, q_head, Hq, D, dtype, fn))) return s;
+  if ((s = check_out_rows("out", out, o_tok, o_head, n_tokens, Hq, D, dtype, fn))) return s;
+  const int es = esize(dtype);
+  const size_t q_n = extent(n_tokens, q_tok, Hq, q_head, D, es), o_n = extent(n_tokens, o_tok, Hq, o_head, D, es);
+  if (overlaps(out, o_n, q, q_n) && !(out == q && o_tok == q_tok && o_head == q_head))
+    return fail(CRVQ_ERR_INVALID, "%s: out overlaps q without being q", fn);
+  if (lse) {
+    const size_t l_n = static_cast<size_t>(n_tokens) * Hq * 4;
+    if (overlaps(lse, l_n, q, q_n) || overlaps(lse, l_n, out, o_n))
+      return fail(CRVQ_ERR_INVALID, "%s: lse overlaps q or out", fn);
+  }
+  if ((s = check_ws(workspace, ws_bytes, crvq_kv_attention_workspace_size(B, Hq, Hkv, D, max_new, max_kv), fn))) return s;
+  return hip_status(launch_kv_attention(c, bt, max_kv, dtype, Hq, {const_cast<void*>(q), q_tok, q_head},
+                                        {out, o_tok, o_head}, scale, causal ? 1 : 0, window, lse, workspace,
+                                        static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+namespace {
+
+crvq_status check_w4(int64_t M, int64_t N, int32_t group, const uint8_t* codes, int64_t ld, const void* scales,
+                     int scale_dtype, int64_t ld_s, const uint8_t* zeros, int64_t ld_z, const char* fn, W4* w) {
+  if (M < 0 || N < 1) return fail(CRVQ_ERR_INVALID, "%s: need M >= 0 and N >= 1", fn);
+  if (M > 0x7fffffffLL || N > 0x7fffffffLL) return fail(CRVQ_ERR_UNSUPPORTED, "%s: M or N exceeds 2^31 - 1", fn);
+  int log2 = 5;
+  while (log2 < 8 && (1 << log2) != group) ++log2;
+  if ((1 << log2) != group) return fail(CRVQ_ERR_UNSUPPORTED, "%s: group = %d is not 32, 64, 128 or 256", fn, group);
+  if (!dtype_ok(scale_dtype)) return fail(CRVQ_ERR_INVALID, "%s: scale_dtype %d is not CRVQ_F32 or CRVQ_BF16", fn, scale_dtype);
+  *w = {const_cast<uint8_t*>(codes), const_cast<void*>(scales), const_cast<uint8_t*>(zeros), M, N, ld, ld_s, ld_z, log2,
+        scale_dtype};
+  if (M == 0) return CRVQ_OK;
+  if (!codes || !scales) return fail(CRVQ_ERR_INVALID, "%s: codes and scales must not be NULL", fn);
+  if (ld % 16 || 2 * ld < N || (reinterpret_cast<uintptr_t>(codes) & 15))
+    return fail(CRVQ_ERR_INVALID, "%s: codes must be 16-byte aligned with ld a multiple of 16 and 2 ld >= N", fn);
+  const int64_t groups = cdiv(N, group);
+  if (ld_s < groups || (zeros && ld_z < groups))
+    return fail(CRVQ_ERR_INVALID, "%s: ld_s and ld_z must be at least ceil(N / group) = %lld", fn, (long long)groups);
+  if (reinterpret_cast<uintptr_t>(scales) % esize(scale_dtype))
+    return fail(CRVQ_ERR_INVALID, "%s: scales are not aligned to their type", fn);
+  return CRVQ_OK;
+}
+
+crvq_status check_matrix(const char* what, const void* p, int64_t rows, int64_t ld, int64_t cols, int dtype, const char* fn) {
+  if (!dtype_ok(dtype)) return fail(CRVQ_ERR_INVALID, "%s: the type of %s is not CRVQ_F32 or CRVQ_BF16", fn, what);
+  if (rows == 0) return CRVQ_OK;
+  if (!p) return fail(CRVQ_ERR_INVALID, "%s: %s must not be NULL", fn, what);
+  if (ld < cols) return fail(CRVQ_ERR_INVALID, "%s: row stride of %s below its %lld columns", fn, what, (long long)cols);
+  if (reinterpret_cast<uintptr_t>(p) % esize(dtype)) return fail(CRVQ_ERR_INVALID, "%s: %s is not aligned to its type", fn, what);
+  return CRVQ_OK;
+}
+
+}  // namespace
+
+crvq_status crvq_w4_quantize(int64_t M, int64_t N, int32_t group, const void* W, int64_t ldw, int dtype, uint8_t* codes,
+                             int64_t ld, void* scales, int scale_dtype, int64_t ld_s, uint8_t* zeros, int64_t ld_z,
+                             void* stream) {
+  const ApiRange range("crvq_w4_quantize");
+  static const char* fn = "crvq_w4_quantize";
+  g_err.clear();
+  W4 w;
+  crvq_status s = check_w4(M, N, group, codes, ld, scales, scale_dtype, ld_s, zeros, ld_z, fn, &w);
+  if (s || (s = check_matrix("W", W, M, ldw, N, dtype, fn))) return s;
+  if (M == 0) return CRVQ_OK;
+  const size_t w_n = extent(M, ldw, 1, 0, N, esize(dtype)), c_n = extent(M, ld, 1, 0, cdiv(N, 32) * 16, 1);
+  const size_t s_n = extent(M, ld_s, 1, 0, cdiv(N, group), esize(scale_dtype)), z_n = extent(M, ld_z, 1, 0, cdiv(N, group), 1);
+  if (overlaps(codes, c_n, W, w_n) || overlaps(scales, s_n, W, w_n) || overlaps(codes, c_n, scales, s_n) ||
+      (zeros && (overlaps(zeros, z_n, W, w_n) || overlaps(zeros, z_n, codes, c_n) || overlaps(zeros, z_n, scales, s_n))))
+    return fail(CRVQ_ERR_INVALID, "%s: W, codes, scales and zeros must not overlap", fn);
+  return hip_status(launch_w4_quantize(W, ldw, dtype, w, static_cast<hipStream_t>(stream)), fn);
+}
+
+crvq_status crvq_w4_dequant(int64_t M, int64_t N, int32_t group, const uint8_t* codes, int64_t ld, const void* scales,
+                            int scale_dtype, int64_t ld_s, const uint8_t* zeros, int64_t ld_z, void* out, int64_t ldo,
+                            int dtype, void* stream) {
+  const ApiRange range("crvq_w4_dequant");
+  static const char* fn = "crvq_w4_dequant";
+  g_err.clear();
+  W4 w;
+  crvq_status s = check_w4(M, N, group, codes, ld, scales, scale_dtype, ld_s, zeros, ld_z, fn, &w);
+  if (s || (s = check_matrix("out", out, M, ldo, N, dtype, fn))) return s;
+  if (M == 0) return CRVQ_OK;
+  const size_t o_n = extent(M, ldo, 1, 0, N, esize(dtype));
+  if (overlaps(out, o_n, codes, extent(M, ld, 1, 0, cdiv(N, 32) * 16, 1)) ||
+      overlaps(out, o_n, scales, extent(M, ld_s, 1, 0, cdiv(N, group), esize(scale_dtype))) ||
+      (zeros && overlaps(out, o_n, zeros, extent(M, ld_z, 1, 0, cdiv(N, group), 1))))
+    return fail(CRVQ_ERR_INVALID, "%s: out overlaps an input", fn);
+  return hip_status(launch_w4_dequant(w, out, ldo, dtype, static_cast<hipStream_t>(stream)), fn);
+}
+
+size_t crvq_w4_gemv_workspace_size(int64_t M, int64_t N, int64_t T) {
+  if (M < 1 || N < 1 || T < 1 || M > 0x7fffffffLL || N > 0x7fffffffLL || T > 0x7fffffffLL) return 0;
+  return w4_gemv_ws_bytes(M, N, T);
+}
+
+crvq_status crvq_w4_gemv(int64_t M, int64_t N, int64_t T, int32_t group, const uint8_t* codes, int64_t ld,
+                         const void* scales, int scale_dtype, int64_t ld_s, const uint8_t* zeros, int64_t ld_z,
+                         const void* x, int64_t ldx, int x_dtype, void* y, int64_t ldy, int y_dtype, void* workspace,
+                         size_t ws_bytes, void* stream) {
+  const ApiRange range("crvq_w4_gemv");
+  static const char* fn = "crvq_w4_gemv";
+  g_err.clear();
+  W4 w;
+  crvq_status s = check_w4(M, N, group, codes, ld, scales, scale_dtype, ld_s, zeros, ld_z, fn, &w);
+  if (s) return s;
+  if (T < 0 || T > 0x7fffffffLL) return fail(CRVQ_ERR_INVALID, "%s: T = %lld", fn, (long long)T);
+  const int64_t rows = M ? T : 0;
+  if ((s = check_matrix("x", x, rows, ldx, N, x_dtype, fn)) || (s = check_matrix("y", y, rows, ldy, M, y_dtype, fn))) return s;
+  if (rows == 0) return CRVQ_OK;
+  const size_t y_n = extent(T, ldy, 1, 0, M, esize(y_dtype));
+  if (overlaps(y, y_n, x, extent(T, ldx, 1, 0, N, esize(x_dtype))) ||
+      overlaps(y, y_n, codes, extent(M, ld, 1, 0, cdiv(N, 32) * 16, 1)) ||
+      overlaps(y, y_n, scales, extent(M, ld_s, 1, 0, cdiv(N, group), esize(scale_dtype))) ||
+      (zeros && overlaps(y, y_n, zeros, extent(M, ld_z, 1, 0, cdiv(N, group), 1))))
+    return fail(CRVQ_ERR_INVALID, "%s: y overlaps an input", fn);
+  if ((s = check_ws(workspace, ws_bytes, crvq_w4_gemv_workspace_size(M, N, T), fn))) return s;
+  return hip_status(launch_w4_gemv(w, T, x, ldx, x_dtype, y, ldy, y_dtype, workspace, static_cast<hipStream_t>(stream)), fn);
 }

@@ -250,4 +250,54 @@ hipError_t launch_refine_book(int64_t M, int64_t N, int d, int64_t n_cols, doubl
                               int64_t ldh, const void* Cb, int c_type, int64_t K, int32_t* codes, int64_t ldq,
                               void* ws, hipStream_t stream);
 
+// ---- 8-bit key / value cache (k_kv.hip) and attention over it (k_attn.hip) ------------------------
+struct KvCache {
+  int8_t* k;       // [n_pages][Hkv][page][D]
+  int8_t* v;       // [n_pages][Hkv][D][page]
+  float* k_scale;  // [n_pages][Hkv]
+  float* v_scale;
+  int64_t n_pages;
+  int Hkv, D, page_log2;
+};
+struct KvBatch {
+  const int32_t* table;  // [B][ld_table] pages
+  int64_t ld_table;
+  const int32_t* start;   // [B + 1] first rows
+  const int32_t* kv_len;  // [B]
+  int64_t n_tokens;
+  int B, max_new;
+};
+struct KvRows {  // rows of heads of D elements
+  void* p;
+  int64_t tok, head;  // strides in elements
+};
+struct KvRotation {
+  const float *cos, *sin;  // [n_angles][rot / 2]; cos NULL: no rotation
+  int64_t n_angles;
+  const int32_t* positions;
+  int rot, interleaved;
+};
+hipError_t launch_kv_append(const KvCache& c, const KvBatch& bt, int type, const KvRows& k, const KvRows& v, int Hq,
+                            const KvRows& q, const KvRows& q_out, const KvRotation& rt, hipStream_t stream);
+hipError_t launch_kv_read(const KvCache& c, const KvBatch& bt, int type, const KvRows& k_out, const KvRows& v_out,
+                          hipStream_t stream);
+size_t kv_attention_ws_bytes(int B, int Hq, int Hkv, int D, int max_new, int max_kv);
+hipError_t launch_kv_attention(const KvCache& c, const KvBatch& bt, int max_kv, int type, int Hq, const KvRows& q,
+                               const KvRows& out, float scale, int causal, int window, float* lse, void* ws,
+                               hipStream_t stream);
+
+// ---- 4-bit matrices with group scales (k_w4.hip) --------------------------------------------------
+struct W4 {
+  uint8_t* codes;
+  void* scales;
+  uint8_t* zeros;  // NULL: every zero point is 8
+  int64_t M, N, ld, ld_s, ld_z;
+  int group_log2, s_type;
+};
+hipError_t launch_w4_quantize(const void* W, int64_t ldw, int type, const W4& w, hipStream_t stream);
+hipError_t launch_w4_dequant(const W4& w, void* out, int64_t ldo, int type, hipStream_t stream);
+size_t w4_gemv_ws_bytes(int64_t M, int64_t N, int64_t T);
+hipError_t launch_w4_gemv(const W4& w, int64_t T, const void* x, int64_t ldx, int x_type, void* y, int64_t ldy, int y_type,
+                          void* ws, hipStream_t stream);
+
 }  // namespace crvq

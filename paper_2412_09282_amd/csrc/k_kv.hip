@@ -1,0 +1,469 @@
+// The paged 8-bit cache of keys and values: appending (rotation, quantization, storage) and reading back.
+//
+// Append: one workgroup owns one head of one page of keys or of values and the new tokens that fall into
+// it, so the page's scale has one writer.  It takes the largest magnitude of its rotated elements, settles
+// the scale, brings older codes to it if it grew, and stores the new codes; the elements are read twice,
+// the second time from the caches.  Values are stored transposed: whole runs of 16 slots go through an LDS
+// tile and leave as 16-byte stores, single tokens as bytes.  The same launch rotates the queries.
+#include "kv_common.h"
+
+namespace crvq {
+namespace {
+
+constexpr float kMinScale = 7.888609052210118e-31f;  // 2^-100
+constexpr int kSeg = 64;                             // slots of the LDS tile of a page of values
+constexpr int kTileLd = kSeg + 4;
+
+template <typename T>
+__device__ __forceinline__ float ld1(const T* p) {
+  if constexpr (sizeof(T) == 4)
+    return *reinterpret_cast<const float*>(p);
+  else
+    return bf16_f(*p);
+}
+
+// Eight consecutive elements; VEC: 16-byte aligned.
+template <typename T, bool VEC>
+__device__ __forceinline__ void ld8(const T* p, float (&x)[8]) {
+  if constexpr (!VEC) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = ld1(p + i);
+  } else if constexpr (sizeof(T) == 4) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(u[i] << 16);
+      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void st1(T* p, float x) {
+  if constexpr (sizeof(T) == 4)
+    *reinterpret_cast<float*>(p) = x;
+  else
+    *p = static_cast<T>(f_bf16(x));
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void st8(T* p, const float (&x)[8]) {
+  if constexpr (!VEC) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) st1(p + i, x[i]);
+  } else if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    uint4 a;
+    a.x = f_bf16(x[0]) | (f_bf16(x[1]) << 16);
+    a.y = f_bf16(x[2]) | (f_bf16(x[3]) << 16);
+    a.z = f_bf16(x[4]) | (f_bf16(x[5]) << 16);
+    a.w = f_bf16(x[6]) | (f_bf16(x[7]) << 16);
+    *reinterpret_cast<uint4*>(p) = a;
+  }
+}
+
+// The angles of one row; ok = 0: its place lies outside the table.
+struct Angles {
+  const float *c, *s;
+  int ok;
+};
+__device__ __forceinline__ Angles angles(const KvRotation& rt, int row, int place) {
+  const int64_t p = rt.positions ? rt.positions[row] : place;
+  Angles a;
+  a.ok = p >= 0 && p < rt.n_angles;
+  const int64_t at = a.ok ? p * (rt.rot >> 1) : 0;
+  a.c = rt.cos + at;
+  a.s = rt.sin + at;
+  return a;
+}
+
+// Pair j of a row, (a, b) -> (a c - b s, b c + a s).
+__device__ __forceinline__ void turn(const Angles& an, int j, float& a, float& b) {
+  const float c = an.ok ? an.c[j] : __uint_as_float(0x7fc00000u), s = an.ok ? an.s[j] : 0.f;
+  const float u = a * c - b * s, w = b * c + a * s;
+  a = u;
+  b = w;
+}
+
+// Elements e0 .. e0 + 7 of a head's row, rotated.
+template <typename T, bool VEC>
+__device__ __forceinline__ void rotated8(const T* row, int e0, const KvRotation& rt, const Angles& an, float (&x)[8]) {
+  ld8<T, VEC>(row + e0, x);
+  if (!rt.cos || e0 >= rt.rot) return;
+  const int r = rt.rot >> 1;
+  if (rt.interleaved) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2)
+      if (e0 + i < rt.rot) turn(an, (e0 + i) >> 1, x[i], x[i + 1]);
+    return;
+  }
+  if (VEC && (r & 7) == 0) {  // the partners are a chunk too, and all eight are first or second elements
+    float y[8];
+    const bool first = e0 < r;
+    ld8<T, VEC>(row + (first ? e0 + r : e0 - r), y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (first)
+        turn(an, e0 + i, x[i], y[i]);
+      else
+        turn(an, e0 - r + i, y[i], x[i]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int e = e0 + i;
+    if (e < r) {
+      float y = ld1(row + e + r);
+      turn(an, e, x[i], y);
+    } else if (e < rt.rot) {
+      float y = ld1(row + e - r);
+      turn(an, e - r, y, x[i]);
+    }
+  }
+}
+
+template <int NT>
+__device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t* lds) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o)));
+  if (NT > 64) {
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = lds[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) m = max(m, lds[w]);
+  }
+  return m;
+}
+
+__device__ __forceinline__ uint32_t rescale4(uint32_t c, float f) {
+  uint32_t o = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float x = rintf(static_cast<float>(static_cast<int8_t>(c >> (8 * i))) * f);
+    o |= (static_cast<uint32_t>(static_cast<int>(x)) & 255u) << (8 * i);
+  }
+  return o;
+}
+
+__device__ __forceinline__ uint32_t quantize1(float x, float scale) {
+  const float q = fminf(fmaxf(rintf(x / scale), -127.f), 127.f);
+  return static_cast<uint32_t>(static_cast<int>(q)) & 255u;
+}
+
+struct AppendArgs {
+  KvCache c;
+  KvBatch bt;
+  KvRows k, v, q, q_out;
+  KvRotation rt;
+  int Hq;
+  int64_t kv_blocks;  // B * pages * Hkv * 2 workgroups of pages; the queries' follow
+  int pages;          // pages a sequence's new tokens may touch
+};
+
+template <typename T, bool VEC, int NT>
+__device__ __forceinline__ void rotate_queries(const AppendArgs& a, int64_t block) {
+  const int D = a.c.D, r = a.rt.cos ? a.rt.rot >> 1 : 0;
+  const bool halves = r && !a.rt.interleaved;
+  // a unit is what one thread reads before it writes, so q_out may be q: a chunk and its partner chunk, or
+  // single pairs where the halves are not whole chunks
+  const bool single = !VEC || (halves && (r & 7));
+  const int per = single ? D - r : (halves ? D - r : D) >> 3;
+  const int64_t u = block * NT + threadIdx.x;
+  const int64_t head = u / per;
+  if (head >= a.bt.n_tokens * a.Hq) return;
+  const int unit = static_cast<int>(u - head * per);
+  const int row = static_cast<int>(head / a.Hq), h = static_cast<int>(head - static_cast<int64_t>(row) * a.Hq);
+  const T* in = static_cast<const T*>(a.q.p) + row * a.q.tok + h * a.q.head;
+  T* out = static_cast<T*>(a.q_out.p) + row * a.q_out.tok + h * a.q_out.head;
+  Angles an = {nullptr, nullptr, 0};
+  if (r) {
+    int place = 0;
+    if (!a.rt.positions) {  // the sequence of this row
+      int lo = 0, hi = a.bt.B;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (a.bt.start[mid + 1] > row) hi = mid; else lo = mid + 1;
+      }
+      if (lo >= a.bt.B) return;
+      const KvSeq s = kv_seq(a.bt, lo, a.c.page_log2);
+      if (!s.ok || s.n > s.len || row < s.row0) return;
+      place = s.len - s.n + row - s.row0;
+    }
+    an = angles(a.rt, row, place);
+  }
+  if (single) {
+    if (unit < r) {
+      const int e = a.rt.interleaved ? 2 * unit : unit, f = a.rt.interleaved ? e + 1 : e + r;
+      float x = ld1(in + e), y = ld1(in + f);
+      turn(an, unit, x, y);
+      st1(out + e, x);
+      st1(out + f, y);
+    } else {
+      out[unit + r] = in[unit + r];
+    }
+    return;
+  }
+  const int e0 = unit * 8 + (halves && unit * 8 >= r ? r : 0);
+  float x[8], y[8];
+  if (halves && e0 < r) {
+    ld8<T, VEC>(in + e0, x);
+    ld8<T, VEC>(in + e0 + r, y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) turn(an, e0 + i, x[i], y[i]);
+    st8<T, VEC>(out + e0, x);
+    st8<T, VEC>(out + e0 + r, y);
+  } else {
+    rotated8<T, VEC>(in, e0, a.rt, an, x);
+    st8<T, VEC>(out + e0, x);
+  }
+}
+
+template <typename T, bool VEC, int NT>
+__global__ __launch_bounds__(NT) void kv_append_kernel(const AppendArgs a) {
+  __shared__ uint32_t red[8];
+  __shared__ __align__(16) uint8_t tile[NT > 64 ? CRVQ_KV_MAX_D * kTileLd : 16];
+  if (blockIdx.x >= a.kv_blocks) {
+    rotate_queries<T, VEC, NT>(a, static_cast<int64_t>(blockIdx.x) - a.kv_blocks);
+    return;
+  }
+  const int tid = threadIdx.x, D = a.c.D, P = 1 << a.c.page_log2;
+  int64_t item = blockIdx.x;
+  const bool values = item & 1;
+  item >>= 1;
+  const int h = static_cast<int>(item % a.c.Hkv);
+  item /= a.c.Hkv;
+  const int j = static_cast<int>(item % a.pages), b = static_cast<int>(item / a.pages);
+  const KvSeq sq = kv_seq(a.bt, b, a.c.page_log2);
+  if (!sq.ok || sq.n == 0 || sq.n > sq.len) return;
+  const int first = sq.len - sq.n, p = (first >> a.c.page_log2) + j;
+  if ((static_cast<int64_t>(p) << a.c.page_log2) >= sq.len) return;
+  const int64_t page = a.bt.table[b * a.bt.ld_table + p];
+  if (page < 0 || page >= a.c.n_pages) return;
+  const int t0 = p << a.c.page_log2;
+  const int lo = max(first, t0) - t0, hi = min(sq.len - t0, P);  // its new slots; older ones before lo
+  const KvRows src = values ? a.v : a.k;
+  const T* base = static_cast<const T*>(src.p) + h * src.head;
+  const int cpr = D >> 3, chunks = (hi - lo) * cpr;
+  const int row_lo = sq.row0 + t0 + lo - first;
+
+  auto load = [&](int c, int& slot, int& e0, float (&x)[8]) {
+    const int i = c / cpr;
+    e0 = (c - i * cpr) * 8;
+    slot = lo + i;
+    const int row = row_lo + i;
+    const T* r = base + row * src.tok;
+    if (values)
+      ld8<T, VEC>(r + e0, x);
+    else
+      rotated8<T, VEC>(r, e0, a.rt, a.rt.cos ? angles(a.rt, row, t0 + slot) : Angles{nullptr, nullptr, 0}, x);
+  };
+
+  uint32_t m = 0;  // largest magnitude, as bits: a NaN is larger than every number
+  for (int c = tid; c < chunks; c += NT) {
+    int slot, e0;
+    float x[8];
+    load(c, slot, e0, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+  }
+  m = block_max<NT>(m, red);
+  float* sp = (values ? a.c.v_scale : a.c.k_scale) + page * a.c.Hkv + h;
+  const int64_t head_at = (page * a.c.Hkv + h) * (static_cast<int64_t>(D) << a.c.page_log2);
+  int8_t* codes = (values ? a.c.v : a.c.k) + head_at;
+  const bool finite = m < 0x7f800000u;
+  float scale = finite ? fmaxf(__uint_as_float(m) / 127.f, kMinScale) : __uint_as_float(0x7fc00000u);
+  if (lo > 0) {
+    const float old = *sp;
+    if (finite && !(scale > old)) scale = old;
+    if (scale > old) {  // the older codes move to the larger scale, 16 at a time
+      const float f = old / scale;
+      const int rows = values ? D : lo, units = values ? (lo + 15) >> 4 : D >> 4;
+      for (int u = tid; u < rows * units; u += NT) {
+        const int r = u / units;
+        uint4* at = reinterpret_cast<uint4*>(codes + (values ? r << a.c.page_log2 : r * D)) + (u - r * units);
+        uint4 w = *at;
+        w.x = rescale4(w.x, f);
+        w.y = rescale4(w.y, f);
+        w.z = rescale4(w.z, f);
+        w.w = rescale4(w.w, f);
+        *at = w;
+      }
+    }
+    __syncthreads();  // every thread has the old scale, and the older codes are in place
+  }
+  if (tid == 0) *sp = scale;
+  const bool number = scale == scale;
+
+  if (!values || NT == 64) {
+    for (int c = tid; c < chunks; c += NT) {
+      int slot, e0;
+      float x[8];
+      load(c, slot, e0, x);
+      uint32_t q[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[i] = number ? quantize1(x[i], scale) : 0u;
+      if (!values) {
+        uint2 w;
+        w.x = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
+        w.y = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
+        *reinterpret_cast<uint2*>(codes + slot * D + e0) = w;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) codes[((e0 + i) << a.c.page_log2) + slot] = static_cast<int8_t>(q[i]);
+      }
+    }
+    return;
+  }
+  // values of many tokens: segments of kSeg slots through the tile
+  for (int s0 = lo & ~(kSeg - 1); s0 < hi; s0 += kSeg) {
+    const int from = max(lo, s0), to = min(hi, s0 + kSeg);
+    __syncthreads();
+    for (int c = (from - lo) * cpr + tid; c < (to - lo) * cpr; c += NT) {
+      int slot, e0;
+      float x[8];
+      load(c, slot, e0, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        tile[(e0 + i) * kTileLd + slot - s0] = static_cast<uint8_t>(number ? quantize1(x[i], scale) : 0u);
+    }
+    __syncthreads();
+    const int runs = (to - s0 + 15) >> 4;
+    for (int u = tid; u < D * runs; u += NT) {
+      const int d = u / runs, g = (u - d * runs) * 16;
+      const uint8_t* t = tile + d * kTileLd + g;
+      int8_t* out = codes + (d << a.c.page_log2) + s0 + g;
+      if (s0 + g >= from && s0 + g + 16 <= to) {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(t);
+        *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+        for (int i = 0; i < 16; ++i)
+          if (s0 + g + i >= from && s0 + g + i < to) out[i] = static_cast<int8_t>(t[i]);
+      }
+    }
+  }
+}
+
+struct ReadArgs {
+  KvCache c;
+  KvBatch bt;
+  KvRows k, v;
+  int segs, seg_log2;  // segments a sequence's tokens may touch; slots of one (min(page, kSeg))
+};
+
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void kv_read_kernel(const ReadArgs a) {
+  __shared__ __align__(16) uint8_t tile[CRVQ_KV_MAX_D * kTileLd];
+  const int tid = threadIdx.x, D = a.c.D;
+  int64_t item = blockIdx.x;
+  const bool values = item & 1;
+  item >>= 1;
+  const int h = static_cast<int>(item % a.c.Hkv);
+  item /= a.c.Hkv;
+  const int j = static_cast<int>(item % a.segs), b = static_cast<int>(item / a.segs);
+  const KvRows dst = values ? a.v : a.k;
+  const KvSeq sq = kv_seq(a.bt, b, a.c.page_log2);
+  if (!dst.p || !sq.ok || sq.n == 0 || sq.n > sq.len) return;
+  const int first = sq.len - sq.n, S = 1 << a.seg_log2, t0 = ((first >> a.seg_log2) + j) << a.seg_log2;
+  if (t0 >= sq.len) return;
+  const int64_t page = a.bt.table[b * a.bt.ld_table + (t0 >> a.c.page_log2)];
+  const bool there = page >= 0 && page < a.c.n_pages;
+  const int slot0 = t0 & ((1 << a.c.page_log2) - 1);
+  const int64_t head = (there ? page : 0) * a.c.Hkv + h;
+  const int8_t* codes = (values ? a.c.v : a.c.k) + head * (static_cast<int64_t>(D) << a.c.page_log2);
+  const float scale = there ? (values ? a.c.v_scale : a.c.k_scale)[head] : __uint_as_float(0x7fc00000u);
+  const int lo = max(first - t0, 0), hi = min(sq.len - t0, S), cpr = D >> 3;
+  if (values && there) {  // the segment of every d, 16 slots at a time
+    const int runs = S >> 4;
+    for (int u = tid; u < D * runs; u += 256) {
+      const int d = u / runs, g = (u - d * runs) * 16;
+      const uint4 w = *reinterpret_cast<const uint4*>(codes + (d << a.c.page_log2) + slot0 + g);
+      uint32_t* t = reinterpret_cast<uint32_t*>(tile + d * kTileLd + g);
+      t[0] = w.x; t[1] = w.y; t[2] = w.z; t[3] = w.w;
+    }
+    __syncthreads();
+  }
+  T* base = static_cast<T*>(dst.p) + h * dst.head;
+  for (int c = tid; c < (hi - lo) * cpr; c += 256) {
+    const int i = lo + c / cpr, e0 = (c % cpr) * 8;
+    float x[8];
+    if (!there) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = scale;
+    } else if (values) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = static_cast<float>(static_cast<int8_t>(tile[(e0 + e) * kTileLd + i])) * scale;
+    } else {
+      const uint2 w = *reinterpret_cast<const uint2*>(codes + (slot0 + i) * D + e0);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        x[e] = static_cast<float>(static_cast<int8_t>((e < 4 ? w.x : w.y) >> (8 * (e & 3)))) * scale;
+    }
+    st8<T, VEC>(base + (sq.row0 + t0 + i - first) * dst.tok + e0, x);
+  }
+}
+
+// Rows whose chunks of eight elements are 16-byte aligned.
+bool aligned_rows(const KvRows& r, int type) {
+  const int64_t per = type == ET_F32 ? 4 : 8;
+  return !r.p || ((reinterpret_cast<uintptr_t>(r.p) & 15) == 0 && r.tok % per == 0 && r.head % per == 0);
+}
+
+template <typename T, int NT>
+hipError_t append_as(bool vec, const AppendArgs& a, int64_t blocks, hipStream_t stream) {
+  if (vec)
+    kv_append_kernel<T, true, NT><<<dim3(static_cast<uint32_t>(blocks)), NT, 0, stream>>>(a);
+  else
+    kv_append_kernel<T, false, NT><<<dim3(static_cast<uint32_t>(blocks)), NT, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const KvCache& c, const KvBatch& bt, int type, const KvRows& k, const KvRows& v, int Hq,
+                            const KvRows& q, const KvRows& q_out, const KvRotation& rt, hipStream_t stream) {
+  AppendArgs a = {c, bt, k, v, q, q_out, rt, Hq, 0, 0};
+  const int P = 1 << c.page_log2;
+  a.pages = static_cast<int>((static_cast<int64_t>(bt.max_new) + P - 2) / P + 1);
+  a.kv_blocks = static_cast<int64_t>(bt.B) * a.pages * c.Hkv * 2;
+  const bool vec = aligned_rows(k, type) && aligned_rows(v, type) && aligned_rows(q, type) && aligned_rows(q_out, type);
+  const bool few = bt.max_new <= 4;
+  const int nt = few ? 64 : 256;
+  const int64_t q_units = q.p ? bt.n_tokens * Hq * (vec ? c.D >> 3 : c.D) : 0;
+  const int r = rt.cos ? rt.rot >> 1 : 0;
+  const bool single = !vec || (r && !rt.interleaved && (r & 7));
+  const int64_t per = single ? c.D - r : (r && !rt.interleaved ? c.D - r : c.D) >> 3;
+  const int64_t blocks = a.kv_blocks + (q_units ? cdiv(bt.n_tokens * Hq * per, nt) : 0);
+  if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  if (few)
+    return type == ET_F32 ? append_as<uint32_t, 64>(vec, a, blocks, stream) : append_as<uint16_t, 64>(vec, a, blocks, stream);
+  return type == ET_F32 ? append_as<uint32_t, 256>(vec, a, blocks, stream) : append_as<uint16_t, 256>(vec, a, blocks, stream);
+}
+
+hipError_t launch_kv_read(const KvCache& c, const KvBatch& bt, int type, const KvRows& k_out, const KvRows& v_out,
+                          hipStream_t stream) {
+  ReadArgs a = {c, bt, k_out, v_out, 0, 0};
+  a.seg_log2 = c.page_log2 < 6 ? c.page_log2 : 6;
+  const int S = 1 << a.seg_log2;
+  a.segs = static_cast<int>((static_cast<int64_t>(bt.max_new) + S - 2) / S + 1);
+  const int64_t blocks = static_cast<int64_t>(bt.B) * a.segs * c.Hkv * 2;
+  if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  const bool vec = aligned_rows(k_out, type) && aligned_rows(v_out, type);
+  const dim3 grid(static_cast<uint32_t>(blocks));
+  if (type == ET_F32) {
+    if (vec) kv_read_kernel<uint32_t, true><<<grid, 256, 0, stream>>>(a);
+    else kv_read_kernel<uint32_t, false><<<grid, 256, 0, stream>>>(a);
+  } else {
+    if (vec) kv_read_kernel<uint16_t, true><<<grid, 256, 0, stream>>>(a);
+    else kv_read_kernel<uint16_t, false><<<grid, 256, 0, stream>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace crvq
