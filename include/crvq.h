@@ -416,7 +416,8 @@ crvq_status crvq_dequant_gemv(int64_t M, int64_t N, int64_t n_crit, const uint8_
  *   v_cache  int8 [n_pages][Hkv][D][page]      value of slot s: v_scale * v_cache[.][h][:][s]
  *   k_scale, v_scale  float [n_pages][Hkv]     one scale for a head's tokens in a page
  * (values are stored transposed, so that both products of attention read
- * their operand along the contracted index).  Both arrays 16-byte aligned.
+ * their operand along the contracted index).  Both arrays 16-byte aligned;
+ * scales are not negative.
  * Token t of sequence b is in slot t % page of page block_table[b * ld_table +
  * t / page].  A page may belong to several sequences as long as no call
  * appends to it.
@@ -432,6 +433,7 @@ crvq_status crvq_dequant_gemv(int64_t M, int64_t N, int64_t n_crit, const uint8_
  * h * Hq/Hkv .. share key head h.  Element type CRVQ_F32 or CRVQ_BF16.
  * ------------------------------------------------------------------------- */
 #define CRVQ_KV_MAX_D 256
+#define CRVQ_KV_MAX_LEN (1 << 30) /* tokens of a sequence; a longer kv_len counts as one past its block table */
 
 /* crvq_kv_append -- rotates, quantizes and stores the new keys and values, and
  * rotates the queries, in one launch.
@@ -488,10 +490,10 @@ crvq_status crvq_kv_read(int32_t B, int32_t Hkv, int32_t D, int32_t page, int64_
  * strides; it may be q itself (same strides), and may not overlap it otherwise.
  * Arithmetic: a query row is held as fixed-point digits (16 bits below its
  * largest element for CRVQ_BF16, 24 for CRVQ_F32) whose products with the key
- * codes are exact; softmax statistics and sums are fp32; weights enter the
- * product with the values rounded to fp16 (CRVQ_BF16) or to a pair of fp16 (CRVQ_F32).
+ * codes are exact; softmax statistics and sums are fp32; for CRVQ_BF16 weights enter the
+ * product with the values rounded to fp16 (where that would lose bits of a small one, to 16 bits).
  * A row with a NaN or infinite query element is NaN, as is a row that sees a
- * page outside [0, n_pages) or a page whose scale is not finite.  Rows of a sequence
+ * page outside [0, n_pages) or a page with a scale that is negative or not finite.  Rows of a sequence
  * with kv_len[b] < 0 or > ld_table * page are NaN, as are the first max_new rows of one
  * with more than max_new; a sequence whose rows are not within [0, n_tokens] is
  * left out.  Deterministic.

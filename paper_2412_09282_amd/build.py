@@ -4,7 +4,8 @@
 
 Each kernel file compiles on its own; the screen kernels additionally get
 -fno-honor-nans (lets min/med3 run without NaN canonicalisation; inputs must be
-finite) and the VGPR form of MFMA (results land in VGPRs, no accumulator copies).
+finite) and, like the attention, the VGPR form of MFMA (results land in VGPRs, no
+accumulator copies).
 """
 from __future__ import annotations
 
@@ -35,7 +36,7 @@ SOURCES = {
     "k_refine.hip": [],
     "k_hinv.hip": [],
     "k_kv.hip": [],
-    "k_attn.hip": [],
+    "k_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "k_w4.hip": [],
 }
 

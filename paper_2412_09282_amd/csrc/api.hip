@@ -955,7 +955,8 @@ crvq_status crvq_kv_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int
                               kv_len, max_new, n_tokens, dtype, fn, &c, &bt);
   if (s) return s;
   if (Hq < 1 || Hq % Hkv) return fail(CRVQ_ERR_INVALID, "%s: Hq = %d is not a multiple of Hkv = %d", fn, Hq, Hkv);
-  if (max_kv < 0) return fail(CRVQ_ERR_INVALID, "%s: max_kv < 0", fn);
+  if (max_kv < 0 || max_kv > CRVQ_KV_MAX_LEN)
+    return fail(CRVQ_ERR_INVALID, "%s: max_kv = %d outside [0, 2^30]", fn, max_kv);
   if (!std::isfinite(scale)) return fail(CRVQ_ERR_INVALID, "%s: scale is not finite", fn);
   if (window < 0 || (window && !causal)) return fail(CRVQ_ERR_INVALID, "%s: window < 0, or a window without causal", fn);
   if (B == 0 || max_new == 0 || n_tokens == 0) return CRVQ_OK;

@@ -23,7 +23,7 @@ __device__ __forceinline__ KvSeq kv_seq(const KvBatch& bt, int b, int page_log2)
   s.len = bt.kv_len[b];
   s.in_rows = r0 >= 0 && r1 >= r0 && r1 <= bt.n_tokens;
   s.n = s.in_rows ? r1 - r0 : 0;
-  s.ok = s.in_rows && s.n <= bt.max_new && s.len >= 0 && s.len <= (bt.ld_table << page_log2);
+  s.ok = s.in_rows && s.n <= bt.max_new && s.len >= 0 && s.len <= CRVQ_KV_MAX_LEN && s.len <= (bt.ld_table << page_log2);
   return s;
 }
 
