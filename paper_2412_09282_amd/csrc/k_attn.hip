@@ -431,7 +431,7 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnArgs a) {
       }
     } else {
       if (a.o_vec) {
-        *reinterpret_cast<uint2*>(out) = make_uint2(f_bf16(x[0]) | f_bf16(x[1]) << 16, f_bf16(x[2]) | f_bf16(x[3]) << 16);
+        *reinterpret_cast<uint2*>(out) = make_uint2(f_bf16x2(x[0], x[1]), f_bf16x2(x[2], x[3]));
       } else {
         for (int k = 0; k < 4; ++k) out[k] = static_cast<T>(f_bf16(x[k]));
       }
@@ -480,42 +480,47 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnArgs a) {
   }
 }
 
-// Joins the splits of one (row, head): 256 threads, 4 elements each, in groups that share the splits.
+// Joins the splits of one (row, head): the factors of the splits first, a thread each, then 4 elements a thread in
+// groups that share the splits.
+constexpr int kSplits = 256;
 template <typename T>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(const AttnArgs a) {
   __shared__ __align__(16) at_f4 part[256];
-  __shared__ float part_l[256];
-  int64_t item = blockIdx.x;
+  __shared__ float factor[kSplits], red[8];
+  const int tid = threadIdx.x;
+  uint32_t item = blockIdx.x;
   const int h = static_cast<int>(item % a.Hq);
   item /= a.Hq;
   const int i = static_cast<int>(item % a.bt.max_new), b = static_cast<int>(item / a.bt.max_new);
   const KvSeq sq = kv_seq(a.bt, b, a.c.page_log2);
   if (i >= sq.n) return;
-  const int per = a.c.D >> 2, groups = 256 / per;
-  const int g = threadIdx.x / per, d = (threadIdx.x - g * per) * 4;
   const int64_t stride = static_cast<int64_t>(a.bt.B) * a.bt.max_new * a.Hq;
   const int64_t at = (static_cast<int64_t>(b) * a.bt.max_new + i) * a.Hq + h;
-  float m = -kInf;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.pm[s * stride + at]);
-  float l = 0.f;
+  // a split that saw nothing has l = 0 and stored no output; a NaN goes on into l
+  const float ms = tid < a.splits ? a.pm[tid * stride + at] : -kInf, ls = tid < a.splits ? a.pl[tid * stride + at] : 0.f;
+  float m = ls == 0.f ? -kInf : ms;
+  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if ((tid & 63) == 0) red[tid >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const float f = ls == 0.f ? 0.f : ls == ls ? __builtin_amdgcn_exp2f(ms - m) : ls;
+  float l = f == f ? f * ls : f;
+  for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
+  if ((tid & 63) == 0) red[4 + (tid >> 6)] = l;
+  if (tid < kSplits) factor[tid] = f == f ? f : 0.f;
+  __syncthreads();
+  l = (red[4] + red[5]) + (red[6] + red[7]);
+  const int per = a.c.D >> 2, groups = 256 / per, g = tid / per, d = (tid - g * per) * 4;
   at_f4 y = {0.f, 0.f, 0.f, 0.f};
   if (g < groups) {
-    for (int s = g; s < a.splits; s += groups) {
-      const float ll = a.pl[s * stride + at];
-      if (ll == 0.f) continue;  // saw nothing and stored no output; a NaN goes on
-      const float f = __builtin_amdgcn_exp2f(a.pm[s * stride + at] - m);
-      l = fmaf(f, ll, l);
-      if (ll == ll) y += f * *reinterpret_cast<const at_f4*>(a.po + (s * stride + at) * a.c.D + d);
-    }
+#pragma unroll 4
+    for (int s = g; s < a.splits; s += groups)
+      if (factor[s] != 0.f) y += factor[s] * *reinterpret_cast<const at_f4*>(a.po + (s * stride + at) * a.c.D + d);
   }
-  part[threadIdx.x] = y;
-  part_l[threadIdx.x] = l;
+  part[tid] = y;
   __syncthreads();
   if (g != 0) return;
-  for (int s = 1; s < groups; ++s) {
-    y += part[s * per + threadIdx.x];
-    l += part_l[s * per + threadIdx.x];
-  }
+  for (int s = 1; s < groups; ++s) y += part[s * per + tid];
   const float bad = l - l;  // 0, or NaN
   const int64_t row = sq.row0 + i;
 #pragma unroll
@@ -547,8 +552,8 @@ AttnPlan plan_attention(int B, int Hq, int Hkv, int max_new, int max_kv) {
   p.tiles = static_cast<int>(cdiv(cols, p.prompt ? 64 * kPromptBlocks : 16));
   const int64_t groups = static_cast<int64_t>(B) * Hkv * p.tiles;
   const int64_t most = cdiv(max_kv, kShare), want = cdiv(kWorkgroups, groups);
-  p.splits = static_cast<int>(want < most ? want : most);
-  if (p.splits < 1) p.splits = 1;
+  const int64_t n = want < most ? want : most;
+  p.splits = static_cast<int>(n < 1 ? 1 : n > kSplits ? kSplits : n);
   return p;
 }
 

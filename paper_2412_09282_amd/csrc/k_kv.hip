@@ -2,9 +2,10 @@
 //
 // Append: one workgroup owns one head of one page of keys or of values and the new tokens that fall into
 // it, so the page's scale has one writer.  It takes the largest magnitude of its rotated elements, settles
-// the scale, brings older codes to it if it grew, and stores the new codes; the elements are read twice,
-// the second time from the caches.  Values are stored transposed: whole runs of 16 slots go through an LDS
-// tile and leave as 16-byte stores, single tokens as bytes.  The same launch rotates the queries.
+// the scale, brings older codes to it if it grew, and stores the new codes; the elements stay in registers meanwhile
+// (those of long pages past the first kKept chunks of a thread are read again).  Values are stored transposed: the
+// new tokens go through an LDS tile and leave as 16-byte runs of slots, a few of them as bytes.  The same launch
+// rotates the queries, a workgroup a row.
 #include "kv_common.h"
 
 namespace crvq {
@@ -60,10 +61,10 @@ __device__ __forceinline__ void st8(T* p, const float (&x)[8]) {
     reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
   } else {
     uint4 a;
-    a.x = f_bf16(x[0]) | (f_bf16(x[1]) << 16);
-    a.y = f_bf16(x[2]) | (f_bf16(x[3]) << 16);
-    a.z = f_bf16(x[4]) | (f_bf16(x[5]) << 16);
-    a.w = f_bf16(x[6]) | (f_bf16(x[7]) << 16);
+    a.x = f_bf16x2(x[0], x[1]);
+    a.y = f_bf16x2(x[2], x[3]);
+    a.z = f_bf16x2(x[4], x[5]);
+    a.w = f_bf16x2(x[6], x[7]);
     *reinterpret_cast<uint4*>(p) = a;
   }
 }
@@ -128,18 +129,20 @@ __device__ __forceinline__ void rotated8(const T* row, int e0, const KvRotation&
   }
 }
 
-template <int NT>
+// How a head's row is cut into units, each read by one thread before it writes (so q_out may be q): chunks of eight
+// elements; the first chunks of a rotation by halves together with their partner chunks; or, where chunks are not
+// aligned or the halves are not whole chunks, single pairs and elements.
+enum Units : int { kChunks, kPairs, kSingle };
+__host__ __device__ inline int units_of(int kind, int D, int r) {
+  return kind == kSingle ? D - r : kind == kPairs ? (D - r) >> 3 : D >> 3;
+}
+
 __device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t* lds) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o)));
-  if (NT > 64) {
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
-    __syncthreads();
-    m = lds[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) m = max(m, lds[w]);
-  }
-  return m;
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
+  __syncthreads();
+  return max(max(lds[0], lds[1]), max(lds[2], lds[3]));
 }
 
 __device__ __forceinline__ uint32_t rescale4(uint32_t c, float f) {
@@ -157,31 +160,25 @@ __device__ __forceinline__ uint32_t quantize1(float x, float scale) {
   return static_cast<uint32_t>(static_cast<int>(q)) & 255u;
 }
 
+constexpr int kThreads = 256;
+constexpr int kKept = 4;   // chunks of new elements a thread keeps between the two uses: pages of 64 x 128 in registers
+constexpr int kFew = 16;   // new tokens below which values are stored as bytes
+
 struct AppendArgs {
   KvCache c;
   KvBatch bt;
   KvRows k, v, q, q_out;
   KvRotation rt;
   int Hq;
-  int64_t kv_blocks;  // B * pages * Hkv * 2 workgroups of pages; the queries' follow
+  int64_t kv_blocks;  // B * pages * Hkv * 2 workgroups of pages; one a row of queries follows
   int pages;          // pages a sequence's new tokens may touch
+  int units;          // of the queries
 };
 
-template <typename T, bool VEC, int NT>
-__device__ __forceinline__ void rotate_queries(const AppendArgs& a, int64_t block) {
+// One row of queries: a thread's unit is the same for all of its heads where it can be, and so are its angles.
+template <typename T, bool VEC>
+__device__ __forceinline__ void rotate_queries(const AppendArgs& a, int row) {
   const int D = a.c.D, r = a.rt.cos ? a.rt.rot >> 1 : 0;
-  const bool halves = r && !a.rt.interleaved;
-  // a unit is what one thread reads before it writes, so q_out may be q: a chunk and its partner chunk, or
-  // single pairs where the halves are not whole chunks
-  const bool single = !VEC || (halves && (r & 7));
-  const int per = single ? D - r : (halves ? D - r : D) >> 3;
-  const int64_t u = block * NT + threadIdx.x;
-  const int64_t head = u / per;
-  if (head >= a.bt.n_tokens * a.Hq) return;
-  const int unit = static_cast<int>(u - head * per);
-  const int row = static_cast<int>(head / a.Hq), h = static_cast<int>(head - static_cast<int64_t>(row) * a.Hq);
-  const T* in = static_cast<const T*>(a.q.p) + row * a.q.tok + h * a.q.head;
-  T* out = static_cast<T*>(a.q_out.p) + row * a.q_out.tok + h * a.q_out.head;
   Angles an = {nullptr, nullptr, 0};
   if (r) {
     int place = 0;
@@ -198,43 +195,79 @@ __device__ __forceinline__ void rotate_queries(const AppendArgs& a, int64_t bloc
     }
     an = angles(a.rt, row, place);
   }
-  if (single) {
-    if (unit < r) {
-      const int e = a.rt.interleaved ? 2 * unit : unit, f = a.rt.interleaved ? e + 1 : e + r;
-      float x = ld1(in + e), y = ld1(in + f);
-      turn(an, unit, x, y);
-      st1(out + e, x);
-      st1(out + f, y);
-    } else {
-      out[unit + r] = in[unit + r];
+  const int per = units_of(a.units, D, r);
+  const T* in0 = static_cast<const T*>(a.q.p) + row * a.q.tok;
+  T* out0 = static_cast<T*>(a.q_out.p) + row * a.q_out.tok;
+  if (a.units == kPairs && kThreads % per == 0 && (kThreads / per) * 4 >= a.Hq) {  // angles once, up to four heads
+    const int unit = threadIdx.x % per, e0 = unit * 8 + (unit * 8 >= r ? r : 0);
+    const bool pair = e0 < r;
+    float cs[8], sn[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      cs[i] = pair ? (an.ok ? an.c[e0 + i] : __uint_as_float(0x7fc00000u)) : 1.f;
+      sn[i] = pair && an.ok ? an.s[e0 + i] : 0.f;
+    }
+    for (int h = threadIdx.x / per; h < a.Hq; h += kThreads / per) {
+      const T* in = in0 + h * a.q.head;
+      T* out = out0 + h * a.q_out.head;
+      float x[8], y[8];
+      ld8<T, VEC>(in + e0, x);
+      if (pair) {
+        ld8<T, VEC>(in + e0 + r, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float u = x[i] * cs[i] - y[i] * sn[i], w = y[i] * cs[i] + x[i] * sn[i];
+          x[i] = u;
+          y[i] = w;
+        }
+        st8<T, VEC>(out + e0 + r, y);
+      }
+      st8<T, VEC>(out + e0, x);
     }
     return;
   }
-  const int e0 = unit * 8 + (halves && unit * 8 >= r ? r : 0);
-  float x[8], y[8];
-  if (halves && e0 < r) {
-    ld8<T, VEC>(in + e0, x);
-    ld8<T, VEC>(in + e0 + r, y);
+  for (int u = threadIdx.x; u < a.Hq * per; u += kThreads) {
+    const int h = u / per, unit = u - h * per;
+    const T* in = in0 + h * a.q.head;
+    T* out = out0 + h * a.q_out.head;
+    if (a.units == kSingle) {
+      if (unit < r) {
+        const int e = a.rt.interleaved ? 2 * unit : unit, f = a.rt.interleaved ? e + 1 : e + r;
+        float x = ld1(in + e), y = ld1(in + f);
+        turn(an, unit, x, y);
+        st1(out + e, x);
+        st1(out + f, y);
+      } else {
+        out[unit + r] = in[unit + r];
+      }
+      continue;
+    }
+    const int e0 = unit * 8 + (a.units == kPairs && unit * 8 >= r ? r : 0);
+    float x[8], y[8];
+    if (a.units == kPairs && e0 < r) {
+      ld8<T, VEC>(in + e0, x);
+      ld8<T, VEC>(in + e0 + r, y);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn(an, e0 + i, x[i], y[i]);
-    st8<T, VEC>(out + e0, x);
-    st8<T, VEC>(out + e0 + r, y);
-  } else {
-    rotated8<T, VEC>(in, e0, a.rt, an, x);
-    st8<T, VEC>(out + e0, x);
+      for (int i = 0; i < 8; ++i) turn(an, e0 + i, x[i], y[i]);
+      st8<T, VEC>(out + e0, x);
+      st8<T, VEC>(out + e0 + r, y);
+    } else {
+      rotated8<T, VEC>(in, e0, a.rt, an, x);
+      st8<T, VEC>(out + e0, x);
+    }
   }
 }
 
-template <typename T, bool VEC, int NT>
-__global__ __launch_bounds__(NT) void kv_append_kernel(const AppendArgs a) {
-  __shared__ uint32_t red[8];
-  __shared__ __align__(16) uint8_t tile[NT > 64 ? CRVQ_KV_MAX_D * kTileLd : 16];
+template <typename T, bool VEC>
+__global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a) {
+  __shared__ uint32_t red[4];
+  extern __shared__ __align__(16) uint8_t tile[];  // [D][page + 4]
   if (blockIdx.x >= a.kv_blocks) {
-    rotate_queries<T, VEC, NT>(a, static_cast<int64_t>(blockIdx.x) - a.kv_blocks);
+    rotate_queries<T, VEC>(a, static_cast<int>(blockIdx.x - a.kv_blocks));
     return;
   }
   const int tid = threadIdx.x, D = a.c.D, P = 1 << a.c.page_log2;
-  int64_t item = blockIdx.x;
+  uint32_t item = blockIdx.x;
   const bool values = item & 1;
   item >>= 1;
   const int h = static_cast<int>(item % a.c.Hkv);
@@ -252,6 +285,8 @@ __global__ __launch_bounds__(NT) void kv_append_kernel(const AppendArgs a) {
   const T* base = static_cast<const T*>(src.p) + h * src.head;
   const int cpr = D >> 3, chunks = (hi - lo) * cpr;
   const int row_lo = sq.row0 + t0 + lo - first;
+  float* sp = (values ? a.c.v_scale : a.c.k_scale) + page * a.c.Hkv + h;
+  const float old = *sp;
 
   auto load = [&](int c, int& slot, int& e0, float (&x)[8]) {
     const int i = c / cpr;
@@ -264,88 +299,95 @@ __global__ __launch_bounds__(NT) void kv_append_kernel(const AppendArgs a) {
     else
       rotated8<T, VEC>(r, e0, a.rt, a.rt.cos ? angles(a.rt, row, t0 + slot) : Angles{nullptr, nullptr, 0}, x);
   };
+  auto largest = [](const float (&x)[8], uint32_t m) {  // magnitude as bits: a NaN is larger than every number
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+    return m;
+  };
 
-  uint32_t m = 0;  // largest magnitude, as bits: a NaN is larger than every number
-  for (int c = tid; c < chunks; c += NT) {
+  uint32_t m = 0;
+  float kept[kKept][8];
+  int slots[kKept], at[kKept];
+#pragma unroll
+  for (int i = 0; i < kKept; ++i)
+    if (tid + i * kThreads < chunks) {
+      load(tid + i * kThreads, slots[i], at[i], kept[i]);
+      m = largest(kept[i], m);
+    }
+  for (int c = tid + kKept * kThreads; c < chunks; c += kThreads) {
     int slot, e0;
     float x[8];
     load(c, slot, e0, x);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+    m = largest(x, m);
   }
-  m = block_max<NT>(m, red);
-  float* sp = (values ? a.c.v_scale : a.c.k_scale) + page * a.c.Hkv + h;
+  m = block_max(m, red);
   const int64_t head_at = (page * a.c.Hkv + h) * (static_cast<int64_t>(D) << a.c.page_log2);
   int8_t* codes = (values ? a.c.v : a.c.k) + head_at;
   const bool finite = m < 0x7f800000u;
   float scale = finite ? fmaxf(__uint_as_float(m) / 127.f, kMinScale) : __uint_as_float(0x7fc00000u);
   if (lo > 0) {
-    const float old = *sp;
     if (finite && !(scale > old)) scale = old;
     if (scale > old) {  // the older codes move to the larger scale, 16 at a time
       const float f = old / scale;
-      const int rows = values ? D : lo, units = values ? (lo + 15) >> 4 : D >> 4;
-      for (int u = tid; u < rows * units; u += NT) {
-        const int r = u / units;
-        uint4* at = reinterpret_cast<uint4*>(codes + (values ? r << a.c.page_log2 : r * D)) + (u - r * units);
-        uint4 w = *at;
+      const int per = values ? (lo + 15) >> 4 : D >> 4, n = (values ? D : lo) * per;
+#pragma unroll 4
+      for (int u = tid; u < n; u += kThreads) {
+        const int r = u / per;
+        uint4* to = reinterpret_cast<uint4*>(codes + (values ? r << a.c.page_log2 : r * D)) + (u - r * per);
+        uint4 w = *to;
         w.x = rescale4(w.x, f);
         w.y = rescale4(w.y, f);
         w.z = rescale4(w.z, f);
         w.w = rescale4(w.w, f);
-        *at = w;
+        *to = w;
       }
+      __syncthreads();  // before new codes go into the words rewritten here
     }
-    __syncthreads();  // every thread has the old scale, and the older codes are in place
   }
-  if (tid == 0) *sp = scale;
+  if (tid == 0) *sp = scale;  // every thread read the old one before block_max
   const bool number = scale == scale;
+  const bool tiled = values && hi - lo >= kFew;
+  const int tile_ld = P + 4;
 
-  if (!values || NT == 64) {
-    for (int c = tid; c < chunks; c += NT) {
-      int slot, e0;
-      float x[8];
-      load(c, slot, e0, x);
-      uint32_t q[8];
+  auto store = [&](int slot, int e0, const float (&x)[8]) {
+    uint32_t q[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) q[i] = number ? quantize1(x[i], scale) : 0u;
-      if (!values) {
-        uint2 w;
-        w.x = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
-        w.y = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
-        *reinterpret_cast<uint2*>(codes + slot * D + e0) = w;
-      } else {
+    for (int i = 0; i < 8; ++i) q[i] = number ? quantize1(x[i], scale) : 0u;
+    if (!values) {
+      uint2 w;
+      w.x = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
+      w.y = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
+      *reinterpret_cast<uint2*>(codes + slot * D + e0) = w;
+    } else if (tiled) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) codes[((e0 + i) << a.c.page_log2) + slot] = static_cast<int8_t>(q[i]);
-      }
+      for (int i = 0; i < 8; ++i) tile[(e0 + i) * tile_ld + slot] = static_cast<uint8_t>(q[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) codes[((e0 + i) << a.c.page_log2) + slot] = static_cast<int8_t>(q[i]);
     }
-    return;
+  };
+#pragma unroll
+  for (int i = 0; i < kKept; ++i)
+    if (tid + i * kThreads < chunks) store(slots[i], at[i], kept[i]);
+  for (int c = tid + kKept * kThreads; c < chunks; c += kThreads) {
+    int slot, e0;
+    float x[8];
+    load(c, slot, e0, x);
+    store(slot, e0, x);
   }
-  // values of many tokens: segments of kSeg slots through the tile
-  for (int s0 = lo & ~(kSeg - 1); s0 < hi; s0 += kSeg) {
-    const int from = max(lo, s0), to = min(hi, s0 + kSeg);
-    __syncthreads();
-    for (int c = (from - lo) * cpr + tid; c < (to - lo) * cpr; c += NT) {
-      int slot, e0;
-      float x[8];
-      load(c, slot, e0, x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        tile[(e0 + i) * kTileLd + slot - s0] = static_cast<uint8_t>(number ? quantize1(x[i], scale) : 0u);
-    }
-    __syncthreads();
-    const int runs = (to - s0 + 15) >> 4;
-    for (int u = tid; u < D * runs; u += NT) {
-      const int d = u / runs, g = (u - d * runs) * 16;
-      const uint8_t* t = tile + d * kTileLd + g;
-      int8_t* out = codes + (d << a.c.page_log2) + s0 + g;
-      if (s0 + g >= from && s0 + g + 16 <= to) {
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(t);
-        *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
-      } else {
-        for (int i = 0; i < 16; ++i)
-          if (s0 + g + i >= from && s0 + g + i < to) out[i] = static_cast<int8_t>(t[i]);
-      }
+  if (!tiled) return;
+  __syncthreads();
+  const int run0 = lo >> 4, runs = ((hi + 15) >> 4) - run0;  // of 16 slots
+  for (int u = tid; u < D * runs; u += kThreads) {
+    const int d = u / runs, g = (run0 + u - d * runs) * 16;
+    const uint8_t* t = tile + d * tile_ld + g;
+    int8_t* out = codes + (d << a.c.page_log2) + g;
+    if (g >= lo && g + 16 <= hi) {
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(t);
+      *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+      for (int i = 0; i < 16; ++i)
+        if (g + i >= lo && g + i < hi) out[i] = static_cast<int8_t>(t[i]);
     }
   }
 }
@@ -415,15 +457,6 @@ bool aligned_rows(const KvRows& r, int type) {
   return !r.p || ((reinterpret_cast<uintptr_t>(r.p) & 15) == 0 && r.tok % per == 0 && r.head % per == 0);
 }
 
-template <typename T, int NT>
-hipError_t append_as(bool vec, const AppendArgs& a, int64_t blocks, hipStream_t stream) {
-  if (vec)
-    kv_append_kernel<T, true, NT><<<dim3(static_cast<uint32_t>(blocks)), NT, 0, stream>>>(a);
-  else
-    kv_append_kernel<T, false, NT><<<dim3(static_cast<uint32_t>(blocks)), NT, 0, stream>>>(a);
-  return hipGetLastError();
-}
-
 }  // namespace
 
 hipError_t launch_kv_append(const KvCache& c, const KvBatch& bt, int type, const KvRows& k, const KvRows& v, int Hq,
@@ -433,17 +466,21 @@ hipError_t launch_kv_append(const KvCache& c, const KvBatch& bt, int type, const
   a.pages = static_cast<int>((static_cast<int64_t>(bt.max_new) + P - 2) / P + 1);
   a.kv_blocks = static_cast<int64_t>(bt.B) * a.pages * c.Hkv * 2;
   const bool vec = aligned_rows(k, type) && aligned_rows(v, type) && aligned_rows(q, type) && aligned_rows(q_out, type);
-  const bool few = bt.max_new <= 4;
-  const int nt = few ? 64 : 256;
-  const int64_t q_units = q.p ? bt.n_tokens * Hq * (vec ? c.D >> 3 : c.D) : 0;
   const int r = rt.cos ? rt.rot >> 1 : 0;
-  const bool single = !vec || (r && !rt.interleaved && (r & 7));
-  const int64_t per = single ? c.D - r : (r && !rt.interleaved ? c.D - r : c.D) >> 3;
-  const int64_t blocks = a.kv_blocks + (q_units ? cdiv(bt.n_tokens * Hq * per, nt) : 0);
+  const bool halves = r && !rt.interleaved;
+  a.units = !vec || (halves && (r & 7)) ? kSingle : halves ? kPairs : kChunks;
+  const int64_t blocks = a.kv_blocks + (q.p ? bt.n_tokens : 0);
   if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-  if (few)
-    return type == ET_F32 ? append_as<uint32_t, 64>(vec, a, blocks, stream) : append_as<uint16_t, 64>(vec, a, blocks, stream);
-  return type == ET_F32 ? append_as<uint32_t, 256>(vec, a, blocks, stream) : append_as<uint16_t, 256>(vec, a, blocks, stream);
+  const dim3 grid(static_cast<uint32_t>(blocks));
+  const size_t lds = bt.max_new < kFew ? 0 : static_cast<size_t>(c.D) * (P + 4);
+  if (type == ET_F32) {
+    if (vec) kv_append_kernel<uint32_t, true><<<grid, kThreads, lds, stream>>>(a);
+    else kv_append_kernel<uint32_t, false><<<grid, kThreads, lds, stream>>>(a);
+  } else {
+    if (vec) kv_append_kernel<uint16_t, true><<<grid, kThreads, lds, stream>>>(a);
+    else kv_append_kernel<uint16_t, false><<<grid, kThreads, lds, stream>>>(a);
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const KvCache& c, const KvBatch& bt, int type, const KvRows& k_out, const KvRows& v_out,

@@ -30,31 +30,58 @@ __device__ __forceinline__ float zero_at(const W4& w, int64_t r, int64_t g) {
   return w.zeros ? static_cast<float>(w.zeros[r * w.ld_z + g]) : 8.f;
 }
 
+// A workgroup's threads are 256 / L rows of L lanes, L a power of two, and L lanes walk a row in blocks of L: no
+// division.
+struct Lanes {
+  int log2;         // of L
+  int64_t blocks;   // of L units in a row
+};
+
 // ---- quantization: a lane owns eight columns (four bytes of codes), group / 8 lanes share a group -------
 template <typename T, typename TS>
-__global__ __launch_bounds__(256) void w4_quantize_kernel(const T* W, int64_t ldw, const W4 w, int64_t units, int64_t stored) {
-  const int64_t u = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;  // eight columns of a row
-  const int64_t r = u / units, j0 = (u - r * units) * 8;
+__global__ __launch_bounds__(256) void w4_quantize_kernel(const T* W, int64_t ldw, const W4 w, int vec, const Lanes ln,
+                                                          int64_t stored) {
+  const uint32_t rows = 256u >> ln.log2;
+  const int64_t band = blockIdx.x / static_cast<uint32_t>(ln.blocks), part = blockIdx.x % static_cast<uint32_t>(ln.blocks);
+  const int64_t r = band * rows + (threadIdx.x >> ln.log2);
+  const int64_t j0 = ((part << ln.log2) + (threadIdx.x & ((1 << ln.log2) - 1))) * 8;
   const bool in = r < w.M;
   float x[8];
   float lo = 0.f, hi = 0.f;
   bool finite = true;
+  const T* p = W + r * ldw + j0;
+  if (vec && in && j0 + 8 <= w.N) {
+    if constexpr (sizeof(T) == 4) {
+      const uint4 u = ld_stream(p), v = ld_stream(p + 4);
+      x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y); x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
+      x[4] = __uint_as_float(v.x); x[5] = __uint_as_float(v.y); x[6] = __uint_as_float(v.z); x[7] = __uint_as_float(v.w);
+    } else {
+      const uint4 u = ld_stream(p);
+      const uint32_t e[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(e[i] << 16);
+        x[2 * i + 1] = __uint_as_float(e[i] & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = in && j0 + i < w.N ? ld1(p + i) : 0.f;
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    x[i] = in && j0 + i < w.N ? ld1(W + r * ldw + j0 + i) : 0.f;
     finite &= fabsf(x[i]) < __uint_as_float(0x7f800000u);
     lo = fminf(lo, x[i]);
     hi = fmaxf(hi, x[i]);
   }
-  int bad = !finite;
+  if (!finite) hi = __uint_as_float(0x7f800000u);  // and so the scale is not finite
   for (int o = 1; o < 1 << (w.group_log2 - 3); o <<= 1) {
     lo = fminf(lo, __shfl_xor(lo, o));
     hi = fmaxf(hi, __shfl_xor(hi, o));
-    bad |= __shfl_xor(bad, o);
   }
   if (!in) return;
   float s = fmaxf(w.zeros ? (hi - lo) / 15.f : fmaxf(hi, -lo) / 7.f, kMinScale);
-  if (bad || !(s < __uint_as_float(0x7f800000u))) s = __uint_as_float(0x7fc00000u);
+  if (!(s < __uint_as_float(0x7f800000u))) s = __uint_as_float(0x7fc00000u);
   if (sizeof(TS) == 2) s = bf16_f(f_bf16(s));
   const bool number = s == s;
   const float z = !w.zeros ? 8.f : number ? fminf(fmaxf(rintf(-lo / s), 0.f), 15.f) : 0.f;
@@ -72,16 +99,32 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* W, int64_t ld
   }
 }
 
+// ---- reconstruction: a lane owns 16 bytes of the output, so that a wave stores 1 KB at once -------------------
 template <typename T, typename TS>
-__global__ __launch_bounds__(256) void w4_dequant_kernel(const W4 w, T* out, int64_t ldo, int64_t units) {
-  const int64_t u = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  const int64_t r = u / units, j0 = (u - r * units) * 8;
-  if (r >= w.M) return;
-  const uint32_t c = *reinterpret_cast<const uint32_t*>(w.codes + r * w.ld + (j0 >> 1));
+__global__ __launch_bounds__(256) void w4_dequant_kernel(const W4 w, T* out, int64_t ldo, int vec, const Lanes ln) {
+  constexpr int E = 16 / sizeof(T);
+  const uint32_t rows = 256u >> ln.log2;
+  const int64_t band = blockIdx.x / static_cast<uint32_t>(ln.blocks), part = blockIdx.x % static_cast<uint32_t>(ln.blocks);
+  const int64_t r = band * rows + (threadIdx.x >> ln.log2);
+  const int64_t j0 = ((part << ln.log2) + (threadIdx.x & ((1 << ln.log2) - 1))) * E;
+  if (r >= w.M || j0 >= w.N) return;
+  const uint8_t* p = w.codes + r * w.ld + (j0 >> 1);
+  const uint32_t c = E == 8 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
   const float s = scale_at<TS>(w, r, j0 >> w.group_log2), z = zero_at(w, r, j0 >> w.group_log2);
+  float x[E];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (j0 + i < w.N) st1(out + r * ldo + j0 + i, (static_cast<float>((c >> (4 * i)) & 15) - z) * s);
+  for (int i = 0; i < E; ++i) x[i] = (static_cast<float>((c >> (4 * i)) & 15) - z) * s;
+  T* o = out + r * ldo + j0;
+  if (vec && j0 + E <= w.N) {
+    if constexpr (E == 4)
+      st_stream(o, make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])));
+    else
+      st_stream(o, make_uint4(f_bf16x2(x[0], x[1]), f_bf16x2(x[2], x[3]), f_bf16x2(x[4], x[5]), f_bf16x2(x[6], x[7])));
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (j0 + i < w.N) st1(o + i, x[i]);
+  }
 }
 
 // ---- product ----------------------------------------------------------------------------------------------
@@ -315,46 +358,53 @@ __global__ __launch_bounds__(1024) void w4_gemv_kernel(const GemvArgs a) {
   }
 }
 
-hipError_t blocks_of(int64_t items, int per, dim3* grid) {
-  const int64_t n = cdiv(items, per);
+// L lanes for rows of `units`, at least `least` of them (a power of two), and the grid for M rows.
+hipError_t lanes_of(int64_t M, int64_t units, int least, Lanes* ln, dim3* grid) {
+  ln->log2 = 0;
+  while ((1 << ln->log2) < least || (ln->log2 < 8 && (int64_t{1} << ln->log2) < units)) ++ln->log2;
+  ln->blocks = cdiv(units, int64_t{1} << ln->log2);
+  const int64_t n = cdiv(M, 256 >> ln->log2) * ln->blocks;
   if (n > 0x7fffffffLL) return hipErrorInvalidConfiguration;
   *grid = dim3(static_cast<uint32_t>(n));
   return hipSuccess;
 }
 
-}  // namespace
+bool aligned16(const void* p, int64_t ld, int es) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * es % 16 == 0; }
 
-hipError_t launch_w4_quantize(const void* W, int64_t ldw, int type, const W4& w, hipStream_t stream) {
-  // the units of a row are padded to whole groups of lanes, so that no group straddles two waves; codes are
-  // stored up to a multiple of 16 bytes, which every row stride holds
-  const int64_t span = w.group_log2 > 5 ? int64_t{1} << w.group_log2 : 32, stored = cdiv(w.N, 32) * 32;
-  const int64_t units = cdiv(w.N, span) * span / 8;
+template <typename T, typename TS>
+hipError_t quantize_as(const void* W, int64_t ldw, const W4& w, hipStream_t stream) {
+  // codes are stored up to a multiple of 16 bytes, which every row stride holds; the lanes of a group stay together
+  const int64_t stored = cdiv(w.N, 32) * 32;
+  Lanes ln;
   dim3 grid;
-  const hipError_t e = blocks_of(w.M * units, 256, &grid);
+  const hipError_t e = lanes_of(w.M, stored / 8, 1 << (w.group_log2 - 3), &ln, &grid);
   if (e != hipSuccess) return e;
-  if (type == ET_F32) {
-    if (w.s_type == ET_F32) w4_quantize_kernel<uint32_t, uint32_t><<<grid, 256, 0, stream>>>(static_cast<const uint32_t*>(W), ldw, w, units, stored);
-    else w4_quantize_kernel<uint32_t, uint16_t><<<grid, 256, 0, stream>>>(static_cast<const uint32_t*>(W), ldw, w, units, stored);
-  } else {
-    if (w.s_type == ET_F32) w4_quantize_kernel<uint16_t, uint32_t><<<grid, 256, 0, stream>>>(static_cast<const uint16_t*>(W), ldw, w, units, stored);
-    else w4_quantize_kernel<uint16_t, uint16_t><<<grid, 256, 0, stream>>>(static_cast<const uint16_t*>(W), ldw, w, units, stored);
-  }
+  w4_quantize_kernel<T, TS><<<grid, 256, 0, stream>>>(static_cast<const T*>(W), ldw, w, aligned16(W, ldw, sizeof(T)), ln, stored);
   return hipGetLastError();
 }
 
-hipError_t launch_w4_dequant(const W4& w, void* out, int64_t ldo, int type, hipStream_t stream) {
-  const int64_t units = cdiv(w.N, 8);
+template <typename T, typename TS>
+hipError_t dequant_as(const W4& w, void* out, int64_t ldo, hipStream_t stream) {
+  Lanes ln;
   dim3 grid;
-  const hipError_t e = blocks_of(w.M * units, 256, &grid);
+  const hipError_t e = lanes_of(w.M, cdiv(w.N, 16 / sizeof(T)), 1, &ln, &grid);
   if (e != hipSuccess) return e;
-  if (type == ET_F32) {
-    if (w.s_type == ET_F32) w4_dequant_kernel<uint32_t, uint32_t><<<grid, 256, 0, stream>>>(w, static_cast<uint32_t*>(out), ldo, units);
-    else w4_dequant_kernel<uint32_t, uint16_t><<<grid, 256, 0, stream>>>(w, static_cast<uint32_t*>(out), ldo, units);
-  } else {
-    if (w.s_type == ET_F32) w4_dequant_kernel<uint16_t, uint32_t><<<grid, 256, 0, stream>>>(w, static_cast<uint16_t*>(out), ldo, units);
-    else w4_dequant_kernel<uint16_t, uint16_t><<<grid, 256, 0, stream>>>(w, static_cast<uint16_t*>(out), ldo, units);
-  }
+  w4_dequant_kernel<T, TS><<<grid, 256, 0, stream>>>(w, static_cast<T*>(out), ldo, aligned16(out, ldo, sizeof(T)), ln);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_w4_quantize(const void* W, int64_t ldw, int type, const W4& w, hipStream_t stream) {
+  if (type == ET_F32)
+    return w.s_type == ET_F32 ? quantize_as<uint32_t, uint32_t>(W, ldw, w, stream) : quantize_as<uint32_t, uint16_t>(W, ldw, w, stream);
+  return w.s_type == ET_F32 ? quantize_as<uint16_t, uint32_t>(W, ldw, w, stream) : quantize_as<uint16_t, uint16_t>(W, ldw, w, stream);
+}
+
+hipError_t launch_w4_dequant(const W4& w, void* out, int64_t ldo, int type, hipStream_t stream) {
+  if (type == ET_F32)
+    return w.s_type == ET_F32 ? dequant_as<uint32_t, uint32_t>(w, out, ldo, stream) : dequant_as<uint32_t, uint16_t>(w, out, ldo, stream);
+  return w.s_type == ET_F32 ? dequant_as<uint16_t, uint32_t>(w, out, ldo, stream) : dequant_as<uint16_t, uint16_t>(w, out, ldo, stream);
 }
 
 size_t w4_gemv_ws_bytes(int64_t, int64_t, int64_t) { return 0; }

@@ -29,11 +29,12 @@ __device__ __forceinline__ KvSeq kv_seq(const KvBatch& bt, int b, int page_log2)
 
 __device__ __forceinline__ float bf16_f(uint32_t bits16) { return __uint_as_float(bits16 << 16); }
 
-// fp32 to bf16 bits, round to nearest even; a NaN stays one.
-__device__ __forceinline__ uint32_t f_bf16(float f) {
-  const uint32_t u = __float_as_uint(f);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return (u >> 16) | 0x40u;
-  return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+// fp32 to bf16, round to nearest even (a NaN stays one): two at a time, and one.
+typedef float kv_f2 __attribute__((ext_vector_type(2)));
+typedef __bf16 kv_b2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t f_bf16x2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((kv_f2{a, b}), kv_b2));
 }
+__device__ __forceinline__ uint32_t f_bf16(float f) { return f_bf16x2(f, 0.f) & 0xffffu; }
 
 }  // namespace crvq
