@@ -907,7 +907,7 @@ crvq_status crvq_kv_append(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_
   const size_t page_bytes = static_cast<size_t>(n_pages) * Hkv * D * page, scales = static_cast<size_t>(n_pages) * Hkv * 4;
   if (overlaps(k_cache, page_bytes, v_cache, page_bytes) || overlaps(k_scale, scales, v_scale, scales))
     return fail(CRVQ_ERR_INVALID, "%s: the cache's arrays overlap", fn);
-  const KvRotation rt = {cos, sin, n_angles, positions, rot, interleaved ? 1 : 0};
+  const KvRotation rt = {cos, sin, n_angles, positions, rot, interleaved ? 1 : 0, 0};
   return hip_status(launch_kv_append(c, bt, dtype, {const_cast<void*>(k), k_tok, k_head}, {const_cast<void*>(v), v_tok, v_head},
                                      Hq, {const_cast<void*>(q), q_tok, q_head}, {q_out, qo_tok, qo_head}, rt,
                                      static_cast<hipStream_t>(stream)),

@@ -276,6 +276,7 @@ struct KvRotation {
   int64_t n_angles;
   const int32_t* positions;
   int rot, interleaved;
+  int vec;  // rows of cos and sin are 16-byte aligned (set by the launcher)
 };
 hipError_t launch_kv_append(const KvCache& c, const KvBatch& bt, int type, const KvRows& k, const KvRows& v, int Hq,
                             const KvRows& q, const KvRows& q_out, const KvRotation& rt, hipStream_t stream);

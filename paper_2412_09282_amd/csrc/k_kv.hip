@@ -84,6 +84,23 @@ __device__ __forceinline__ Angles angles(const KvRotation& rt, int row, int plac
   return a;
 }
 
+// The angles of pairs j .. j + 7 (j a multiple of 8).
+__device__ __forceinline__ void angles8(const KvRotation& rt, const Angles& an, int j, float (&c)[8], float (&s)[8]) {
+  if (rt.vec) {
+    const float4 c0 = reinterpret_cast<const float4*>(an.c + j)[0], c1 = reinterpret_cast<const float4*>(an.c + j)[1];
+    const float4 s0 = reinterpret_cast<const float4*>(an.s + j)[0], s1 = reinterpret_cast<const float4*>(an.s + j)[1];
+    c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
+    s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w; s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = an.c[j + i], s[i] = an.s[j + i];
+  }
+  if (!an.ok) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = __uint_as_float(0x7fc00000u);
+  }
+}
+
 // Pair j of a row, (a, b) -> (a c - b s, b c + a s).
 __device__ __forceinline__ void turn(const Angles& an, int j, float& a, float& b) {
   const float c = an.ok ? an.c[j] : __uint_as_float(0x7fc00000u), s = an.ok ? an.s[j] : 0.f;
@@ -102,18 +119,6 @@ __device__ __forceinline__ void rotated8(const T* row, int e0, const KvRotation&
 #pragma unroll
     for (int i = 0; i < 8; i += 2)
       if (e0 + i < rt.rot) turn(an, (e0 + i) >> 1, x[i], x[i + 1]);
-    return;
-  }
-  if (VEC && (r & 7) == 0) {  // the partners are a chunk too, and all eight are first or second elements
-    float y[8];
-    const bool first = e0 < r;
-    ld8<T, VEC>(row + (first ? e0 + r : e0 - r), y);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (first)
-        turn(an, e0 + i, x[i], y[i]);
-      else
-        turn(an, e0 - r + i, y[i], x[i]);
     return;
   }
 #pragma unroll
@@ -172,7 +177,7 @@ struct AppendArgs {
   int Hq;
   int64_t kv_blocks;  // B * pages * Hkv * 2 workgroups of pages; one a row of queries follows
   int pages;          // pages a sequence's new tokens may touch
-  int units;          // of the queries
+  int units, key_units;  // of the queries, of the keys
 };
 
 // One row of queries: a thread's unit is the same for all of its heads where it can be, and so are its angles.
@@ -202,11 +207,7 @@ __device__ __forceinline__ void rotate_queries(const AppendArgs& a, int row) {
     const int unit = threadIdx.x % per, e0 = unit * 8 + (unit * 8 >= r ? r : 0);
     const bool pair = e0 < r;
     float cs[8], sn[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      cs[i] = pair ? (an.ok ? an.c[e0 + i] : __uint_as_float(0x7fc00000u)) : 1.f;
-      sn[i] = pair && an.ok ? an.s[e0 + i] : 0.f;
-    }
+    if (pair) angles8(a.rt, an, e0, cs, sn);
     for (int h = threadIdx.x / per; h < a.Hq; h += kThreads / per) {
       const T* in = in0 + h * a.q.head;
       T* out = out0 + h * a.q_out.head;
@@ -299,6 +300,27 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
     else
       rotated8<T, VEC>(r, e0, a.rt, a.rt.cos ? angles(a.rt, row, t0 + slot) : Angles{nullptr, nullptr, 0}, x);
   };
+  // a unit of keys rotated by halves: two chunks, or one that is not rotated (e1 < 0)
+  const bool pairs = !values && a.key_units == kPairs;
+  const int r = pairs ? a.rt.rot >> 1 : 0, upt = units_of(kPairs, D, r), units = (hi - lo) * upt;
+  auto load_pair = [&](int u, int& slot, int& e0, int& e1, float (&x)[8], float (&y)[8]) {
+    const int i = u / upt, unit = u - i * upt;
+    e0 = unit * 8 + (unit * 8 >= r ? r : 0);
+    e1 = e0 < r ? e0 + r : -1;
+    slot = lo + i;
+    const T* row = base + (row_lo + i) * src.tok;
+    ld8<T, VEC>(row + e0, x);
+    if (e1 < 0) return;
+    ld8<T, VEC>(row + e1, y);
+    float cs[8], sn[8];
+    angles8(a.rt, angles(a.rt, row_lo + i, t0 + slot), e0, cs, sn);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float u2 = x[k] * cs[k] - y[k] * sn[k], w2 = y[k] * cs[k] + x[k] * sn[k];
+      x[k] = u2;
+      y[k] = w2;
+    }
+  };
   auto largest = [](const float (&x)[8], uint32_t m) {  // magnitude as bits: a NaN is larger than every number
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
@@ -309,16 +331,36 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
   float kept[kKept][8];
   int slots[kKept], at[kKept];
 #pragma unroll
-  for (int i = 0; i < kKept; ++i)
-    if (tid + i * kThreads < chunks) {
-      load(tid + i * kThreads, slots[i], at[i], kept[i]);
-      m = largest(kept[i], m);
+  for (int i = 0; i < kKept; ++i) at[i] = -1;
+  if (pairs) {
+#pragma unroll
+    for (int i = 0; i < kKept; i += 2)
+      if (tid + (i >> 1) * kThreads < units) {
+        load_pair(tid + (i >> 1) * kThreads, slots[i], at[i], at[i + 1], kept[i], kept[i + 1]);
+        slots[i + 1] = slots[i];
+        m = largest(kept[i], m);
+        if (at[i + 1] >= 0) m = largest(kept[i + 1], m);
+      }
+    for (int u = tid + kKept / 2 * kThreads; u < units; u += kThreads) {
+      int slot, e0, e1;
+      float x[8], y[8];
+      load_pair(u, slot, e0, e1, x, y);
+      m = largest(x, m);
+      if (e1 >= 0) m = largest(y, m);
     }
-  for (int c = tid + kKept * kThreads; c < chunks; c += kThreads) {
-    int slot, e0;
-    float x[8];
-    load(c, slot, e0, x);
-    m = largest(x, m);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kKept; ++i)
+      if (tid + i * kThreads < chunks) {
+        load(tid + i * kThreads, slots[i], at[i], kept[i]);
+        m = largest(kept[i], m);
+      }
+    for (int c = tid + kKept * kThreads; c < chunks; c += kThreads) {
+      int slot, e0;
+      float x[8];
+      load(c, slot, e0, x);
+      m = largest(x, m);
+    }
   }
   m = block_max(m, red);
   const int64_t head_at = (page * a.c.Hkv + h) * (static_cast<int64_t>(D) << a.c.page_log2);
@@ -368,12 +410,22 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
   };
 #pragma unroll
   for (int i = 0; i < kKept; ++i)
-    if (tid + i * kThreads < chunks) store(slots[i], at[i], kept[i]);
-  for (int c = tid + kKept * kThreads; c < chunks; c += kThreads) {
-    int slot, e0;
-    float x[8];
-    load(c, slot, e0, x);
-    store(slot, e0, x);
+    if (at[i] >= 0) store(slots[i], at[i], kept[i]);
+  if (pairs) {
+    for (int u = tid + kKept / 2 * kThreads; u < units; u += kThreads) {
+      int slot, e0, e1;
+      float x[8], y[8];
+      load_pair(u, slot, e0, e1, x, y);
+      store(slot, e0, x);
+      if (e1 >= 0) store(slot, e1, y);
+    }
+  } else {
+    for (int c = tid + kKept * kThreads; c < chunks; c += kThreads) {
+      int slot, e0;
+      float x[8];
+      load(c, slot, e0, x);
+      store(slot, e0, x);
+    }
   }
   if (!tiled) return;
   __syncthreads();
@@ -461,7 +513,7 @@ bool aligned_rows(const KvRows& r, int type) {
 
 hipError_t launch_kv_append(const KvCache& c, const KvBatch& bt, int type, const KvRows& k, const KvRows& v, int Hq,
                             const KvRows& q, const KvRows& q_out, const KvRotation& rt, hipStream_t stream) {
-  AppendArgs a = {c, bt, k, v, q, q_out, rt, Hq, 0, 0};
+  AppendArgs a = {c, bt, k, v, q, q_out, rt, Hq, 0, 0, 0, 0};
   const int P = 1 << c.page_log2;
   a.pages = static_cast<int>((static_cast<int64_t>(bt.max_new) + P - 2) / P + 1);
   a.kv_blocks = static_cast<int64_t>(bt.B) * a.pages * c.Hkv * 2;
@@ -469,6 +521,8 @@ hipError_t launch_kv_append(const KvCache& c, const KvBatch& bt, int type, const
   const int r = rt.cos ? rt.rot >> 1 : 0;
   const bool halves = r && !rt.interleaved;
   a.units = !vec || (halves && (r & 7)) ? kSingle : halves ? kPairs : kChunks;
+  a.key_units = a.units == kPairs ? kPairs : kChunks;
+  a.rt.vec = (r & 3) == 0 && ((reinterpret_cast<uintptr_t>(rt.cos) | reinterpret_cast<uintptr_t>(rt.sin)) & 15) == 0;
   const int64_t blocks = a.kv_blocks + (q.p ? bt.n_tokens : 0);
   if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
   const dim3 grid(static_cast<uint32_t>(blocks));
