@@ -491,7 +491,7 @@ crvq_status crvq_kv_read(int32_t B, int32_t Hkv, int32_t D, int32_t page, int64_
  * Arithmetic: a query row is held as fixed-point digits (16 bits below its
  * largest element for CRVQ_BF16, 24 for CRVQ_F32) whose products with the key
  * codes are exact; softmax statistics and sums are fp32; for CRVQ_BF16 weights enter the
- * product with the values rounded to fp16 (where that would lose bits of a small one, to 16 bits).
+ * product with the values rounded to 11 bits.
  * A row with a NaN or infinite query element is NaN, as is a row that sees a
  * page outside [0, n_pages) or a page with a scale that is negative or not finite.  Rows of a sequence
  * with kv_len[b] < 0 or > ld_table * page are NaN, as are the first max_new rows of one

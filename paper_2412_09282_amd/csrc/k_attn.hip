@@ -9,11 +9,12 @@
 //   O^T += V^T P^T on v_mfma_f32_16x16x32_f16: the value codes lie transposed in the cache, 16 tokens of an
 //     element in 16 bytes, and are widened to fp16 in registers (exact); the weights are rounded to fp16.  The page's
 //     value scale goes into the weights, relative to a power of two 2^e that follows the largest scale met so far.
-//     A step with a weight below fp16's normal numbers (2^-21 of the row's largest) takes its weights as
-//     two bf16 terms, whose range is fp32's, and so keeps 16 bits of every weight; fp32 queries take three terms always.
+//     Weights below fp16's normal numbers (2^-21 of the row's largest) are added in further passes over the step, 2^14
+//     times as large each, so that they keep their 11 bits too; a pass is taken only where there are any.  For fp32
+//     queries the weights are three bf16 terms, which hold all of their 24 bits.
 // The token in row 4 c + i of tile u is 16 c + 4 u + i: a lane (column r = lane % 16, quarter c = lane / 16) then
 // holds the scores of 16 consecutive tokens, which are exactly its operands of the second product and, pages being
-// multiples of 16, belong to one page.  Operands go from the cache to registers without LDS.
+// multiples of 16, belong to one page.
 #include "kv_common.h"
 
 namespace crvq {
@@ -107,157 +108,105 @@ __device__ __forceinline__ float elem(const T* p, int i) {
     return bf16_f(p[i]);
 }
 
-// DT tiles of 16 elements hold a head; a wave has 16 QB columns; WK waves of a workgroup share their columns and
-// take turns at the tokens, the others (4 / WK) have columns of their own.  SMALL: pages below 64 tokens.
-template <typename T, int DT, int QB, int WK, bool SMALL>
-__global__ __launch_bounds__(256) void kv_attention_kernel(const AttnArgs a) {
-  constexpr int DC = (DT + 3) / 4;                // 64-element chunks of a head
-  constexpr int NT = sizeof(T) == 4 ? 3 : 2;      // digits of a query element
-  constexpr int PT = sizeof(T) == 4 ? 3 : 2;      // bf16 terms of a weight
-  constexpr double kSteps = NT == 3 ? 8355711.0 : 32639.0;  // 127 in every digit
-  constexpr int kRow = DT * 16 + 4;               // floats of a column in LDS
-  __shared__ __align__(16) float join[WK > 1 ? WK * 16 * QB * kRow : 4];
-  __shared__ float join_m[WK > 1 ? WK * 16 * QB : 1], join_l[WK > 1 ? WK * 16 * QB : 1];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int r = lane & 15, c = lane >> 4;
-  const int D = a.c.D, pl2 = a.c.page_log2;
-
-  // which columns: tiles of a sequence last to first, so that the longest rows of a causal prompt start first
-  int64_t item = blockIdx.x;
-  const int hk = static_cast<int>(item % a.c.Hkv);
+// Which sequence, key head, split and tile of columns a workgroup has: tiles of a sequence last to first, so that the
+// longest rows of a causal prompt start first.
+struct Place {
+  int hk, b, split, tile;
+};
+__device__ __forceinline__ Place place_of(const AttnArgs& a) {
+  uint32_t item = blockIdx.x;
+  Place p;
+  p.hk = static_cast<int>(item % a.c.Hkv);
   item /= a.c.Hkv;
-  const int b = static_cast<int>(item % a.bt.B);
+  p.b = static_cast<int>(item % a.bt.B);
   item /= a.bt.B;
-  const int split = static_cast<int>(item % a.splits);
-  const int tile = a.tiles - 1 - static_cast<int>(item / a.splits);
-  const KvSeq sq = kv_seq(a.bt, b, pl2);
-  const int cols = min(sq.n, a.bt.max_new) * a.G;
-  const int col0 = (tile * (4 / WK) + (WK == 1 ? wave : 0)) * (16 * QB);
-  if (col0 >= cols) return;  // with WK > 1 all waves of the workgroup
-  const bool ok = sq.ok && (sq.len == 0 || a.c.n_pages > 0);
+  p.split = static_cast<int>(item % a.splits);
+  p.tile = a.tiles - 1 - static_cast<int>(item / a.splits);
+  return p;
+}
 
-  // queries: fixed point, 16 elements of a column and chunk in a lane
+// The state of a wave's 16 QB columns; DT tiles of 16 elements hold a head.
+template <typename T, int DT, int QB>
+struct Columns {
+  static constexpr int DC = (DT + 3) / 4;                            // 64-element chunks of a head
+  static constexpr int NT = sizeof(T) == 4 ? 3 : 2;                  // digits of a query element
+  static constexpr double kSteps = NT == 3 ? 8355711.0 : 32639.0;    // 127 in every digit
   at_i4 q[QB][DC][NT];
-  float step[QB];
-  int lo[QB], hi[QB];
-#pragma unroll
-  for (int n = 0; n < QB; ++n) {
-    const int col = min(col0 + n * 16 + r, cols - 1);  // columns past the last one repeat it
-    const int i = col / a.G, h = hk * a.G + col - i * a.G;
-    const T* row = static_cast<const T*>(a.q.p) + (sq.row0 + i) * a.q.tok + h * a.q.head;
-    uint32_t most = 0;
-#pragma unroll
-    for (int ch = 0; ch < DC; ++ch)
-      if (ch * 64 + c * 16 < D)
-        for (int e = 0; e < 16; ++e)
-          most = max(most, __float_as_uint(elem(row, ch * 64 + c * 16 + e)) & 0x7fffffffu);
-    most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 16)));
-    most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32)));
-    const bool finite = most < 0x7f800000u;
-    const double inv = finite && most ? (a.scale < 0.f ? -kSteps : kSteps) / static_cast<double>(__uint_as_float(most)) : 0.0;
-    step[n] = finite ? static_cast<float>(static_cast<double>(__uint_as_float(most)) / kSteps * fabs(static_cast<double>(a.scale)) *
-                                          static_cast<double>(kLog2e))
-                     : __uint_as_float(0x7fc00000u);
-#pragma unroll
-    for (int ch = 0; ch < DC; ++ch) {
-      uint32_t w[4][NT] = {};
-      if (finite && ch * 64 + c * 16 < D) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          digits<NT>(static_cast<int>(rint(static_cast<double>(elem(row, ch * 64 + c * 16 + e)) * inv)), e & 3, w[e >> 2]);
-      }
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        q[n][ch][t] = at_i4{static_cast<int>(w[0][t]), static_cast<int>(w[1][t]), static_cast<int>(w[2][t]), static_cast<int>(w[3][t])};
-    }
-    hi[n] = ok ? sq.len : 0;
-    lo[n] = 0;
-    if (a.causal) {
-      const int place = sq.len - sq.n + i;
-      hi[n] = min(hi[n], max(place + 1, 0));
-      if (a.window) lo[n] = max(place + 1 - a.window, 0);
-    }
-    if (lo[n] >= hi[n]) lo[n] = hi[n] = 0;
-  }
-  // the wave's tokens, and those that all of its columns see
-  int first = 0x7fffffff, last = 0, all_lo = 0, all_hi = 0x7fffffff;
-#pragma unroll
-  for (int n = 0; n < QB; ++n) {
-    if (hi[n] > 0) first = min(first, lo[n]);
-    last = max(last, hi[n]);
-    all_lo = max(all_lo, lo[n]);
-    all_hi = min(all_hi, hi[n]);
-  }
-  first = wave_min(first);
-  last = wave_max(last);
-  all_lo = wave_max(all_lo);
-  all_hi = wave_min(all_hi);
-  first = min(first, last) & ~(kTokens - 1);
-  if (a.splits > 1) {  // an equal share of the tokens, in whole rounds of the waves
-    const int span = (last - first + a.splits - 1) / a.splits, round = kTokens * WK;
-    const int share = (span + round - 1) / round * round;
-    const int64_t from = first + static_cast<int64_t>(split) * share;
-    first = static_cast<int>(from < last ? from : last);
-    last = min(last, first + share);
-  }
-  const int from = first + (WK > 1 ? wave * kTokens : 0);
-
+  float step[QB], m[QB], l[QB];
+  int lo[QB], hi[QB];                 // the tokens a column sees
+  int first, last, all_lo, all_hi;    // the tokens any of them sees, and those that all of them see
   at_f4 o[QB][DT];
-  float m[QB], l[QB];
-  int e = -126;  // exponent that value scales are taken relative to
-#pragma unroll
-  for (int n = 0; n < QB; ++n) {
-    m[n] = -kInf;
-    l[n] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[n][d] = at_f4{0.f, 0.f, 0.f, 0.f};
-  }
+  int e;  // exponent that value scales are taken relative to
 
-  const int32_t* table = a.bt.table + static_cast<int64_t>(b) * a.bt.ld_table;
-  // the page of the 16 tokens from t on: uniform unless pages are small; past the length that of token t0
-  auto page_of = [&](int t, int t0) { return table[(t < sq.len ? t : t0) >> pl2]; };
-  auto there = [&](int p) { return static_cast<uint32_t>(p) < static_cast<uint32_t>(a.c.n_pages); };
-  const int k_group = r >> 2;  // the 16 tokens of a step that this lane's row of a key tile belongs to
-  const int64_t head_bytes = static_cast<int64_t>(D) << pl2;
-
-  at_i4 kreg[4][DC];
-  auto load_keys = [&](int t0) {
-    const int g = SMALL ? t0 + 16 * k_group : t0;
-    const int p = page_of(g, t0);
-    const int64_t head = static_cast<int64_t>(there(p) ? p : 0) * a.c.Hkv + hk;
-    const int slot = (SMALL ? g & ((1 << pl2) - 1) : (t0 & ((1 << pl2) - 1)) + 16 * k_group) + (r & 3);
-    const int8_t* k = a.c.k + head * head_bytes + slot * D;
+  // Queries: fixed point, 16 elements of a column and chunk in a lane.
+  __device__ __forceinline__ void begin(const AttnArgs& a, const KvSeq& sq, bool ok, int hk, int col0, int cols) {
+    const int r = threadIdx.x & 15, c = (threadIdx.x >> 4) & 3, D = a.c.D;
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int n = 0; n < QB; ++n) {
+      const int col = min(col0 + n * 16 + r, cols - 1);  // columns past the last one repeat it
+      const int i = col / a.G, h = hk * a.G + col - i * a.G;
+      const T* row = static_cast<const T*>(a.q.p) + (sq.row0 + i) * a.q.tok + h * a.q.head;
+      uint32_t most = 0;
+#pragma unroll
+      for (int ch = 0; ch < DC; ++ch)
+        if (ch * 64 + c * 16 < D)
+          for (int x = 0; x < 16; ++x)
+            most = max(most, __float_as_uint(elem(row, ch * 64 + c * 16 + x)) & 0x7fffffffu);
+      most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 16)));
+      most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32)));
+      const bool finite = most < 0x7f800000u;
+      const double size = static_cast<double>(__uint_as_float(most));
+      const double inv = finite && most ? (a.scale < 0.f ? -kSteps : kSteps) / size : 0.0;
+      step[n] = finite ? static_cast<float>(size / kSteps * fabs(static_cast<double>(a.scale)) * static_cast<double>(kLog2e))
+                       : __uint_as_float(0x7fc00000u);
 #pragma unroll
       for (int ch = 0; ch < DC; ++ch) {
-        const int d = ch * 64 + c * 16;
-        kreg[u][ch] = *reinterpret_cast<const at_i4*>(k + 4 * u * D + (d < D ? d : 0));  // past D the digits are 0
+        uint32_t w[4][NT] = {};
+        if (finite && ch * 64 + c * 16 < D) {
+#pragma unroll
+          for (int x = 0; x < 16; ++x)
+            digits<NT>(static_cast<int>(rint(static_cast<double>(elem(row, ch * 64 + c * 16 + x)) * inv)), x & 3, w[x >> 2]);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          q[n][ch][t] = at_i4{static_cast<int>(w[0][t]), static_cast<int>(w[1][t]), static_cast<int>(w[2][t]), static_cast<int>(w[3][t])};
       }
-  };
-
-  if (from < last) load_keys(from);
-  for (int t0 = from; t0 < last; t0 += kTokens * WK) {
-    // values, and the scales of this lane's 16 tokens
-    const int g = SMALL ? t0 + 16 * c : t0;
-    const int p = page_of(g, t0);
-    const bool have = there(p);
-    const int64_t head = static_cast<int64_t>(have ? p : 0) * a.c.Hkv + hk;
-    const int slot = SMALL ? g & ((1 << pl2) - 1) : (t0 & ((1 << pl2) - 1)) + 16 * c;
-    const int8_t* v = a.c.v + head * head_bytes + slot;
-    at_u4 vreg[DT];
+      hi[n] = ok ? sq.len : 0;
+      lo[n] = 0;
+      if (a.causal) {
+        const int place = sq.len - sq.n + i;
+        hi[n] = min(hi[n], max(place + 1, 0));
+        if (a.window) lo[n] = max(place + 1 - a.window, 0);
+      }
+      if (lo[n] >= hi[n]) lo[n] = hi[n] = 0;
+      m[n] = -kInf;
+      l[n] = 0.f;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-      vreg[d] = *reinterpret_cast<const at_u4*>(v + (static_cast<int64_t>(min(d * 16 + r, D - 1)) << pl2));
-    const float ks = a.c.k_scale[head];
-    float vs = a.c.v_scale[head];
-    const bool good = have && ks >= 0.f && ks < kInf && vs >= 0.f && vs < kInf;
-    if (!good) vs = 0.f;
-
-    // scores
-    at_f4 s[QB][4];
+      for (int d = 0; d < DT; ++d) o[n][d] = at_f4{0.f, 0.f, 0.f, 0.f};
+    }
+    e = -126;
+    first = 0x7fffffff, last = 0, all_lo = 0, all_hi = 0x7fffffff;
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int n = 0; n < QB; ++n) {
+      if (hi[n] > 0) first = min(first, lo[n]);
+      last = max(last, hi[n]);
+      all_lo = max(all_lo, lo[n]);
+      all_hi = min(all_hi, hi[n]);
+    }
+    last = wave_max(last);
+    first = min(wave_min(first), last) & ~(kTokens - 1);
+    all_lo = wave_max(all_lo);
+    all_hi = wave_min(all_hi);
+  }
+
+  // The scores of 64 tokens, in query steps: key(u, ch) is the left operand of tile u and chunk ch.
+  template <class Key>
+  __device__ __forceinline__ void scores(at_f4 (&s)[QB][4], Key&& key) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      at_i4 k[DC];
+#pragma unroll
+      for (int ch = 0; ch < DC; ++ch) k[ch] = key(u, ch);
 #pragma unroll
       for (int n = 0; n < QB; ++n) {
         at_i4 acc[NT];
@@ -265,7 +214,7 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnArgs a) {
         for (int t = 0; t < NT; ++t) {
           acc[t] = at_i4{0, 0, 0, 0};
 #pragma unroll
-          for (int ch = 0; ch < DC; ++ch) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kreg[u][ch], q[n][ch][t], acc[t], 0, 0, 0);
+          for (int ch = 0; ch < DC; ++ch) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[ch], q[n][ch][t], acc[t], 0, 0, 0);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -273,86 +222,130 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnArgs a) {
           s[n][u][i] = NT == 3 ? fmaf(static_cast<float>(acc[0][i]), 65536.f, low) : low;
         }
       }
-    if (t0 + kTokens * WK < last) load_keys(t0 + kTokens * WK);
+    }
+  }
 
+  // Scores to weights; ks and vs are the scales of this lane's 16 tokens, `good` whether they can be used.
+  template <bool SMALL>
+  __device__ __forceinline__ void weigh(at_f4 (&s)[QB][4], int t0, float ks, float vs, bool good) {
+    const int c = (threadIdx.x >> 4) & 3;
+    if (!good) vs = 0.f;
     // the power of two that value scales are relative to
-    const int ve = SMALL ? wave_max((static_cast<int>(__float_as_uint(vs)) >> 23) - 126)
-                         : __builtin_amdgcn_readfirstlane((static_cast<int>(__float_as_uint(vs)) >> 23) - 126);
+    const int at = (static_cast<int>(__float_as_uint(vs)) >> 23) - 126;
+    const int ve = SMALL ? wave_max(at) : __builtin_amdgcn_readfirstlane(at);
     float fall = 1.f;
     if (ve > e) {
       fall = ldexpf(1.f, max(e - ve, -126));
       e = ve;
     }
     const float weight = fmaxf(ldexpf(vs, -e), 0x1p-40f) * static_cast<float>(1 << kLift);
-    const float unweight = 1.f / weight;
+    const float unweight = __builtin_amdgcn_rcpf(weight), weight_log = __builtin_amdgcn_logf(weight);
     const bool whole = t0 >= all_lo && t0 + kTokens <= all_hi;
-
+    uint32_t seen[QB];  // which of the lane's 16 tokens its column sees
+    if (!whole) {
+      asm volatile("; a branch, not selections");
+      const int base = t0 + 16 * c;
+#pragma unroll
+      for (int n = 0; n < QB; ++n) {
+        const int x = min(max(lo[n] - base, 0), 16), y = min(max(hi[n] - base, 0), 16);
+        seen[n] = ((1u << y) - 1u) & ~((1u << x) - 1u);
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (!(seen[n] >> j & 1)) s[n][j >> 2][j & 3] = -3e38f;
+      }
+    }
 #pragma unroll
     for (int n = 0; n < QB; ++n) {
       const float alpha = good ? step[n] * ks : __uint_as_float(0x7fc00000u);
-      uint32_t seen = 0xffffu;  // which of the lane's 16 tokens its column sees
-      if (!whole) {
-        const int base = t0 + 16 * c;
-        const int x = min(max(lo[n] - base, 0), 16), y = min(max(hi[n] - base, 0), 16);
-        seen = ((1u << y) - 1u) & ~((1u << x) - 1u);
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (!(seen >> j & 1)) s[n][j >> 2][j & 3] = -3e38f;
-      }
       float top = fmaxf(fmaxf(s[n][0][0], s[n][0][1]), s[n][0][2]);
 #pragma unroll
       for (int j = 3; j < 16; ++j) top = fmaxf(top, s[n][j >> 2][j & 3]);
       top *= alpha;
-      float keep = fall;
       if (__any(top > m[n] + kSlack || fall != 1.f)) {
+        asm volatile("; a branch, not selections");
         const float now = fmaxf(m[n], quarters_max(top));
         const float f = m[n] > -kInf ? __builtin_amdgcn_exp2f(m[n] - now) : 0.f;
         m[n] = now;
         l[n] *= f;
-        keep *= f;
+        const float keep = f * fall;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[n][d] *= keep;
       }
       // weights p 2^.. = exp2(score - m) weight, as exp2 of one fused multiply-add
-      float sum = 0.f;
-      const float shift = __builtin_amdgcn_logf(weight) - m[n];
+      const float shift = weight_log - m[n];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        float pj = __builtin_amdgcn_exp2f(fmaf(s[n][j >> 2][j & 3], alpha, shift));
-        if (!whole && !(seen >> j & 1)) pj = 0.f;
-        sum += pj;
-        s[n][j >> 2][j & 3] = pj;
-      }
-      l[n] = fmaf(sum, unweight, l[n]);
+      for (int j = 0; j < 16; ++j)
+        s[n][j >> 2][j & 3] = __builtin_amdgcn_exp2f(fmaf(s[n][j >> 2][j & 3], alpha, shift));
     }
-    // values
-    bool wide = sizeof(T) == 4;
-    at_h8 pw[QB][2];
-    if constexpr (sizeof(T) == 2) {
-      at_s2 least = {0x7fff, 0x7fff};
+    if (!whole) {
+      asm volatile("; a branch, not selections");
 #pragma unroll
       for (int n = 0; n < QB; ++n)
 #pragma unroll
-        for (int j = 0; j < 16; j += 2) {
-          const at_h2 h = __builtin_convertvector((at_f2{s[n][j >> 2][j & 3], s[n][j >> 2][(j & 3) + 1]}), at_h2);
-          least = __builtin_elementwise_min(least, __builtin_bit_cast(at_s2, h));
-          pw[n][j >> 3][j & 7] = h[0];
-          pw[n][j >> 3][(j & 7) + 1] = h[1];
-        }
-      wide = __any(least[0] < 0x0400 || least[1] < 0x0400);
+        for (int j = 0; j < 16; ++j)
+          if (!(seen[n] >> j & 1)) s[n][j >> 2][j & 3] = 0.f;
     }
-    if (!wide) {
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const at_h8 v0 = widen8(vreg[d][0], vreg[d][1]), v1 = widen8(vreg[d][2], vreg[d][3]);
+    for (int n = 0; n < QB; ++n) {
+      float sum = 0.f;
 #pragma unroll
-        for (int n = 0; n < QB; ++n) {
-          o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[n][0], o[n][d], 0, 0, 0);
-          o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pw[n][1], o[n][d], 0, 0, 0);
+      for (int j = 0; j < 16; ++j) sum += s[n][j >> 2][j & 3];
+      l[n] = fmaf(sum, unweight, l[n]);
+    }
+  }
+
+  // Adds the values of 64 tokens: value(d, w) is the left operand (fp16; bf16 for fp32 queries) of tile d and half w.
+  template <class Value>
+  __device__ __forceinline__ void add(at_f4 (&s)[QB][4], Value&& value) {
+    if constexpr (sizeof(T) == 2) {
+      for (int pass = 0;; ++pass) {
+        at_h8 pw[QB][2];
+        at_s2 least = {0x7fff, 0x7fff};
+#pragma unroll
+        for (int n = 0; n < QB; ++n)
+#pragma unroll
+          for (int j = 0; j < 16; j += 2) {
+            const at_h2 h = __builtin_convertvector((at_f2{s[n][j >> 2][j & 3], s[n][j >> 2][(j & 3) + 1]}), at_h2);
+            least = __builtin_elementwise_min(least, __builtin_bit_cast(at_s2, h));
+            pw[n][j >> 3][j & 7] = h[0];
+            pw[n][j >> 3][(j & 7) + 1] = h[1];
+          }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const at_h8 v0 = __builtin_bit_cast(at_h8, value(d, 0)), v1 = __builtin_bit_cast(at_h8, value(d, 1));
+#pragma unroll
+          for (int n = 0; n < QB; ++n) {
+            o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[n][0], o[n][d], 0, 0, 0);
+            o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pw[n][1], o[n][d], 0, 0, 0);
+          }
         }
+        // weights below fp16's normal numbers: what the rounding left of them, 2^14 times as large, once more
+        bool more = false;
+        if (__any(least[0] < 0x0400 || least[1] < 0x0400)) {
+          asm volatile("; a branch, not selections");
+#pragma unroll
+          for (int n = 0; n < QB; ++n)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const float x = s[n][j >> 2][j & 3];
+              const float rest = fabsf(x) < 0x1p-14f ? (x - static_cast<float>(pw[n][j >> 3][j & 7])) * 0x1p14f : 0.f;
+              s[n][j >> 2][j & 3] = rest;
+              more |= rest != 0.f;
+            }
+          more = __any(more) && pass < 5;
+        }
+        if (more || pass) {
+          asm volatile("; a branch, not selections");
+          const float by = more ? 0x1p14f : ldexpf(1.f, -14 * pass);
+#pragma unroll
+          for (int n = 0; n < QB; ++n)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[n][d] *= by;
+        }
+        if (!more) break;
       }
     } else {
-      at_b8 pb[QB][2][PT];
+      at_b8 pb[QB][2][3];
 #pragma unroll
       for (int n = 0; n < QB; ++n)
 #pragma unroll
@@ -361,7 +354,7 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnArgs a) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) p[j] = s[n][2 * w + (j >> 2)][j & 3];
 #pragma unroll
-          for (int t = 0; t < PT; ++t) {  // the upper halves, then what they leave
+          for (int t = 0; t < 3; ++t) {  // the upper halves, then what they leave
             at_u4 x;
 #pragma unroll
             for (int j = 0; j < 8; j += 2)
@@ -373,11 +366,11 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnArgs a) {
         }
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        const at_b8 v0 = widen8_bf16(vreg[d][0], vreg[d][1]), v1 = widen8_bf16(vreg[d][2], vreg[d][3]);
+        const at_b8 v0 = __builtin_bit_cast(at_b8, value(d, 0)), v1 = __builtin_bit_cast(at_b8, value(d, 1));
 #pragma unroll
         for (int n = 0; n < QB; ++n)
 #pragma unroll
-          for (int t = PT - 1; t >= 0; --t) {
+          for (int t = 2; t >= 0; --t) {
             o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pb[n][0][t], o[n][d], 0, 0, 0);
             o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pb[n][1][t], o[n][d], 0, 0, 0);
           }
@@ -385,42 +378,62 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnArgs a) {
     }
   }
 
-  const float back = ldexpf(1.f, e - kLift);
+  // Sums over the quarters, and o back from its power of two.
+  __device__ __forceinline__ void end() {
+    const float back = ldexpf(1.f, e - kLift);
 #pragma unroll
-  for (int n = 0; n < QB; ++n) {
-    l[n] = quarters_sum(l[n]);
+    for (int n = 0; n < QB; ++n) {
+      l[n] = quarters_sum(l[n]);
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[n][d] *= back;
-  }
-  const float nan = __uint_as_float(0x7fc00000u);
-
-  // a column's result: to the output, or to the partial results of this split
-  auto row_of = [&](int col, int& i, int& h) {
-    i = col / a.G;
-    h = hk * a.G + col - i * a.G;
-  };
-  auto stats = [&](int col, float mm, float ll) {
-    int i, h;
-    row_of(col, i, h);
-    if (a.splits > 1) {
-      const int64_t at = ((static_cast<int64_t>(split) * a.bt.B + b) * a.bt.max_new + i) * a.Hq + h;
-      a.pm[at] = mm;
-      a.pl[at] = ok ? ll : nan;
-    } else if (a.lse) {
-      a.lse[static_cast<int64_t>(sq.row0 + i) * a.Hq + h] = !ok ? nan : ll == 0.f ? -kInf : (mm + __builtin_amdgcn_logf(ll)) * kLn2;
+      for (int d = 0; d < DT; ++d) o[n][d] *= back;
     }
-  };
-  auto put = [&](int col, int d, at_f4 x, float ll) {
-    if (d >= D) return;
+  }
+};
+
+// Eight value codes as the second product takes them.
+template <typename T>
+__device__ __forceinline__ at_u4 widen(uint32_t a, uint32_t b) {
+  if constexpr (sizeof(T) == 4)
+    return __builtin_bit_cast(at_u4, widen8_bf16(a, b));
+  else
+    return __builtin_bit_cast(at_u4, widen8(a, b));
+}
+
+// A column's result, to the output or to the partial results of a split.
+template <typename T>
+struct Results {
+  const AttnArgs& a;
+  const KvSeq& sq;
+  const Place& p;
+  bool ok;
+  __device__ __forceinline__ void row_of(int col, int& i, int& h) const {
+    i = col / a.G;
+    h = p.hk * a.G + col - i * a.G;
+  }
+  __device__ __forceinline__ int64_t part(int i, int h) const {
+    return ((static_cast<int64_t>(p.split) * a.bt.B + p.b) * a.bt.max_new + i) * a.Hq + h;
+  }
+  __device__ __forceinline__ void stats(int col, float m, float l) const {
+    int i, h;
+    row_of(col, i, h);
+    const float nan = __uint_as_float(0x7fc00000u);
+    if (a.splits > 1) {
+      a.pm[part(i, h)] = m;
+      a.pl[part(i, h)] = ok ? l : nan;
+    } else if (a.lse) {
+      a.lse[static_cast<int64_t>(sq.row0 + i) * a.Hq + h] = !ok ? nan : l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+  }
+  __device__ __forceinline__ void put(int col, int d, at_f4 x, float l) const {
+    if (d >= a.c.D) return;
     int i, h;
     row_of(col, i, h);
     if (a.splits > 1) {
-      const int64_t at = ((static_cast<int64_t>(split) * a.bt.B + b) * a.bt.max_new + i) * a.Hq + h;
-      if (ll != 0.f) *reinterpret_cast<at_f4*>(a.po + at * D + d) = x;
+      if (l != 0.f) *reinterpret_cast<at_f4*>(a.po + part(i, h) * a.c.D + d) = x;
       return;
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = !ok ? nan : ll == 0.f ? 0.f : x[k] / ll;
+    for (int k = 0; k < 4; ++k) x[k] = !ok ? __uint_as_float(0x7fc00000u) : l == 0.f ? 0.f : x[k] / l;
     T* out = static_cast<T*>(a.out.p) + (sq.row0 + i) * a.out.tok + h * a.out.head + d;
     if constexpr (sizeof(T) == 4) {
       float* f = reinterpret_cast<float*>(out);
@@ -436,47 +449,245 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnArgs a) {
         for (int k = 0; k < 4; ++k) out[k] = static_cast<T>(f_bf16(x[k]));
       }
     }
+  }
+};
+
+// What the tokens of a step need from the block table and the scales.
+struct Pages {
+  const int32_t* table;
+  int64_t n_pages;
+  int len, log2;
+  // the page of the 16 tokens from t on in the step at t0; past the length that of t0, whose codes are as good as any
+  __device__ __forceinline__ int of(int t, int t0) const { return table[(t < len ? t : t0) >> log2]; }
+  __device__ __forceinline__ bool there(int p) const { return static_cast<uint32_t>(p) < static_cast<uint32_t>(n_pages); }
+};
+__device__ __forceinline__ bool usable(float ks, float vs) { return ks >= 0.f && ks < kInf && vs >= 0.f && vs < kInf; }
+
+// An equal share of the tokens first .. last for a split, in whole rounds.
+__device__ __forceinline__ void share_of(const AttnArgs& a, int split, int round, int& first, int& last) {
+  if (a.splits == 1) return;
+  const int span = (last - first + a.splits - 1) / a.splits, share = (span + round - 1) / round * round;
+  const int64_t from = first + static_cast<int64_t>(split) * share;
+  first = static_cast<int>(from < last ? from : last);
+  last = min(last, first + share);
+}
+
+// Few columns: the four waves of a workgroup share 16 and take turns at the tokens; the cache is read once, from
+// memory into the operands' registers, a step's keys while the step before is computed.  Reads bound it.
+template <typename T, int DT, bool SMALL>
+__global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel(const AttnArgs a) {
+  constexpr int kRow = DT * 16 + 4, kStride = 4 * kTokens;
+  __shared__ __align__(16) float join[4 * 16 * kRow];
+  __shared__ float join_m[64], join_l[64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = threadIdx.x & 15, c = (threadIdx.x >> 4) & 3;
+  const int D = a.c.D, pl2 = a.c.page_log2, in_page = (1 << pl2) - 1;
+  const Place pc = place_of(a);
+  const KvSeq sq = kv_seq(a.bt, pc.b, pl2);
+  const int cols = min(sq.n, a.bt.max_new) * a.G, col0 = pc.tile * 16;
+  if (col0 >= cols) return;
+  const bool ok = sq.ok && (sq.len == 0 || a.c.n_pages > 0);
+  Columns<T, DT, 1> w;
+  w.begin(a, sq, ok, pc.hk, col0, cols);
+  int first = w.first, last = w.last;
+  share_of(a, pc.split, kStride, first, last);
+  const int from = first + wave * kTokens;
+
+  // addresses: the page's (uniform; SMALL: of this lane's 16 tokens) plus a lane's constant offset
+  const Pages pages = {a.bt.table + static_cast<int64_t>(pc.b) * a.bt.ld_table, a.c.n_pages, sq.len, pl2};
+  const int group = r >> 2;  // the 16 tokens of a step that this lane's row of a key tile belongs to
+  auto uniform = [](int x) { return SMALL ? x : __builtin_amdgcn_readfirstlane(x); };
+  auto head_of = [&](int p) { return static_cast<int64_t>(pages.there(p) ? p : 0) * a.c.Hkv + pc.hk; };
+  auto key_page = [&](int t0) { return t0 < last ? uniform(pages.of(SMALL ? t0 + 16 * group : t0, t0)) : 0; };
+  auto value_page = [&](int t0) { return t0 < last ? uniform(pages.of(SMALL ? t0 + 16 * c : t0, t0)) : 0; };
+  const int64_t head_bytes = static_cast<int64_t>(D) << pl2;
+  uint32_t koff[(DT + 3) / 4];
+#pragma unroll
+  for (int ch = 0; ch < (DT + 3) / 4; ++ch)  // past D the digits are 0, and any codes will do
+    koff[ch] = ((SMALL ? 0 : 16 * group) + (r & 3)) * D + (ch * 64 + c * 16 < D ? ch * 64 + c * 16 : 0);
+  const uint32_t voff = (static_cast<uint32_t>(r) << pl2) + (SMALL ? 0 : 16 * c);
+  const int tiles = D >> 4;
+  at_i4 kreg[4][(DT + 3) / 4];
+  auto load_keys = [&](int t0, int p) {
+    const int8_t* k = a.c.k + head_of(p) * head_bytes + ((SMALL ? t0 + 16 * group : t0) & in_page) * D;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int ch = 0; ch < (DT + 3) / 4; ++ch) kreg[u][ch] = *reinterpret_cast<const at_i4*>(k + (koff[ch] + 4 * u * D));
   };
 
-  if constexpr (WK == 1) {
+  int kp = key_page(from), vp = SMALL ? value_page(from) : kp;
+  if (from < last) load_keys(from, kp);
+  kp = key_page(from + kStride);
+  for (int t0 = from; t0 < last; t0 += kStride) {
+    const int64_t head = head_of(vp);
+    const int8_t* v = a.c.v + head * head_bytes + ((SMALL ? t0 + 16 * c : t0) & in_page);
+    at_u4 vreg[DT];
 #pragma unroll
-    for (int n = 0; n < QB; ++n) {
-      const int col = col0 + n * 16 + r;
-      if (col >= cols) continue;
-      if (c == 0) stats(col, m[n], l[n]);
+    for (int d = 0; d < DT; ++d)
+      vreg[d] = *reinterpret_cast<const at_u4*>(v + (static_cast<int64_t>(min(d, tiles - 1) * 16) << pl2) + voff);
+    const float ks = a.c.k_scale[head], vs = a.c.v_scale[head];
+    const bool good = pages.there(vp) && usable(ks, vs);
+    at_f4 s[1][4];
+    w.scores(s, [&](int u, int ch) { return kreg[u][ch]; });
+    if (t0 + kStride < last) load_keys(t0 + kStride, kp);
+    vp = SMALL ? value_page(t0 + kStride) : kp;
+    kp = key_page(t0 + 2 * kStride);
+    w.template weigh<SMALL>(s, t0, ks, vs, good);
+    w.add(s, [&](int d, int half) {
+      asm volatile("" : "+v"(vreg[d]));  // widened where it is used, in every pass
+      return widen<T>(vreg[d][2 * half], vreg[d][2 * half + 1]);
+    });
+  }
+  w.end();
+
+  const int at0 = wave * 16 + r;
+  if (c == 0) {
+    join_m[at0] = w.m[0];
+    join_l[at0] = w.l[0];
+  }
 #pragma unroll
-      for (int d = 0; d < DT; ++d) put(col, d * 16 + 4 * c, o[n][d], l[n]);
+  for (int d = 0; d < DT; ++d) *reinterpret_cast<at_f4*>(join + at0 * kRow + d * 16 + 4 * c) = w.o[0][d];
+  __syncthreads();
+  const Results<T> out = {a, sq, pc, ok};
+  for (int x = threadIdx.x; x < 16 * DT * 4; x += 256) {
+    const int col = x / (DT * 4), d = (x - col * (DT * 4)) * 4;
+    if (col0 + col >= cols) break;
+    float mm = -kInf;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mm = fmaxf(mm, join_m[k * 16 + col]);
+    float ll = 0.f;
+    at_f4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int at = k * 16 + col;
+      const float f = join_m[at] == -kInf ? 0.f : __builtin_amdgcn_exp2f(join_m[at] - mm);
+      ll = fmaf(f, join_l[at], ll);
+      y += f * *reinterpret_cast<const at_f4*>(join + at * kRow + d);
     }
-  } else {
+    if (d == 0) out.stats(col0 + col, mm, ll);
+    out.put(col0 + col, d, y, ll);
+  }
+}
+
+// Many columns: every wave has 16 QB of its own, and the four of a workgroup walk the same tokens.  A step's keys
+// and values pass through LDS, two steps of them: keys as they are, values widened once for all four waves.  Rows of
+// LDS are padded by 16 bytes, and a key's row is u * 16 + r for the token that is row r of tile u, so that the 16 rows
+// an instruction reads lie in different banks.  The vector units bound it (the softmax's exponentials).
+template <typename T, int DT, int QB, bool SMALL>
+__global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kernel(const AttnArgs a) {
+  constexpr int kKeyRow = DT * 16 + 16, kValueRow = kTokens * 2 + 16;
+  constexpr int kKeyBytes = kTokens * kKeyRow, kBuffer = kKeyBytes + DT * 16 * kValueRow;
+  constexpr int kPer = (DT * 16 * 4 + 255) / 256;  // 16-byte pieces of keys, and of values, that a thread moves
+  extern __shared__ __align__(16) uint8_t lds[];   // [2][kBuffer]
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tid = threadIdx.x, r = tid & 15, c = (tid >> 4) & 3;
+  const int D = a.c.D, pl2 = a.c.page_log2, in_page = (1 << pl2) - 1;
+  const Place pc = place_of(a);
+  const KvSeq sq = kv_seq(a.bt, pc.b, pl2);
+  const int cols = min(sq.n, a.bt.max_new) * a.G, tile0 = pc.tile * (64 * QB), col0 = tile0 + wave * (16 * QB);
+  if (tile0 >= cols) return;
+  const bool ok = sq.ok && (sq.len == 0 || a.c.n_pages > 0), mine = col0 < cols;
+  Columns<T, DT, QB> w;
+  w.begin(a, sq, ok, pc.hk, min(col0, cols - 1), cols);
+  // the workgroup's tokens
+  int* shared = reinterpret_cast<int*>(lds);
+  if ((tid & 63) == 0) {
+    shared[2 * wave] = w.first;
+    shared[2 * wave + 1] = w.last;
+  }
+  __syncthreads();
+  int first = 0x7fffffff, last = 0;
 #pragma unroll
-    for (int n = 0; n < QB; ++n) {
-      const int at = (wave * QB + n) * 16 + r;
-      if (c == 0) {
-        join_m[at] = m[n];
-        join_l[at] = l[n];
-      }
+  for (int k = 0; k < 4; ++k) {
+    if (shared[2 * k + 1] > 0) first = min(first, shared[2 * k]);
+    last = max(last, shared[2 * k + 1]);
+  }
+  last = __builtin_amdgcn_readfirstlane(last);
+  first = min(__builtin_amdgcn_readfirstlane(first), last);
+  __syncthreads();
+  share_of(a, pc.split, kTokens, first, last);
+
+  const Pages pages = {a.bt.table + static_cast<int64_t>(pc.b) * a.bt.ld_table, a.c.n_pages, sq.len, pl2};
+  auto uniform = [](int x) { return SMALL ? x : __builtin_amdgcn_readfirstlane(x); };
+  auto head_of = [&](int p) { return static_cast<int64_t>(pages.there(p) ? p : 0) * a.c.Hkv + pc.hk; };
+  const int64_t head_bytes = static_cast<int64_t>(D) << pl2;
+  // the pieces this thread moves: of keys, 16 elements of a token; of values, 16 tokens of an element
+  const int pieces = 4 * D, d16 = D >> 4;
+  int kt[kPer], ke[kPer];
 #pragma unroll
-      for (int d = 0; d < DT; ++d) *reinterpret_cast<at_f4*>(join + at * kRow + d * 16 + 4 * c) = o[n][d];
+  for (int i = 0; i < kPer; ++i) {
+    const int x = min(tid + i * 256, pieces - 1);
+    kt[i] = x / d16;
+    ke[i] = x - kt[i] * d16;
+  }
+  at_u4 kreg[kPer], vreg[kPer];
+  auto fetch = [&](int t0) {
+    const int page0 = SMALL ? 0 : uniform(pages.of(t0, t0));
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int p = SMALL ? pages.of(t0 + (kt[i] & ~15), t0) : page0;
+      const int8_t* k = a.c.k + head_of(p) * head_bytes;
+      kreg[i] = *reinterpret_cast<const at_u4*>(k + (((t0 + kt[i]) & in_page) * D + ke[i] * 16));
     }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int x = min(tid + i * 256, pieces - 1), g = (x & 3) * 16;
+      const int p = SMALL ? pages.of(t0 + g, t0) : page0;
+      const int8_t* v = a.c.v + head_of(p) * head_bytes;
+      vreg[i] = *reinterpret_cast<const at_u4*>(v + (((x >> 2) << pl2) + ((t0 + g) & in_page)));
+    }
+  };
+  auto settle = [&](uint8_t* to) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int x = min(tid + i * 256, pieces - 1);
+      const int row = ((kt[i] >> 2) & 3) * 16 + (kt[i] >> 4) * 4 + (kt[i] & 3);
+      *reinterpret_cast<at_u4*>(to + row * kKeyRow + ke[i] * 16) = kreg[i];
+      uint8_t* v = to + kKeyBytes + (x >> 2) * kValueRow + (x & 3) * 32;
+      *reinterpret_cast<at_u4*>(v) = widen<T>(vreg[i][0], vreg[i][1]);
+      *reinterpret_cast<at_u4*>(v + 16) = widen<T>(vreg[i][2], vreg[i][3]);
+    }
+  };
+  // what no piece fills: elements past D of the keys (their digits are 0) and value rows past D (their sums are
+  // not stored) may hold anything that is finite, and are cleared once
+  if (D < DT * 16) {
+    for (int x = tid * 16; x < 2 * kBuffer; x += 256 * 16) *reinterpret_cast<at_u4*>(lds + x) = at_u4{0, 0, 0, 0};
     __syncthreads();
-    for (int x = threadIdx.x; x < 16 * QB * DT * 4; x += 256) {
-      const int col = x / (DT * 4), d = (x - col * (DT * 4)) * 4;
-      if (col0 + col >= cols) break;
-      float mm = -kInf;
-#pragma unroll
-      for (int w = 0; w < WK; ++w) mm = fmaxf(mm, join_m[w * QB * 16 + col]);
-      float ll = 0.f;
-      at_f4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < WK; ++w) {
-        const int at = w * QB * 16 + col;
-        const float f = join_m[at] == -kInf ? 0.f : __builtin_amdgcn_exp2f(join_m[at] - mm);
-        ll = fmaf(f, join_l[at], ll);
-        y += f * *reinterpret_cast<const at_f4*>(join + at * kRow + d);
-      }
-      if (d == 0) stats(col0 + col, mm, ll);
-      put(col0 + col, d, y, ll);
+  }
+
+  if (first < last) {
+    fetch(first);
+    settle(lds);
+  }
+  __syncthreads();
+  int buffer = 0;
+  for (int t0 = first; t0 < last; t0 += kTokens) {
+    const uint8_t* from = lds + buffer * kBuffer;
+    if (t0 + kTokens < last) fetch(t0 + kTokens);
+    if (t0 + kTokens > w.first && t0 < w.last) {
+      const int p = uniform(pages.of(SMALL ? t0 + 16 * c : t0, t0));
+      const int64_t head = head_of(p);
+      const float ks = a.c.k_scale[head], vs = a.c.v_scale[head];
+      const bool good = pages.there(p) && usable(ks, vs);
+      at_f4 s[QB][4];
+      w.scores(s, [&](int u, int ch) { return *reinterpret_cast<const at_i4*>(from + (u * 16 + r) * kKeyRow + ch * 64 + c * 16); });
+      w.template weigh<SMALL>(s, t0, ks, vs, good);
+      const uint8_t* v = from + kKeyBytes + r * kValueRow + c * 32;
+      w.add(s, [&](int d, int half) { return *reinterpret_cast<const at_u4*>(v + d * 16 * kValueRow + half * 16); });
     }
+    buffer ^= 1;
+    if (t0 + kTokens < last) settle(lds + buffer * kBuffer);
+    __syncthreads();
+  }
+  w.end();
+  if (!mine) return;
+  const Results<T> out = {a, sq, pc, ok};
+#pragma unroll
+  for (int n = 0; n < QB; ++n) {
+    const int col = col0 + n * 16 + r;
+    if (col >= cols) continue;
+    if (c == 0) out.stats(col, w.m[n], w.l[n]);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) out.put(col, d * 16 + 4 * c, w.o[n][d], w.l[n]);
   }
 }
 
@@ -536,20 +747,20 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(const AttnArgs a
 }
 
 // How a call is divided.  One tile of columns: its workgroups' four waves share the columns (16) and take turns at the
-// tokens; more: every wave has 16 kPromptBlocks columns of its own.  Tokens are split over workgroups until
+// tokens; more: every wave has 16 prompt_blocks columns of its own.  Tokens are split over workgroups until
 // kWorkgroups are at work, a share being at least kShare tokens.
 struct AttnPlan {
   bool prompt;
   int tiles, splits;
 };
-constexpr int kPromptBlocks = 2;
+constexpr int prompt_blocks(int D) { return D <= 128 ? 2 : 1; }  // what the registers hold
 constexpr int64_t kWorkgroups = 1024;
 constexpr int kShare = 512;
-AttnPlan plan_attention(int B, int Hq, int Hkv, int max_new, int max_kv) {
+AttnPlan plan_attention(int B, int Hq, int Hkv, int D, int max_new, int max_kv) {
   AttnPlan p;
   const int64_t cols = static_cast<int64_t>(max_new) * (Hq / Hkv);
   p.prompt = cols > 16;
-  p.tiles = static_cast<int>(cdiv(cols, p.prompt ? 64 * kPromptBlocks : 16));
+  p.tiles = static_cast<int>(cdiv(cols, p.prompt ? 64 * prompt_blocks(D) : 16));
   const int64_t groups = static_cast<int64_t>(B) * Hkv * p.tiles;
   const int64_t most = cdiv(max_kv, kShare), want = cdiv(kWorkgroups, groups);
   const int64_t n = want < most ? want : most;
@@ -572,16 +783,18 @@ AttnWs carve_attention(WsCursor& c, const AttnPlan& p, int B, int Hq, int D, int
 
 template <typename T, int DT>
 hipError_t attend_as(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
+  constexpr int QB = prompt_blocks(DT * 16);
   const int64_t blocks = static_cast<int64_t>(p.tiles) * p.splits * a.bt.B * a.c.Hkv;
   if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
   const dim3 grid(static_cast<uint32_t>(blocks));
   const bool small = a.c.page_log2 < 6;
+  const size_t lds = 2 * (kTokens * (DT * 16 + 16) + DT * 16 * (kTokens * 2 + 16));
   if (p.prompt) {
-    if (small) kv_attention_kernel<T, DT, kPromptBlocks, 1, true><<<grid, 256, 0, stream>>>(a);
-    else kv_attention_kernel<T, DT, kPromptBlocks, 1, false><<<grid, 256, 0, stream>>>(a);
+    if (small) kv_attention_prompt_kernel<T, DT, QB, true><<<grid, 256, lds, stream>>>(a);
+    else kv_attention_prompt_kernel<T, DT, QB, false><<<grid, 256, lds, stream>>>(a);
   } else {
-    if (small) kv_attention_kernel<T, DT, 1, 4, true><<<grid, 256, 0, stream>>>(a);
-    else kv_attention_kernel<T, DT, 1, 4, false><<<grid, 256, 0, stream>>>(a);
+    if (small) kv_attention_step_kernel<T, DT, true><<<grid, 256, 0, stream>>>(a);
+    else kv_attention_step_kernel<T, DT, false><<<grid, 256, 0, stream>>>(a);
   }
   return hipGetLastError();
 }
@@ -602,14 +815,14 @@ hipError_t attend(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
 
 size_t kv_attention_ws_bytes(int B, int Hq, int Hkv, int D, int max_new, int max_kv) {
   WsCursor c(nullptr);
-  carve_attention(c, plan_attention(B, Hq, Hkv, max_new, max_kv), B, Hq, D, max_new);
+  carve_attention(c, plan_attention(B, Hq, Hkv, D, max_new, max_kv), B, Hq, D, max_new);
   return c.used;
 }
 
 hipError_t launch_kv_attention(const KvCache& c, const KvBatch& bt, int max_kv, int type, int Hq, const KvRows& q,
                                const KvRows& out, float scale, int causal, int window, float* lse, void* ws,
                                hipStream_t stream) {
-  const AttnPlan p = plan_attention(bt.B, Hq, c.Hkv, bt.max_new, max_kv);
+  const AttnPlan p = plan_attention(bt.B, Hq, c.Hkv, c.D, bt.max_new, max_kv);
   WsCursor cur(ws);
   const AttnWs w = carve_attention(cur, p, bt.B, Hq, c.D, bt.max_new);
   AttnArgs a = {c, bt, q, out, lse, w.po, w.pm, w.pl, scale, Hq, Hq / c.Hkv, causal, window, p.splits, p.tiles, 0};
