@@ -108,8 +108,11 @@ __device__ __forceinline__ float elem(const T* p, int i) {
     return bf16_f(p[i]);
 }
 
-// Which sequence, key head, split and tile of columns a workgroup has: tiles of a sequence last to first, so that the
-// longest rows of a causal prompt start first.
+// Which sequence, key head, split and tile of columns a workgroup has.  Key heads are neighbours, so that with a
+// multiple of eight of them a chip's die reads few heads; the tiles of a sequence go last to first, so that the longest
+// rows of a causal prompt start first; sequences come one after the other: the workgroups that a short one has no work for
+// are then a run (as every second one they left half of the CUs idle: 556 against 400 us for two prompts of 2048
+// and about 300).
 struct Place {
   int hk, b, split, tile;
 };
@@ -118,10 +121,10 @@ __device__ __forceinline__ Place place_of(const AttnArgs& a) {
   Place p;
   p.hk = static_cast<int>(item % a.c.Hkv);
   item /= a.c.Hkv;
-  p.b = static_cast<int>(item % a.bt.B);
-  item /= a.bt.B;
   p.split = static_cast<int>(item % a.splits);
-  p.tile = a.tiles - 1 - static_cast<int>(item / a.splits);
+  item /= a.splits;
+  p.tile = a.tiles - 1 - static_cast<int>(item % a.tiles);
+  p.b = static_cast<int>(item / a.tiles);
   return p;
 }
 
