@@ -128,20 +128,25 @@ __device__ __forceinline__ Place place_of(const AttnArgs& a) {
   return p;
 }
 
-// The state of a wave's 16 QB columns; DT tiles of 16 elements hold a head.
-template <typename T, int DT, int QB>
+// The state of a wave's 16 QB columns; DT tiles of 16 elements hold a head.  HALF: keys come widened to fp16, and a
+// query row is fp16 relative to a power of two (a bf16 element keeps its 8 bits down to 2^-28 of the row's largest).
+// SMALL: the 16 tokens of a lane may have a page, and scales, of their own.
+template <typename T, int DT, int QB, bool HALF, bool SMALL>
 struct Columns {
-  static constexpr int DC = (DT + 3) / 4;                            // 64-element chunks of a head
-  static constexpr int NT = sizeof(T) == 4 ? 3 : 2;                  // digits of a query element
+  static constexpr int DC = HALF ? (DT + 1) / 2 : (DT + 3) / 4;      // chunks of a head: 32 (HALF) or 64 elements
+  static constexpr int NT = HALF ? 1 : sizeof(T) == 4 ? 3 : 2;       // digits of a query element
   static constexpr double kSteps = NT == 3 ? 8355711.0 : 32639.0;    // 127 in every digit
+  // Where a step's weights have one factor, their sum is a product with ones (of the rounded weights, as the values are).
+  static constexpr bool kSumByProduct = sizeof(T) == 2 && !SMALL;
   at_i4 q[QB][DC][NT];
   float step[QB], m[QB], l[QB];
   int lo[QB], hi[QB];                 // the tokens a column sees
   int first, last, all_lo, all_hi;    // the tokens any of them sees, and those that all of them see
   at_f4 o[QB][DT];
   int e;  // exponent that value scales are taken relative to
+  float unweight;  // of the present step: 1 / (the weight of p = 1)
 
-  // Queries: fixed point, 16 elements of a column and chunk in a lane.
+  // Queries: fixed point, 16 elements of a column and chunk in a lane; HALF: 8 of them.
   __device__ __forceinline__ void begin(const AttnArgs& a, const KvSeq& sq, bool ok, int hk, int col0, int cols) {
     const int r = threadIdx.x & 15, c = (threadIdx.x >> 4) & 3, D = a.c.D;
 #pragma unroll
@@ -149,26 +154,39 @@ struct Columns {
       const int col = min(col0 + n * 16 + r, cols - 1);  // columns past the last one repeat it
       const int i = col / a.G, h = hk * a.G + col - i * a.G;
       const T* row = static_cast<const T*>(a.q.p) + (sq.row0 + i) * a.q.tok + h * a.q.head;
+      constexpr int E = HALF ? 8 : 16;
       uint32_t most = 0;
 #pragma unroll
       for (int ch = 0; ch < DC; ++ch)
-        if (ch * 64 + c * 16 < D)
-          for (int x = 0; x < 16; ++x)
-            most = max(most, __float_as_uint(elem(row, ch * 64 + c * 16 + x)) & 0x7fffffffu);
+        if ((ch * 4 + c) * E < D)
+          for (int x = 0; x < E; ++x) most = max(most, __float_as_uint(elem(row, (ch * 4 + c) * E + x)) & 0x7fffffffu);
       most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 16)));
       most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32)));
       const bool finite = most < 0x7f800000u;
-      const double size = static_cast<double>(__uint_as_float(most));
+      const double size = static_cast<double>(__uint_as_float(most)), slope = fabs(static_cast<double>(a.scale)) * kLog2e;
+      const int up = 14 - (static_cast<int>(most >> 23) - 127);  // HALF: elements below 2^15
       const double inv = finite && most ? (a.scale < 0.f ? -kSteps : kSteps) / size : 0.0;
-      step[n] = finite ? static_cast<float>(size / kSteps * fabs(static_cast<double>(a.scale)) * static_cast<double>(kLog2e))
-                       : __uint_as_float(0x7fc00000u);
+      step[n] = !finite ? __uint_as_float(0x7fc00000u) : static_cast<float>(HALF ? ldexp(slope, -up) : size / kSteps * slope);
 #pragma unroll
       for (int ch = 0; ch < DC; ++ch) {
+        const int at = (ch * 4 + c) * E;
+        if constexpr (HALF) {
+          at_h8 h = {};
+          if (finite && at < D) {
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              const float v = ldexpf(elem(row, at + x), up);
+              h[x] = static_cast<_Float16>(a.scale < 0.f ? -v : v);
+            }
+          }
+          q[n][ch][0] = __builtin_bit_cast(at_i4, h);
+          continue;
+        }
         uint32_t w[4][NT] = {};
-        if (finite && ch * 64 + c * 16 < D) {
+        if (finite && at < D) {
 #pragma unroll
           for (int x = 0; x < 16; ++x)
-            digits<NT>(static_cast<int>(rint(static_cast<double>(elem(row, ch * 64 + c * 16 + x)) * inv)), x & 3, w[x >> 2]);
+            digits<NT>(static_cast<int>(rint(static_cast<double>(elem(row, at + x)) * inv)), x & 3, w[x >> 2]);
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -212,6 +230,15 @@ struct Columns {
       for (int ch = 0; ch < DC; ++ch) k[ch] = key(u, ch);
 #pragma unroll
       for (int n = 0; n < QB; ++n) {
+        if constexpr (HALF) {
+          at_f4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ch = 0; ch < DC; ++ch)
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(at_h8, k[ch]), __builtin_bit_cast(at_h8, q[n][ch][0]),
+                                                         acc, 0, 0, 0);
+          s[n][u] = acc;
+          continue;
+        }
         at_i4 acc[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -221,7 +248,7 @@ struct Columns {
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float low = static_cast<float>((acc[NT - 2][i] << 8) + acc[NT - 1][i]);
+          const float low = static_cast<float>((acc[NT > 1 ? NT - 2 : 0][i] << 8) + acc[NT - 1][i]);
           s[n][u][i] = NT == 3 ? fmaf(static_cast<float>(acc[0][i]), 65536.f, low) : low;
         }
       }
@@ -229,7 +256,6 @@ struct Columns {
   }
 
   // Scores to weights; ks and vs are the scales of this lane's 16 tokens, `good` whether they can be used.
-  template <bool SMALL>
   __device__ __forceinline__ void weigh(at_f4 (&s)[QB][4], int t0, float ks, float vs, bool good) {
     const int c = (threadIdx.x >> 4) & 3;
     if (!good) vs = 0.f;
@@ -242,7 +268,8 @@ struct Columns {
       e = ve;
     }
     const float weight = fmaxf(ldexpf(vs, -e), 0x1p-40f) * static_cast<float>(1 << kLift);
-    const float unweight = __builtin_amdgcn_rcpf(weight), weight_log = __builtin_amdgcn_logf(weight);
+    const float weight_log = __builtin_amdgcn_logf(weight);
+    unweight = __builtin_amdgcn_rcpf(weight);
     const bool whole = t0 >= all_lo && t0 + kTokens <= all_hi;
     uint32_t seen[QB];  // which of the lane's 16 tokens its column sees
     if (!whole) {
@@ -288,12 +315,14 @@ struct Columns {
         for (int j = 0; j < 16; ++j)
           if (!(seen[n] >> j & 1)) s[n][j >> 2][j & 3] = 0.f;
     }
+    if constexpr (!kSumByProduct) {
 #pragma unroll
-    for (int n = 0; n < QB; ++n) {
-      float sum = 0.f;
+      for (int n = 0; n < QB; ++n) {
+        float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) sum += s[n][j >> 2][j & 3];
-      l[n] = fmaf(sum, unweight, l[n]);
+        for (int j = 0; j < 16; ++j) sum += s[n][j >> 2][j & 3];
+        l[n] = fmaf(sum, unweight, l[n]);
+      }
     }
   }
 
@@ -313,6 +342,18 @@ struct Columns {
             pw[n][j >> 3][j & 7] = h[0];
             pw[n][j >> 3][(j & 7) + 1] = h[1];
           }
+        if constexpr (kSumByProduct) {
+          const _Float16 one = 1;
+          const at_h8 ones = {one, one, one, one, one, one, one, one};
+#pragma unroll
+          for (int n = 0; n < QB; ++n) {
+            at_f4 sum = {0.f, 0.f, 0.f, 0.f};
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pw[n][0], sum, 0, 0, 0);
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pw[n][1], sum, 0, 0, 0);
+            l[n] = fmaf(sum[0], unweight * 0.25f, l[n]);  // all quarters have the whole sum, and are added up in end()
+          }
+          unweight *= 0x1p-14f;  // for another pass
+        }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           const at_h8 v0 = __builtin_bit_cast(at_h8, value(d, 0)), v1 = __builtin_bit_cast(at_h8, value(d, 1));
@@ -489,7 +530,7 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel
   const int cols = min(sq.n, a.bt.max_new) * a.G, col0 = pc.tile * 16;
   if (col0 >= cols) return;
   const bool ok = sq.ok && (sq.len == 0 || a.c.n_pages > 0);
-  Columns<T, DT, 1> w;
+  Columns<T, DT, 1, false, SMALL> w;
   w.begin(a, sq, ok, pc.hk, col0, cols);
   int first = w.first, last = w.last;
   share_of(a, pc.split, kStride, first, last);
@@ -535,7 +576,7 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel
     if (t0 + kStride < last) load_keys(t0 + kStride, kp);
     vp = SMALL ? value_page(t0 + kStride) : kp;
     kp = key_page(t0 + 2 * kStride);
-    w.template weigh<SMALL>(s, t0, ks, vs, good);
+    w.weigh(s, t0, ks, vs, good);
     w.add(s, [&](int d, int half) {
       asm volatile("" : "+v"(vreg[d]));  // widened where it is used, in every pass
       return widen<T>(vreg[d][2 * half], vreg[d][2 * half + 1]);
@@ -573,12 +614,13 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel
 }
 
 // Many columns: every wave has 16 QB of its own, and the four of a workgroup walk the same tokens.  A step's keys
-// and values pass through LDS, two steps of them: keys as they are, values widened once for all four waves.  Rows of
+// and values pass through LDS, two steps of them, widened once for all four waves (keys of fp32 queries as they are).  Rows of
 // LDS are padded by 16 bytes, and a key's row is u * 16 + r for the token that is row r of tile u, so that the 16 rows
 // an instruction reads lie in different banks.  The vector units bound it (the softmax's exponentials).
 template <typename T, int DT, int QB, bool SMALL>
 __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kernel(const AttnArgs a) {
-  constexpr int kKeyRow = DT * 16 + 16, kValueRow = kTokens * 2 + 16;
+  constexpr bool HALF = sizeof(T) == 2;
+  constexpr int kKeyRow = DT * 16 * (HALF ? 2 : 1) + 16, kValueRow = kTokens * 2 + 16;
   constexpr int kKeyBytes = kTokens * kKeyRow, kBuffer = kKeyBytes + DT * 16 * kValueRow;
   constexpr int kPer = (DT * 16 * 4 + 255) / 256;  // 16-byte pieces of keys, and of values, that a thread moves
   extern __shared__ __align__(16) uint8_t lds[];   // [2][kBuffer]
@@ -589,7 +631,7 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kern
   const int cols = min(sq.n, a.bt.max_new) * a.G, tile0 = pc.tile * (64 * QB), col0 = tile0 + wave * (16 * QB);
   if (tile0 >= cols) return;
   const bool ok = sq.ok && (sq.len == 0 || a.c.n_pages > 0), mine = col0 < cols;
-  Columns<T, DT, QB> w;
+  Columns<T, DT, QB, HALF, SMALL> w;
   w.begin(a, sq, ok, pc.hk, min(col0, cols - 1), cols);
   // the workgroup's tokens
   int* shared = reinterpret_cast<int*>(lds);
@@ -610,7 +652,6 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kern
   share_of(a, pc.split, kTokens, first, last);
 
   const Pages pages = {a.bt.table + static_cast<int64_t>(pc.b) * a.bt.ld_table, a.c.n_pages, sq.len, pl2};
-  auto uniform = [](int x) { return SMALL ? x : __builtin_amdgcn_readfirstlane(x); };
   auto head_of = [&](int p) { return static_cast<int64_t>(pages.there(p) ? p : 0) * a.c.Hkv + pc.hk; };
   const int64_t head_bytes = static_cast<int64_t>(D) << pl2;
   // the pieces this thread moves: of keys, 16 elements of a token; of values, 16 tokens of an element
@@ -622,29 +663,53 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kern
     kt[i] = x / d16;
     ke[i] = x - kt[i] * d16;
   }
+  // A step's pages are looked up two steps ahead, its keys, values and scales are read one step ahead.
+  int kp[SMALL ? kPer : 1], vp[SMALL ? kPer : 1], sp = 0;
+  auto look_up = [&](int t0) {
+    if (t0 >= last) return;
+    if constexpr (SMALL) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        kp[i] = pages.of(t0 + (kt[i] & ~15), t0);
+        vp[i] = pages.of(t0 + (min(tid + i * 256, pieces - 1) & 3) * 16, t0);
+      }
+      sp = pages.of(t0 + 16 * c, t0);
+    } else {
+      sp = __builtin_amdgcn_readfirstlane(pages.of(t0, t0));
+    }
+  };
   at_u4 kreg[kPer], vreg[kPer];
+  float ks_next = 0.f, vs_next = 0.f;
+  bool good_next = false;
   auto fetch = [&](int t0) {
-    const int page0 = SMALL ? 0 : uniform(pages.of(t0, t0));
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int p = SMALL ? pages.of(t0 + (kt[i] & ~15), t0) : page0;
-      const int8_t* k = a.c.k + head_of(p) * head_bytes;
+      const int8_t* k = a.c.k + head_of(SMALL ? kp[SMALL ? i : 0] : sp) * head_bytes;
       kreg[i] = *reinterpret_cast<const at_u4*>(k + (((t0 + kt[i]) & in_page) * D + ke[i] * 16));
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int x = min(tid + i * 256, pieces - 1), g = (x & 3) * 16;
-      const int p = SMALL ? pages.of(t0 + g, t0) : page0;
-      const int8_t* v = a.c.v + head_of(p) * head_bytes;
+      const int8_t* v = a.c.v + head_of(SMALL ? vp[SMALL ? i : 0] : sp) * head_bytes;
       vreg[i] = *reinterpret_cast<const at_u4*>(v + (((x >> 2) << pl2) + ((t0 + g) & in_page)));
     }
+    const int64_t head = head_of(sp);
+    ks_next = a.c.k_scale[head];
+    vs_next = a.c.v_scale[head];
+    good_next = pages.there(sp);
   };
   auto settle = [&](uint8_t* to) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int x = min(tid + i * 256, pieces - 1);
       const int row = ((kt[i] >> 2) & 3) * 16 + (kt[i] >> 4) * 4 + (kt[i] & 3);
-      *reinterpret_cast<at_u4*>(to + row * kKeyRow + ke[i] * 16) = kreg[i];
+      if constexpr (HALF) {
+        uint8_t* k = to + row * kKeyRow + ke[i] * 32;
+        *reinterpret_cast<at_u4*>(k) = widen<T>(kreg[i][0], kreg[i][1]);
+        *reinterpret_cast<at_u4*>(k + 16) = widen<T>(kreg[i][2], kreg[i][3]);
+      } else {
+        *reinterpret_cast<at_u4*>(to + row * kKeyRow + ke[i] * 16) = kreg[i];
+      }
       uint8_t* v = to + kKeyBytes + (x >> 2) * kValueRow + (x & 3) * 32;
       *reinterpret_cast<at_u4*>(v) = widen<T>(vreg[i][0], vreg[i][1]);
       *reinterpret_cast<at_u4*>(v + 16) = widen<T>(vreg[i][2], vreg[i][3]);
@@ -657,25 +722,30 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kern
     __syncthreads();
   }
 
+  look_up(first);
   if (first < last) {
     fetch(first);
     settle(lds);
   }
+  look_up(first + kTokens);
   __syncthreads();
   int buffer = 0;
   for (int t0 = first; t0 < last; t0 += kTokens) {
     const uint8_t* from = lds + buffer * kBuffer;
+    const float ks = ks_next, vs = vs_next;
+    const bool good = good_next && usable(ks, vs);
     if (t0 + kTokens < last) fetch(t0 + kTokens);
+    look_up(t0 + 2 * kTokens);
     if (t0 + kTokens > w.first && t0 < w.last) {
-      const int p = uniform(pages.of(SMALL ? t0 + 16 * c : t0, t0));
-      const int64_t head = head_of(p);
-      const float ks = a.c.k_scale[head], vs = a.c.v_scale[head];
-      const bool good = pages.there(p) && usable(ks, vs);
       at_f4 s[QB][4];
+      __builtin_amdgcn_s_setprio(1);
       w.scores(s, [&](int u, int ch) { return *reinterpret_cast<const at_i4*>(from + (u * 16 + r) * kKeyRow + ch * 64 + c * 16); });
-      w.template weigh<SMALL>(s, t0, ks, vs, good);
+      __builtin_amdgcn_s_setprio(0);
+      w.weigh(s, t0, ks, vs, good);
+      __builtin_amdgcn_s_setprio(1);
       const uint8_t* v = from + kKeyBytes + r * kValueRow + c * 32;
       w.add(s, [&](int d, int half) { return *reinterpret_cast<const at_u4*>(v + d * 16 * kValueRow + half * 16); });
+      __builtin_amdgcn_s_setprio(0);
     }
     buffer ^= 1;
     if (t0 + kTokens < last) settle(lds + buffer * kBuffer);
@@ -791,7 +861,7 @@ hipError_t attend_as(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
   if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
   const dim3 grid(static_cast<uint32_t>(blocks));
   const bool small = a.c.page_log2 < 6;
-  const size_t lds = 2 * (kTokens * (DT * 16 + 16) + DT * 16 * (kTokens * 2 + 16));
+  const size_t lds = 2 * (kTokens * (DT * 16 * (sizeof(T) == 2 ? 2 : 1) + 16) + DT * 16 * (kTokens * 2 + 16));
   if (p.prompt) {
     if (small) kv_attention_prompt_kernel<T, DT, QB, true><<<grid, 256, lds, stream>>>(a);
     else kv_attention_prompt_kernel<T, DT, QB, false><<<grid, 256, lds, stream>>>(a);
