@@ -221,13 +221,20 @@ struct Columns {
   }
 
   // The scores of 64 tokens, in query steps: key(u, ch) is the left operand of tile u and chunk ch.
-  template <class Key>
+  // LDS: operands come from LDS, and are asked for a tile (of values two) before they are used.
+  template <bool LDS, class Key>
   __device__ __forceinline__ void scores(at_f4 (&s)[QB][4], Key&& key) {
+    at_i4 ahead[2][DC];
+#pragma unroll
+    for (int ch = 0; ch < DC; ++ch) ahead[0][ch] = key(0, ch);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      at_i4 k[DC];
+      const at_i4 (&k)[DC] = ahead[u & 1];
+      if (u < 3) {
 #pragma unroll
-      for (int ch = 0; ch < DC; ++ch) k[ch] = key(u, ch);
+        for (int ch = 0; ch < DC; ++ch) ahead[(u + 1) & 1][ch] = key(u + 1, ch);
+      }
+      if constexpr (LDS) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int n = 0; n < QB; ++n) {
         if constexpr (HALF) {
@@ -327,7 +334,7 @@ struct Columns {
   }
 
   // Adds the values of 64 tokens: value(d, w) is the left operand (fp16; bf16 for fp32 queries) of tile d and half w.
-  template <class Value>
+  template <bool LDS, class Value>
   __device__ __forceinline__ void add(at_f4 (&s)[QB][4], Value&& value) {
     if constexpr (sizeof(T) == 2) {
       for (int pass = 0;; ++pass) {
@@ -342,6 +349,12 @@ struct Columns {
             pw[n][j >> 3][j & 7] = h[0];
             pw[n][j >> 3][(j & 7) + 1] = h[1];
           }
+        at_u4 ahead[3][2];
+        if constexpr (LDS) {
+#pragma unroll
+          for (int d = 0; d < 2; ++d) ahead[d][0] = value(d, 0), ahead[d][1] = value(d, 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
         if constexpr (kSumByProduct) {
           const _Float16 one = 1;
           const at_h8 ones = {one, one, one, one, one, one, one, one};
@@ -356,12 +369,18 @@ struct Columns {
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const at_h8 v0 = __builtin_bit_cast(at_h8, value(d, 0)), v1 = __builtin_bit_cast(at_h8, value(d, 1));
-#pragma unroll
-          for (int n = 0; n < QB; ++n) {
-            o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[n][0], o[n][d], 0, 0, 0);
-            o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pw[n][1], o[n][d], 0, 0, 0);
+          if constexpr (LDS) {
+            if (d + 2 < DT) ahead[(d + 2) % 3][0] = value(d + 2, 0), ahead[(d + 2) % 3][1] = value(d + 2, 1);
+            __builtin_amdgcn_sched_barrier(0);
+          } else {
+            ahead[d % 3][0] = value(d, 0);
+            ahead[d % 3][1] = value(d, 1);
           }
+          const at_h8 v0 = __builtin_bit_cast(at_h8, ahead[d % 3][0]), v1 = __builtin_bit_cast(at_h8, ahead[d % 3][1]);
+#pragma unroll
+          for (int n = 0; n < QB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[n][0], o[n][d], 0, 0, 0);
+#pragma unroll
+          for (int n = 0; n < QB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pw[n][1], o[n][d], 0, 0, 0);
         }
         // weights below fp16's normal numbers: what the rounding left of them, 2^14 times as large, once more
         bool more = false;
@@ -572,12 +591,12 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel
     const float ks = a.c.k_scale[head], vs = a.c.v_scale[head];
     const bool good = pages.there(vp) && usable(ks, vs);
     at_f4 s[1][4];
-    w.scores(s, [&](int u, int ch) { return kreg[u][ch]; });
+    w.template scores<false>(s, [&](int u, int ch) { return kreg[u][ch]; });
     if (t0 + kStride < last) load_keys(t0 + kStride, kp);
     vp = SMALL ? value_page(t0 + kStride) : kp;
     kp = key_page(t0 + 2 * kStride);
     w.weigh(s, t0, ks, vs, good);
-    w.add(s, [&](int d, int half) {
+    w.template add<false>(s, [&](int d, int half) {
       asm volatile("" : "+v"(vreg[d]));  // widened where it is used, in every pass
       return widen<T>(vreg[d][2 * half], vreg[d][2 * half + 1]);
     });
@@ -739,12 +758,12 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kern
     if (t0 + kTokens > w.first && t0 < w.last) {
       at_f4 s[QB][4];
       __builtin_amdgcn_s_setprio(1);
-      w.scores(s, [&](int u, int ch) { return *reinterpret_cast<const at_i4*>(from + (u * 16 + r) * kKeyRow + ch * 64 + c * 16); });
+      w.template scores<true>(s, [&](int u, int ch) { return *reinterpret_cast<const at_i4*>(from + (u * 16 + r) * kKeyRow + ch * 64 + c * 16); });
       __builtin_amdgcn_s_setprio(0);
       w.weigh(s, t0, ks, vs, good);
       __builtin_amdgcn_s_setprio(1);
       const uint8_t* v = from + kKeyBytes + r * kValueRow + c * 32;
-      w.add(s, [&](int d, int half) { return *reinterpret_cast<const at_u4*>(v + d * 16 * kValueRow + half * 16); });
+      w.template add<true>(s, [&](int d, int half) { return *reinterpret_cast<const at_u4*>(v + d * 16 * kValueRow + half * 16); });
       __builtin_amdgcn_s_setprio(0);
     }
     buffer ^= 1;

@@ -134,37 +134,45 @@ __global__ __launch_bounds__(256) void w4_dequant_kernel(const W4 w, T* out, int
 // right operand of one v_mfma_f32_16x16x32_bf16; the left one holds x.  What that instruction would add up over the four
 // quarters c, different groups when group < 128, is kept apart by its 16 left rows: they are 16 / TB segments of
 // TB vectors, and the row of (segment, vector) holds x in the segment's quarters and zeros elsewhere.  TB = 4, 8,
-// 16 gives segments of 32, 64, 128 columns.  A fifth to eighth instruction with ones on the right gives the
-// segment's sum X of x, and a row's total takes  s (acc - (16 + z) X),  where acc and X are fp32.
-// Waves of a workgroup share the rows and take every waves-th step of the columns; x (fp32: three bf16 terms, which
-// hold all of its 24 bits, as three vectors) waits in LDS in the order of the codes, all of it or a chunk of columns
-// at a time.
+// 16 gives segments of 32, 64, 128 columns.  A row's total takes  s (acc - (16 + z) X),  X the sum of x over the segment
+// (the same instruction with ones on the right, once for all rows); acc and X are fp32.
+// A workgroup keeps a chunk of the columns of x in LDS, in the order of the codes (fp32: three bf16 terms, which hold
+// all of its 24 bits, as three vectors), and walks blocks of 16 rows, the next block's codes on their way while one is
+// computed; its waves share the rows and take every waves-th step of the columns.  Chunks are joined by a second
+// launch.  Reading the codes bounds it.
 typedef __bf16 w4_bf8 __attribute__((ext_vector_type(8)));
 typedef float w4_f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t w4_u4 __attribute__((ext_vector_type(4)));
 
-constexpr int kStep = 128;    // columns of a step
-constexpr int kXPad = 8;      // elements between rows of x in LDS
-constexpr int kXBytes = 68 << 10;  // two workgroups a CU
+constexpr int kStep = 128;             // columns of a step
+constexpr int kXPad = 8;               // elements between rows of x in LDS
+constexpr int kXBytes = 73 << 10;      // of x in LDS: two workgroups a CU
+constexpr int kWaves = 256 * 16;       // waves that fill the chip
 
+struct GemvPlan4 {
+  int tb, nb;        // vectors of a block, blocks
+  int per_pass;      // vectors of a pass (grid z)
+  int waves, batches;  // a chunk is waves * batches * (steps of a batch) steps of columns
+  int chunks;        // grid y
+  int64_t groups;    // workgroups of a chunk and pass (grid x)
+};
 struct GemvArgs {
   W4 w;
   const void* x;
   void* y;
+  float* part;  // [chunk][T][M] when there are several
   int64_t ldx, ldy, T;
   int x_f32, y_f32, x_vec;
-  int per_pass;  // vectors of one workgroup (grid y passes)
-  int steps;     // steps of a wave within a chunk of columns
-  int chunks;
+  int per_pass, batches, chunks;
 };
+constexpr int batch_steps(int nb) { return nb == 1 ? 4 : 2; }
 
 // Two bf16 of x in the order of the codes' halves: (u.lo, v.lo) and (u.hi, v.hi).
 __device__ __forceinline__ uint32_t lo2(uint32_t u, uint32_t v) { return __builtin_amdgcn_perm(v, u, 0x05040100u); }
 __device__ __forceinline__ uint32_t hi2(uint32_t u, uint32_t v) { return __builtin_amdgcn_perm(v, u, 0x07060302u); }
 
-// Eight codes of a word as bf16 16 + code, columns 0 4 1 5 2 6 3 7.
-__device__ __forceinline__ w4_bf8 widen8(uint32_t c) {
-  constexpr uint32_t mask = 0x00780078u, base = 0x41804180u;
+// Eight codes of a word as bf16 16 + code, columns 0 4 1 5 2 6 3 7; mask and base in registers, for one and-or.
+__device__ __forceinline__ w4_bf8 widen8(uint32_t c, uint32_t mask, uint32_t base) {
   const w4_u4 v = {((c << 3) & mask) | base, ((c >> 1) & mask) | base, ((c >> 5) & mask) | base, ((c >> 9) & mask) | base};
   return __builtin_bit_cast(w4_bf8, v);
 }
@@ -207,155 +215,171 @@ __device__ __forceinline__ void stage8(const GemvArgs& a, int64_t t, int64_t j, 
   }
 }
 
-// NB blocks of TB vectors; NR of a lane's four sums of a block in use; RB blocks of 16 rows; U steps loaded at once.
-template <int TB, int NB, int NR, int RB, int U, typename TS>
+// NB blocks of TB vectors; NR of a lane's four sums of a block in use.
+template <int TB, int NB, int NR, typename TS>
 __global__ __launch_bounds__(1024) void w4_gemv_kernel(const GemvArgs a) {
+  constexpr int U = batch_steps(NB);
   extern __shared__ __align__(16) uint16_t xs[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
   const int r = lane & 15, c = lane >> 4;
-  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * (16 * RB);
-  const int64_t t0 = static_cast<int64_t>(blockIdx.y) * a.per_pass;
+  const int64_t t0 = static_cast<int64_t>(blockIdx.z) * a.per_pass;
   const int nt = static_cast<int>(min(a.T - t0, static_cast<int64_t>(a.per_pass)));
   const int held = a.x_f32 ? 3 * nt : nt;  // rows of x in LDS
-  const int chunk_cols = a.steps * waves * kStep, ld = chunk_cols + kXPad;
-  uint16_t* zero = xs + held * ld;         // eight zeros, for rows of other segments
+  const int steps = a.batches * U * waves, cols = steps * kStep, ld = cols + kXPad;
+  const int64_t k0 = static_cast<int64_t>(blockIdx.y) * cols;
+  uint16_t* zero = xs + held * ld;                               // eight zeros, for rows of other segments
+  float* sums = reinterpret_cast<float*>(zero + 8);              // X: [step][block][quarter][NR]
+  float* part = sums + steps * (NB * 4 * NR);                    // [2][wave][block][vector][16 rows of W]
 
-  // weights: this lane's row of every block, its 32 columns
-  const uint8_t* codes[RB];
-  const TS* scales[RB];
-  const uint8_t* zeros[RB];
+  // this lane's codes and scales: row r of a block of 16, columns 32 c of a step
   const int64_t stored = (a.w.N + 31) & ~int64_t{31}, last_group = (a.w.N - 1) >> a.w.group_log2;
-#pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    const int64_t row = min(row0 + b * 16 + r, a.w.M - 1);
-    codes[b] = a.w.codes + row * a.w.ld;
-    scales[b] = static_cast<const TS*>(a.w.scales) + row * a.w.ld_s;
-    zeros[b] = a.w.zeros ? a.w.zeros + row * a.w.ld_z : nullptr;
-  }
+  const int64_t blocks = (a.w.M + 15) >> 4;
   const int seg_col = ((c * 4) / TB) * (8 * TB);  // first column of the segment whose sums this lane holds
-  uint4 wq[U][RB];
-  float sc[U][RB], zp[U][RB];
-  auto column = [&](int n) {  // first column of this wave's n-th step
-    const int chunk = n / a.steps;
-    return static_cast<int64_t>(chunk) * chunk_cols + static_cast<int64_t>((n - chunk * a.steps) * waves + wave) * kStep;
-  };
-  auto load = [&](int n) {
+  const TS* const scales = static_cast<const TS*>(a.w.scales);
+  uint4 wq[U];
+  float sc[U], zp[U];
+  auto load = [&](int64_t block, int batch) {
+    const int64_t row = min(block * 16 + r, a.w.M - 1);
+    const uint8_t* codes = a.w.codes + row * a.w.ld;
+    const TS* scale = scales + row * a.w.ld_s;
+    const uint8_t* zeros = a.w.zeros + row * a.w.ld_z;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t kb = column(n + u);
-      if (kb >= a.w.N) break;
+      const int64_t kb = k0 + static_cast<int64_t>((batch * U + u) * waves + wave) * kStep;
       const int64_t col = kb + 32 * c, g = min((kb + seg_col) >> a.w.group_log2, last_group);
-#pragma unroll
-      for (int b = 0; b < RB; ++b) {
-        wq[u][b] = ld_stream(codes[b] + (col < stored ? col >> 1 : 0));
-        sc[u][b] = ld1(scales[b] + g);
-        zp[u][b] = zeros[b] ? static_cast<float>(zeros[b][g]) : 8.f;
-      }
+      wq[u] = ld_stream(codes + (col < stored ? col >> 1 : 0));  // past the row: x is zero there
+      sc[u] = ld1(scale + g);
+      zp[u] = a.w.zeros ? static_cast<float>(zeros[g]) : 8.f;
     }
   };
+  int64_t block = blockIdx.x;
+  load(block, 0);
 
-  w4_f4 tot[RB][NB];
-#pragma unroll
-  for (int b = 0; b < RB; ++b)
-#pragma unroll
-    for (int n = 0; n < NB; ++n) tot[b][n] = w4_f4{0.f, 0.f, 0.f, 0.f};
+  const int per = cols >> 3;
+  for (int i = tid; i < nt * per; i += blockDim.x) {
+    const int t = i / per, j = (i - t * per) * 8;
+    stage8(a, t0 + t, k0 + j, xs + j, ld, t, nt);
+  }
+  if (tid < 2) reinterpret_cast<uint2*>(zero)[tid] = make_uint2(0u, 0u);
+  __syncthreads();
+
   // left operand: this lane's row is a vector of a segment; it reads x where the segment has this lane's columns
   const uint16_t* xp[NB];
-  int xstep[NB];
+  int live[NB];
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     const int v = n * TB + (r & (TB - 1));
-    const bool live = r / TB == (c * 4) / TB && v < held;
-    xp[n] = live ? xs + v * ld + 32 * c : zero;
-    xstep[n] = live ? 1 : 0;
+    live[n] = r / TB == (c * 4) / TB && v < held;
+    xp[n] = live[n] ? xs + v * ld + 32 * c : zero;
   }
   const w4_bf8 ones = __builtin_bit_cast(w4_bf8, w4_u4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
-
-  load(0);
-  const int total = a.chunks * a.steps;
-  for (int n0 = 0; n0 < total; n0 += U) {
-    if (n0 % a.steps == 0) {  // the next chunk of x
-      const int64_t k0 = static_cast<int64_t>(n0 / a.steps) * chunk_cols;
-      if (n0) __syncthreads();
-      const int per = chunk_cols >> 3;
-      for (int i = tid; i < nt * per; i += blockDim.x) {
-        const int t = i / per, j = (i - t * per) * 8;
-        stage8(a, t0 + t, k0 + j, xs + j, ld, t, nt);
+  for (int s = wave; s < steps; s += waves) {
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      w4_f4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const w4_bf8*>(xp[n] + live[n] * (s * kStep + 8 * i)), ones,
+                                                      sum, 0, 0, 0);
+      if (r == 0) {
+#pragma unroll
+        for (int i = 0; i < NR; ++i) sums[((s * NB + n) * 4 + c) * NR + i] = sum[i];
       }
-      if (tid < 2) reinterpret_cast<uint2*>(zero)[tid] = make_uint2(0u, 0u);
-      __syncthreads();
-    }
-    uint4 cur[U][RB];
-    float cs[U][RB], cz[U][RB];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int b = 0; b < RB; ++b) cur[u][b] = wq[u][b], cs[u][b] = sc[u][b], cz[u][b] = zp[u][b];
-    if (n0 + U < total) load(n0 + U);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (column(n0 + u) >= a.w.N) break;
-      const int at = ((n0 + u) % a.steps * waves + wave) * kStep;
-      w4_f4 acc[RB][NB], sum[NB];
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        sum[n] = w4_f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int b = 0; b < RB; ++b) acc[b][n] = sum[n];
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w4_bf8 right[RB];
-#pragma unroll
-        for (int b = 0; b < RB; ++b) {
-          const uint32_t word = i == 0 ? cur[u][b].x : i == 1 ? cur[u][b].y : i == 2 ? cur[u][b].z : cur[u][b].w;
-          right[b] = widen8(word);
-        }
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          const w4_bf8 left = *reinterpret_cast<const w4_bf8*>(xp[n] + xstep[n] * (at + 8 * i));
-          sum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(left, ones, sum[n], 0, 0, 0);
-#pragma unroll
-          for (int b = 0; b < RB; ++b)
-            acc[b][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(left, right[b], acc[b][n], 0, 0, 0);
-        }
-      }
-#pragma unroll
-      for (int b = 0; b < RB; ++b)
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-          for (int i = 0; i < NR; ++i)
-            tot[b][n][i] = fmaf(cs[u][b], fmaf(-16.f - cz[u][b], sum[n][i], acc[b][n][i]), tot[b][n][i]);
     }
   }
-
-  // joined over waves, segments and terms, in that order
   __syncthreads();
-  float* part = reinterpret_cast<float*>(xs);  // [wave][RB][NB][16 left rows][16 rows of W]
+
+  uint32_t mask = 0x00780078u, base = 0x41804180u;
+  asm volatile("" : "+s"(mask), "+v"(base));
+  w4_f4 tot[NB];
 #pragma unroll
-  for (int b = 0; b < RB; ++b)
+  for (int n = 0; n < NB; ++n) tot[n] = w4_f4{0.f, 0.f, 0.f, 0.f};
+  int batch = 0, buffer = 0;
+  while (block < blocks) {
+    uint4 cur[U];
+    float cs[U], cz[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) cur[u] = wq[u], cs[u] = sc[u], cz[u] = -16.f - zp[u];
+    const bool last = batch + 1 == a.batches;
+    const int64_t next = last ? block + gridDim.x : block;
+    if (next < blocks) load(next, last ? 0 : batch + 1);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = (batch * U + u) * waves + wave;
+      w4_f4 acc[NB];
+#pragma unroll
+      for (int n = 0; n < NB; ++n) acc[n] = w4_f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const w4_bf8 right = widen8(i == 0 ? cur[u].x : i == 1 ? cur[u].y : i == 2 ? cur[u].z : cur[u].w, mask, base);
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+          acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const w4_bf8*>(xp[n] + live[n] * (s * kStep + 8 * i)),
+                                                           right, acc[n], 0, 0, 0);
+      }
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+          tot[n][i] = fmaf(cs[u], fmaf(cz[u], sums[((s * NB + n) * 4 + c) * NR + i], acc[n][i]), tot[n][i]);
+    }
+    if (!last) {
+      ++batch;
+      continue;
+    }
+    // joined over the segments in the wave, then over waves and terms, in that order
+    float* mine = part + (buffer * waves + wave) * (NB * TB * 16);
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
-      for (int i = 0; i < NR; ++i) part[(((wave * RB + b) * NB + n) * 16 + 4 * c + i) * 16 + r] = tot[b][n][i];
-  __syncthreads();
-  for (int o = tid; o < nt * 16 * RB; o += blockDim.x) {
-    const int t = o / (16 * RB), rr = o - t * (16 * RB), b = rr >> 4;
-    if (row0 + rr >= a.w.M) continue;
-    float y = 0.f;
-    for (int v = t; v < held; v += nt) {
-      const int n = v / TB, at = v - n * TB;
-      for (int w = 0; w < waves; ++w)
-#pragma unroll
-        for (int s = 0; s < 16 / TB; ++s) y += part[(((w * RB + b) * NB + n) * 16 + s * TB + at) * 16 + (rr & 15)];
+      for (int i = 0; i < NR; ++i) {
+        float x = tot[n][i];
+        if (TB <= 8) {
+          const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+          x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+        }
+        if (TB == 4) {
+          const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+          x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+        }
+        if (4 * c < TB) mine[(n * TB + 4 * c + i) * 16 + r] = x;
+        tot[n][i] = 0.f;
+      }
+    __syncthreads();
+    const float* all = part + buffer * waves * (NB * TB * 16);
+    for (int o = tid; o < nt * 16; o += blockDim.x) {
+      const int t = o >> 4;
+      const int64_t row = block * 16 + (o & 15);
+      if (row >= a.w.M) continue;
+      float y = 0.f;
+      for (int v = t; v < held; v += nt)
+#pragma unroll 4
+        for (int w = 0; w < waves; ++w) y += all[(w * (NB * TB) + v) * 16 + (o & 15)];
+      if (a.chunks > 1)
+        a.part[(static_cast<int64_t>(blockIdx.y) * a.T + t0 + t) * a.w.M + row] = y;
+      else if (a.y_f32)
+        static_cast<float*>(a.y)[(t0 + t) * a.ldy + row] = y;
+      else
+        static_cast<uint16_t*>(a.y)[(t0 + t) * a.ldy + row] = static_cast<uint16_t>(f_bf16(y));
     }
-    const int64_t to = (t0 + t) * a.ldy + row0 + rr;
-    if (a.y_f32)
-      static_cast<float*>(a.y)[to] = y;
-    else
-      static_cast<uint16_t*>(a.y)[to] = static_cast<uint16_t>(f_bf16(y));
+    buffer ^= 1;
+    batch = 0;
+    block = next;
   }
+}
+
+// y = the sum of the chunks' parts, in order.
+__global__ __launch_bounds__(256) void w4_join_kernel(const GemvArgs a) {
+  const int64_t n = a.T * a.w.M, i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= n) return;
+  float y = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < a.chunks; ++s) y += a.part[s * n + i];
+  const int64_t t = i / a.w.M, at = t * a.ldy + i - t * a.w.M;
+  if (a.y_f32)
+    static_cast<float*>(a.y)[at] = y;
+  else
+    static_cast<uint16_t*>(a.y)[at] = static_cast<uint16_t>(f_bf16(y));
 }
 
 // L lanes for rows of `units`, at least `least` of them (a power of two), and the grid for M rows.
@@ -407,41 +431,70 @@ hipError_t launch_w4_dequant(const W4& w, void* out, int64_t ldo, int type, hipS
   return w.s_type == ET_F32 ? dequant_as<uint16_t, uint32_t>(w, out, ldo, stream) : dequant_as<uint16_t, uint16_t>(w, out, ldo, stream);
 }
 
-size_t w4_gemv_ws_bytes(int64_t, int64_t, int64_t) { return 0; }
+// The widest segments that stay within a group and are needed take the fewest instructions; the columns are cut where
+// x does not fit into LDS, and, where there are few rows, until the chip is filled.
+static GemvPlan4 plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2) {
+  GemvPlan4 p;
+  const int terms = x_f32 ? 3 : 1, widest = group_log2 >= 7 ? 16 : 1 << (group_log2 - 3);
+  const int64_t rows = T * terms;
+  p.tb = rows <= 4 || widest == 4 ? 4 : rows <= 8 || widest == 8 ? 8 : 16;
+  const int most = 2 * p.tb / terms;
+  p.per_pass = static_cast<int>(T < most ? T : most);
+  p.nb = static_cast<int>(cdiv(static_cast<int64_t>(p.per_pass) * terms, p.tb));
+  const int U = batch_steps(p.nb), most_waves = p.nb == 1 ? 16 : 8;
+  const int64_t fit = (kXBytes / 2 / (p.per_pass * terms) - kXPad) / kStep;  // steps of x in LDS: at least 8
+  const int64_t steps = cdiv(N, kStep), blocks = cdiv(M, 16), passes = cdiv(T, p.per_pass);
+  int64_t chunk = steps < fit ? steps : fit;
+  if (blocks * passes < 64 && steps > 32) {  // few rows: chunks of at least 8 steps
+    const int64_t want = cdiv(256, blocks * passes), c = cdiv(steps, want);
+    if (c < chunk) chunk = c < 8 ? 8 : c;
+  }
+  const int64_t w = cdiv(chunk, U);
+  p.waves = static_cast<int>(w < most_waves ? w : most_waves);
+  int64_t batches = cdiv(chunk, p.waves * U);
+  if (batches * p.waves * U > fit) {
+    if (batches > 1) --batches;
+    else p.waves = static_cast<int>(fit / U);
+  }
+  p.batches = static_cast<int>(batches);
+  p.chunks = static_cast<int>(cdiv(steps, static_cast<int64_t>(p.waves) * p.batches * U));
+  const int64_t fill = cdiv(kWaves, static_cast<int64_t>(p.waves) * p.chunks * passes);
+  p.groups = blocks < fill ? blocks : fill;
+  return p;
+}
 
-template <int TB, int NB, int NR, int RB, int U>
-static hipError_t gemv_as(GemvArgs a, int waves, hipStream_t stream) {
-  const int rows = a.x_f32 ? 3 * a.per_pass : a.per_pass;
-  // all of x in LDS, or chunks of whole batches of steps; rows <= 64 leaves at least one batch of four waves
-  const int64_t fit = (kXBytes - 16) / 2 / rows - kXPad;
-  while (waves > 1 && static_cast<int64_t>(U) * waves * kStep > fit) waves >>= 1;
-  const int64_t all = cdiv(cdiv(a.w.N, static_cast<int64_t>(kStep) * waves), U);  // batches of a wave
-  const int64_t most = fit / (static_cast<int64_t>(U) * waves * kStep);
-  a.steps = static_cast<int>((all < most ? all : most) * U);
-  a.chunks = static_cast<int>(cdiv(all * U, a.steps));
-  const size_t x_bytes = static_cast<size_t>(rows) * (a.steps * waves * kStep + kXPad) * 2 + 16;
-  const size_t part = static_cast<size_t>(waves) * RB * NB * 256 * 4;
-  const size_t lds = x_bytes > part ? x_bytes : part;
-  const dim3 grid(static_cast<uint32_t>(cdiv(a.w.M, 16 * RB)), static_cast<uint32_t>(cdiv(a.T, a.per_pass)));
+static size_t part_bytes(const GemvPlan4& p, int64_t M, int64_t T) {
+  return p.chunks > 1 ? align256(static_cast<size_t>(p.chunks) * T * M * sizeof(float)) : 0;
+}
+
+size_t w4_gemv_ws_bytes(int64_t M, int64_t N, int64_t T) {
+  size_t most = 0;
+  for (int f32 = 0; f32 < 2; ++f32)
+    for (int g = 5; g <= 7; ++g) {
+      const size_t n = part_bytes(plan_w4_gemv(M, N, T, f32, g), M, T);
+      if (n > most) most = n;
+    }
+  return most;
+}
+
+template <int TB, int NB, int NR>
+static hipError_t gemv_as(const GemvPlan4& p, const GemvArgs& a, hipStream_t stream) {
+  const int held = a.x_f32 ? 3 * p.per_pass : p.per_pass;
+  const int64_t steps = static_cast<int64_t>(p.waves) * p.batches * batch_steps(NB);
+  const size_t lds = static_cast<size_t>(held) * (steps * kStep + kXPad) * 2 + 16 + steps * NB * 4 * NR * sizeof(float) +
+                     size_t{2} * p.waves * NB * TB * 16 * sizeof(float);
+  const int64_t passes = cdiv(a.T, p.per_pass);
+  if (passes > 65535 || p.chunks > 65535) return hipErrorInvalidConfiguration;
+  const dim3 grid(static_cast<uint32_t>(p.groups), static_cast<uint32_t>(p.chunks), static_cast<uint32_t>(passes));
   if (a.w.s_type == ET_F32)
-    w4_gemv_kernel<TB, NB, NR, RB, U, uint32_t><<<grid, waves * 64, lds, stream>>>(a);
+    w4_gemv_kernel<TB, NB, NR, uint32_t><<<grid, p.waves * 64, lds, stream>>>(a);
   else
-    w4_gemv_kernel<TB, NB, NR, RB, U, uint16_t><<<grid, waves * 64, lds, stream>>>(a);
+    w4_gemv_kernel<TB, NB, NR, uint16_t><<<grid, p.waves * 64, lds, stream>>>(a);
   return hipGetLastError();
 }
 
-template <int TB>
-static hipError_t gemv_blocks(int nb, const GemvArgs& a, int waves, hipStream_t stream) {
-  switch (nb) {
-    case 1: return gemv_as<TB, 1, 4, 1, 2>(a, waves, stream);
-    case 2: return gemv_as<TB, 2, 4, 1, 2>(a, waves, stream);
-    case 3: return gemv_as<TB, 3, 4, 1, 1>(a, waves, stream);
-    default: return gemv_as<TB, 4, 4, 1, 1>(a, waves, stream);
-  }
-}
-
 hipError_t launch_w4_gemv(const W4& w, int64_t T, const void* x, int64_t ldx, int x_type, void* y, int64_t ldy, int y_type,
-                          void*, hipStream_t stream) {
+                          void* ws, hipStream_t stream) {
   GemvArgs a = {};
   a.w = w;
   a.x = x;
@@ -451,22 +504,25 @@ hipError_t launch_w4_gemv(const W4& w, int64_t T, const void* x, int64_t ldx, in
   a.T = T;
   a.x_f32 = x_type == ET_F32;
   a.y_f32 = y_type == ET_F32;
-  a.x_vec = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && (ldx * (a.x_f32 ? 4 : 2)) % 16 == 0;
-  const int terms = a.x_f32 ? 3 : 1;
-  // the widest segments that stay within a group and are needed: fewer instructions a vector
-  const int widest = w.group_log2 >= 7 ? 16 : 1 << (w.group_log2 - 3);
-  const int64_t rows = T * terms;
-  const int tb = rows <= 4 || widest == 4 ? 4 : rows <= 8 || widest == 8 ? 8 : 16;
-  const int most = 4 * tb / terms;  // vectors of a pass
-  a.per_pass = static_cast<int>(T < most ? T : most);
-  const int nb = static_cast<int>(cdiv(a.per_pass * terms, tb));
-  if (cdiv(T, a.per_pass) > 65535) return hipErrorInvalidConfiguration;
-  const int64_t steps = cdiv(w.N, kStep);
-  const int waves = steps >= 16 ? 8 : steps >= 8 ? 4 : steps >= 2 ? 2 : 1;
-  if (tb == 4 && rows == 1) return gemv_as<4, 1, 1, 1, 4>(a, waves, stream);
-  if (tb == 4) return gemv_blocks<4>(nb, a, waves, stream);
-  if (tb == 8) return gemv_blocks<8>(nb, a, waves, stream);
-  return gemv_blocks<16>(nb, a, waves, stream);
+  a.x_vec = aligned16(x, ldx, a.x_f32 ? 4 : 2);
+  const GemvPlan4 p = plan_w4_gemv(w.M, w.N, T, a.x_f32, w.group_log2);
+  a.part = static_cast<float*>(ws);
+  a.per_pass = p.per_pass;
+  a.batches = p.batches;
+  a.chunks = p.chunks;
+  const bool one = T == 1 && !a.x_f32;  // one sum of the four in use
+  hipError_t e;
+  if (p.tb == 4)
+    e = one ? gemv_as<4, 1, 1>(p, a, stream) : p.nb == 1 ? gemv_as<4, 1, 4>(p, a, stream) : gemv_as<4, 2, 4>(p, a, stream);
+  else if (p.tb == 8)
+    e = p.nb == 1 ? gemv_as<8, 1, 4>(p, a, stream) : gemv_as<8, 2, 4>(p, a, stream);
+  else
+    e = p.nb == 1 ? gemv_as<16, 1, 4>(p, a, stream) : gemv_as<16, 2, 4>(p, a, stream);
+  if (e != hipSuccess || p.chunks == 1) return e;
+  const int64_t n = cdiv(T * w.M, 256);
+  if (n > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  w4_join_kernel<<<dim3(static_cast<uint32_t>(n)), 256, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace crvq
