@@ -147,7 +147,6 @@ typedef uint32_t w4_u4 __attribute__((ext_vector_type(4)));
 constexpr int kStep = 128;             // columns of a step
 constexpr int kXPad = 8;               // elements between rows of x in LDS
 constexpr int kXBytes = 73 << 10;      // of x in LDS: two workgroups a CU
-constexpr int kWaves = 256 * 16;       // waves that fill the chip
 
 struct GemvPlan4 {
   int tb, nb;        // vectors of a block, blocks
@@ -164,6 +163,7 @@ struct GemvArgs {
   int64_t ldx, ldy, T;
   int x_f32, y_f32, x_vec;
   int per_pass, batches, chunks;
+  int s_vec;  // the scales of a step (and its zero points) can be read with one load
 };
 constexpr int batch_steps(int nb) { return nb == 1 ? 4 : 2; }
 
@@ -215,8 +215,48 @@ __device__ __forceinline__ void stage8(const GemvArgs& a, int64_t t, int64_t j, 
   }
 }
 
-// NB blocks of TB vectors; NR of a lane's four sums of a block in use.
-template <int TB, int NB, int NR, typename TS>
+// E scales that lie next to each other, and their zero points, from group g on.
+template <int E, typename TS>
+struct RawScales {
+  float s[E], z[E];
+  __device__ __forceinline__ void load(const TS* scale, const uint8_t* zero, int64_t g, int64_t last, bool vec) {
+    if (E > 1 && vec && g + E - 1 <= last) {
+      if constexpr (sizeof(TS) == 4) {
+        typedef float V __attribute__((ext_vector_type(E)));
+        const V v = *reinterpret_cast<const V*>(scale + g);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[e] = v[e];
+      } else {
+        typedef uint16_t V __attribute__((ext_vector_type(E)));
+        const V v = *reinterpret_cast<const V*>(scale + g);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[e] = bf16_f(v[e]);
+      }
+      if (zero) {
+        typedef uint8_t Z __attribute__((ext_vector_type(E)));
+        const Z v = *reinterpret_cast<const Z*>(zero + g);
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[e] = static_cast<float>(v[e]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int64_t at = min(g + e, last);
+        s[e] = ld1(scale + at);
+        if (zero) z[e] = static_cast<float>(zero[at]);
+      }
+    }
+    if (!zero) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) z[e] = 8.f;
+    }
+  }
+};
+
+// NB blocks of TB vectors; NR of a lane's four sums of a block in use; E groups in a step (1 for groups of 128 and
+// more).  The scales of a batch are 16 rows times U E groups: a lane reads E of one row, all with one load, and
+// hands them on through LDS (one load of a scale for every step made the kernel 40 % slower).
+template <int TB, int NB, int NR, int E, typename TS>
 __global__ __launch_bounds__(1024) void w4_gemv_kernel(const GemvArgs a) {
   constexpr int U = batch_steps(NB);
   extern __shared__ __align__(16) uint16_t xs[];
@@ -229,27 +269,28 @@ __global__ __launch_bounds__(1024) void w4_gemv_kernel(const GemvArgs a) {
   const int64_t k0 = static_cast<int64_t>(blockIdx.y) * cols;
   uint16_t* zero = xs + held * ld;                               // eight zeros, for rows of other segments
   float* sums = reinterpret_cast<float*>(zero + 8);              // X: [step][block][quarter][NR]
-  float* part = sums + steps * (NB * 4 * NR);                    // [2][wave][block][vector][16 rows of W]
+  float2* held_scales = reinterpret_cast<float2*>(sums + steps * (NB * 4 * NR)) + wave * (16 * U * E);  // [row][step][group]
+  float* part = reinterpret_cast<float*>(held_scales + (waves - wave) * (16 * U * E));  // [2][wave][block][vector][16 rows]
 
   // this lane's codes and scales: row r of a block of 16, columns 32 c of a step
   const int64_t stored = (a.w.N + 31) & ~int64_t{31}, last_group = (a.w.N - 1) >> a.w.group_log2;
   const int64_t blocks = (a.w.M + 15) >> 4;
-  const int seg_col = ((c * 4) / TB) * (8 * TB);  // first column of the segment whose sums this lane holds
+  const int seg_group = ((c * 4) / TB) * (8 * TB) * E / kStep;  // the group in a step of the segment whose sums this lane holds
   const TS* const scales = static_cast<const TS*>(a.w.scales);
   uint4 wq[U];
-  float sc[U], zp[U];
+  RawScales<E, TS> raw;
+  const int sr = lane >> 2, su = lane & 3;  // the row and step whose scales this lane reads
   auto load = [&](int64_t block, int batch) {
-    const int64_t row = min(block * 16 + r, a.w.M - 1);
-    const uint8_t* codes = a.w.codes + row * a.w.ld;
-    const TS* scale = scales + row * a.w.ld_s;
-    const uint8_t* zeros = a.w.zeros + row * a.w.ld_z;
+    const uint8_t* codes = a.w.codes + min(block * 16 + r, a.w.M - 1) * a.w.ld;
+    const int64_t kb = k0 + static_cast<int64_t>((batch * waves + wave) * U) * kStep;
+    if (su < U) {
+      const int64_t row = min(block * 16 + sr, a.w.M - 1), g = min((kb + su * kStep) >> a.w.group_log2, last_group);
+      raw.load(scales + row * a.w.ld_s, a.w.zeros ? a.w.zeros + row * a.w.ld_z : nullptr, g, last_group, a.s_vec);
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t kb = k0 + static_cast<int64_t>((batch * U + u) * waves + wave) * kStep;
-      const int64_t col = kb + 32 * c, g = min((kb + seg_col) >> a.w.group_log2, last_group);
-      wq[u] = ld_stream(codes + (col < stored ? col >> 1 : 0));  // past the row: x is zero there
-      sc[u] = ld1(scale + g);
-      zp[u] = a.w.zeros ? static_cast<float>(zeros[g]) : 8.f;
+      const int64_t col = kb + u * kStep + 32 * c;
+      wq[u] = *reinterpret_cast<const uint4*>(codes + (col < stored ? col >> 1 : 0));  // past the row: x is zero there
     }
   };
   int64_t block = blockIdx.x;
@@ -297,15 +338,21 @@ __global__ __launch_bounds__(1024) void w4_gemv_kernel(const GemvArgs a) {
   int batch = 0, buffer = 0;
   while (block < blocks) {
     uint4 cur[U];
-    float cs[U], cz[U];
+    float2 scale[U];
+    if (su < U) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) cur[u] = wq[u], cs[u] = sc[u], cz[u] = -16.f - zp[u];
+      for (int e = 0; e < E; ++e) held_scales[(sr * U + su) * E + e] = make_float2(raw.s[e], -16.f - raw.z[e]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) cur[u] = wq[u];
+#pragma unroll
+    for (int u = 0; u < U; ++u) scale[u] = held_scales[(r * U + u) * E + seg_group];
     const bool last = batch + 1 == a.batches;
     const int64_t next = last ? block + gridDim.x : block;
     if (next < blocks) load(next, last ? 0 : batch + 1);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int s = (batch * U + u) * waves + wave;
+      const int s = (batch * waves + wave) * U + u;
       w4_f4 acc[NB];
 #pragma unroll
       for (int n = 0; n < NB; ++n) acc[n] = w4_f4{0.f, 0.f, 0.f, 0.f};
@@ -321,7 +368,7 @@ __global__ __launch_bounds__(1024) void w4_gemv_kernel(const GemvArgs a) {
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int i = 0; i < NR; ++i)
-          tot[n][i] = fmaf(cs[u], fmaf(cz[u], sums[((s * NB + n) * 4 + c) * NR + i], acc[n][i]), tot[n][i]);
+          tot[n][i] = fmaf(scale[u].x, fmaf(scale[u].y, sums[((s * NB + n) * 4 + c) * NR + i], acc[n][i]), tot[n][i]);
     }
     if (!last) {
       ++batch;
@@ -438,10 +485,12 @@ static GemvPlan4 plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int g
   const int terms = x_f32 ? 3 : 1, widest = group_log2 >= 7 ? 16 : 1 << (group_log2 - 3);
   const int64_t rows = T * terms;
   p.tb = rows <= 4 || widest == 4 ? 4 : rows <= 8 || widest == 8 ? 8 : 16;
-  const int most = 2 * p.tb / terms;
+  const int most = (p.tb == 4 ? 4 : 2) * p.tb / terms;
   p.per_pass = static_cast<int>(T < most ? T : most);
   p.nb = static_cast<int>(cdiv(static_cast<int64_t>(p.per_pass) * terms, p.tb));
-  const int U = batch_steps(p.nb), most_waves = p.nb == 1 ? 16 : 8;
+  // One row of x: workgroups of 8 waves, three a CU (28672 x 8192: 32.8 us; 16 waves, one a CU: 35.7); a few rows: of 16
+  // (four vectors, groups of 32: 45 us; 8: 62), several blocks: of 8, for the sums' LDS.
+  const int U = batch_steps(p.nb), most_waves = rows > 1 && p.nb == 1 ? 16 : 8, fill_waves = 256 * (rows > 1 && p.nb == 1 ? 16 : 24);
   const int64_t fit = (kXBytes / 2 / (p.per_pass * terms) - kXPad) / kStep;  // steps of x in LDS: at least 8
   const int64_t steps = cdiv(N, kStep), blocks = cdiv(M, 16), passes = cdiv(T, p.per_pass);
   int64_t chunk = steps < fit ? steps : fit;
@@ -458,7 +507,7 @@ static GemvPlan4 plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int g
   }
   p.batches = static_cast<int>(batches);
   p.chunks = static_cast<int>(cdiv(steps, static_cast<int64_t>(p.waves) * p.batches * U));
-  const int64_t fill = cdiv(kWaves, static_cast<int64_t>(p.waves) * p.chunks * passes);
+  const int64_t fill = cdiv(fill_waves, static_cast<int64_t>(p.waves) * p.chunks * passes);
   p.groups = blocks < fill ? blocks : fill;
   return p;
 }
@@ -477,20 +526,36 @@ size_t w4_gemv_ws_bytes(int64_t M, int64_t N, int64_t T) {
   return most;
 }
 
-template <int TB, int NB, int NR>
+template <int TB, int NB, int NR, int E>
 static hipError_t gemv_as(const GemvPlan4& p, const GemvArgs& a, hipStream_t stream) {
   const int held = a.x_f32 ? 3 * p.per_pass : p.per_pass;
   const int64_t steps = static_cast<int64_t>(p.waves) * p.batches * batch_steps(NB);
   const size_t lds = static_cast<size_t>(held) * (steps * kStep + kXPad) * 2 + 16 + steps * NB * 4 * NR * sizeof(float) +
+                     static_cast<size_t>(p.waves) * 16 * batch_steps(NB) * E * sizeof(float2) +
                      size_t{2} * p.waves * NB * TB * 16 * sizeof(float);
   const int64_t passes = cdiv(a.T, p.per_pass);
   if (passes > 65535 || p.chunks > 65535) return hipErrorInvalidConfiguration;
   const dim3 grid(static_cast<uint32_t>(p.groups), static_cast<uint32_t>(p.chunks), static_cast<uint32_t>(passes));
   if (a.w.s_type == ET_F32)
-    w4_gemv_kernel<TB, NB, NR, uint32_t><<<grid, p.waves * 64, lds, stream>>>(a);
+    w4_gemv_kernel<TB, NB, NR, E, uint32_t><<<grid, p.waves * 64, lds, stream>>>(a);
   else
-    w4_gemv_kernel<TB, NB, NR, uint16_t><<<grid, p.waves * 64, lds, stream>>>(a);
+    w4_gemv_kernel<TB, NB, NR, E, uint16_t><<<grid, p.waves * 64, lds, stream>>>(a);
   return hipGetLastError();
+}
+
+template <int E>
+static hipError_t gemv_groups(const GemvPlan4& p, const GemvArgs& a, hipStream_t stream) {
+  if (p.tb == 4) {
+    if (a.T == 1 && !a.x_f32) return gemv_as<4, 1, 1, E>(p, a, stream);  // one sum of the four in use
+    if (p.nb == 1) return gemv_as<4, 1, 4, E>(p, a, stream);
+    if (p.nb == 2) return gemv_as<4, 2, 4, E>(p, a, stream);
+    return p.nb == 3 ? gemv_as<4, 3, 4, E>(p, a, stream) : gemv_as<4, 4, 4, E>(p, a, stream);
+  }
+  if constexpr (E <= 2)
+    if (p.tb == 8) return p.nb == 1 ? gemv_as<8, 1, 4, E>(p, a, stream) : gemv_as<8, 2, 4, E>(p, a, stream);
+  if constexpr (E == 1)
+    if (p.tb == 16) return p.nb == 1 ? gemv_as<16, 1, 4, E>(p, a, stream) : gemv_as<16, 2, 4, E>(p, a, stream);
+  return hipErrorInvalidValue;  // a segment wider than a group: the plan gives none
 }
 
 hipError_t launch_w4_gemv(const W4& w, int64_t T, const void* x, int64_t ldx, int x_type, void* y, int64_t ldy, int y_type,
@@ -510,14 +575,11 @@ hipError_t launch_w4_gemv(const W4& w, int64_t T, const void* x, int64_t ldx, in
   a.per_pass = p.per_pass;
   a.batches = p.batches;
   a.chunks = p.chunks;
-  const bool one = T == 1 && !a.x_f32;  // one sum of the four in use
-  hipError_t e;
-  if (p.tb == 4)
-    e = one ? gemv_as<4, 1, 1>(p, a, stream) : p.nb == 1 ? gemv_as<4, 1, 4>(p, a, stream) : gemv_as<4, 2, 4>(p, a, stream);
-  else if (p.tb == 8)
-    e = p.nb == 1 ? gemv_as<8, 1, 4>(p, a, stream) : gemv_as<8, 2, 4>(p, a, stream);
-  else
-    e = p.nb == 1 ? gemv_as<16, 1, 4>(p, a, stream) : gemv_as<16, 2, 4>(p, a, stream);
+  const int groups = w.group_log2 >= 7 ? 1 : kStep >> w.group_log2, es = w.s_type == ET_F32 ? 4 : 2;
+  a.s_vec = reinterpret_cast<uintptr_t>(w.scales) % (groups * es) == 0 && w.ld_s % groups == 0 &&
+            reinterpret_cast<uintptr_t>(w.zeros) % groups == 0 && w.ld_z % groups == 0;
+  const hipError_t e = groups == 1 ? gemv_groups<1>(p, a, stream)
+                       : groups == 2 ? gemv_groups<2>(p, a, stream) : gemv_groups<4>(p, a, stream);
   if (e != hipSuccess || p.chunks == 1) return e;
   const int64_t n = cdiv(T * w.M, 256);
   if (n > 0x7fffffffLL) return hipErrorInvalidConfiguration;
