@@ -488,9 +488,9 @@ crvq_status crvq_kv_read(int32_t B, int32_t Hkv, int32_t D, int32_t page, int64_
  * 0.  lse (float [n_tokens][Hq] or NULL) = log sum_t exp(scale q_i . K_t), -inf
  * for a row that sees nothing.  out: n_tokens x Hq x D of q's type, its own
  * strides; it may be q itself (same strides), and may not overlap it otherwise.
- * Arithmetic: a query row is held as fixed-point digits (16 bits below its
- * largest element for CRVQ_BF16, 24 for CRVQ_F32) whose products with the key
- * codes are exact; softmax statistics and sums are fp32; for CRVQ_BF16 weights enter the
+ * Arithmetic: a query row is held to 24 bits below its largest element (many
+ * CRVQ_BF16 rows: as fp16 relative to a power of two), and its products with the
+ * key codes are exact; softmax statistics and sums are fp32; for CRVQ_BF16 weights enter the
  * product with the values rounded to 11 bits.
  * A row with a NaN or infinite query element is NaN, as is a row that sees a
  * page outside [0, n_pages) or a page with a scale that is negative or not finite.  Rows of a sequence

@@ -4,8 +4,7 @@
 // c % G of the G that share the key head) and walks a range of tokens 64 at a time, with the running
 // maximum m and sum l of the softmax in registers; nothing of size rows x tokens exists.
 //   S^T = K Q^T on v_mfma_i32_16x16x64_i8: the key codes are the left operand as they lie in the cache, a query row is a
-//     fixed-point number of 2 (bf16) or 3 (fp32) signed 8-bit digits, so the products are exact integers and no
-//     code is widened.  The score is the integer times alpha = (query step) (key scale) |scale| log2(e).
+//     fixed-point number of 3 signed 8-bit digits, so the products are exact integers and no code is widened.  The score is the integer times alpha = (query step) (key scale) |scale| log2(e).
 //   O^T += V^T P^T on v_mfma_f32_16x16x32_f16: the value codes lie transposed in the cache, 16 tokens of an
 //     element in 16 bytes, and are widened to fp16 in registers (exact); the weights are rounded to fp16.  The page's
 //     value scale goes into the weights, relative to a power of two 2^e that follows the largest scale met so far.
@@ -134,17 +133,14 @@ __device__ __forceinline__ Place place_of(const AttnArgs& a) {
 template <typename T, int DT, int QB, bool HALF, bool SMALL>
 struct Columns {
   static constexpr int DC = HALF ? (DT + 1) / 2 : (DT + 3) / 4;      // chunks of a head: 32 (HALF) or 64 elements
-  static constexpr int NT = HALF ? 1 : sizeof(T) == 4 ? 3 : 2;       // digits of a query element
-  static constexpr double kSteps = NT == 3 ? 8355711.0 : 32639.0;    // 127 in every digit
-  // Where a step's weights have one factor, their sum is a product with ones (of the rounded weights, as the values are).
-  static constexpr bool kSumByProduct = sizeof(T) == 2 && !SMALL;
+  static constexpr int NT = HALF ? 1 : 3;                            // digits of a query element
+  static constexpr double kSteps = 8355711.0;                        // 127 in every digit
   at_i4 q[QB][DC][NT];
   float step[QB], m[QB], l[QB];
   int lo[QB], hi[QB];                 // the tokens a column sees
   int first, last, all_lo, all_hi;    // the tokens any of them sees, and those that all of them see
   at_f4 o[QB][DT];
   int e;  // exponent that value scales are taken relative to
-  float unweight;  // of the present step: 1 / (the weight of p = 1)
 
   // Queries: fixed point, 16 elements of a column and chunk in a lane; HALF: 8 of them.
   __device__ __forceinline__ void begin(const AttnArgs& a, const KvSeq& sq, bool ok, int hk, int col0, int cols) {
@@ -221,7 +217,7 @@ struct Columns {
   }
 
   // The scores of 64 tokens, in query steps: key(u, ch) is the left operand of tile u and chunk ch.
-  // LDS: operands come from LDS, and are asked for a tile (of values two) before they are used.
+  // LDS: operands come from LDS, and are asked for a tile before they are used.
   template <bool LDS, class Key>
   __device__ __forceinline__ void scores(at_f4 (&s)[QB][4], Key&& key) {
     at_i4 ahead[2][DC];
@@ -256,7 +252,7 @@ struct Columns {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float low = static_cast<float>((acc[NT > 1 ? NT - 2 : 0][i] << 8) + acc[NT - 1][i]);
-          s[n][u][i] = NT == 3 ? fmaf(static_cast<float>(acc[0][i]), 65536.f, low) : low;
+          s[n][u][i] = fmaf(static_cast<float>(acc[0][i]), 65536.f, low);
         }
       }
     }
@@ -275,8 +271,7 @@ struct Columns {
       e = ve;
     }
     const float weight = fmaxf(ldexpf(vs, -e), 0x1p-40f) * static_cast<float>(1 << kLift);
-    const float weight_log = __builtin_amdgcn_logf(weight);
-    unweight = __builtin_amdgcn_rcpf(weight);
+    const float weight_log = __builtin_amdgcn_logf(weight), unweight = __builtin_amdgcn_rcpf(weight);
     const bool whole = t0 >= all_lo && t0 + kTokens <= all_hi;
     uint32_t seen[QB];  // which of the lane's 16 tokens its column sees
     if (!whole) {
@@ -322,14 +317,12 @@ struct Columns {
         for (int j = 0; j < 16; ++j)
           if (!(seen[n] >> j & 1)) s[n][j >> 2][j & 3] = 0.f;
     }
-    if constexpr (!kSumByProduct) {
 #pragma unroll
-      for (int n = 0; n < QB; ++n) {
-        float sum = 0.f;
+    for (int n = 0; n < QB; ++n) {
+      float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) sum += s[n][j >> 2][j & 3];
-        l[n] = fmaf(sum, unweight, l[n]);
-      }
+      for (int j = 0; j < 16; ++j) sum += s[n][j >> 2][j & 3];
+      l[n] = fmaf(sum, unweight, l[n]);
     }
   }
 
@@ -349,34 +342,17 @@ struct Columns {
             pw[n][j >> 3][j & 7] = h[0];
             pw[n][j >> 3][(j & 7) + 1] = h[1];
           }
-        at_u4 ahead[3][2];
-        if constexpr (LDS) {
-#pragma unroll
-          for (int d = 0; d < 2; ++d) ahead[d][0] = value(d, 0), ahead[d][1] = value(d, 1);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        if constexpr (kSumByProduct) {
-          const _Float16 one = 1;
-          const at_h8 ones = {one, one, one, one, one, one, one, one};
-#pragma unroll
-          for (int n = 0; n < QB; ++n) {
-            at_f4 sum = {0.f, 0.f, 0.f, 0.f};
-            sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pw[n][0], sum, 0, 0, 0);
-            sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pw[n][1], sum, 0, 0, 0);
-            l[n] = fmaf(sum[0], unweight * 0.25f, l[n]);  // all quarters have the whole sum, and are added up in end()
-          }
-          unweight *= 0x1p-14f;  // for another pass
-        }
+        at_u4 ahead[2][2] = {{value(0, 0), value(0, 1)}};
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           if constexpr (LDS) {
-            if (d + 2 < DT) ahead[(d + 2) % 3][0] = value(d + 2, 0), ahead[(d + 2) % 3][1] = value(d + 2, 1);
+            if (d + 1 < DT) ahead[(d + 1) & 1][0] = value(d + 1, 0), ahead[(d + 1) & 1][1] = value(d + 1, 1);
             __builtin_amdgcn_sched_barrier(0);
-          } else {
-            ahead[d % 3][0] = value(d, 0);
-            ahead[d % 3][1] = value(d, 1);
+          } else if (d > 0) {
+            ahead[d & 1][0] = value(d, 0);
+            ahead[d & 1][1] = value(d, 1);
           }
-          const at_h8 v0 = __builtin_bit_cast(at_h8, ahead[d % 3][0]), v1 = __builtin_bit_cast(at_h8, ahead[d % 3][1]);
+          const at_h8 v0 = __builtin_bit_cast(at_h8, ahead[d & 1][0]), v1 = __builtin_bit_cast(at_h8, ahead[d & 1][1]);
 #pragma unroll
           for (int n = 0; n < QB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[n][0], o[n][d], 0, 0, 0);
 #pragma unroll
@@ -838,6 +814,44 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(const AttnArgs a
   if (a.lse && d == 0) a.lse[row * a.Hq + h] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2 + bad;
 }
 
+// The same for few splits and many rows: D / 4 threads a (row, head), which walk the splits.
+template <typename T>
+__global__ __launch_bounds__(256) void kv_attention_join_rows_kernel(const AttnArgs a, int64_t items) {
+  const int per = a.c.D >> 2, g = threadIdx.x / per, d = (threadIdx.x - g * per) * 4;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * (256 / per) + g;
+  if (g >= 256 / per || item >= items) return;
+  const uint32_t row_of = static_cast<uint32_t>(item / a.Hq);
+  const int h = static_cast<int>(item - static_cast<int64_t>(row_of) * a.Hq), b = static_cast<int>(row_of / a.bt.max_new);
+  const int i = static_cast<int>(row_of - static_cast<uint32_t>(b) * a.bt.max_new);
+  const KvSeq sq = kv_seq(a.bt, b, a.c.page_log2);
+  if (i >= sq.n) return;
+  float m = -kInf, l = 0.f;
+  at_f4 y = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.splits; ++s) {
+    const int64_t at = s * items + item;
+    const float ls = a.pl[at], ms = a.pm[at];
+    if (ls == 0.f) continue;  // saw nothing and stored no output; a NaN goes on into l
+    const float now = fmaxf(m, ms), keep = m == -kInf ? 0.f : __builtin_amdgcn_exp2f(m - now);
+    const float f = ls == ls ? __builtin_amdgcn_exp2f(ms - now) : 0.f;
+    l = fmaf(l, keep, ls == ls ? f * ls : ls);
+    y = y * keep;
+    if (f != 0.f) y += f * *reinterpret_cast<const at_f4*>(a.po + at * a.c.D + d);
+    m = now;
+  }
+  const float bad = l - l;  // 0, or NaN
+  const int64_t row = sq.row0 + i;
+  T* out = static_cast<T*>(a.out.p) + row * a.out.tok + h * a.out.head + d;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float x = l == 0.f ? 0.f : y[k] / l + bad;
+    if constexpr (sizeof(T) == 4)
+      reinterpret_cast<float*>(out)[k] = x;
+    else
+      out[k] = static_cast<T>(f_bf16(x));
+  }
+  if (a.lse && d == 0) a.lse[row * a.Hq + h] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2 + bad;
+}
+
 // How a call is divided.  One tile of columns: its workgroups' four waves share the columns (16) and take turns at the
 // tokens; more: every wave has 16 prompt_blocks columns of its own.  Tokens are split over workgroups until
 // kWorkgroups are at work, a share being at least kShare tokens.
@@ -846,7 +860,8 @@ struct AttnPlan {
   int tiles, splits;
 };
 constexpr int prompt_blocks(int D) { return D <= 128 ? 2 : 1; }  // what the registers hold
-constexpr int64_t kWorkgroups = 1024;
+constexpr int64_t kWorkgroups = 512;
+constexpr int kFewSplits = 8;
 constexpr int kShare = 512;
 AttnPlan plan_attention(int B, int Hq, int Hkv, int D, int max_new, int max_kv) {
   AttnPlan p;
@@ -899,6 +914,11 @@ hipError_t attend(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
   if (e != hipSuccess || p.splits == 1) return e;
   const int64_t rows = static_cast<int64_t>(a.bt.B) * a.bt.max_new * a.Hq;
   if (rows > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  if (p.prompt && p.splits <= kFewSplits) {
+    const int64_t each = 256 / (D >> 2);
+    kv_attention_join_rows_kernel<T><<<dim3(static_cast<uint32_t>(cdiv(rows, each))), 256, 0, stream>>>(a, rows);
+    return hipGetLastError();
+  }
   kv_attention_join_kernel<T><<<dim3(static_cast<uint32_t>(rows)), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
