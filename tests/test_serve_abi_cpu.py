@@ -90,8 +90,9 @@ def test_attention_arguments(L):
         assert attend(L, **bad) == 1, bad
     need = L.crvq_kv_attention_workspace_size(1, 64, 8, 128, 1, 131072)
     assert need == L.crvq_workspace_size(10, 1, 1, 0, 0, 128, None, 64, 8, 131072)
-    if need:
-        assert attend(L, B=1, Hq=64, Hkv=8, D=128, max_kv=131072, q_tok=1 << 14, o_tok=1 << 14, wsb=need - 1) == 3
+    need = L.crvq_kv_attention_workspace_size(1, 64, 8, 64, 1, 131072)  # the helper's heads are 64 elements apart
+    assert need > 0 and attend(L, B=1, Hq=64, Hkv=8, max_kv=131072, q_tok=1 << 14, o_tok=1 << 14, wsb=need - 1) == 3
+    assert attend(L, B=1, Hq=64, Hkv=8, max_kv=131072, q_tok=1 << 14, o_tok=1 << 14, wsb=need, ws=None) == 3
     assert L.crvq_kv_attention_workspace_size(1, 6, 4, 64, 1, 100) == 0
     assert L.crvq_kv_attention_workspace_size(1, 8, 4, 65, 1, 100) == 0
 
