@@ -2,6 +2,8 @@
 // reconstruction and the product with a few vectors.
 #include "kv_common.h"
 
+#include <algorithm>
+
 namespace crvq {
 namespace {
 
@@ -507,7 +509,10 @@ static GemvPlan4 plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int g
   }
   p.batches = static_cast<int>(batches);
   p.chunks = static_cast<int>(cdiv(steps, static_cast<int64_t>(p.waves) * p.batches * U));
-  const int64_t fill = cdiv(fill_waves, static_cast<int64_t>(p.waves) * p.chunks * passes);
+  // one round of workgroups: what the CUs hold at once, by waves and by LDS
+  const int64_t lds = static_cast<int64_t>(p.per_pass) * terms * (p.waves * p.batches * U * kStep) * 2 + (12 << 10);
+  const int64_t per_cu = std::min<int64_t>(std::max<int64_t>(1, fill_waves / 256 / p.waves), std::max<int64_t>(1, (160 << 10) / lds));
+  const int64_t fill = std::max<int64_t>(1, 256 * per_cu / (p.chunks * passes));
   p.groups = blocks < fill ? blocks : fill;
   return p;
 }
