@@ -428,6 +428,16 @@ def crvq_dequant_gemv(M: int, N: int, q_base: torch.Tensor, ldq_base: int, C_bas
 
 
 # ---- the attention block on quantized data: 8-bit paged cache, 4-bit matrices ---------------------
+def _workspace_for(nbytes: int, device, stream) -> Optional[torch.Tensor]:
+    """A workspace from the memory of the stream that the call goes to, so that no other stream's work shares it."""
+    if stream is None or nbytes == 0:
+        return _workspace(nbytes, device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(stream), device=device)
+    with torch.cuda.stream(stream):
+        return _workspace(nbytes, device)
+
+
 def _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len):
     """The cache's and batch's arguments, with the shapes and types the C call cannot see checked."""
     n_pages, Hkv, page, D = k_cache.shape
@@ -494,7 +504,7 @@ def crvq_kv_attention(q: torch.Tensor, out: torch.Tensor, k_cache: torch.Tensor,
     B, Hkv, D, page, cache = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len)
     n, Hq = q.shape[0], q.shape[1]
     assert lse is None or (lse.dtype == torch.float32 and lse.shape == (n, Hq) and lse.is_contiguous())
-    ws = _workspace(L.crvq_kv_attention_workspace_size(B, Hq, Hkv, D, max_new, max_kv), q.device)
+    ws = _workspace_for(L.crvq_kv_attention_workspace_size(B, Hq, Hkv, D, max_new, max_kv), q.device, stream)
     _check("crvq_kv_attention", L.crvq_kv_attention(
         B, Hq, Hkv, D, page, *cache, max_new, max_kv, n, dtype_code(q), *_row_args(q, n, Hq, D, q.dtype),
         *_row_args(out, n, Hq, D, q.dtype), D ** -0.5 if scale is None else scale, int(causal), window, _ptr(lse),
@@ -539,7 +549,7 @@ def crvq_w4_gemv(codes: torch.Tensor, scales: torch.Tensor, group: int, x: torch
     T, N = x.shape
     M = codes.shape[0]
     assert y.shape == (T, M) and x.stride(1) == 1 and y.stride(1) == 1 and _w4_holds(codes, scales, group, N)
-    ws = _workspace(L.crvq_w4_gemv_workspace_size(M, N, T), y.device)
+    ws = _workspace_for(L.crvq_w4_gemv_workspace_size(M, N, T), y.device, stream)
     _check("crvq_w4_gemv", L.crvq_w4_gemv(M, N, T, group, *_w4_args(codes, scales, zeros), _ptr(x), x.stride(0),
                                           dtype_code(x), _ptr(y), y.stride(0), dtype_code(y), _ptr(ws),
                                           0 if ws is None else ws.numel(), _stream(stream)))

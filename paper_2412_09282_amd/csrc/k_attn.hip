@@ -110,7 +110,7 @@ __device__ __forceinline__ float elem(const T* p, int i) {
 // Which sequence, key head, split and tile of columns a workgroup has.  Key heads are neighbours, so that with a
 // multiple of eight of them a chip's die reads few heads; the tiles of a sequence go last to first, so that the longest
 // rows of a causal prompt start first; sequences come one after the other: the workgroups that a short one has no work for
-// are then a run (as every second one they left half of the CUs idle: 556 against 400 us for two prompts of 2048
+// are then a run (as every second one they left half of the CUs idle: 556 against 404 us for two prompts of 2048
 // and about 300).
 struct Place {
   int hk, b, split, tile;
@@ -512,7 +512,9 @@ __device__ __forceinline__ void share_of(const AttnArgs& a, int split, int round
 }
 
 // Few columns: the four waves of a workgroup share 16 and take turns at the tokens; the cache is read once, from
-// memory into the operands' registers, a step's keys while the step before is computed.  Reads bound it.
+// memory into the operands' registers, a step's keys while the step before is computed.  Reads bound it: 32 sequences
+// of 2048 to 4096 tokens (682 MB) take 139 us, 4.9 TB/s, the rate of a device copy; one sequence of 131001 tokens in 64
+// shares of 8 heads 64 us (4.2 TB/s; 8 us of it the join).
 template <typename T, int DT, bool SMALL>
 __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel(const AttnArgs a) {
   constexpr int kRow = DT * 16 + 4, kStride = 4 * kTokens;
@@ -611,7 +613,10 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel
 // Many columns: every wave has 16 QB of its own, and the four of a workgroup walk the same tokens.  A step's keys
 // and values pass through LDS, two steps of them, widened once for all four waves (keys of fp32 queries as they are).  Rows of
 // LDS are padded by 16 bytes, and a key's row is u * 16 + r for the token that is row r of tile u, so that the 16 rows
-// an instruction reads lie in different banks.  The vector units bound it (the softmax's exponentials).
+// an instruction reads lie in different banks.  4096 tokens over 8192 take
+// 1.33 ms without a mask (830 TFLOP/s, of 1360 that a large library product of bf16 reaches); what is left is mostly
+// dependences that two waves a SIMD do not hide (without the exponentials 1.28 ms, with one wave a SIMD 1.95).  Smaller
+// calls lose at their end, when the last workgroups run alone: two prompts of 2048 and about 300, 400 us (600 TFLOP/s).
 template <typename T, int DT, int QB, bool SMALL>
 __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kernel(const AttnArgs a) {
   constexpr bool HALF = sizeof(T) == 2;
@@ -852,7 +857,8 @@ __global__ __launch_bounds__(256) void kv_attention_join_rows_kernel(const AttnA
   if (a.lse && d == 0) a.lse[row * a.Hq + h] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2 + bad;
 }
 
-// How a call is divided.  One tile of columns: its workgroups' four waves share the columns (16) and take turns at the
+// How a call is divided.  Shares are joined by a second launch; 512 workgroups are two a CU (256 to 2048 were measured: 1024
+// cost a long sequence 68 us instead of 64 and prompts with heads of 192 elements 437 instead of 318).  One tile of columns: its workgroups' four waves share the columns (16) and take turns at the
 // tokens; more: every wave has 16 prompt_blocks columns of its own.  Tokens are split over workgroups until
 // kWorkgroups are at work, a share being at least kShare tokens.
 struct AttnPlan {

@@ -5,7 +5,9 @@
 // the scale, brings older codes to it if it grew, and stores the new codes; the elements stay in registers meanwhile
 // (those of long pages past the first kKept chunks of a thread are read again).  Values are stored transposed: the
 // new tokens go through an LDS tile and leave as 16-byte runs of slots, a few of them as bytes.  The same launch
-// rotates the queries, a workgroup a row.
+// rotates the queries, a workgroup a row.  Memory bounds prompts (three of up to 2048 tokens, 64 query and 8 key heads:
+// 56 us for 250 MB, 4.5 TB/s), the chain of reads (lengths, page, elements, older codes) a decoding step: 10 us for 32
+// sequences of 32 heads.  Reading back, 25 MB in 10 us, is such a chain too.
 #include "kv_common.h"
 
 namespace crvq {

@@ -39,7 +39,8 @@ struct Lanes {
   int64_t blocks;   // of L units in a row
 };
 
-// ---- quantization: a lane owns eight columns (four bytes of codes), group / 8 lanes share a group -------
+// ---- quantization: a lane owns eight columns (four bytes of codes), group / 8 lanes share a group.  5120 x 5120 from bf16:
+// 31 us; four rows a lane (35) and products with the scale's reciprocal in place of divisions (30) were measured ----
 template <typename T, typename TS>
 __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* W, int64_t ldw, const W4 w, int vec, const Lanes ln,
                                                           int64_t stored) {
@@ -101,7 +102,8 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* W, int64_t ld
   }
 }
 
-// ---- reconstruction: a lane owns 16 bytes of the output, so that a wave stores 1 KB at once -------------------
+// ---- reconstruction: a lane owns 16 bytes of the output, so that a wave stores 1 KB at once.  5120 x 5120 to fp32: 19 us
+// (118 MB) ----
 template <typename T, typename TS>
 __global__ __launch_bounds__(256) void w4_dequant_kernel(const W4 w, T* out, int64_t ldo, int vec, const Lanes ln) {
   constexpr int E = 16 / sizeof(T);
@@ -141,7 +143,8 @@ __global__ __launch_bounds__(256) void w4_dequant_kernel(const W4 w, T* out, int
 // A workgroup keeps a chunk of the columns of x in LDS, in the order of the codes (fp32: three bf16 terms, which hold
 // all of its 24 bits, as three vectors), and walks blocks of 16 rows, the next block's codes on their way while one is
 // computed; its waves share the rows and take every waves-th step of the columns.  Chunks are joined by a second
-// launch.  Reading the codes bounds it.
+// launch.  Reading the codes bounds one vector (28672 x 8192: 121 MB in 32 us, 3.8 TB/s); with more of them the vector units
+// and LDS share it (5120 x 13824, eleven vectors: 27 us, 4.6 of them the join of seven chunks).
 typedef __bf16 w4_bf8 __attribute__((ext_vector_type(8)));
 typedef float w4_f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t w4_u4 __attribute__((ext_vector_type(4)));

@@ -420,3 +420,27 @@ def test_attention_in_a_graph():
         got = out.clone()
         step()
         assert torch.equal(got, out), i
+
+
+def test_attention_on_a_given_stream():
+    """The stream argument, as a stream and as a handle; the workspace is not handed on before the call is done."""
+    say("attention on a given stream")
+    kv, Hq, Hkv, D, page = [9000], 8, 2, 128, 64
+    g, cache, table, start, kv_len = make(61, [1], kv, Hkv, D, page)
+    q = dev(values_of(g, 1, Hq, D, dtype="bf16"), "bf16")
+    a = [*[dev(x) for x in cache], dev(table), dev(start), dev(kv_len), 1, max(kv)]
+    one = torch.empty_like(q)
+    C.crvq_kv_attention(q, one, *a)
+    torch.cuda.synchronize()
+    size = C.lib().crvq_kv_attention_workspace_size(1, Hq, Hkv, D, 1, max(kv))
+    assert size > 0
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        outs = []
+        for _ in range(20):
+            out = torch.empty_like(q)
+            C.crvq_kv_attention(q, out, *a, stream=stream)
+            torch.full((size,), 255, dtype=torch.uint8, device="cuda")  # would take a freed workspace
+            outs.append(out)
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, one) for o in outs)
