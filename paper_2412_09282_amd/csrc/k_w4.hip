@@ -153,7 +153,7 @@ constexpr int kStep = 128;             // columns of a step
 constexpr int kXPad = 8;               // elements between rows of x in LDS
 constexpr int kXBytes = 73 << 10;      // of x in LDS: two workgroups a CU
 
-struct GemvPlan4 {
+struct W4Plan {
   int tb, nb;        // vectors of a block, blocks
   int per_pass;      // vectors of a pass (grid z)
   int waves, batches;  // a chunk is waves * batches * (steps of a batch) steps of columns
@@ -485,8 +485,8 @@ hipError_t launch_w4_dequant(const W4& w, void* out, int64_t ldo, int type, hipS
 
 // The widest segments that stay within a group and are needed take the fewest instructions; the columns are cut where
 // x does not fit into LDS, and, where there are few rows, until the chip is filled.
-static GemvPlan4 plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2) {
-  GemvPlan4 p;
+static W4Plan plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2) {
+  W4Plan p;
   const int terms = x_f32 ? 3 : 1, widest = group_log2 >= 7 ? 16 : 1 << (group_log2 - 3);
   const int64_t rows = T * terms;
   p.tb = rows <= 4 || widest == 4 ? 4 : rows <= 8 || widest == 8 ? 8 : 16;
@@ -520,7 +520,7 @@ static GemvPlan4 plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int g
   return p;
 }
 
-static size_t part_bytes(const GemvPlan4& p, int64_t M, int64_t T) {
+static size_t part_bytes(const W4Plan& p, int64_t M, int64_t T) {
   return p.chunks > 1 ? align256(static_cast<size_t>(p.chunks) * T * M * sizeof(float)) : 0;
 }
 
@@ -535,7 +535,7 @@ size_t w4_gemv_ws_bytes(int64_t M, int64_t N, int64_t T) {
 }
 
 template <int TB, int NB, int NR, int E>
-static hipError_t gemv_as(const GemvPlan4& p, const GemvArgs& a, hipStream_t stream) {
+static hipError_t gemv_as(const W4Plan& p, const GemvArgs& a, hipStream_t stream) {
   const int held = a.x_f32 ? 3 * p.per_pass : p.per_pass;
   const int64_t steps = static_cast<int64_t>(p.waves) * p.batches * batch_steps(NB);
   const size_t lds = static_cast<size_t>(held) * (steps * kStep + kXPad) * 2 + 16 + steps * NB * 4 * NR * sizeof(float) +
@@ -552,7 +552,7 @@ static hipError_t gemv_as(const GemvPlan4& p, const GemvArgs& a, hipStream_t str
 }
 
 template <int E>
-static hipError_t gemv_groups(const GemvPlan4& p, const GemvArgs& a, hipStream_t stream) {
+static hipError_t gemv_groups(const W4Plan& p, const GemvArgs& a, hipStream_t stream) {
   if (p.tb == 4) {
     if (a.T == 1 && !a.x_f32) return gemv_as<4, 1, 1, E>(p, a, stream);  // one sum of the four in use
     if (p.nb == 1) return gemv_as<4, 1, 4, E>(p, a, stream);
@@ -578,7 +578,7 @@ hipError_t launch_w4_gemv(const W4& w, int64_t T, const void* x, int64_t ldx, in
   a.x_f32 = x_type == ET_F32;
   a.y_f32 = y_type == ET_F32;
   a.x_vec = aligned16(x, ldx, a.x_f32 ? 4 : 2);
-  const GemvPlan4 p = plan_w4_gemv(w.M, w.N, T, a.x_f32, w.group_log2);
+  const W4Plan p = plan_w4_gemv(w.M, w.N, T, a.x_f32, w.group_log2);
   a.part = static_cast<float*>(ws);
   a.per_pass = p.per_pass;
   a.batches = p.batches;
