@@ -127,6 +127,22 @@ __device__ __forceinline__ Place place_of(const AttnArgs& a) {
   return p;
 }
 
+// The sequence that is `rank`-th by the mean length of its rows, len - n / 2, longest first, so that a call does not end
+// with long rows on few CUs (two prompts, 2048 rows over 4000 tokens and 393 over 3469: 381 us, in their own order 408).
+// Up to 64 sequences, a lane each; more keep their order.
+__device__ __forceinline__ int ranked(const KvBatch& bt, int rank) {
+  if (bt.B > 64 || bt.B == 1) return rank;
+  const int lane = threadIdx.x & 63;
+  int64_t key = INT64_MIN;  // past the last sequence: after all of them
+  if (lane < bt.B) key = 2 * static_cast<int64_t>(bt.kv_len[lane]) - bt.start[lane + 1] + bt.start[lane];
+  int before = 0;
+  for (int j = 0; j < bt.B; ++j) {
+    const int64_t other = __shfl(key, j);
+    before += other > key || (other == key && j < lane);
+  }
+  return __ffsll(static_cast<unsigned long long>(__ballot(lane < bt.B && before == rank))) - 1;
+}
+
 // The state of a wave's 16 QB columns; DT tiles of 16 elements hold a head.  HALF: keys come widened to fp16, and a
 // query row is fp16 relative to a power of two (a bf16 element keeps its 8 bits down to 2^-28 of the row's largest).
 // SMALL: the 16 tokens of a lane may have a page, and scales, of their own.
@@ -616,7 +632,7 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel
 // an instruction reads lie in different banks.  4096 tokens over 8192 take
 // 1.33 ms without a mask (830 TFLOP/s, of 1360 that a large library product of bf16 reaches); what is left is mostly
 // dependences that two waves a SIMD do not hide (without the exponentials 1.28 ms, with one wave a SIMD 1.95).  Smaller
-// calls lose at their end, when the last workgroups run alone: two prompts of 2048 and about 300, 400 us (600 TFLOP/s).
+// calls lose at their end, when the last workgroups run alone: two prompts of 2048 and 393, 381 us (635 TFLOP/s).
 template <typename T, int DT, int QB, bool SMALL>
 __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kernel(const AttnArgs a) {
   constexpr bool HALF = sizeof(T) == 2;
@@ -626,7 +642,8 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kern
   extern __shared__ __align__(16) uint8_t lds[];   // [2][kBuffer]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tid = threadIdx.x, r = tid & 15, c = (tid >> 4) & 3;
   const int D = a.c.D, pl2 = a.c.page_log2, in_page = (1 << pl2) - 1;
-  const Place pc = place_of(a);
+  Place pc = place_of(a);
+  pc.b = __builtin_amdgcn_readfirstlane(ranked(a.bt, pc.b));
   const KvSeq sq = kv_seq(a.bt, pc.b, pl2);
   const int cols = min(sq.n, a.bt.max_new) * a.G, tile0 = pc.tile * (64 * QB), col0 = tile0 + wave * (16 * QB);
   if (tile0 >= cols) return;
