@@ -444,3 +444,14 @@ def test_attention_on_a_given_stream():
             outs.append(out)
         torch.cuda.synchronize()
         assert all(torch.equal(o, one) for o in outs)
+
+
+@pytest.mark.parametrize("B", [2, 63, 64, 65, 70])
+def test_attention_many_sequences(B):
+    """Prompts of many sequences of different lengths, empty ones among them: whatever order they are taken in."""
+    g = np.random.default_rng(B)
+    new = [int(n) for n in g.integers(0, 5, B)]
+    new[0] = 4
+    kv = [n + int(k) for n, k in zip(new, g.integers(0, 90, B))]
+    check_attention(new, kv, 8, 1, 32, 16, "bf16", seed=B)
+    check_attention(new, kv, 6, 1, 32, 64, "f32", seed=B)
