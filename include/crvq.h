@@ -490,8 +490,9 @@ crvq_status crvq_kv_read(int32_t B, int32_t Hkv, int32_t D, int32_t page, int64_
  * strides; it may be q itself (same strides), and may not overlap it otherwise.
  * Arithmetic: a query row is held to 24 bits below its largest element (many
  * CRVQ_BF16 rows: as fp16 relative to a power of two), and its products with the
- * key codes are exact; softmax statistics and sums are fp32; for CRVQ_BF16 weights enter the
- * product with the values rounded to 11 bits.
+ * key codes are exact; softmax statistics and sums are fp32; weights enter the product with the values
+ * with 24 bits (CRVQ_F32), or rounded to 22 (CRVQ_BF16, max_new * Hq / Hkv <= 16; those below 2^-10 of the
+ * row's largest keep fewer, at least 11) or to 11 bits (CRVQ_BF16, more rows).
  * A row with a NaN or infinite query element is NaN, as is a row that sees a
  * page outside [0, n_pages) or a page with a scale that is negative or not finite.  Rows of a sequence
  * with kv_len[b] < 0 or > ld_table * page are NaN, as are the first max_new rows of one

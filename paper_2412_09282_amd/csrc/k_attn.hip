@@ -6,7 +6,11 @@
 //   S^T = K Q^T on v_mfma_i32_16x16x64_i8: the key codes are the left operand as they lie in the cache, a query row is a
 //     fixed-point number of 3 signed 8-bit digits, so the products are exact integers and no code is widened.  The score is the integer times alpha = (query step) (key scale) |scale| log2(e).
 //   O^T += V^T P^T on v_mfma_f32_16x16x32_f16: the value codes lie transposed in the cache, 16 tokens of an
-//     element in 16 bytes, and are widened to fp16 in registers (exact); the weights are rounded to fp16.  The page's
+//     element in 16 bytes, and are widened to fp16 in registers (exact); the weights are rounded to fp16, once where every
+//     wave has columns of its own (11 bits), else to two terms (22 bits).  Decoding steps wait for memory and take the second
+//     term at no cost (32 sequences of up to 4096 tokens 138 us with it and without, heads of 256 elements 69 for 65); prompts
+//     are bound by these instructions (two of them, 596 us for 384), and their error against 64 bits is that of
+//     rounding the output to bf16 with either (1.67e-3 and 1.66e-3).  The page's
 //     value scale goes into the weights, relative to a power of two 2^e that follows the largest scale met so far.
 //     Weights below fp16's normal numbers (2^-21 of the row's largest) are added in further passes over the step, 2^14
 //     times as large each, so that they keep their 11 bits too; a pass is taken only where there are any.  For fp32
@@ -347,7 +351,7 @@ struct Columns {
   __device__ __forceinline__ void add(at_f4 (&s)[QB][4], Value&& value) {
     if constexpr (sizeof(T) == 2) {
       for (int pass = 0;; ++pass) {
-        at_h8 pw[QB][2];
+        at_h8 pw[QB][2], pl[QB][2];  // the weights as fp16, and what that leaves of them
         at_s2 least = {0x7fff, 0x7fff};
 #pragma unroll
         for (int n = 0; n < QB; ++n)
@@ -357,6 +361,10 @@ struct Columns {
             least = __builtin_elementwise_min(least, __builtin_bit_cast(at_s2, h));
             pw[n][j >> 3][j & 7] = h[0];
             pw[n][j >> 3][(j & 7) + 1] = h[1];
+            if constexpr (!HALF) {
+              pl[n][j >> 3][j & 7] = static_cast<_Float16>(s[n][j >> 2][j & 3] - static_cast<float>(h[0]));
+              pl[n][j >> 3][(j & 7) + 1] = static_cast<_Float16>(s[n][j >> 2][(j & 3) + 1] - static_cast<float>(h[1]));
+            }
           }
         at_u4 ahead[2][2] = {{value(0, 0), value(0, 1)}};
 #pragma unroll
@@ -373,6 +381,13 @@ struct Columns {
           for (int n = 0; n < QB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[n][0], o[n][d], 0, 0, 0);
 #pragma unroll
           for (int n = 0; n < QB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pw[n][1], o[n][d], 0, 0, 0);
+          if constexpr (!HALF) {
+#pragma unroll
+            for (int n = 0; n < QB; ++n) {
+              o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pl[n][0], o[n][d], 0, 0, 0);
+              o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pl[n][1], o[n][d], 0, 0, 0);
+            }
+          }
         }
         // weights below fp16's normal numbers: what the rounding left of them, 2^14 times as large, once more
         bool more = false;

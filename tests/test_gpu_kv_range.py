@@ -1,0 +1,106 @@
+"""GPU attention over the paged 8-bit cache at the ends of its range, against float64: weights' bits, masked pages, scales that
+lie far apart.
+
+Bounds, for a row with probabilities p, S = sum_t p_t |V_t| and N = max_t ||K_t||_1 over what it sees.  A query element
+is held to half a step of max|q| / 8355711 (three digits), below max|q| 2^-24, which moves a score by at most
+delta = |scale| max|q| 2^-24 N and a weight by 2 delta relatively (bf16 prompts hold every bf16 element down to 2^-31 of max|q|:
+less).  Scores, exp and sums in fp32 move a weight by (8 + 2 |s|_max) 2^-23 + n 2^-24, as in test_gpu_kv.py.  The weights in the
+product with the values: fp32 24 bits (2^-23); bf16 prompts 11 bits (2^-11); bf16 single tokens two fp16 terms: the second is off
+by at most 2^-24 of the weight or, where it is subnormal, by 2^-25, and the row's largest weight is at least 2^6, so p_t is off
+by 2^-24 p_t + 2^-31 max p.  The output is rounded by 2^-8 (bf16) or 2^-23 (fp32) of itself."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import serve
+from paper_2412_09282_amd import crvq as C
+
+from gpu_util import say
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(DT[dtype])
+
+
+def is_step(new, Hq, Hkv):
+    return max(new) * (Hq // Hkv) <= 16
+
+
+def reference(cache, table, start, kv_len, q, scale, causal, window, dtype, step):
+    """(out, lse, bound of out, bound of lse) in float64, row by row."""
+    kc, vc = [a.astype(np.float64) for a in cache[:2]]
+    ks, vs = [a.astype(np.float64) for a in cache[2:]]
+    T, Hq, D = q.shape
+    G, P = Hq // kc.shape[1], kc.shape[2]
+    out, tol = np.zeros((T, Hq, D)), np.zeros((T, Hq, D))
+    lse, lse_tol = np.full((T, Hq), -np.inf), np.zeros((T, Hq))
+    rounding, weight = (2.0 ** -8, 2.0 ** -24 if step else 2.0 ** -11) if dtype == "bf16" else (2.0 ** -23, 2.0 ** -23)
+    for b in range(len(kv_len)):
+        n, length = int(start[b + 1] - start[b]), int(kv_len[b])
+        pages = table[b, :-(-length // P)]
+        K = (kc[pages] * ks[pages][:, :, None, None]).transpose(1, 0, 2, 3).reshape(kc.shape[1], -1, D)
+        V = (vc[pages] * vs[pages][:, :, None, None]).transpose(1, 0, 3, 2).reshape(kc.shape[1], -1, D)
+        for i in range(n):
+            place = length - n + i
+            hi = min(length, place + 1) if causal else length
+            lo = max(0, place + 1 - window) if window else 0
+            for h in range(Hq):
+                row, Kh, Vh = (start[b] + i, h), K[h // G, lo:hi], V[h // G, lo:hi]
+                s = Kh @ q[row].astype(np.float64) * scale
+                p = np.exp(s - s.max())
+                lse[row] = np.log(p.sum()) + s.max()
+                p /= p.sum()
+                out[row] = p @ Vh
+                size, most = p @ np.abs(Vh), p.max() * np.abs(Vh).sum(0)
+                move = 2 * abs(scale) * np.abs(q[row]).max() * 2.0 ** -24 * np.abs(Kh).sum(1).max() + \
+                    (8 + 2 * np.abs(s).max()) * 2.0 ** -23 + length * 2.0 ** -24
+                tol[row] = rounding * np.abs(out[row]) + (weight + move) * size
+                if dtype == "bf16" and step:
+                    tol[row] += 2.0 ** -31 * most
+                lse_tol[row] = move + 2.0 ** -22 * (1 + abs(lse[row]))
+    return out, lse, tol, lse_tol
+
+
+def check(cache, table, new, kv, q, scale, dtype, causal=True, window=0, what=""):
+    start = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    kv_len = np.array(kv, np.int32)
+    step = is_step(new, q.shape[1], cache[0].shape[1])
+    exp, lse_exp, tol, lse_tol = reference(cache, table, start, kv_len, q, scale, causal, window, dtype, step)
+    qt = dev(q, dtype)
+    out, lse = torch.full_like(qt, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    C.crvq_kv_attention(qt, out, *[dev(a) for a in cache], dev(table), dev(start), dev(kv_len), max(new), max(kv), scale=scale,
+                        causal=causal, window=window, lse=lse)
+    torch.cuda.synchronize()
+    got, l = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    err = np.abs(got - exp)
+    say(f"{what} {new} of {kv} {q.shape[1:]} {dtype} window {window} {'step' if step else 'prompt'}: "
+        f"{np.max(err / np.maximum(tol, 1e-300)):.3g} of the bound")
+    assert (err <= tol).all() and (np.abs(l - lse_exp) <= lse_tol).all()
+
+
+def random_cache(g, pages, Hkv, D, page):
+    return [g.integers(-127, 128, (pages, Hkv, page, D)).astype(np.int8),
+            g.integers(-127, 128, (pages, Hkv, D, page)).astype(np.int8),
+            np.exp2(g.uniform(-1, 1, (pages, Hkv)) - 6).astype(np.float32),
+            np.exp2(g.uniform(-1, 1, (pages, Hkv)) - 6).astype(np.float32)]
+
+
+def queries(g, dtype, *shape):
+    q = g.standard_normal(shape).astype(np.float32)
+    return serve.bf16_round(q) if dtype == "bf16" else q
+
+
+@pytest.mark.parametrize("D,page", [(64, 16), (128, 64), (96, 32), (192, 64), (256, 16), (256, 256)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_single_tokens_keep_the_weights_bits(D, page, dtype):
+    """Many outputs are small sums of large terms, so that a weight's rounding shows past the output's own."""
+    g = np.random.default_rng(D + page)
+    new, kv, Hq, Hkv = [1, 2, 1, 1], [2, 40, 3, 700], 8, 2
+    per = -(-max(kv) // page)
+    cache = random_cache(g, 4 * per, Hkv, D, page)
+    table = g.permutation(4 * per).reshape(4, per).astype(np.int32)
+    check(cache, table, new, kv, queries(g, dtype, sum(new), Hq, D), D ** -0.5, dtype, what="weights' bits")
