@@ -303,7 +303,7 @@ struct Columns {
         seen[n] = ((1u << y) - 1u) & ~((1u << x) - 1u);
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-          if (!(seen[n] >> j & 1)) s[n][j >> 2][j & 3] = -3e38f;
+          if (!(seen[n] >> j & 1)) s[n][j >> 2][j & 3] = -kInf;  // stays below every score whatever its page's scale is
       }
     }
 #pragma unroll
@@ -312,7 +312,7 @@ struct Columns {
       float top = fmaxf(fmaxf(s[n][0][0], s[n][0][1]), s[n][0][2]);
 #pragma unroll
       for (int j = 3; j < 16; ++j) top = fmaxf(top, s[n][j >> 2][j & 3]);
-      top *= alpha;
+      top *= alpha;  // -infinity where the column sees none of them, or (alpha 0) NaN, which no comparison and no maximum takes
       if (__any(top > m[n] + kSlack || fall != 1.f)) {
         asm volatile("; a branch, not selections");
         const float now = fmaxf(m[n], quarters_max(top));

@@ -7,7 +7,8 @@ delta = |scale| max|q| 2^-24 N and a weight by 2 delta relatively (bf16 prompts 
 less).  Scores, exp and sums in fp32 move a weight by (8 + 2 |s|_max) 2^-23 + n 2^-24, as in test_gpu_kv.py.  The weights in the
 product with the values: fp32 24 bits (2^-23); bf16 prompts 11 bits (2^-11); bf16 single tokens two fp16 terms: the second is off
 by at most 2^-24 of the weight or, where it is subnormal, by 2^-25, and the row's largest weight is at least 2^6, so p_t is off
-by 2^-24 p_t + 2^-31 max p.  The output is rounded by 2^-8 (bf16) or 2^-23 (fp32) of itself."""
+by 2^-24 p_t + 2^-31 max p.  The output is rounded by 2^-8 (bf16) or 2^-23 (fp32) of itself.  Numbers below fp32's normal ones may
+be 0: weights below 2^-126 of the row's largest, and results below 2^-126."""
 import numpy as np
 import pytest
 import torch
@@ -58,7 +59,7 @@ def reference(cache, table, start, kv_len, q, scale, causal, window, dtype, step
                 size, most = p @ np.abs(Vh), p.max() * np.abs(Vh).sum(0)
                 move = 2 * abs(scale) * np.abs(q[row]).max() * 2.0 ** -24 * np.abs(Kh).sum(1).max() + \
                     (8 + 2 * np.abs(s).max()) * 2.0 ** -23 + length * 2.0 ** -24
-                tol[row] = rounding * np.abs(out[row]) + (weight + move) * size
+                tol[row] = rounding * np.abs(out[row]) + (weight + move) * size + 2.0 ** -126 * (1 + np.abs(Vh).sum(0))
                 if dtype == "bf16" and step:
                     tol[row] += 2.0 ** -31 * most
                 lse_tol[row] = move + 2.0 ** -22 * (1 + abs(lse[row]))
@@ -104,3 +105,28 @@ def test_single_tokens_keep_the_weights_bits(D, page, dtype):
     cache = random_cache(g, 4 * per, Hkv, D, page)
     table = g.permutation(4 * per).reshape(4, per).astype(np.int32)
     check(cache, table, new, kv, queries(g, dtype, sum(new), Hq, D), D ** -0.5, dtype, what="weights' bits")
+
+
+@pytest.mark.parametrize("window", [0, 3])
+@pytest.mark.parametrize("new", [4, 40])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pages_that_a_row_does_not_see(dtype, page, new, window):
+    """Scores of about -150 wherever a row looks, and next to them a page that some rows do not see, whose keys are nothing: scale 0,
+    or 2^-100 as an append of zeros leaves it.  It is the last page, which the mask hides from the first rows, or the first, which
+    the window hides from the last ones."""
+    for key_scale in (0.0, 2.0 ** -100):
+        g = np.random.default_rng(page + new)
+        D, Hq, Hkv = 64, 8, 2
+        kv = (page + 5 if new == 4 else page + 35) if window else (2 * page + 2 if new == 4 else 2 * page + 20)
+        per = -(-kv // page)
+        cache = random_cache(g, per + 1, Hkv, D, page)
+        cache[0] = g.integers(-127, -89, cache[0].shape).astype(np.int8)
+        cache[2][:] = g.uniform(0.15, 0.17, cache[2].shape)
+        table = g.permutation(per + 1)[:per].reshape(1, per).astype(np.int32)
+        hidden = [p for p in range(per) if (p * page < 64 and p == 0 if window else p >= 2)]
+        for p in hidden:
+            cache[2][table[0, p]] = key_scale
+        q = (1 + np.abs(queries(g, dtype, new, Hq, D)) / 8).astype(np.float32)
+        q = serve.bf16_round(q) if dtype == "bf16" else q
+        check(cache, table, [new], [kv], q, D ** -0.5, dtype, window=window, what=f"hidden pages of scale {key_scale:g},")
