@@ -11,7 +11,8 @@
 //     term at no cost (32 sequences of up to 4096 tokens 138 us with it and without, heads of 256 elements 69 for 65); prompts
 //     are bound by these instructions (two of them, 596 us for 384), and their error against 64 bits is that of
 //     rounding the output to bf16 with either (1.67e-3 and 1.66e-3).  The page's
-//     value scale goes into the weights, relative to a power of two 2^e that follows the largest scale met so far.
+//     value scale goes into the weights, relative to a power of two 2^e of each column that follows the largest of its weights
+//     times scale: scales of any size then add up as in fp32, and a page that a column does not see does not matter to it.
 //     Weights below fp16's normal numbers (2^-21 of the row's largest) are added in further passes over the step, 2^14
 //     times as large each, so that they keep their 11 bits too; a pass is taken only where there are any.  For fp32
 //     queries the weights are three bf16 terms, which hold all of their 24 bits.
@@ -35,10 +36,12 @@ typedef uint16_t at_s2 __attribute__((ext_vector_type(2)));
 constexpr float kInf = __builtin_inff();
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kTokens = 64;     // tokens of a step
-// The maximum is renewed when a score passes it by more than 2^kSlack, so weights reach 2^kSlack; with the
-// scale's factor at most 2^kLift they stay below fp16's 2^16 and keep 11 bits down to 2^-21 of the maximum.
+// The maximum is renewed when a score, or a score with its page's value scale, passes it by more than 2^kSlack, so
+// weights reach 2^kSlack; with a factor of at most 2^kLift they stay below fp16's 2^16 and keep 11 bits down to 2^-21 of the maximum.
 constexpr float kSlack = 8.f;
 constexpr int kLift = 7;
+constexpr int kFaint = -64;    // pages whose scales are this far below 2^e: the softmax's sum is taken of weights of its own
+constexpr int kNothing = -1024;  // exponent of a value scale of 0
 
 struct AttnArgs {
   KvCache c;
@@ -157,10 +160,10 @@ struct Columns {
   static constexpr double kSteps = 8355711.0;                        // 127 in every digit
   at_i4 q[QB][DC][NT];
   float step[QB], m[QB], l[QB];
+  int e[QB];                          // exponents that value scales are taken relative to
   int lo[QB], hi[QB];                 // the tokens a column sees
   int first, last, all_lo, all_hi;    // the tokens any of them sees, and those that all of them see
-  at_f4 o[QB][DT];
-  int e;  // exponent that value scales are taken relative to
+  at_f4 o[QB][DT];                    // in units of 2^(m + e - kLift)
 
   // Queries: fixed point, 16 elements of a column and chunk in a lane; HALF: 8 of them.
   __device__ __forceinline__ void begin(const AttnArgs& a, const KvSeq& sq, bool ok, int hk, int col0, int cols) {
@@ -218,10 +221,10 @@ struct Columns {
       if (lo[n] >= hi[n]) lo[n] = hi[n] = 0;
       m[n] = -kInf;
       l[n] = 0.f;
+      e[n] = 0;
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[n][d] = at_f4{0.f, 0.f, 0.f, 0.f};
     }
-    e = -126;
     first = 0x7fffffff, last = 0, all_lo = 0, all_hi = 0x7fffffff;
 #pragma unroll
     for (int n = 0; n < QB; ++n) {
@@ -281,19 +284,14 @@ struct Columns {
   // Scores to weights; ks and vs are the scales of this lane's 16 tokens, `good` whether they can be used.
   __device__ __forceinline__ void weigh(at_f4 (&s)[QB][4], int t0, float ks, float vs, bool good) {
     const int c = (threadIdx.x >> 4) & 3;
-    if (!good) vs = 0.f;
-    // the power of two that value scales are relative to
-    const int at = (static_cast<int>(__float_as_uint(vs)) >> 23) - 126;
-    const int ve = SMALL ? wave_max(at) : __builtin_amdgcn_readfirstlane(at);
-    float fall = 1.f;
-    if (ve > e) {
-      fall = ldexpf(1.f, max(e - ve, -126));
-      e = ve;
-    }
-    const float weight = fmaxf(ldexpf(vs, -e), 0x1p-40f) * static_cast<float>(1 << kLift);
-    const float weight_log = __builtin_amdgcn_logf(weight), unweight = __builtin_amdgcn_rcpf(weight);
+    // the value scale as 2^ve times a number in [1/2, 1)
+    const bool some = good && vs > 0.f;
+    const int ve = some ? __builtin_amdgcn_frexp_expf(vs) : kNothing;
+    const float lift = (some ? __builtin_amdgcn_frexp_mantf(vs) : 1.f) * static_cast<float>(1 << kLift);
+    const float lift_log = __builtin_amdgcn_logf(lift), unlift = __builtin_amdgcn_rcpf(lift);
     const bool whole = t0 >= all_lo && t0 + kTokens <= all_hi;
     uint32_t seen[QB];  // which of the lane's 16 tokens its column sees
+    float undo[QB];     // from the sum of the weights that enter the second product to that of the softmax
     if (!whole) {
       asm volatile("; a branch, not selections");
       const int base = t0 + 16 * c;
@@ -313,18 +311,33 @@ struct Columns {
 #pragma unroll
       for (int j = 3; j < 16; ++j) top = fmaxf(top, s[n][j >> 2][j & 3]);
       top *= alpha;  // -infinity where the column sees none of them, or (alpha 0) NaN, which no comparison and no maximum takes
-      if (__any(top > m[n] + kSlack || fall != 1.f)) {
+      if (__any(top > m[n] + (kSlack - static_cast<float>(max(ve - e[n], 0))))) {
         asm volatile("; a branch, not selections");
         const float now = fmaxf(m[n], quarters_max(top));
-        const float f = m[n] > -kInf ? __builtin_amdgcn_exp2f(m[n] - now) : 0.f;
+        const float reach = quarters_max(top + static_cast<float>(ve));  // with the value scales
+        const float ever = m[n] > -kInf ? fmaxf(m[n] + static_cast<float>(e[n]), reach) : reach;
+        const int at = now > -kInf && ever > -kInf ? static_cast<int>(rintf(ever - now)) : 0;
+        const float fall = m[n] > -kInf ? m[n] - now : -kInf;
+        l[n] *= __builtin_amdgcn_exp2f(fall);
+        const float keep = __builtin_amdgcn_exp2f(fall + static_cast<float>(e[n] - at));
         m[n] = now;
-        l[n] *= f;
-        const float keep = f * fall;
+        e[n] = at;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[n][d] *= keep;
       }
-      // weights p 2^.. = exp2(score - m) weight, as exp2 of one fused multiply-add
-      const float shift = weight_log - m[n];
+      const int rel = ve - e[n];
+      undo[n] = ldexpf(unlift, -rel);
+      if (__any(rel < kFaint)) {  // their products with the value scale may vanish where they themselves do not
+        asm volatile("; a branch, not selections");
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (whole || (seen[n] >> j & 1)) sum += __builtin_amdgcn_exp2f(fmaf(s[n][j >> 2][j & 3], alpha, -m[n]));
+        l[n] += sum;
+        undo[n] = 0.f;
+      }
+      // weights p 2^.. = exp2(score - m) times the scale's factor, as exp2 of one fused multiply-add
+      const float shift = (lift_log + static_cast<float>(rel)) - m[n];
 #pragma unroll
       for (int j = 0; j < 16; ++j)
         s[n][j >> 2][j & 3] = __builtin_amdgcn_exp2f(fmaf(s[n][j >> 2][j & 3], alpha, shift));
@@ -342,7 +355,7 @@ struct Columns {
       float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < 16; ++j) sum += s[n][j >> 2][j & 3];
-      l[n] = fmaf(sum, unweight, l[n]);
+      l[n] = fmaf(sum, undo[n], l[n]);
     }
   }
 
@@ -450,12 +463,13 @@ struct Columns {
 
   // Sums over the quarters, and o back from its power of two.
   __device__ __forceinline__ void end() {
-    const float back = ldexpf(1.f, e - kLift);
 #pragma unroll
     for (int n = 0; n < QB; ++n) {
       l[n] = quarters_sum(l[n]);
 #pragma unroll
-      for (int d = 0; d < DT; ++d) o[n][d] *= back;
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][d][i] = ldexpf(o[n][d][i], e[n] - kLift);
     }
   }
 };

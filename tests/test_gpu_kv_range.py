@@ -130,3 +130,47 @@ def test_pages_that_a_row_does_not_see(dtype, page, new, window):
         q = (1 + np.abs(queries(g, dtype, new, Hq, D)) / 8).astype(np.float32)
         q = serve.bf16_round(q) if dtype == "bf16" else q
         check(cache, table, [new], [kv], q, D ** -0.5, dtype, window=window, what=f"hidden pages of scale {key_scale:g},")
+
+
+def paged(g, D, Hq, Hkv, page, n_pages, dtype, n, scores, value_scales):
+    """A sequence of n_pages whole pages: score about scores[p] in page p (queries near 1, codes of keys 90 to 127), values of random
+    codes with value_scales[p]."""
+    cache = random_cache(g, n_pages, Hkv, D, page)
+    cache[0] = g.integers(90, 128, cache[0].shape).astype(np.int8)
+    table = g.permutation(n_pages).reshape(1, n_pages).astype(np.int32)
+    for p in range(n_pages):
+        cache[2][table[0, p]] = scores[p] / (D ** 0.5 * 108.5 * 1.1)
+        cache[3][table[0, p]] = value_scales[p]
+    q = (1 + np.abs(queries(g, dtype, n, Hq, D)) / 8).astype(np.float32)
+    return cache, table, serve.bf16_round(q) if dtype == "bf16" else q
+
+
+# The scales of the first and of the other pages, and by how much the pages with the larger ones score less: nothing of them is
+# left (200, 300), or as much as of the others, the sums then holding both (2^60 = e^41.6, 2^100 = e^69.3).
+SPREADS = [(0, -60, 200), (-60, 0, 200), (-60, 0, 41.6), (0, -60, 41.6), (50, -50, 69.3), (-50, 50, 69.3), (100, -100, 300),
+           (-100, 100, 300), (60, 0, 0), (0, 60, 0)]
+
+
+@pytest.mark.parametrize("first,second,less", SPREADS)
+@pytest.mark.parametrize("page,new", [(64, 1), (16, 1), (64, 40), (16, 40)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_value_scales_far_apart(dtype, page, new, first, second, less):
+    """512 tokens, the first half with one magnitude of value scales and the second with another: a wave meets both."""
+    g = np.random.default_rng(page + new)
+    pages = 512 // page
+    half = [p < pages // 2 for p in range(pages)]
+    big_first = first > second
+    scores = [0.1 if f == big_first else less + 0.1 for f in half]
+    cache, table, q = paged(g, 64, 8, 2, page, pages, dtype, new, scores, [2.0 ** (first if f else second) for f in half])
+    check(cache, table, [new], [512], q, 64 ** -0.5, dtype, causal=False, what=f"value scales 2^{first}, 2^{second}, scores {less},")
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_value_scales_of_zero(dtype, new):
+    """A page whose value scale is 0 adds nothing, whatever its codes are."""
+    g = np.random.default_rng(new)
+    for scales in ([0.0] * 8, [1.0, 0.0, 0.0, 2.0 ** -60] * 2, [0.0, 2.0 ** -60, 1.0, 0.0] * 2):
+        scores = [300.0 if s < 1 else 0.1 for s in scales]
+        cache, table, q = paged(g, 64, 8, 2, 64, 8, dtype, new, scores, scales)
+        check(cache, table, [new], [512], q, 64 ** -0.5, dtype, causal=False, what=f"value scales {scales[:4]},")
