@@ -14,8 +14,8 @@
 //     value scale goes into the weights, relative to a power of two 2^e of each column that follows the largest of its weights
 //     times scale: scales of any size then add up as in fp32, and a page that a column does not see does not matter to it.
 //     Weights below fp16's normal numbers (2^-21 of the row's largest) are added in further passes over the step, 2^14
-//     times as large each, so that they keep their 11 bits too; a pass is taken only where there are any.  For fp32
-//     queries the weights are three bf16 terms, which hold all of their 24 bits.
+//     times as large each, so that they keep their 11 bits too, down to fp32's smallest normal number; a pass is taken only
+//     where there are any.  For fp32 queries the weights are three bf16 terms, which hold all of their 24 bits.
 // The token in row 4 c + i of tile u is 16 c + 4 u + i: a lane (column r = lane % 16, quarter c = lane / 16) then
 // holds the scores of 16 consecutive tokens, which are exactly its operands of the second product and, pages being
 // multiples of 16, belong to one page.
@@ -363,9 +363,9 @@ struct Columns {
   template <bool LDS, class Value>
   __device__ __forceinline__ void add(at_f4 (&s)[QB][4], Value&& value) {
     if constexpr (sizeof(T) == 2) {
-      for (int pass = 0;; ++pass) {
-        at_h8 pw[QB][2], pl[QB][2];  // the weights as fp16, and what that leaves of them
-        at_s2 least = {0x7fff, 0x7fff};
+      at_h8 pw[QB][2], pl[QB][2];  // the weights as fp16, and what that leaves of them
+      at_s2 least = {0x7fff, 0x7fff};
+      auto round = [&]() {
 #pragma unroll
         for (int n = 0; n < QB; ++n)
 #pragma unroll
@@ -379,53 +379,67 @@ struct Columns {
               pl[n][j >> 3][(j & 7) + 1] = static_cast<_Float16>(s[n][j >> 2][(j & 3) + 1] - static_cast<float>(h[1]));
             }
           }
-        at_u4 ahead[2][2] = {{value(0, 0), value(0, 1)}};
+      };
+      round();
+      at_u4 ahead[2][2] = {{value(0, 0), value(0, 1)}};
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        if constexpr (LDS) {
+          if (d + 1 < DT) ahead[(d + 1) & 1][0] = value(d + 1, 0), ahead[(d + 1) & 1][1] = value(d + 1, 1);
+          __builtin_amdgcn_sched_barrier(0);
+        } else if (d > 0) {
+          ahead[d & 1][0] = value(d, 0);
+          ahead[d & 1][1] = value(d, 1);
+        }
+        const at_h8 v0 = __builtin_bit_cast(at_h8, ahead[d & 1][0]), v1 = __builtin_bit_cast(at_h8, ahead[d & 1][1]);
+#pragma unroll
+        for (int n = 0; n < QB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[n][0], o[n][d], 0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < QB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pw[n][1], o[n][d], 0, 0, 0);
+        if constexpr (!HALF) {
+#pragma unroll
+          for (int n = 0; n < QB; ++n) {
+            o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pl[n][0], o[n][d], 0, 0, 0);
+            o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pl[n][1], o[n][d], 0, 0, 0);
+          }
+        }
+      }
+      // weights below fp16's normal numbers: what the rounding left of them, 2^14 times as large in every pass; nine of them reach
+      // fp32's smallest normal number
+      if (!__any(least[0] < 0x0400 || least[1] < 0x0400)) return;
+      asm volatile("; a branch, not selections");
+      float by = 1.f;
+#pragma unroll 1
+      for (int pass = 1; pass < 10; ++pass) {
+        bool more = false;
+#pragma unroll
+        for (int n = 0; n < QB; ++n)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float x = s[n][j >> 2][j & 3];
+            const float rest = fabsf(x) < 0x1p-14f ? (x - static_cast<float>(pw[n][j >> 3][j & 7])) * 0x1p14f : 0.f;
+            s[n][j >> 2][j & 3] = rest;
+            more |= rest != 0.f;
+          }
+        if (!__any(more)) return;
+        by *= 0x1p-14f;
+        round();
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          if constexpr (LDS) {
-            if (d + 1 < DT) ahead[(d + 1) & 1][0] = value(d + 1, 0), ahead[(d + 1) & 1][1] = value(d + 1, 1);
-            __builtin_amdgcn_sched_barrier(0);
-          } else if (d > 0) {
-            ahead[d & 1][0] = value(d, 0);
-            ahead[d & 1][1] = value(d, 1);
-          }
-          const at_h8 v0 = __builtin_bit_cast(at_h8, ahead[d & 1][0]), v1 = __builtin_bit_cast(at_h8, ahead[d & 1][1]);
+          const at_h8 v0 = __builtin_bit_cast(at_h8, value(d, 0)), v1 = __builtin_bit_cast(at_h8, value(d, 1));
 #pragma unroll
-          for (int n = 0; n < QB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[n][0], o[n][d], 0, 0, 0);
-#pragma unroll
-          for (int n = 0; n < QB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pw[n][1], o[n][d], 0, 0, 0);
-          if constexpr (!HALF) {
-#pragma unroll
-            for (int n = 0; n < QB; ++n) {
-              o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pl[n][0], o[n][d], 0, 0, 0);
-              o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pl[n][1], o[n][d], 0, 0, 0);
+          for (int n = 0; n < QB; ++n) {
+            at_f4 part = {0.f, 0.f, 0.f, 0.f};
+            part = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[n][0], part, 0, 0, 0);
+            part = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pw[n][1], part, 0, 0, 0);
+            if constexpr (!HALF) {
+              part = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pl[n][0], part, 0, 0, 0);
+              part = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pl[n][1], part, 0, 0, 0);
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[n][d][i] = fmaf(part[i], by, o[n][d][i]);
           }
         }
-        // weights below fp16's normal numbers: what the rounding left of them, 2^14 times as large, once more
-        bool more = false;
-        if (__any(least[0] < 0x0400 || least[1] < 0x0400)) {
-          asm volatile("; a branch, not selections");
-#pragma unroll
-          for (int n = 0; n < QB; ++n)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const float x = s[n][j >> 2][j & 3];
-              const float rest = fabsf(x) < 0x1p-14f ? (x - static_cast<float>(pw[n][j >> 3][j & 7])) * 0x1p14f : 0.f;
-              s[n][j >> 2][j & 3] = rest;
-              more |= rest != 0.f;
-            }
-          more = __any(more) && pass < 5;
-        }
-        if (more || pass) {
-          asm volatile("; a branch, not selections");
-          const float by = more ? 0x1p14f : ldexpf(1.f, -14 * pass);
-#pragma unroll
-          for (int n = 0; n < QB; ++n)
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[n][d] *= by;
-        }
-        if (!more) break;
       }
     } else {
       at_b8 pb[QB][2][3];

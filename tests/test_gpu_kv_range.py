@@ -165,6 +165,20 @@ def test_value_scales_far_apart(dtype, page, new, first, second, less):
     check(cache, table, [new], [512], q, 64 ** -0.5, dtype, causal=False, what=f"value scales 2^{first}, 2^{second}, scores {less},")
 
 
+@pytest.mark.parametrize("window", [0, 20])
+@pytest.mark.parametrize("page,new", [(64, 4), (16, 4), (64, 40), (16, 40)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_value_scales_of_pages_that_a_row_does_not_see(dtype, page, new, window):
+    """Next to pages of value scale 2^-60 one of 2^60 that some rows of a tile do not see: the last one under the mask, or the first
+    one under the window."""
+    g = np.random.default_rng(page + new)
+    n_pages = -(-(page + 40) // page) if window else 3
+    kv = page + 18 + new // 2 if window else 2 * page + new // 2
+    scales = [2.0 ** (60 if (p == 0 if window else p == 2) else -60) for p in range(max(n_pages, -(-kv // page)))]
+    cache, table, q = paged(g, 64, 8, 2, page, len(scales), dtype, new, [0.5] * len(scales), scales)
+    check(cache, table, [new], [kv], q, 64 ** -0.5, dtype, window=window, what="hidden value scales,")
+
+
 @pytest.mark.parametrize("new", [1, 40])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_value_scales_of_zero(dtype, new):
