@@ -473,6 +473,8 @@ def crvq_kv_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_ca
     if cos is not None:
         assert cos.dtype == sin.dtype == torch.float32 and cos.shape == sin.shape and cos.dim() == 2
         assert cos.is_contiguous() and sin.is_contiguous()
+        if n and cos.shape[0] == 0:  # its pointer would be NULL, which stands for no rotation
+            raise ValueError("the angle table has no rows")
         angles = (cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1])
     assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == n)
     _check("crvq_kv_append", lib().crvq_kv_append(

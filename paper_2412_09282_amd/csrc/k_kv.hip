@@ -86,9 +86,12 @@ __device__ __forceinline__ Angles angles(const KvRotation& rt, int row, int plac
   return a;
 }
 
-// The angles of pairs j .. j + 7 (j a multiple of 8).
+// The angles of pairs j .. j + 7 (j a multiple of 8).  A table may have no rows at all: outside it nothing is read.
 __device__ __forceinline__ void angles8(const KvRotation& rt, const Angles& an, int j, float (&c)[8], float (&s)[8]) {
-  if (rt.vec) {
+  if (!an.ok) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = __uint_as_float(0x7fc00000u), s[i] = 0.f;
+  } else if (rt.vec) {
     const float4 c0 = reinterpret_cast<const float4*>(an.c + j)[0], c1 = reinterpret_cast<const float4*>(an.c + j)[1];
     const float4 s0 = reinterpret_cast<const float4*>(an.s + j)[0], s1 = reinterpret_cast<const float4*>(an.s + j)[1];
     c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
@@ -96,10 +99,6 @@ __device__ __forceinline__ void angles8(const KvRotation& rt, const Angles& an, 
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) c[i] = an.c[j + i], s[i] = an.s[j + i];
-  }
-  if (!an.ok) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = __uint_as_float(0x7fc00000u);
   }
 }
 
