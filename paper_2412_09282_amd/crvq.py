@@ -467,6 +467,10 @@ def crvq_kv_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_ca
     rotates the queries q into q_out (which may be q); see include/crvq.h for the cache and the batch."""
     B, Hkv, D, page, cache = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len)
     n, dt = k.shape[0], k.dtype
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin go together")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
     Hq = 0 if q is None else q.shape[1]
     rows = (None, 0, 0, None, 0, 0) if q is None else _row_args(q, n, Hq, D, dt) + _row_args(q_out, n, Hq, D, dt)
     angles = (None, None, 0, 0)
