@@ -438,12 +438,22 @@ def _workspace_for(nbytes: int, device, stream) -> Optional[torch.Tensor]:
         return _workspace(nbytes, device)
 
 
+def _reachable(*tensors) -> None:
+    """The kernels follow these pointers: memory of the GPU, or pinned memory of the host."""
+    for t in tensors:
+        if t is not None and not t.is_cuda and not t.is_pinned():
+            raise ValueError("a tensor in host memory that is not pinned")
+
+
 def _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len):
     """The cache's and batch's arguments, with the shapes and types the C call cannot see checked."""
     n_pages, Hkv, page, D = k_cache.shape
     assert v_cache.shape == (n_pages, Hkv, D, page) and k_cache.dtype == v_cache.dtype == torch.int8
     assert k_scale.shape == v_scale.shape == (n_pages, Hkv) and k_scale.dtype == v_scale.dtype == torch.float32
     assert k_cache.is_contiguous() and v_cache.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()
+    if not (k_cache.is_cuda and v_cache.is_cuda and k_scale.is_cuda and v_scale.is_cuda and block_table.is_cuda and
+            start.is_cuda and kv_len.is_cuda):
+        _reachable(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len)
     B = kv_len.numel()
     assert start.dtype == kv_len.dtype == block_table.dtype == torch.int32 and start.numel() == B + 1
     assert start.is_contiguous() and kv_len.is_contiguous()
@@ -453,8 +463,12 @@ def _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len):
 
 
 def _row_args(t, n_tokens, heads, D, dtype):
-    assert t.shape == (n_tokens, heads, D) and t.dtype == dtype and (D == 1 or t.stride(2) == 1)
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    assert t.shape == (n_tokens, heads, D) and t.dtype == dtype
+    token, head, element = t.stride()
+    assert D == 1 or element == 1
+    if not t.is_cuda:
+        _reachable(t)
+    return t.data_ptr(), token, head
 
 
 def crvq_kv_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -465,15 +479,16 @@ def crvq_kv_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_ca
                    stream=None) -> None:
     """Rotates, quantizes and stores the new keys and values k, v (tokens x Hkv x D) in the paged 8-bit cache, and
     rotates the queries q into q_out (which may be q); see include/crvq.h for the cache and the batch."""
-    B, Hkv, D, page, cache = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len)
-    n, dt = k.shape[0], k.dtype
     if (cos is None) != (sin is None):
         raise ValueError("cos and sin go together")
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
+    B, Hkv, D, page, cache = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len)
+    n, dt = k.shape[0], k.dtype
     Hq = 0 if q is None else q.shape[1]
     rows = (None, 0, 0, None, 0, 0) if q is None else _row_args(q, n, Hq, D, dt) + _row_args(q_out, n, Hq, D, dt)
     angles = (None, None, 0, 0)
+    _reachable(cos, sin, positions)
     if cos is not None:
         assert cos.dtype == sin.dtype == torch.float32 and cos.shape == sin.shape and cos.dim() == 2
         assert cos.is_contiguous() and sin.is_contiguous()
@@ -510,19 +525,25 @@ def crvq_kv_attention(q: torch.Tensor, out: torch.Tensor, k_cache: torch.Tensor,
     B, Hkv, D, page, cache = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len)
     n, Hq = q.shape[0], q.shape[1]
     assert lse is None or (lse.dtype == torch.float32 and lse.shape == (n, Hq) and lse.is_contiguous())
+    _reachable(lse)
+    rows = _row_args(q, n, Hq, D, q.dtype) + _row_args(out, n, Hq, D, q.dtype)
     ws = _workspace_for(L.crvq_kv_attention_workspace_size(B, Hq, Hkv, D, max_new, max_kv), q.device, stream)
     _check("crvq_kv_attention", L.crvq_kv_attention(
-        B, Hq, Hkv, D, page, *cache, max_new, max_kv, n, dtype_code(q), *_row_args(q, n, Hq, D, q.dtype),
-        *_row_args(out, n, Hq, D, q.dtype), D ** -0.5 if scale is None else scale, int(causal), window, _ptr(lse),
-        _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+        B, Hq, Hkv, D, page, *cache, max_new, max_kv, n, dtype_code(q), *rows, D ** -0.5 if scale is None else scale,
+        int(causal), window, _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
 
 
-def _w4_args(codes, scales, zeros):
-    assert codes.dim() == 2 and codes.dtype == torch.uint8 and codes.stride(1) == 1
-    assert scales.dim() == 2 and scales.shape[0] == codes.shape[0] and scales.stride(1) == 1
-    assert zeros is None or (zeros.dtype == torch.uint8 and zeros.shape == scales.shape and zeros.stride(1) == 1)
-    return (codes.data_ptr(), codes.stride(0), scales.data_ptr(), dtype_code(scales), scales.stride(0), _ptr(zeros),
-            0 if zeros is None else zeros.stride(0))
+def _w4_args(codes, scales, zeros, *others):
+    assert codes.dim() == 2 and codes.dtype == torch.uint8 and scales.dim() == 2 and scales.shape[0] == codes.shape[0]
+    (ld, one), (ld_s, one_s) = codes.stride(), scales.stride()
+    assert one == 1 and one_s == 1
+    ld_z = 0
+    if zeros is not None:
+        assert zeros.dtype == torch.uint8 and zeros.shape == scales.shape
+        ld_z, one_z = zeros.stride()
+        assert one_z == 1
+    _reachable(codes, scales, zeros, *others)
+    return codes.data_ptr(), ld, scales.data_ptr(), dtype_code(scales), ld_s, _ptr(zeros), ld_z
 
 
 def _w4_holds(codes, scales, group, N):
@@ -534,7 +555,7 @@ def crvq_w4_quantize(W: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
     """The 4-bit codes (two a byte), group scales and (if given) zero points of W; see include/crvq.h."""
     M, N = W.shape
     assert W.stride(1) == 1 and codes.shape[0] == M and _w4_holds(codes, scales, group, N)
-    c, ld, s, st, ld_s, z, ld_z = _w4_args(codes, scales, zeros)
+    c, ld, s, st, ld_s, z, ld_z = _w4_args(codes, scales, zeros, W)
     _check("crvq_w4_quantize", lib().crvq_w4_quantize(M, N, group, _ptr(W), W.stride(0), dtype_code(W), c, ld, s, st,
                                                       ld_s, z, ld_z, _stream(stream)))
 
@@ -544,7 +565,7 @@ def crvq_w4_dequant(codes: torch.Tensor, scales: torch.Tensor, group: int, out: 
     """out (M x N) = the values of a 4-bit matrix."""
     M, N = out.shape
     assert out.stride(1) == 1 and codes.shape[0] == M and _w4_holds(codes, scales, group, N)
-    _check("crvq_w4_dequant", lib().crvq_w4_dequant(M, N, group, *_w4_args(codes, scales, zeros), _ptr(out),
+    _check("crvq_w4_dequant", lib().crvq_w4_dequant(M, N, group, *_w4_args(codes, scales, zeros, out), _ptr(out),
                                                     out.stride(0), dtype_code(out), _stream(stream)))
 
 
@@ -554,8 +575,9 @@ def crvq_w4_gemv(codes: torch.Tensor, scales: torch.Tensor, group: int, x: torch
     L = lib()
     T, N = x.shape
     M = codes.shape[0]
-    assert y.shape == (T, M) and x.stride(1) == 1 and y.stride(1) == 1 and _w4_holds(codes, scales, group, N)
+    (ldx, one_x), (ldy, one_y) = x.stride(), y.stride()
+    assert y.shape == (T, M) and one_x == 1 and one_y == 1 and _w4_holds(codes, scales, group, N)
+    w = _w4_args(codes, scales, zeros, x, y)
     ws = _workspace_for(L.crvq_w4_gemv_workspace_size(M, N, T), y.device, stream)
-    _check("crvq_w4_gemv", L.crvq_w4_gemv(M, N, T, group, *_w4_args(codes, scales, zeros), _ptr(x), x.stride(0),
-                                          dtype_code(x), _ptr(y), y.stride(0), dtype_code(y), _ptr(ws),
-                                          0 if ws is None else ws.numel(), _stream(stream)))
+    _check("crvq_w4_gemv", L.crvq_w4_gemv(M, N, T, group, *w, _ptr(x), ldx, dtype_code(x), _ptr(y), ldy, dtype_code(y),
+                                          _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
