@@ -297,6 +297,14 @@ struct W4 {
 };
 hipError_t launch_w4_quantize(const void* W, int64_t ldw, int type, const W4& w, hipStream_t stream);
 hipError_t launch_w4_dequant(const W4& w, void* out, int64_t ldo, int type, hipStream_t stream);
+struct W4Plan {
+  int tb, nb;        // vectors of a block, blocks
+  int per_pass;      // vectors of a pass (grid z)
+  int waves, batches;  // a chunk is waves * batches * (steps of a batch) steps of columns
+  int chunks;        // grid y
+  int64_t groups;    // workgroups of a chunk and pass (grid x)
+};
+W4Plan plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2);
 size_t w4_gemv_ws_bytes(int64_t M, int64_t N, int64_t T);
 hipError_t launch_w4_gemv(const W4& w, int64_t T, const void* x, int64_t ldx, int x_type, void* y, int64_t ldy, int y_type,
                           void* ws, hipStream_t stream);

@@ -153,13 +153,6 @@ constexpr int kStep = 128;             // columns of a step
 constexpr int kXPad = 8;               // elements between rows of x in LDS
 constexpr int kXBytes = 73 << 10;      // of x in LDS: two workgroups a CU
 
-struct W4Plan {
-  int tb, nb;        // vectors of a block, blocks
-  int per_pass;      // vectors of a pass (grid z)
-  int waves, batches;  // a chunk is waves * batches * (steps of a batch) steps of columns
-  int chunks;        // grid y
-  int64_t groups;    // workgroups of a chunk and pass (grid x)
-};
 struct GemvArgs {
   W4 w;
   const void* x;
@@ -258,6 +251,14 @@ struct RawScales {
   }
 };
 
+// Between stores to LDS and the loads of other lanes of the same wave: a wave's LDS instructions execute in order, the
+// compiler has to keep them so.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // NB blocks of TB vectors; NR of a lane's four sums of a block in use; E groups in a step (1 for groups of 128 and
 // more).  The scales of a batch are 16 rows times U E groups: a lane reads E of one row, all with one load, and
 // hands them on through LDS (one load of a scale for every step made the kernel 40 % slower).
@@ -344,12 +345,14 @@ __global__ __launch_bounds__(1024) void w4_gemv_kernel(const GemvArgs a) {
   while (block < blocks) {
     uint4 cur[U];
     float2 scale[U];
+    wave_lds_order();
     if (su < U) {
 #pragma unroll
       for (int e = 0; e < E; ++e) held_scales[(sr * U + su) * E + e] = make_float2(raw.s[e], -16.f - raw.z[e]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) cur[u] = wq[u];
+    wave_lds_order();
 #pragma unroll
     for (int u = 0; u < U; ++u) scale[u] = held_scales[(r * U + u) * E + seg_group];
     const bool last = batch + 1 == a.batches;
@@ -485,7 +488,7 @@ hipError_t launch_w4_dequant(const W4& w, void* out, int64_t ldo, int type, hipS
 
 // The widest segments that stay within a group and are needed take the fewest instructions; the columns are cut where
 // x does not fit into LDS, and, where there are few rows, until the chip is filled.
-static W4Plan plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2) {
+W4Plan plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2) {
   W4Plan p;
   const int terms = x_f32 ? 3 : 1, widest = group_log2 >= 7 ? 16 : 1 << (group_log2 - 3);
   const int64_t rows = T * terms;
