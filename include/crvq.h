@@ -535,8 +535,9 @@ crvq_status crvq_w4_dequant(int64_t M, int64_t N, int32_t group, const uint8_t* 
 
 /* crvq_w4_gemv -- y[t] = W x[t] for T >= 0 vectors: x is T x N of x_dtype (row
  * stride ldx), y is T x M of y_dtype (row stride ldy).  Products are exact
- * (bf16 x as it is, fp32 x as the sum of three bf16 terms), sums fp32 per group and across groups, rounded
- * once.  An infinite or NaN element of x[t] makes y[t] NaN.  y may not overlap x.  Deterministic.
+ * (bf16 x as it is, fp32 x as the sum of three bf16 terms), sums fp32 per group and across groups in units of
+ * 2^-12 (results below 2^-114 are held to multiples of 2^-137 times a scale), rounded
+ * once.  Every finite x has the result of its sums; an infinite or NaN element of x[t] makes y[t] NaN.  y may not overlap x.  Deterministic.
  * Meant for few vectors: codes are read again for every 5 to 32 of them, and the workspace grows with T.
  * workspace: crvq_w4_gemv_workspace_size(M, N, T) bytes. */
 size_t crvq_w4_gemv_workspace_size(int64_t M, int64_t N, int64_t T);

@@ -134,12 +134,13 @@ __global__ __launch_bounds__(256) void w4_dequant_kernel(const W4 w, T* out, int
 // ---- product ----------------------------------------------------------------------------------------------
 // A step is 16 rows of W by 128 columns: lane l = 16 c + r loads the 16 bytes of row r's columns 32 c .. 32 c + 31,
 // so a wave reads 1 KB with one load and every lane's codes belong to one group.  Each of the four words is
-// turned into eight bf16 numbers 16 + code (code in the upper mantissa bits of 16: a shift and an and-or for two), the
+// turned into eight bf16 numbers 2^-12 (16 + code) (code in the upper mantissa bits of 2^-8: a shift and an and-or for two), the
 // right operand of one v_mfma_f32_16x16x32_bf16; the left one holds x.  What that instruction would add up over the four
 // quarters c, different groups when group < 128, is kept apart by its 16 left rows: they are 16 / TB segments of
 // TB vectors, and the row of (segment, vector) holds x in the segment's quarters and zeros elsewhere.  TB = 4, 8,
-// 16 gives segments of 32, 64, 128 columns.  A row's total takes  s (acc - (16 + z) X),  X the sum of x over the segment
-// (the same instruction with ones on the right, once for all rows); acc and X are fp32.
+// 16 gives segments of 32, 64, 128 columns.  A row's total takes  s (acc - (16 + z) X),  X 2^-12 times the sum of x over the
+// segment (the same instruction with 2^-12 on the right, once for all rows); acc and X are fp32, and the factor, which the end takes
+// back, keeps them finite for every finite x (31 x 128 < 2^12).
 // A workgroup keeps a chunk of the columns of x in LDS, in the order of the codes (fp32: three bf16 terms, which hold
 // all of its 24 bits, as three vectors), and walks blocks of 16 rows, the next block's codes on their way while one is
 // computed; its waves share the rows and take every waves-th step of the columns.  Chunks are joined by a second
@@ -150,6 +151,7 @@ typedef float w4_f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t w4_u4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 128;             // columns of a step
+constexpr float kBack = 4096.f;        // from the sums' unit to y's
 constexpr int kXPad = 8;               // elements between rows of x in LDS
 constexpr int kXBytes = 73 << 10;      // of x in LDS: two workgroups a CU
 
@@ -169,7 +171,7 @@ constexpr int batch_steps(int nb) { return nb == 1 ? 4 : 2; }
 __device__ __forceinline__ uint32_t lo2(uint32_t u, uint32_t v) { return __builtin_amdgcn_perm(v, u, 0x05040100u); }
 __device__ __forceinline__ uint32_t hi2(uint32_t u, uint32_t v) { return __builtin_amdgcn_perm(v, u, 0x07060302u); }
 
-// Eight codes of a word as bf16 16 + code, columns 0 4 1 5 2 6 3 7; mask and base in registers, for one and-or.
+// Eight codes of a word as bf16 2^-12 (16 + code), columns 0 4 1 5 2 6 3 7; mask and base in registers, for one and-or.
 __device__ __forceinline__ w4_bf8 widen8(uint32_t c, uint32_t mask, uint32_t base) {
   const w4_u4 v = {((c << 3) & mask) | base, ((c >> 1) & mask) | base, ((c >> 5) & mask) | base, ((c >> 9) & mask) | base};
   return __builtin_bit_cast(w4_bf8, v);
@@ -319,7 +321,7 @@ __global__ __launch_bounds__(1024) void w4_gemv_kernel(const GemvArgs a) {
     live[n] = r / TB == (c * 4) / TB && v < held;
     xp[n] = live[n] ? xs + v * ld + 32 * c : zero;
   }
-  const w4_bf8 ones = __builtin_bit_cast(w4_bf8, w4_u4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+  const w4_bf8 ones = __builtin_bit_cast(w4_bf8, w4_u4{0x39803980u, 0x39803980u, 0x39803980u, 0x39803980u});  // of 2^-12
   for (int s = wave; s < steps; s += waves) {
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
@@ -336,7 +338,7 @@ __global__ __launch_bounds__(1024) void w4_gemv_kernel(const GemvArgs a) {
   }
   __syncthreads();
 
-  uint32_t mask = 0x00780078u, base = 0x41804180u;
+  uint32_t mask = 0x00780078u, base = 0x3b803b80u;
   asm volatile("" : "+s"(mask), "+v"(base));
   w4_f4 tot[NB];
 #pragma unroll
@@ -413,9 +415,9 @@ __global__ __launch_bounds__(1024) void w4_gemv_kernel(const GemvArgs a) {
       if (a.chunks > 1)
         a.part[(static_cast<int64_t>(blockIdx.y) * a.T + t0 + t) * a.w.M + row] = y;
       else if (a.y_f32)
-        static_cast<float*>(a.y)[(t0 + t) * a.ldy + row] = y;
+        static_cast<float*>(a.y)[(t0 + t) * a.ldy + row] = y * kBack;
       else
-        static_cast<uint16_t*>(a.y)[(t0 + t) * a.ldy + row] = static_cast<uint16_t>(f_bf16(y));
+        static_cast<uint16_t*>(a.y)[(t0 + t) * a.ldy + row] = static_cast<uint16_t>(f_bf16(y * kBack));
     }
     buffer ^= 1;
     batch = 0;
@@ -432,9 +434,9 @@ __global__ __launch_bounds__(256) void w4_join_kernel(const GemvArgs a) {
   for (int s = 0; s < a.chunks; ++s) y += a.part[s * n + i];
   const int64_t t = i / a.w.M, at = t * a.ldy + i - t * a.w.M;
   if (a.y_f32)
-    static_cast<float*>(a.y)[at] = y;
+    static_cast<float*>(a.y)[at] = y * kBack;
   else
-    static_cast<uint16_t*>(a.y)[at] = static_cast<uint16_t>(f_bf16(y));
+    static_cast<uint16_t*>(a.y)[at] = static_cast<uint16_t>(f_bf16(y * kBack));
 }
 
 // L lanes for rows of `units`, at least `least` of them (a power of two), and the grid for M rows.
