@@ -305,6 +305,7 @@ struct W4Plan {
   int64_t groups;    // workgroups of a chunk and pass (grid x)
 };
 W4Plan plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2);
+size_t w4_gemv_lds(const W4Plan& p, int64_t T, bool x_f32, int group_log2);  // of a workgroup
 size_t w4_gemv_ws_bytes(int64_t M, int64_t N, int64_t T);
 hipError_t launch_w4_gemv(const W4& w, int64_t T, const void* x, int64_t ldx, int x_type, void* y, int64_t ldy, int y_type,
                           void* ws, hipStream_t stream);

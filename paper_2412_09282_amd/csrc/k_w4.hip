@@ -153,7 +153,8 @@ typedef uint32_t w4_u4 __attribute__((ext_vector_type(4)));
 constexpr int kStep = 128;             // columns of a step
 constexpr float kBack = 4096.f;        // from the sums' unit to y's
 constexpr int kXPad = 8;               // elements between rows of x in LDS
-constexpr int kXBytes = 73 << 10;      // of x in LDS: two workgroups a CU
+constexpr int kStaging = 4;            // of the plan: what staging x costs a workgroup, in blocks of rows (1 and 16 measure the same)
+constexpr int kXBytes = 73 << 10;      // of x in LDS at most
 
 struct GemvArgs {
   W4 w;
@@ -166,6 +167,8 @@ struct GemvArgs {
   int s_vec;  // the scales of a step (and its zero points) can be read with one load
 };
 constexpr int batch_steps(int nb) { return nb == 1 ? 4 : 2; }
+constexpr int groups_of_step(int group_log2) { return group_log2 >= 7 ? 1 : kStep >> group_log2; }
+constexpr int sums_of(int64_t T, bool x_f32, int tb) { return tb == 4 && T == 1 && !x_f32 ? 1 : 4; }  // of a lane's four, in use
 
 // Two bf16 of x in the order of the codes' halves: (u.lo, v.lo) and (u.hi, v.hi).
 __device__ __forceinline__ uint32_t lo2(uint32_t u, uint32_t v) { return __builtin_amdgcn_perm(v, u, 0x05040100u); }
@@ -488,6 +491,15 @@ hipError_t launch_w4_dequant(const W4& w, void* out, int64_t ldo, int type, hipS
   return w.s_type == ET_F32 ? dequant_as<uint16_t, uint32_t>(w, out, ldo, stream) : dequant_as<uint16_t, uint16_t>(w, out, ldo, stream);
 }
 
+// What a workgroup holds in LDS: x and eight zeros, its sums, the scales of a batch, and the parts of y.
+size_t w4_gemv_lds(const W4Plan& p, int64_t T, bool x_f32, int group_log2) {
+  const int U = batch_steps(p.nb), held = p.per_pass * (x_f32 ? 3 : 1);
+  const size_t steps = static_cast<size_t>(p.waves) * p.batches * U;
+  return held * (steps * kStep + kXPad) * 2 + 16 + steps * p.nb * 4 * sums_of(T, x_f32, p.tb) * sizeof(float) +
+         static_cast<size_t>(p.waves) * 16 * U * groups_of_step(group_log2) * sizeof(float2) +
+         size_t{2} * p.waves * p.nb * p.tb * 16 * sizeof(float);
+}
+
 // The widest segments that stay within a group and are needed take the fewest instructions; the columns are cut where
 // x does not fit into LDS, and, where there are few rows, until the chip is filled.
 W4Plan plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2) {
@@ -517,11 +529,18 @@ W4Plan plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2)
   }
   p.batches = static_cast<int>(batches);
   p.chunks = static_cast<int>(cdiv(steps, static_cast<int64_t>(p.waves) * p.batches * U));
-  // one round of workgroups: what the CUs hold at once, by waves and by LDS
-  const int64_t lds = static_cast<int64_t>(p.per_pass) * terms * (p.waves * p.batches * U * kStep) * 2 + (12 << 10);
+  // A round of workgroups is what the CUs hold at once, by waves and by LDS; the rows are divided so that whole rounds walk
+  // them (4096 x 4096, sixteen vectors, groups of 32: 16.2 us; twice as many workgroups, half a round too many: 22.4).  Several
+  // rounds are taken where one would leave CUs idle (5120 x 13824, 300 vectors, groups of 64: 424 us, one round of 171: 755).
+  const int64_t lds = static_cast<int64_t>(w4_gemv_lds(p, T, x_f32, group_log2));
   const int64_t per_cu = std::min<int64_t>(std::max<int64_t>(1, fill_waves / 256 / p.waves), std::max<int64_t>(1, (160 << 10) / lds));
-  const int64_t fill = std::max<int64_t>(1, 256 * per_cu / (p.chunks * passes));
-  p.groups = blocks < fill ? blocks : fill;
+  const int64_t round = 256 * per_cu, each = p.chunks * passes;
+  int64_t least = INT64_MAX;
+  for (int r = 1; r <= 4; ++r) {
+    const int64_t g = std::min(blocks, std::max<int64_t>(1, r * round / each));
+    const int64_t cost = cdiv(g * each, round) * (cdiv(blocks, g) + kStaging);
+    if (cost < least) least = cost, p.groups = g;
+  }
   return p;
 }
 
@@ -541,11 +560,7 @@ size_t w4_gemv_ws_bytes(int64_t M, int64_t N, int64_t T) {
 
 template <int TB, int NB, int NR, int E>
 static hipError_t gemv_as(const W4Plan& p, const GemvArgs& a, hipStream_t stream) {
-  const int held = a.x_f32 ? 3 * p.per_pass : p.per_pass;
-  const int64_t steps = static_cast<int64_t>(p.waves) * p.batches * batch_steps(NB);
-  const size_t lds = static_cast<size_t>(held) * (steps * kStep + kXPad) * 2 + 16 + steps * NB * 4 * NR * sizeof(float) +
-                     static_cast<size_t>(p.waves) * 16 * batch_steps(NB) * E * sizeof(float2) +
-                     size_t{2} * p.waves * NB * TB * 16 * sizeof(float);
+  const size_t lds = w4_gemv_lds(p, a.T, a.x_f32, a.w.group_log2);
   const int64_t passes = cdiv(a.T, p.per_pass);
   if (passes > 65535 || p.chunks > 65535) return hipErrorInvalidConfiguration;
   const dim3 grid(static_cast<uint32_t>(p.groups), static_cast<uint32_t>(p.chunks), static_cast<uint32_t>(passes));
@@ -559,7 +574,7 @@ static hipError_t gemv_as(const W4Plan& p, const GemvArgs& a, hipStream_t stream
 template <int E>
 static hipError_t gemv_groups(const W4Plan& p, const GemvArgs& a, hipStream_t stream) {
   if (p.tb == 4) {
-    if (a.T == 1 && !a.x_f32) return gemv_as<4, 1, 1, E>(p, a, stream);  // one sum of the four in use
+    if (sums_of(a.T, a.x_f32, p.tb) == 1) return gemv_as<4, 1, 1, E>(p, a, stream);
     if (p.nb == 1) return gemv_as<4, 1, 4, E>(p, a, stream);
     if (p.nb == 2) return gemv_as<4, 2, 4, E>(p, a, stream);
     return p.nb == 3 ? gemv_as<4, 3, 4, E>(p, a, stream) : gemv_as<4, 4, 4, E>(p, a, stream);
@@ -588,7 +603,7 @@ hipError_t launch_w4_gemv(const W4& w, int64_t T, const void* x, int64_t ldx, in
   a.per_pass = p.per_pass;
   a.batches = p.batches;
   a.chunks = p.chunks;
-  const int groups = w.group_log2 >= 7 ? 1 : kStep >> w.group_log2, es = w.s_type == ET_F32 ? 4 : 2;
+  const int groups = groups_of_step(w.group_log2), es = w.s_type == ET_F32 ? 4 : 2;
   a.s_vec = reinterpret_cast<uintptr_t>(w.scales) % (groups * es) == 0 && w.ld_s % groups == 0 &&
             reinterpret_cast<uintptr_t>(w.zeros) % groups == 0 && w.ld_z % groups == 0;
   const hipError_t e = groups == 1 ? gemv_groups<1>(p, a, stream)
