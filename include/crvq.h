@@ -538,7 +538,8 @@ crvq_status crvq_w4_dequant(int64_t M, int64_t N, int32_t group, const uint8_t* 
  * (bf16 x as it is, fp32 x as the sum of three bf16 terms), sums fp32 per group and across groups in units of
  * 2^-12 (results below 2^-114 are held to multiples of 2^-137 times a scale), rounded
  * once.  Every finite x has the result of its sums; an infinite or NaN element of x[t] makes y[t] NaN.  y may not overlap x.  Deterministic.
- * Meant for few vectors: codes are read again for every 5 to 32 of them, and the workspace grows with T.
+ * Meant for few vectors: codes are read again for every 5 to 32 of them.  Many go in several launches, so that the
+ * workspace stays within 64 MiB, or what one such pass needs where that is more.
  * workspace: crvq_w4_gemv_workspace_size(M, N, T) bytes. */
 size_t crvq_w4_gemv_workspace_size(int64_t M, int64_t N, int64_t T);
 crvq_status crvq_w4_gemv(int64_t M, int64_t N, int64_t T, int32_t group, const uint8_t* codes, int64_t ld,

@@ -154,6 +154,8 @@ constexpr int kStep = 128;             // columns of a step
 constexpr float kBack = 4096.f;        // from the sums' unit to y's
 constexpr int kXPad = 8;               // elements between rows of x in LDS
 constexpr int kStaging = 4;            // of the plan: what staging x costs a workgroup, in blocks of rows (1 and 16 measure the same)
+constexpr int64_t kMostPasses = 65535;   // grid z
+constexpr int64_t kPartBytes = 64 << 20;  // of the chunks' parts: many vectors go in several launches, whose parts stay in the cache
 constexpr int kXBytes = 73 << 10;      // of x in LDS at most
 
 struct GemvArgs {
@@ -548,12 +550,21 @@ static size_t part_bytes(const W4Plan& p, int64_t M, int64_t T) {
   return p.chunks > 1 ? align256(static_cast<size_t>(p.chunks) * T * M * sizeof(float)) : 0;
 }
 
+// Vectors of one launch: whole passes whose parts fit kPartBytes, and at least one pass.
+static int64_t launch_vectors(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2) {
+  const W4Plan p = plan_w4_gemv(M, N, T, x_f32, group_log2);
+  int64_t passes = kMostPasses;
+  if (p.chunks > 1) passes = std::min(passes, kPartBytes / (p.chunks * M * static_cast<int64_t>(sizeof(float)) * p.per_pass));
+  return std::min(T, std::max<int64_t>(1, passes) * p.per_pass);
+}
+
 size_t w4_gemv_ws_bytes(int64_t M, int64_t N, int64_t T) {
   size_t most = 0;
   for (int f32 = 0; f32 < 2; ++f32)
     for (int g = 5; g <= 7; ++g) {
-      const size_t n = part_bytes(plan_w4_gemv(M, N, T, f32, g), M, T);
-      if (n > most) most = n;
+      const int64_t each = launch_vectors(M, N, T, f32, g), rest = T % each;
+      most = std::max(most, part_bytes(plan_w4_gemv(M, N, each, f32, g), M, each));
+      if (rest) most = std::max(most, part_bytes(plan_w4_gemv(M, N, rest, f32, g), M, rest));
     }
   return most;
 }
@@ -562,7 +573,7 @@ template <int TB, int NB, int NR, int E>
 static hipError_t gemv_as(const W4Plan& p, const GemvArgs& a, hipStream_t stream) {
   const size_t lds = w4_gemv_lds(p, a.T, a.x_f32, a.w.group_log2);
   const int64_t passes = cdiv(a.T, p.per_pass);
-  if (passes > 65535 || p.chunks > 65535) return hipErrorInvalidConfiguration;
+  if (p.chunks > 65535) return hipErrorInvalidConfiguration;
   const dim3 grid(static_cast<uint32_t>(p.groups), static_cast<uint32_t>(p.chunks), static_cast<uint32_t>(passes));
   if (a.w.s_type == ET_F32)
     w4_gemv_kernel<TB, NB, NR, E, uint32_t><<<grid, p.waves * 64, lds, stream>>>(a);
@@ -590,29 +601,35 @@ hipError_t launch_w4_gemv(const W4& w, int64_t T, const void* x, int64_t ldx, in
                           void* ws, hipStream_t stream) {
   GemvArgs a = {};
   a.w = w;
-  a.x = x;
-  a.y = y;
   a.ldx = ldx;
   a.ldy = ldy;
-  a.T = T;
   a.x_f32 = x_type == ET_F32;
   a.y_f32 = y_type == ET_F32;
   a.x_vec = aligned16(x, ldx, a.x_f32 ? 4 : 2);
-  const W4Plan p = plan_w4_gemv(w.M, w.N, T, a.x_f32, w.group_log2);
   a.part = static_cast<float*>(ws);
-  a.per_pass = p.per_pass;
-  a.batches = p.batches;
-  a.chunks = p.chunks;
   const int groups = groups_of_step(w.group_log2), es = w.s_type == ET_F32 ? 4 : 2;
   a.s_vec = reinterpret_cast<uintptr_t>(w.scales) % (groups * es) == 0 && w.ld_s % groups == 0 &&
             reinterpret_cast<uintptr_t>(w.zeros) % groups == 0 && w.ld_z % groups == 0;
-  const hipError_t e = groups == 1 ? gemv_groups<1>(p, a, stream)
-                       : groups == 2 ? gemv_groups<2>(p, a, stream) : gemv_groups<4>(p, a, stream);
-  if (e != hipSuccess || p.chunks == 1) return e;
-  const int64_t n = cdiv(T * w.M, 256);
-  if (n > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-  w4_join_kernel<<<dim3(static_cast<uint32_t>(n)), 256, 0, stream>>>(a);
-  return hipGetLastError();
+  const int64_t each = launch_vectors(w.M, w.N, T, a.x_f32, w.group_log2);
+  for (int64_t t = 0; t < T; t += each) {
+    a.T = std::min(each, T - t);
+    a.x = static_cast<const char*>(x) + t * ldx * (a.x_f32 ? 4 : 2);
+    a.y = static_cast<char*>(y) + t * ldy * (a.y_f32 ? 4 : 2);
+    const W4Plan p = plan_w4_gemv(w.M, w.N, a.T, a.x_f32, w.group_log2);
+    a.per_pass = p.per_pass;
+    a.batches = p.batches;
+    a.chunks = p.chunks;
+    const hipError_t e = groups == 1 ? gemv_groups<1>(p, a, stream)
+                         : groups == 2 ? gemv_groups<2>(p, a, stream) : gemv_groups<4>(p, a, stream);
+    if (e != hipSuccess) return e;
+    if (p.chunks == 1) continue;
+    const int64_t n = cdiv(a.T * w.M, 256);
+    if (n > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    w4_join_kernel<<<dim3(static_cast<uint32_t>(n)), 256, 0, stream>>>(a);
+    const hipError_t joined = hipGetLastError();
+    if (joined != hipSuccess) return joined;
+  }
+  return hipSuccess;
 }
 
 }  // namespace crvq

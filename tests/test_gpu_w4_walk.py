@@ -69,3 +69,35 @@ def test_product_over_many_blocks(M, N, T, group, zeros, sdt, xdt, batches):
     say(f"w4 product {M}x{N} x {T} group {group} {sdt} {xdt}: walk {walk}, {p.batches} batches, {p.chunks} chunks: {np.max(err / tol):.3f} of the bound")
     assert (err <= tol).all()
     assert torch.isfinite(y).all()
+
+
+@pytest.mark.parametrize("M,N,T,group,zeros,xdt", [
+    (12288, 4096, 1200, 128, False, "bf16"), (5120, 13824, 333, 64, True, "bf16"), (4100, 4096, 1025, 32, True, "f32"),
+    (28672, 8192, 130, 128, True, "bf16"), (1031, 3000, 301, 32, True, "f32"), (16, 96, 70000, 32, False, "bf16")])
+def test_product_of_a_prompt(M, N, T, group, zeros, xdt):
+    """As many vectors as a prompt has, in more than one launch where their parts are large: sampled rows and vectors, all written."""
+    g = torch.Generator(device="cuda").manual_seed(M + T)
+    G, ld = -(-N // group), -(-N // 32) * 16
+    codes = torch.randint(0, 256, (M, ld), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.rand(M, G, generator=g, device="cuda") * 0.01 + 0.001
+    zp = torch.randint(0, 16, (M, G), generator=g, device="cuda", dtype=torch.uint8) if zeros else None
+    x = torch.randn(T, N, generator=g, device="cuda").to(DT[xdt])
+    wide = torch.full((T, M + 3), float("nan"), device="cuda")
+    y = wide[:, 1:M + 1]
+    C.crvq_w4_gemv(codes, scales, group, x, y, zeros=zp)
+    torch.cuda.synchronize()
+    assert torch.isfinite(y).all() and torch.isnan(wide[:, 0]).all() and torch.isnan(wide[:, M + 1:]).all()
+    rows = torch.unique(torch.cat((torch.arange(min(M, 20)), torch.arange(max(0, M - 20), M), torch.arange(0, M, 97))))
+    at = torch.unique(torch.cat((torch.arange(T - 40, T), torch.arange(0, T, max(1, T // 200)))))
+    c = codes.cpu()[rows].numpy()
+    c = np.stack((c & 15, c >> 4), -1).reshape(len(rows), -1)[:, :N].astype(np.float64)
+    s = scales.cpu()[rows].numpy().astype(np.float64)
+    z = zp.cpu()[rows].numpy().astype(np.float64) if zeros else np.full(s.shape, 8.0)
+    each = lambda a: np.repeat(a, group, 1)[:, :N]  # noqa: E731
+    x = x[at.cuda()].float().cpu().numpy().astype(np.float64)
+    exp = x @ ((c - each(z)) * each(s)).T
+    A = np.add.reduceat(np.abs(x), np.arange(0, N, group), axis=1) @ (s * (24 + z)).T
+    err = np.abs(y.cpu()[at][:, rows].numpy().astype(np.float64) - exp)
+    tol = (N / 32 + 64) * 2.0 ** -24 * A + 2.0 ** -23 * np.abs(exp)
+    say(f"w4 product {M}x{N} x {T} group {group} {xdt}: {np.max(err / tol):.4f} of the bound")
+    assert (err <= tol).all()

@@ -43,3 +43,13 @@ def test_every_workgroup_fits(library):
                         assert 1 <= p.groups <= -(-M // 16) and 1 <= p.waves <= 16 and p.batches >= 1
                         steps = p.waves * p.batches * (4 if p.nb == 1 else 2)
                         assert p.chunks * steps * 128 >= N > (p.chunks - 1) * steps * 128
+
+
+def test_workspace_of_many_vectors():
+    """A prompt's workspace does not grow with its length."""
+    from paper_2412_09282_amd import crvq
+    size = crvq.lib().crvq_w4_gemv_workspace_size
+    for M, N in ((12288, 4096), (5120, 13824), (28672, 8192), (4096, 14336)):
+        for T in (64, 300, 1200, 2049, 8192, 100000, 3000000):
+            one_pass = max(size(M, N, t) for t in (5, 10, 16, 32))
+            assert size(M, N, T) <= max(64 << 20, one_pass), (M, N, T)
