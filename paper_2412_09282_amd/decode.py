@@ -72,6 +72,8 @@ class PagedCache:
         """Room for counts[b] more tokens of every sequence, and the batch arrays of the call that brings them."""
         if len(counts) != len(self.lengths):
             raise ValueError(f"{len(counts)} counts for {len(self.lengths)} sequences")
+        if min(counts, default=0) < 0:
+            raise ValueError("a sequence cannot bring a negative number of tokens")
         need = [max(0, -(-(n + k) // self.page) - len(p)) for n, k, p in zip(counts, self.lengths, self.pages)]
         if sum(need) > len(self.free):
             raise RuntimeError(f"the cache is full: {sum(need)} pages needed, {len(self.free)} free")
@@ -84,7 +86,8 @@ class PagedCache:
             starts.append(starts[-1] + n)
         ints = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)  # noqa: E731
         table = ints([p + [0] * (width - len(p)) for p in self.pages]).view(len(self.pages), width)
-        return Batch(table, ints(starts), ints(self.lengths), max(counts, default=0), max(self.lengths, default=0))
+        return Batch(table, ints(starts), ints(self.lengths), max(counts, default=0), max(self.lengths, default=0),
+                     starts[-1])
 
     @property
     def tensors(self):
@@ -99,6 +102,7 @@ class Batch:
     kv_len: torch.Tensor
     max_new: int
     max_kv: int
+    tokens: Optional[int] = None  # new tokens of all sequences
 
 
 def rotary_angles(n: int, rot: int, base: float = 10000.0, device="cuda"):
@@ -122,6 +126,8 @@ class AttentionBlock:
 
     def __call__(self, x: torch.Tensor, batch: Batch) -> torch.Tensor:
         """x: the new tokens' activations, T x channels, sequence after sequence."""
+        if batch.tokens is not None and x.shape[0] != batch.tokens:
+            raise ValueError(f"{x.shape[0]} rows for a batch of {batch.tokens} new tokens")
         H, K, D = self.heads, self.kv_heads, self.D
         q, k, v = (t.unflatten(1, (-1, D)) for t in self.qkv.product(x).split([H * D, K * D, K * D], 1))
         where = (*self.cache.tensors, batch.table, batch.start, batch.kv_len)
