@@ -504,7 +504,7 @@ size_t w4_gemv_lds(const W4Plan& p, int64_t T, bool x_f32, int group_log2) {
 
 // The widest segments that stay within a group and are needed take the fewest instructions; the columns are cut where
 // x does not fit into LDS, and, where there are few rows, until the chip is filled.
-W4Plan plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2) {
+static W4Plan plan_columns(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2) {
   W4Plan p;
   const int terms = x_f32 ? 3 : 1, widest = group_log2 >= 7 ? 16 : 1 << (group_log2 - 3);
   const int64_t rows = T * terms;
@@ -514,7 +514,7 @@ W4Plan plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2)
   p.nb = static_cast<int>(cdiv(static_cast<int64_t>(p.per_pass) * terms, p.tb));
   // One row of x: workgroups of 8 waves, three a CU (28672 x 8192: 32.8 us; 16 waves, one a CU: 35.7); a few rows: of 16
   // (four vectors, groups of 32: 45 us; 8: 62), several blocks: of 8, for the sums' LDS.
-  const int U = batch_steps(p.nb), most_waves = rows > 1 && p.nb == 1 ? 16 : 8, fill_waves = 256 * (rows > 1 && p.nb == 1 ? 16 : 24);
+  const int U = batch_steps(p.nb), most_waves = rows > 1 && p.nb == 1 ? 16 : 8;
   const int64_t fit = (kXBytes / 2 / (p.per_pass * terms) - kXPad) / kStep;  // steps of x in LDS: at least 8
   const int64_t steps = cdiv(N, kStep), blocks = cdiv(M, 16), passes = cdiv(T, p.per_pass);
   int64_t chunk = steps < fit ? steps : fit;
@@ -531,14 +531,21 @@ W4Plan plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2)
   }
   p.batches = static_cast<int>(batches);
   p.chunks = static_cast<int>(cdiv(steps, static_cast<int64_t>(p.waves) * p.batches * U));
+  p.groups = 0;
+  return p;
+}
+
+W4Plan plan_w4_gemv(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2) {
+  W4Plan p = plan_columns(M, N, T, x_f32, group_log2);
   // A round of workgroups is what the CUs hold at once, by waves and by LDS; the rows are divided so that whole rounds walk
   // them (4096 x 4096, sixteen vectors, groups of 32: 16.2 us; twice as many workgroups, half a round too many: 22.4).  Several
   // rounds are taken where one would leave CUs idle (5120 x 13824, 300 vectors, groups of 64: 424 us, one round of 171: 755).
   const int64_t lds = static_cast<int64_t>(w4_gemv_lds(p, T, x_f32, group_log2));
-  const int64_t per_cu = std::min<int64_t>(std::max<int64_t>(1, fill_waves / 256 / p.waves), std::max<int64_t>(1, (160 << 10) / lds));
-  const int64_t round = 256 * per_cu, each = p.chunks * passes;
+  const int waves = T * (x_f32 ? 3 : 1) > 1 && p.nb == 1 ? 16 : 24;  // of a CU
+  const int64_t per_cu = std::min<int64_t>(std::max<int64_t>(1, waves / p.waves), std::max<int64_t>(1, (160 << 10) / lds));
+  const int64_t blocks = cdiv(M, 16), round = 256 * per_cu, each = p.chunks * cdiv(T, p.per_pass);
   int64_t least = INT64_MAX;
-  for (int r = 1; r <= 4; ++r) {
+  for (int r = 1; r <= 4 && p.groups < blocks; ++r) {
     const int64_t g = std::min(blocks, std::max<int64_t>(1, r * round / each));
     const int64_t cost = cdiv(g * each, round) * (cdiv(blocks, g) + kStaging);
     if (cost < least) least = cost, p.groups = g;
@@ -550,9 +557,8 @@ static size_t part_bytes(const W4Plan& p, int64_t M, int64_t T) {
   return p.chunks > 1 ? align256(static_cast<size_t>(p.chunks) * T * M * sizeof(float)) : 0;
 }
 
-// Vectors of one launch: whole passes whose parts fit kPartBytes, and at least one pass.
-static int64_t launch_vectors(int64_t M, int64_t N, int64_t T, bool x_f32, int group_log2) {
-  const W4Plan p = plan_w4_gemv(M, N, T, x_f32, group_log2);
+// Vectors of one launch of T that are planned as p: whole passes whose parts fit kPartBytes, and at least one pass.
+static int64_t launch_vectors(const W4Plan& p, int64_t M, int64_t T) {
   int64_t passes = kMostPasses;
   if (p.chunks > 1) passes = std::min(passes, kPartBytes / (p.chunks * M * static_cast<int64_t>(sizeof(float)) * p.per_pass));
   return std::min(T, std::max<int64_t>(1, passes) * p.per_pass);
@@ -562,9 +568,11 @@ size_t w4_gemv_ws_bytes(int64_t M, int64_t N, int64_t T) {
   size_t most = 0;
   for (int f32 = 0; f32 < 2; ++f32)
     for (int g = 5; g <= 7; ++g) {
-      const int64_t each = launch_vectors(M, N, T, f32, g), rest = T % each;
-      most = std::max(most, part_bytes(plan_w4_gemv(M, N, each, f32, g), M, each));
-      if (rest) most = std::max(most, part_bytes(plan_w4_gemv(M, N, rest, f32, g), M, rest));
+      W4Plan p = plan_columns(M, N, T, f32, g);
+      const int64_t each = launch_vectors(p, M, T), rest = T % each;
+      if (each < T) p = plan_columns(M, N, each, f32, g);
+      most = std::max(most, part_bytes(p, M, each));
+      if (rest) most = std::max(most, part_bytes(plan_columns(M, N, rest, f32, g), M, rest));
     }
   return most;
 }
@@ -610,12 +618,13 @@ hipError_t launch_w4_gemv(const W4& w, int64_t T, const void* x, int64_t ldx, in
   const int groups = groups_of_step(w.group_log2), es = w.s_type == ET_F32 ? 4 : 2;
   a.s_vec = reinterpret_cast<uintptr_t>(w.scales) % (groups * es) == 0 && w.ld_s % groups == 0 &&
             reinterpret_cast<uintptr_t>(w.zeros) % groups == 0 && w.ld_z % groups == 0;
-  const int64_t each = launch_vectors(w.M, w.N, T, a.x_f32, w.group_log2);
+  W4Plan p = plan_w4_gemv(w.M, w.N, T, a.x_f32, w.group_log2);
+  const int64_t each = launch_vectors(p, w.M, T);
   for (int64_t t = 0; t < T; t += each) {
     a.T = std::min(each, T - t);
     a.x = static_cast<const char*>(x) + t * ldx * (a.x_f32 ? 4 : 2);
     a.y = static_cast<char*>(y) + t * ldy * (a.y_f32 ? 4 : 2);
-    const W4Plan p = plan_w4_gemv(w.M, w.N, a.T, a.x_f32, w.group_log2);
+    if (a.T < T) p = plan_w4_gemv(w.M, w.N, a.T, a.x_f32, w.group_log2);
     a.per_pass = p.per_pass;
     a.batches = p.batches;
     a.chunks = p.chunks;
