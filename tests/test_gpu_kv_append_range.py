@@ -1,4 +1,4 @@
-"""GPU append to the paged 8-bit cache: angle tables without rows."""
+"""GPU append to the paged 8-bit cache at the ends of its range: angle tables without rows, caches past 4 GiB."""
 import pytest
 import torch
 
@@ -32,3 +32,35 @@ def test_angle_table_without_rows(dtype, rot, interleaved):
     with pytest.raises(ValueError):
         C.crvq_kv_append(k, v, kc, vc, ks, vs, table.view(1, 1), start, kv_len, n, cos=empty, sin=empty)
     C.crvq_kv_append(k[:0], v[:0], kc, vc, ks, vs, table.view(1, 1), start * 0, kv_len * 0, 0, cos=empty, sin=empty)
+
+
+@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_cache_past_4_gib(dtype, new):
+    """Pages whose offsets pass 32 bits give what the same pages give in a small cache, bit for bit: append, read and attention."""
+    say(f"cache past 4 GiB, {new} new tokens, {dtype}")
+    Hq, Hkv, D, page, kv = 8, 2, 128, 256, 700
+    here, far = [0, 1, 2], [40001, 65540, 32769]  # 64 KiB a page in each array
+    n_pages = max(far) + 1
+    assert n_pages * Hkv * page * D > 2 ** 32
+    g = torch.Generator(device="cuda").manual_seed(new)
+    codes = lambda *s: torch.randint(-127, 128, s, generator=g, device="cuda", dtype=torch.int8)  # noqa: E731
+    small = [codes(3, Hkv, page, D), codes(3, Hkv, D, page), torch.rand(3, Hkv, generator=g, device="cuda") / 32,
+             torch.rand(3, Hkv, generator=g, device="cuda") / 32]
+    large = [torch.empty((n_pages, *t.shape[1:]), dtype=t.dtype, device="cuda") for t in small]
+    for s, t in zip(small, large):
+        t[far] = s
+    k, v, q = [torch.randn(new, h, D, generator=g, device="cuda").to(dtype) for h in (Hkv, Hkv, Hq)]
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    start, kv_len, every = ints(0, new), ints(kv), ints(0, kv)
+    got = []
+    for cache, pages in ((small, here), (large, far)):
+        table = ints(pages)
+        C.crvq_kv_append(k, v, *cache, table, start, kv_len, new)
+        out, lse = torch.empty_like(q), torch.empty(new, Hq, device="cuda")
+        C.crvq_kv_attention(q, out, *cache, table, start, kv_len, new, kv, lse=lse)
+        ko, vo = torch.empty(kv, Hkv, D, dtype=dtype, device="cuda"), torch.empty(kv, Hkv, D, dtype=dtype, device="cuda")
+        C.crvq_kv_read(ko, vo, *cache, table, every, kv_len, kv)
+        got.append([out, lse, ko, vo] + [t[pages] for t in cache])
+    for x, y in zip(*got):
+        assert torch.isfinite(x.float()).all() and torch.equal(x, y)
