@@ -8,8 +8,8 @@
 //   O^T += V^T P^T on v_mfma_f32_16x16x32_f16: the value codes lie transposed in the cache, 16 tokens of an
 //     element in 16 bytes, and are widened to fp16 in registers (exact); the weights are rounded to fp16, once where every
 //     wave has columns of its own (11 bits), else to two terms (22 bits).  Decoding steps wait for memory and take the second
-//     term at no cost (32 sequences of up to 4096 tokens 138 us with it and without, heads of 256 elements 69 for 65); prompts
-//     are bound by these instructions (two of them, 596 us for 384), and their error against 64 bits is that of
+//     term at no cost (one run: 32 sequences of up to 4096 tokens 138 us with it and without, heads of 256 elements 69 for 65);
+//     prompts are bound by these instructions (with two 596 us for 384), and their error against 64 bits is that of
 //     rounding the output to bf16 with either (1.67e-3 and 1.66e-3).  The page's
 //     value scale goes into the weights, relative to a power of two 2^e of each column that follows the largest of its weights
 //     times scale: scales of any size then add up as in fp32, and a page that a column does not see does not matter to it.
@@ -118,7 +118,7 @@ __device__ __forceinline__ float elem(const T* p, int i) {
 // multiple of eight of them a chip's die reads few heads; the tiles of a sequence go last to first, so that the longest
 // rows of a causal prompt start first; sequences come one after the other: the workgroups that a short one has no work for
 // are then a run (as every second one they left half of the CUs idle: 556 against 404 us for two prompts of 2048
-// and about 300).
+// and about 300, when that was changed).
 struct Place {
   int hk, b, split, tile;
 };
@@ -135,7 +135,7 @@ __device__ __forceinline__ Place place_of(const AttnArgs& a) {
 }
 
 // The sequence that is `rank`-th by the mean length of its rows, len - n / 2, longest first, so that a call does not end
-// with long rows on few CUs (two prompts, 2048 rows over 4000 tokens and 393 over 3469: 381 us, in their own order 408).
+// with long rows on few CUs (one run: two prompts, 2048 rows over 4000 tokens and 393 over 3469: 392 us, in their own order 424).
 // Up to 64 sequences, a lane each; more keep their order.
 __device__ __forceinline__ int ranked(const KvBatch& bt, int rank) {
   if (bt.B > 64 || bt.B == 1) return rank;
@@ -572,8 +572,8 @@ __device__ __forceinline__ void share_of(const AttnArgs& a, int split, int round
 
 // Few columns: the four waves of a workgroup share 16 and take turns at the tokens; the cache is read once, from
 // memory into the operands' registers, a step's keys while the step before is computed.  Reads bound it: 32 sequences
-// of 2048 to 4096 tokens (682 MB) take 139 us, 4.9 TB/s, the rate of a device copy; one sequence of 131001 tokens in 64
-// shares of 8 heads 64 us (4.2 TB/s; 8 us of it the join).
+// of 2048 to 4096 tokens (682 MB) take 133 us, 5.1 TB/s (a device copy, which writes as much as it reads, moves 4.9); one
+// sequence of 131001 tokens (268 MB) in 64 shares of 8 heads 62.5 us, 4.3 TB/s, 8 us of it the join.
 template <typename T, int DT, bool SMALL>
 __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel(const AttnArgs a) {
   constexpr int kRow = DT * 16 + 4, kStride = 4 * kTokens;
@@ -672,10 +672,12 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel
 // Many columns: every wave has 16 QB of its own, and the four of a workgroup walk the same tokens.  A step's keys
 // and values pass through LDS, two steps of them, widened once for all four waves (keys of fp32 queries as they are).  Rows of
 // LDS are padded by 16 bytes, and a key's row is u * 16 + r for the token that is row r of tile u, so that the 16 rows
-// an instruction reads lie in different banks.  4096 tokens over 8192 take
-// 1.33 ms without a mask (830 TFLOP/s, of 1360 that a large library product of bf16 reaches); what is left is mostly
-// dependences that two waves a SIMD do not hide (without the exponentials 1.28 ms, with one wave a SIMD 1.95).  Smaller
-// calls lose at their end, when the last workgroups run alone: two prompts of 2048 and 393, 381 us (635 TFLOP/s).
+// an instruction reads lie in different banks.  4096 tokens over 8192, 64 heads over 8, take
+// 1.36 ms without a mask (810 TFLOP/s, of 1360 that a large library product of bf16 reaches).  A wave reads a step's keys and
+// values, 32 KB, for 32 columns: 128 KB a workgroup and step, as many cycles of LDS as the products take of the matrix cores, and
+// in one wave they come one after the other, as do scores, weights and values.  Two waves a SIMD hide a part of that (one: 1.95 for
+// 1.33 ms, when that was measured).  Smaller calls lose at their end, when the last workgroups run alone: two prompts of 2048 and
+// 393, 337 us (718 TFLOP/s; 345 to 392 with the calls in a graph, from one card to another).
 template <typename T, int DT, int QB, bool SMALL>
 __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kernel(const AttnArgs a) {
   constexpr bool HALF = sizeof(T) == 2;

@@ -6,8 +6,9 @@
 // (those of long pages past the first kKept chunks of a thread are read again).  Values are stored transposed: the
 // new tokens go through an LDS tile and leave as 16-byte runs of slots, a few of them as bytes.  The same launch
 // rotates the queries, a workgroup a row.  Memory bounds prompts (three of up to 2048 tokens, 64 query and 8 key heads:
-// 56 us for 250 MB, 4.5 TB/s), the chain of reads (lengths, page, elements, older codes) a decoding step: 10 us for 32
-// sequences of 32 heads.  Reading back, 25 MB in 10 us, is such a chain too.
+// 47 us for 196 MB, 4.2 TB/s).  A decoding step, 9.8 us for the 1.2 MB of 32 sequences of 32 heads, is latency: a workgroup
+// looks up lengths, page and scale before it reads one token's 128 elements, for which 16 of its 256 threads have work.  So is
+// reading back, 25 MB in 10.6 us (2.3 TB/s): look-ups, one read and one store a thread.
 #include "kv_common.h"
 
 namespace crvq {
