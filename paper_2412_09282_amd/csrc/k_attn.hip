@@ -41,6 +41,7 @@ constexpr int kTokens = 64;     // tokens of a step
 constexpr float kSlack = 8.f;
 constexpr int kLift = 7;
 constexpr int kFaint = -64;    // pages whose scales are this far below 2^e: the softmax's sum is taken of weights of its own
+constexpr float kFar = 0x1p23f;  // maxima from here on are whole numbers or coarser
 constexpr int kNothing = -1024;  // exponent of a value scale of 0
 
 struct AttnArgs {
@@ -162,6 +163,7 @@ struct Columns {
   float step[QB], m[QB], l[QB];
   int e[QB];                          // exponents that value scales are taken relative to
   int lo[QB], hi[QB];                 // the tokens a column sees
+  float slack;                        // kSlack; once a maximum has passed kFar, so low that every step renews it
   int first, last, all_lo, all_hi;    // the tokens any of them sees, and those that all of them see
   at_f4 o[QB][DT];                    // in units of 2^(m + e - kLift)
 
@@ -225,6 +227,7 @@ struct Columns {
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[n][d] = at_f4{0.f, 0.f, 0.f, 0.f};
     }
+    slack = kSlack;
     first = 0x7fffffff, last = 0, all_lo = 0, all_hi = 0x7fffffff;
 #pragma unroll
     for (int n = 0; n < QB; ++n) {
@@ -306,24 +309,33 @@ struct Columns {
     }
 #pragma unroll
     for (int n = 0; n < QB; ++n) {
-      const float alpha = good ? step[n] * ks : __uint_as_float(0x7fc00000u);
+      float alpha = good ? step[n] * ks : __uint_as_float(0x7fc00000u);
       float top = fmaxf(fmaxf(s[n][0][0], s[n][0][1]), s[n][0][2]);
 #pragma unroll
       for (int j = 3; j < 16; ++j) top = fmaxf(top, s[n][j >> 2][j & 3]);
       top *= alpha;  // -infinity where the column sees none of them, or (alpha 0) NaN, which no comparison and no maximum takes
-      if (__any(top > m[n] + (kSlack - static_cast<float>(max(ve - e[n], 0))))) {
+      float from = m[n];
+      if (__any(top > m[n] + (slack - static_cast<float>(max(ve - e[n], 0))))) {
         asm volatile("; a branch, not selections");
         const float now = fmaxf(m[n], quarters_max(top));
-        const float reach = quarters_max(top + static_cast<float>(ve));  // with the value scales
-        const float ever = m[n] > -kInf ? fmaxf(m[n] + static_cast<float>(e[n]), reach) : reach;
-        const int at = now > -kInf && ever > -kInf ? static_cast<int>(rintf(ever - now)) : 0;
         const float fall = m[n] > -kInf ? m[n] - now : -kInf;
+        // the largest with its value scale, relative to `now` before exponents are added: scores may be past 2^24
+        const float reach = fmaxf(fall + static_cast<float>(e[n]), quarters_max((top - now) + static_cast<float>(ve)));
+        const int at = now > -kInf && reach > -kInf ? static_cast<int>(rintf(reach)) : 0;
         l[n] *= __builtin_amdgcn_exp2f(fall);
         const float keep = __builtin_amdgcn_exp2f(fall + static_cast<float>(e[n] - at));
         m[n] = now;
         e[n] = at;
+        if (__any(now > -kInf && fabsf(now) >= kFar)) slack = -3e38f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[n][d] *= keep;
+        from = now;
+        if (slack < 0.f) {  // scores are rounded before the maximum is taken off, as it is: fused they would differ by 1 and more
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s[n][j >> 2][j & 3] = s[n][j >> 2][j & 3] * alpha - now;
+          alpha = 1.f;
+          from = 0.f;
+        }
       }
       const int rel = ve - e[n];
       undo[n] = ldexpf(unlift, -rel);
@@ -332,12 +344,12 @@ struct Columns {
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-          if (whole || (seen[n] >> j & 1)) sum += __builtin_amdgcn_exp2f(fmaf(s[n][j >> 2][j & 3], alpha, -m[n]));
+          if (whole || (seen[n] >> j & 1)) sum += __builtin_amdgcn_exp2f(fmaf(s[n][j >> 2][j & 3], alpha, -from));
         l[n] += sum;
         undo[n] = 0.f;
       }
       // weights p 2^.. = exp2(score - m) times the scale's factor, as exp2 of one fused multiply-add
-      const float shift = (lift_log + static_cast<float>(rel)) - m[n];
+      const float shift = (lift_log + static_cast<float>(rel)) - from;
 #pragma unroll
       for (int j = 0; j < 16; ++j)
         s[n][j >> 2][j & 3] = __builtin_amdgcn_exp2f(fmaf(s[n][j >> 2][j & 3], alpha, shift));

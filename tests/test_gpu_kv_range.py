@@ -188,3 +188,26 @@ def test_value_scales_of_zero(dtype, new):
         scores = [300.0 if s < 1 else 0.1 for s in scales]
         cache, table, q = paged(g, 64, 8, 2, 64, 8, dtype, new, scores, scales)
         check(cache, table, [new], [512], q, 64 ** -0.5, dtype, causal=False, what=f"value scales {scales[:4]},")
+
+
+@pytest.mark.parametrize("value_log", [-40, 0, 40])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_past_2_24(dtype, new, value_log):
+    """Scores so large that an exponent added to them is lost in their rounding.  All keys are the same, so the weights are equal
+    whatever a score's rounding is, and an output is the mean of the values, up to the weights' own bits and n sums in fp32."""
+    g = np.random.default_rng(new)
+    D, Hq, Hkv, page, n = 64, 8, 2, 64, 300
+    cache = random_cache(g, 5, Hkv, D, page)
+    cache[0][:] = 100
+    cache[2][:], cache[3][:] = 2.0 ** 10, 2.0 ** value_log
+    table = np.array([[3, 0, 4, 1, 2]], np.int32)
+    q = np.full((new, Hq, D), 2.0 ** 12, np.float32)
+    start, kv_len = np.array([0, new], np.int32), np.array([n], np.int32)
+    out = torch.full((new, Hq, D), 7.0, device="cuda").to(DT[dtype])
+    C.crvq_kv_attention(dev(q, dtype), out, *[dev(a) for a in cache], dev(table), dev(start), dev(kv_len), new, n, causal=False)
+    V = cache[1][table[0]].astype(np.float64).transpose(1, 0, 3, 2).reshape(Hkv, -1, D)[:, :n] * 2.0 ** value_log
+    exp, size = np.repeat(V.mean(1), Hq // Hkv, 0)[None], np.repeat(np.abs(V).mean(1), Hq // Hkv, 0)[None]
+    rounding, weight = (2.0 ** -8, 2.0 ** -11) if dtype == "bf16" else (2.0 ** -23, 2.0 ** -23)
+    err = np.abs(out.double().cpu().numpy() - exp)
+    assert (err <= rounding * np.abs(exp) + (weight + n * 2.0 ** -24) * size).all()
