@@ -83,7 +83,8 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* W, int64_t ld
     hi = fmaxf(hi, __shfl_xor(hi, o));
   }
   if (!in) return;
-  float s = fmaxf(w.zeros ? (hi - lo) / 15.f : fmaxf(hi, -lo) / 7.f, kMinScale);
+  // (hi - lo) / 15 as half of each, which rounds the same and stays within fp32's range
+  float s = fmaxf(w.zeros ? (0.5f * hi - 0.5f * lo) / 7.5f : fmaxf(hi, -lo) / 7.f, kMinScale);
   if (!(s < __uint_as_float(0x7f800000u))) s = __uint_as_float(0x7fc00000u);
   if (sizeof(TS) == 2) s = bf16_f(f_bf16(s));
   const bool number = s == s;

@@ -41,3 +41,25 @@ def test_product_at_the_ends_of_the_range(T, group, xdt, low, high):
     err = np.abs(got - exp)
     say(f"w4 product of 2^{low} to 2^{high}, {T} x {group} {xdt}: {np.max(err / tol):.3g} of the bound")
     assert np.isfinite(got).all() and (err <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_quantize_weights_whose_spread_passes_fp32(dtype):
+    """Finite weights from -3e38 to 3e38: 15 steps of 4e37 around a zero point, each weight within half a step and a rounding of it."""
+    say(f"w4 quantize: a spread past fp32's range, {dtype}")
+    W = (torch.linspace(-1, 1, 64, device="cuda") * 3e38).to(dtype).repeat(3, 1)
+    W[1] = 0
+    W[2] *= 0.4                                          # 2.4e38 wide: within the range
+    codes = torch.zeros(3, 32, dtype=torch.uint8, device="cuda")
+    s, z = torch.zeros(3, 2, device="cuda"), torch.zeros(3, 2, dtype=torch.uint8, device="cuda")
+    C.crvq_w4_quantize(W, codes, s, 32, zeros=z)
+    s64 = torch.zeros(3, 1, device="cuda")
+    z64 = torch.zeros(3, 1, dtype=torch.uint8, device="cuda")
+    C.crvq_w4_quantize(W, codes, s64, 64, zeros=z64)
+    out = torch.empty(3, 64, device="cuda")
+    C.crvq_w4_dequant(codes, s64, 64, out, zeros=z64)
+    w = W.double()
+    spread = (w.clamp(min=0).amax(1) - w.clamp(max=0).amin(1)).clamp(min=15 * 2.0 ** -100)
+    assert ((s64[:, 0].double() - spread / 15).abs() <= 2.0 ** -23 * spread / 15).all()
+    step = s64.double()
+    assert torch.isfinite(s).all() and ((out.double() - w).abs() <= step * (1 + 2.0 ** -20)).all()
