@@ -294,6 +294,7 @@ struct Columns {
     const float lift_log = __builtin_amdgcn_logf(lift), unlift = __builtin_amdgcn_rcpf(lift);
     const bool whole = t0 >= all_lo && t0 + kTokens <= all_hi;
     uint32_t seen[QB];  // which of the lane's 16 tokens its column sees
+    float by[QB], shift[QB];  // a weight, with its value scale, is exp2(score by + shift)
     float undo[QB];     // from the sum of the weights that enter the second product to that of the softmax
     if (!whole) {
       asm volatile("; a branch, not selections");
@@ -309,13 +310,13 @@ struct Columns {
     }
 #pragma unroll
     for (int n = 0; n < QB; ++n) {
-      float alpha = good ? step[n] * ks : __uint_as_float(0x7fc00000u);
+      by[n] = good ? step[n] * ks : __uint_as_float(0x7fc00000u);
       float top = fmaxf(fmaxf(s[n][0][0], s[n][0][1]), s[n][0][2]);
 #pragma unroll
       for (int j = 3; j < 16; ++j) top = fmaxf(top, s[n][j >> 2][j & 3]);
-      top *= alpha;  // -infinity where the column sees none of them, or (alpha 0) NaN, which no comparison and no maximum takes
+      top *= by[n];  // -infinity where the column sees none of them, or (alpha 0) NaN, which no comparison and no maximum takes
       float from = m[n];
-      if (__any(top > m[n] + (slack - static_cast<float>(max(ve - e[n], 0))))) {
+      if (__builtin_expect(__any(top > m[n] + (slack - static_cast<float>(max(ve - e[n], 0)))), 0)) {
         asm volatile("; a branch, not selections");
         const float now = fmaxf(m[n], quarters_max(top));
         const float fall = m[n] > -kInf ? m[n] - now : -kInf;
@@ -330,30 +331,32 @@ struct Columns {
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[n][d] *= keep;
         from = now;
-        if (slack < 0.f) {  // scores are rounded before the maximum is taken off, as it is: fused they would differ by 1 and more
+        if (__builtin_expect(slack < 0.f, 0)) {  // scores are rounded before the maximum is taken off, as it is: fused they would differ by 1 and more
 #pragma unroll
-          for (int j = 0; j < 16; ++j) s[n][j >> 2][j & 3] = s[n][j >> 2][j & 3] * alpha - now;
-          alpha = 1.f;
+          for (int j = 0; j < 16; ++j) s[n][j >> 2][j & 3] = s[n][j >> 2][j & 3] * by[n] - now;
+          by[n] = 1.f;
           from = 0.f;
         }
       }
       const int rel = ve - e[n];
       undo[n] = ldexpf(unlift, -rel);
-      if (__any(rel < kFaint)) {  // their products with the value scale may vanish where they themselves do not
+      if (__builtin_expect(__any(rel < kFaint), 0)) {  // their products with the value scale may vanish where they themselves do not
         asm volatile("; a branch, not selections");
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-          if (whole || (seen[n] >> j & 1)) sum += __builtin_amdgcn_exp2f(fmaf(s[n][j >> 2][j & 3], alpha, -from));
+          if (whole || (seen[n] >> j & 1)) sum += __builtin_amdgcn_exp2f(fmaf(s[n][j >> 2][j & 3], by[n], -from));
         l[n] += sum;
         undo[n] = 0.f;
       }
       // weights p 2^.. = exp2(score - m) times the scale's factor, as exp2 of one fused multiply-add
-      const float shift = (lift_log + static_cast<float>(rel)) - from;
+      shift[n] = (lift_log + static_cast<float>(rel)) - from;
+    }
+#pragma unroll
+    for (int n = 0; n < QB; ++n)
 #pragma unroll
       for (int j = 0; j < 16; ++j)
-        s[n][j >> 2][j & 3] = __builtin_amdgcn_exp2f(fmaf(s[n][j >> 2][j & 3], alpha, shift));
-    }
+        s[n][j >> 2][j & 3] = __builtin_amdgcn_exp2f(fmaf(s[n][j >> 2][j & 3], by[n], shift[n]));
     if (!whole) {
       asm volatile("; a branch, not selections");
 #pragma unroll
