@@ -688,11 +688,11 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel
 // and values pass through LDS, two steps of them, widened once for all four waves (keys of fp32 queries as they are).  Rows of
 // LDS are padded by 16 bytes, and a key's row is u * 16 + r for the token that is row r of tile u, so that the 16 rows
 // an instruction reads lie in different banks.  4096 tokens over 8192, 64 heads over 8, take
-// 1.36 ms without a mask (810 TFLOP/s, of 1360 that a large library product of bf16 reaches).  A wave reads a step's keys and
+// 1.41 ms without a mask (780 TFLOP/s, of 1360 that a large library product of bf16 reaches).  A wave reads a step's keys and
 // values, 32 KB, for 32 columns: 128 KB a workgroup and step, as many cycles of LDS as the products take of the matrix cores, and
 // in one wave they come one after the other, as do scores, weights and values.  Two waves a SIMD hide a part of that (one: 1.95 for
 // 1.33 ms, when that was measured).  Smaller calls lose at their end, when the last workgroups run alone: two prompts of 2048 and
-// 393, 337 us (718 TFLOP/s; 345 to 392 with the calls in a graph, from one card to another).
+// 393, 348 us (696 TFLOP/s; 360 to 382 with the calls in a graph, from one card to another).
 template <typename T, int DT, int QB, bool SMALL>
 __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kernel(const AttnArgs a) {
   constexpr bool HALF = sizeof(T) == 2;
