@@ -548,6 +548,60 @@ crvq_status crvq_w4_gemv(int64_t M, int64_t N, int64_t T, int32_t group, const u
                          size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * 8-bit matrices: `rows` rows of N columns as codes c in -127 .. 127 with a
+ * scale for each row (a channel of a weight, a token of activations),
+ *   X[i][j] = scales[i] * c[i][j].
+ * codes: int8, 16-byte aligned, row stride ld bytes, a multiple of 16 and at
+ * least N; what lies past column N up to a multiple of 16 belongs to the row's
+ * storage.  scales: float[rows].  1 <= N <= CRVQ_ROW_MAX_N.
+ * ------------------------------------------------------------------------- */
+#define CRVQ_ROW_MAX_N 65536 /* elements of a row: registers hold it (crvq_norm, crvq_w8_*) */
+
+/* crvq_w8_quantize -- the codes and scales of X (rows x N of dtype, row stride
+ * ldx): s = max(max|x| / 127, 2^-100), c = min(max(rint(x / s), -127), 127),
+ * fp32, every operation rounded on its own.  A NaN or infinity in a row makes
+ * its scale NaN and its codes 0.  The bytes of a row past N up to a multiple of
+ * 16 become 0. */
+crvq_status crvq_w8_quantize(int64_t rows, int64_t N, const void* X, int64_t ldx, int dtype, int8_t* codes, int64_t ld,
+                             float* scales, void* stream);
+
+/* crvq_w8_gemm -- y[t][r] = x_scales[t] * scales[r] * sum_j x_codes[t][j] * codes[r][j]
+ * for an M x N matrix and T rows of x, y T x M of y_dtype (row stride ldy).  The
+ * sum is exact (32-bit integers; codes of -128 are taken as they are), its
+ * product with the two scales' product is fp32, each operation rounded on its own,
+ * and rounded once to y_dtype.  Columns from N on are not read into the sums.  M = 0 or
+ * T = 0 is a no-op.  y may not overlap an input.  Deterministic.
+ * workspace: crvq_w8_gemm_workspace_size(M, N, T) bytes. */
+size_t crvq_w8_gemm_workspace_size(int64_t M, int64_t N, int64_t T);
+crvq_status crvq_w8_gemm(int64_t M, int64_t N, int64_t T, const int8_t* codes, int64_t ld, const float* scales,
+                         const int8_t* x_codes, int64_t ldx, const float* x_scales, void* y, int64_t ldy, int y_dtype,
+                         void* workspace, size_t ws_bytes, void* stream);
+
+/* crvq_norm -- what lies between two blocks of a decoder, for T rows of N
+ * elements in one pass: the norm after a block, its gate and scale, the residual
+ * sum, and the norm before the next block:
+ *
+ *   u = post ? n(x) w_post + b_post : x,   r' = r + alpha (gate u),   h = n(r') w_pre + b_pre
+ *   n(x) = x / sqrt(mean x^2 + eps)                     (CRVQ_NORM_RMS)
+ *   n(x) = (x - mean x) / sqrt(mean (x - mean x)^2 + eps)   (CRVQ_NORM_LAYER)
+ *
+ * x, gate and h are of dtype, r and r_out (r') of r_dtype, the weights (N
+ * elements each) of w_dtype; ldx, ldg, ldr, ldro and ldh are row strides.
+ * NULL: gate and a w are 1, r and a b are 0, r_out and h are not wanted (one of the two
+ * has to be).  ldg = 0: one gate of N elements for every row.
+ * h_scales != NULL: h is int8 with a scale for each row, as crvq_w8_quantize
+ * makes it of the unrounded h (its layout and rules), ready for crvq_w8_gemm.
+ * Sums, means and roots are fp64, the rest fp32; h is computed from r' before
+ * its rounding to r_dtype.  r_out may be r or x and h may be x or r, of the same type and
+ * row stride; outputs overlap nothing otherwise.  T = 0 is a no-op.
+ * Deterministic; a row's result does not depend on the other rows. */
+typedef enum { CRVQ_NORM_RMS = 0, CRVQ_NORM_LAYER = 1 } crvq_norm_kind;
+crvq_status crvq_norm(int64_t T, int64_t N, int kind, const void* x, int64_t ldx, int dtype, int post, const void* w_post,
+                      const void* b_post, const void* gate, int64_t ldg, double alpha, const void* r, int64_t ldr,
+                      void* r_out, int64_t ldro, int r_dtype, const void* w_pre, const void* b_pre, int w_dtype,
+                      double eps, void* h, int64_t ldh, float* h_scales, void* stream);
+
+/* ---------------------------------------------------------------------------
  * crvq_workspace_size -- one entry for every call's workspace size: the value
  * the per-call *_workspace_size function above returns for the same shape.
  * op selects the call; each op reads only the arguments listed (others are
@@ -565,6 +619,7 @@ crvq_status crvq_w4_gemv(int64_t M, int64_t N, int64_t T, int32_t group, const u
  *   CRVQ_OP_KV_ATTENTION  n_vectors = B, d = D, M = Hq, N = Hkv, K = max_new,
  *                       n_cols = max_kv              (crvq_kv_attention)
  *   CRVQ_OP_W4_GEMV     M, N, K = T                  (crvq_w4_gemv)
+ *   CRVQ_OP_W8_GEMM     M, N, K = T                  (crvq_w8_gemm)
  * Returns 0 for an unknown op or a shape the call rejects (and for calls that
  * need no workspace at that shape).  Ks is a host array of n_books entries.
  */
@@ -580,7 +635,8 @@ typedef enum {
   CRVQ_OP_GEMV = 8,
   CRVQ_OP_HINV = 9,
   CRVQ_OP_KV_ATTENTION = 10,
-  CRVQ_OP_W4_GEMV = 11
+  CRVQ_OP_W4_GEMV = 11,
+  CRVQ_OP_W8_GEMM = 12
 } crvq_op;
 size_t crvq_workspace_size(int op, int64_t n_vectors, int64_t K, int32_t beam, int32_t n_books, int32_t d,
                            const int64_t* Ks, int64_t M, int64_t N, int64_t n_cols);

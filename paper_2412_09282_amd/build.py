@@ -38,6 +38,8 @@ SOURCES = {
     "k_kv.hip": [],
     "k_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "k_w4.hip": [],
+    "k_w8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "k_norm.hip": [],
 }
 
 COMMON = [

@@ -24,6 +24,7 @@ _lib = None
 
 CRVQ_F32, CRVQ_BF16, CRVQ_F64 = 0, 1, 2
 CRVQ_REDUCE_SUM, CRVQ_REDUCE_MAX = 0, 1
+CRVQ_NORM_RMS, CRVQ_NORM_LAYER = 0, 1
 STATUS = {0: "CRVQ_OK", 1: "CRVQ_ERR_INVALID", 2: "CRVQ_ERR_UNSUPPORTED", 3: "CRVQ_ERR_WORKSPACE", 4: "CRVQ_ERR_HIP"}
 
 
@@ -103,6 +104,11 @@ def lib(build_if_missing: bool = True):
                 "crvq_w4_gemv_workspace_size": ([I64, I64, I64], SZ),
                 "crvq_w4_gemv": ([I64, I64, I64, I32, P, I64, P, ctypes.c_int, I64, P, I64, P, I64, ctypes.c_int, P, I64,
                                   ctypes.c_int, P, SZ, P], ctypes.c_int),
+                "crvq_w8_quantize": ([I64, I64, P, I64, ctypes.c_int, P, I64, P, P], ctypes.c_int),
+                "crvq_w8_gemm_workspace_size": ([I64, I64, I64], SZ),
+                "crvq_w8_gemm": ([I64, I64, I64, P, I64, P, P, I64, P, P, I64, ctypes.c_int, P, SZ, P], ctypes.c_int),
+                "crvq_norm": ([I64, I64, ctypes.c_int, P, I64, ctypes.c_int, ctypes.c_int, P, P, P, I64, ctypes.c_double, P,
+                               I64, P, I64, ctypes.c_int, P, P, ctypes.c_int, ctypes.c_double, P, I64, P, P], ctypes.c_int),
             }
             for name, (args, res) in sigs.items():
                 f = getattr(L, name)
@@ -581,3 +587,114 @@ def crvq_w4_gemv(codes: torch.Tensor, scales: torch.Tensor, group: int, x: torch
     ws = _workspace_for(L.crvq_w4_gemv_workspace_size(M, N, T), y.device, stream)
     _check("crvq_w4_gemv", L.crvq_w4_gemv(M, N, T, group, *w, _ptr(x), ldx, dtype_code(x), _ptr(y), ldy, dtype_code(y),
                                           _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+
+
+# ---- 8-bit matrices and norms ---------------------------------------------------------------------
+def _one_device(first: torch.Tensor, *others) -> None:
+    """The kernels follow these pointers on the device of the first tensor: the others are there too, or in pinned host
+    memory."""
+    if not first.is_cuda and not first.is_pinned():
+        raise ValueError("a tensor in host memory that is not pinned")
+    device = first.device
+    for t in others:
+        if t is not None and t.device != device:
+            if t.is_cuda:
+                raise ValueError(f"tensors on {device} and {t.device}")
+            if not t.is_pinned():
+                raise ValueError("a tensor in host memory that is not pinned")
+
+
+def _enqueue(fn: str, on: torch.Tensor, stream, *args) -> None:
+    """The C call, on the device that its tensors are on."""
+    call = getattr(lib(), fn)
+    if on.is_cuda and on.device.index != torch.cuda.current_device():
+        with torch.cuda.device(on.device):
+            status = call(*args, _stream(stream))
+    else:
+        status = call(*args, _stream(stream))
+    if status != 0:
+        _check(fn, status)
+
+
+def _w8_args(codes: torch.Tensor, scales: torch.Tensor):
+    assert codes.dim() == 2 and codes.dtype == torch.int8 and codes.shape[0] == scales.numel()
+    assert scales.dtype == torch.float32 and scales.is_contiguous()
+    ld, one = codes.stride()
+    assert one == 1
+    return codes.data_ptr(), ld, scales.data_ptr()
+
+
+def crvq_w8_quantize(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
+    """The 8-bit codes of X (rows x N) and a scale for each row; codes: int8, rows x (N up to a multiple of 16)."""
+    rows, N = X.shape
+    assert X.stride(1) == 1 and codes.shape[0] == rows and codes.shape[1] >= -(-N // 16) * 16
+    c, ld, s = _w8_args(codes, scales)
+    _one_device(X, codes, scales)
+    _enqueue("crvq_w8_quantize", X, stream, rows, N, X.data_ptr(), X.stride(0), dtype_code(X), c, ld, s)
+
+
+def crvq_w8_gemm(codes: torch.Tensor, scales: torch.Tensor, x_codes: torch.Tensor, x_scales: torch.Tensor,
+                 y: torch.Tensor, n_cols: Optional[int] = None, stream=None) -> None:
+    """y (T x M) = the product of 8-bit activations x (T rows) with an 8-bit matrix (M rows), over their first n_cols
+    columns (all of them unless given)."""
+    M, T = codes.shape[0], x_codes.shape[0]
+    N = min(codes.shape[1], x_codes.shape[1]) if n_cols is None else n_cols
+    assert (codes.shape[1] == x_codes.shape[1] if n_cols is None else
+            0 < N <= -(-N // 16) * 16 <= min(codes.shape[1], x_codes.shape[1])) and y.shape == (T, M) and y.stride(1) == 1
+    c, ld, s = _w8_args(codes, scales)
+    xc, ldx, xs = _w8_args(x_codes, x_scales)
+    _one_device(y, codes, scales, x_codes, x_scales)
+    nbytes = lib().crvq_w8_gemm_workspace_size(M, N, T)
+    ws = _workspace_for(nbytes, y.device, stream) if nbytes else None
+    _enqueue("crvq_w8_gemm", y, stream, M, N, T, c, ld, s, xc, ldx, xs, y.data_ptr(), y.stride(0), dtype_code(y),
+             _ptr(ws), nbytes)
+
+
+def crvq_norm(x: torch.Tensor, h: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+              residual_out: Optional[torch.Tensor] = None, w_pre: Optional[torch.Tensor] = None,
+              b_pre: Optional[torch.Tensor] = None, w_post: Optional[torch.Tensor] = None,
+              b_post: Optional[torch.Tensor] = None, post: Optional[bool] = None, gate: Optional[torch.Tensor] = None,
+              alpha: float = 1.0, eps: float = 1e-6, kind: str = "rms", h_scales: Optional[torch.Tensor] = None,
+              stream=None) -> None:
+    """residual_out = residual + alpha gate u with u = norm(x) w_post + b_post (post; by default where w_post is given) or
+    x, and h = norm(that) w_pre + b_pre: as x's type, or int8 with h_scales (the operand of crvq_w8_gemm).  gate: T x N, or
+    N elements for all rows; kind: "rms" or "layer"."""
+    T, N = x.shape
+    post = w_post is not None if post is None else post
+    if kind not in ("rms", "layer"):
+        raise ValueError(f"unknown kind of norm {kind!r}")
+    ldg = 0
+    if gate is not None:
+        assert gate.dtype == x.dtype and gate.shape in ((N,), (T, N)) and gate.stride(-1) == 1
+        # rows that are all the same memory are one gate; a stride of 0 says so
+        ldg = gate.stride(0) if gate.dim() == 2 and T > 1 else 0
+    r_dtype, ldr, ldro = CRVQ_F32, 0, 0
+    for t in (residual, residual_out):
+        if t is not None:
+            assert t.shape == (T, N) and t.stride(1) == 1
+            r_dtype = dtype_code(t)
+    if residual is not None:
+        assert residual_out is None or residual_out.dtype == residual.dtype
+        ldr = residual.stride(0)
+    if residual_out is not None:
+        ldro = residual_out.stride(0)
+    assert x.stride(1) == 1
+    ldh = 0
+    if h is not None:
+        ldh = h.stride(0)
+        assert h.dim() == 2 and h.shape[0] == T and h.stride(1) == 1
+        if h_scales is None:
+            assert h.shape[1] == N and h.dtype == x.dtype
+        else:
+            assert h.dtype == torch.int8 and h.shape[1] >= -(-N // 16) * 16
+            assert h_scales.dtype == torch.float32 and h_scales.numel() == T and h_scales.is_contiguous()
+    w_dtype = None
+    for w in (w_pre, b_pre, w_post, b_post):
+        if w is not None:
+            assert w.shape == (N,) and w.is_contiguous() and w_dtype in (None, w.dtype)
+            w_dtype = w.dtype
+    _one_device(x, h, residual, residual_out, w_pre, b_pre, w_post, b_post, gate, h_scales)
+    _enqueue("crvq_norm", x, stream, T, N, CRVQ_NORM_LAYER if kind == "layer" else CRVQ_NORM_RMS, x.data_ptr(), x.stride(0),
+             dtype_code(x), int(post), _ptr(w_post), _ptr(b_post), _ptr(gate), ldg, alpha, _ptr(residual), ldr,
+             _ptr(residual_out), ldro, r_dtype, _ptr(w_pre), _ptr(b_pre),
+             CRVQ_F32 if w_dtype is None else _DTYPE_CODES[w_dtype], eps, _ptr(h), ldh, _ptr(h_scales))

@@ -755,6 +755,7 @@ size_t crvq_workspace_size(int op, int64_t n_vectors, int64_t K, int32_t beam, i
                                               static_cast<int32_t>(N), d, static_cast<int32_t>(K),
                                               static_cast<int32_t>(n_cols));
     case CRVQ_OP_W4_GEMV: return crvq_w4_gemv_workspace_size(M, N, K);
+    case CRVQ_OP_W8_GEMM: return crvq_w8_gemm_workspace_size(M, N, K);
     default: return 0;
   }
 }
@@ -1076,4 +1077,123 @@ crvq_status crvq_w4_gemv(int64_t M, int64_t N, int64_t T, int32_t group, const u
     return fail(CRVQ_ERR_INVALID, "%s: y overlaps an input", fn);
   if ((s = check_ws(workspace, ws_bytes, crvq_w4_gemv_workspace_size(M, N, T), fn))) return s;
   return hip_status(launch_w4_gemv(w, T, x, ldx, x_dtype, y, ldy, y_dtype, workspace, static_cast<hipStream_t>(stream)), fn);
+}
+
+// ---- 8-bit matrices and norms -----------------------------------------------------------------------
+namespace {
+
+crvq_status check_w8(const char* what, int64_t rows, int64_t N, const int8_t* codes, int64_t ld, const float* scales, const char* fn) {
+  if (rows < 0 || N < 1) return fail(CRVQ_ERR_INVALID, "%s: need rows >= 0 of %s and N >= 1", fn, what);
+  if (rows > 0x7fffffffLL) return fail(CRVQ_ERR_UNSUPPORTED, "%s: %lld rows of %s exceed 2^31 - 1", fn, (long long)rows, what);
+  if (N > CRVQ_ROW_MAX_N) return fail(CRVQ_ERR_UNSUPPORTED, "%s: N = %lld exceeds %d", fn, (long long)N, CRVQ_ROW_MAX_N);
+  if (rows == 0) return CRVQ_OK;
+  if (!codes || !scales) return fail(CRVQ_ERR_INVALID, "%s: codes and scales of %s must not be NULL", fn, what);
+  if (ld % 16 || ld < N || (reinterpret_cast<uintptr_t>(codes) & 15))
+    return fail(CRVQ_ERR_INVALID, "%s: codes of %s must be 16-byte aligned with a row stride that is a multiple of 16 and at least N", fn, what);
+  if (reinterpret_cast<uintptr_t>(scales) & 3) return fail(CRVQ_ERR_INVALID, "%s: scales of %s are not aligned to their type", fn, what);
+  return CRVQ_OK;
+}
+
+size_t w8_bytes(int64_t rows, int64_t ld, int64_t N) { return extent(rows, ld, 1, 0, cdiv(N, 16) * 16, 1); }
+
+}  // namespace
+
+crvq_status crvq_w8_quantize(int64_t rows, int64_t N, const void* X, int64_t ldx, int dtype, int8_t* codes, int64_t ld,
+                             float* scales, void* stream) {
+  const ApiRange range("crvq_w8_quantize");
+  static const char* fn = "crvq_w8_quantize";
+  g_err.clear();
+  crvq_status s = check_w8("the result", rows, N, codes, ld, scales, fn);
+  if (s || (s = check_matrix("X", X, rows, ldx, N, dtype, fn))) return s;
+  if (rows == 0) return CRVQ_OK;
+  const size_t x_n = extent(rows, ldx, 1, 0, N, esize(dtype)), c_n = w8_bytes(rows, ld, N), s_n = static_cast<size_t>(rows) * 4;
+  if (overlaps(codes, c_n, X, x_n) || overlaps(scales, s_n, X, x_n) || overlaps(codes, c_n, scales, s_n))
+    return fail(CRVQ_ERR_INVALID, "%s: X, codes and scales must not overlap", fn);
+  return hip_status(launch_w8_quantize(X, ldx, dtype, rows, N, codes, ld, scales, static_cast<hipStream_t>(stream)), fn);
+}
+
+size_t crvq_w8_gemm_workspace_size(int64_t M, int64_t N, int64_t T) {
+  if (M < 1 || N < 1 || T < 1 || M > 0x7fffffffLL || N > CRVQ_ROW_MAX_N || T > 0x7fffffffLL) return 0;
+  return w8_gemm_ws_bytes(M, N, T);
+}
+
+crvq_status crvq_w8_gemm(int64_t M, int64_t N, int64_t T, const int8_t* codes, int64_t ld, const float* scales,
+                         const int8_t* x_codes, int64_t ldx, const float* x_scales, void* y, int64_t ldy, int y_dtype,
+                         void* workspace, size_t ws_bytes, void* stream) {
+  const ApiRange range("crvq_w8_gemm");
+  static const char* fn = "crvq_w8_gemm";
+  g_err.clear();
+  crvq_status s = check_w8("the matrix", M, N, codes, ld, scales, fn);
+  if (s || (s = check_w8("x", T, N, x_codes, ldx, x_scales, fn))) return s;
+  if ((s = check_matrix("y", y, M ? T : 0, ldy, M, y_dtype, fn))) return s;
+  if (M == 0 || T == 0) return CRVQ_OK;
+  const size_t y_n = extent(T, ldy, 1, 0, M, esize(y_dtype));
+  if (overlaps(y, y_n, codes, w8_bytes(M, ld, N)) || overlaps(y, y_n, scales, static_cast<size_t>(M) * 4) ||
+      overlaps(y, y_n, x_codes, w8_bytes(T, ldx, N)) || overlaps(y, y_n, x_scales, static_cast<size_t>(T) * 4))
+    return fail(CRVQ_ERR_INVALID, "%s: y overlaps an input", fn);
+  if ((s = check_ws(workspace, ws_bytes, crvq_w8_gemm_workspace_size(M, N, T), fn))) return s;
+  return hip_status(launch_w8_gemm({codes, scales, M, ld}, {x_codes, x_scales, T, ldx}, N, y, ldy, y_dtype, workspace,
+                                   static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+crvq_status crvq_norm(int64_t T, int64_t N, int kind, const void* x, int64_t ldx, int dtype, int post, const void* w_post,
+                      const void* b_post, const void* gate, int64_t ldg, double alpha, const void* r, int64_t ldr,
+                      void* r_out, int64_t ldro, int r_dtype, const void* w_pre, const void* b_pre, int w_dtype,
+                      double eps, void* h, int64_t ldh, float* h_scales, void* stream) {
+  const ApiRange range("crvq_norm");
+  static const char* fn = "crvq_norm";
+  g_err.clear();
+  if (kind != CRVQ_NORM_RMS && kind != CRVQ_NORM_LAYER) return fail(CRVQ_ERR_INVALID, "%s: unknown kind %d", fn, kind);
+  if (T < 0 || N < 1) return fail(CRVQ_ERR_INVALID, "%s: need T >= 0 and N >= 1", fn);
+  if (T > 0x7fffffffLL) return fail(CRVQ_ERR_UNSUPPORTED, "%s: T = %lld exceeds 2^31 - 1", fn, (long long)T);
+  if (N > CRVQ_ROW_MAX_N) return fail(CRVQ_ERR_UNSUPPORTED, "%s: N = %lld exceeds %d", fn, (long long)N, CRVQ_ROW_MAX_N);
+  if (!dtype_ok(dtype) || !dtype_ok(r_dtype) || !dtype_ok(w_dtype))
+    return fail(CRVQ_ERR_INVALID, "%s: a type is not CRVQ_F32 or CRVQ_BF16", fn);
+  if (!std::isfinite(static_cast<float>(alpha)) || !(eps >= 0.0) || !std::isfinite(eps))
+    return fail(CRVQ_ERR_INVALID, "%s: alpha must be finite and eps finite and not negative", fn);
+  if (T == 0) return CRVQ_OK;
+  if (!post && (w_post || b_post)) return fail(CRVQ_ERR_INVALID, "%s: w_post and b_post need post", fn);
+  if (!h && (w_pre || b_pre || h_scales)) return fail(CRVQ_ERR_INVALID, "%s: w_pre, b_pre and h_scales need h", fn);
+  if (!h && !r_out) return fail(CRVQ_ERR_INVALID, "%s: h and r_out are both NULL", fn);
+  crvq_status s = check_matrix("x", x, T, ldx, N, dtype, fn);
+  if (s || (gate && (s = check_matrix("gate", gate, T, ldg ? ldg : N, N, dtype, fn))) ||
+      (r && (s = check_matrix("r", r, T, ldr, N, r_dtype, fn))) ||
+      (r_out && (s = check_matrix("r_out", r_out, T, ldro, N, r_dtype, fn))))
+    return s;
+  if (gate && ldg < 0) return fail(CRVQ_ERR_INVALID, "%s: negative row stride of gate", fn);
+  if (h && h_scales) s = check_w8("h", T, N, static_cast<const int8_t*>(h), ldh, h_scales, fn);
+  else if (h) s = check_matrix("h", h, T, ldh, N, dtype, fn);
+  if (s) return s;
+  for (const void* w : {w_post, b_post, w_pre, b_pre})
+    if (reinterpret_cast<uintptr_t>(w) % esize(w_dtype)) return fail(CRVQ_ERR_INVALID, "%s: a weight is not aligned to its type", fn);
+  // a row is read whole before anything of it is written, so an output may take the place of x or r row by row
+  const int es = esize(dtype), rs = esize(r_dtype), ws = esize(w_dtype);
+  const size_t n_x = extent(T, ldx, 1, 0, N, es), n_g = gate ? extent(ldg ? T : 1, ldg, 1, 0, N, es) : 0;
+  const size_t n_r = r ? extent(T, ldr, 1, 0, N, rs) : 0, n_w = static_cast<size_t>(N) * ws;
+  struct Out {
+    const void* p;
+    size_t n;
+    int64_t ld;
+    int type;  // -1: codes or scales, in nobody's place
+  };
+  const Out outs[3] = {{r_out, r_out ? extent(T, ldro, 1, 0, N, rs) : 0, ldro, r_dtype},
+                       {h, !h ? 0 : h_scales ? w8_bytes(T, ldh, N) : extent(T, ldh, 1, 0, N, es), ldh, h_scales ? -1 : dtype},
+                       {h_scales, h_scales ? static_cast<size_t>(T) * 4 : 0, 0, -1}};
+  for (const Out& o : outs) {
+    if (!o.p) continue;
+    const bool as_x = o.p == x && o.ld == ldx && o.type == dtype, as_r = o.p == r && o.ld == ldr && o.type == r_dtype;
+    if ((overlaps(o.p, o.n, x, n_x) && !as_x) || (r && overlaps(o.p, o.n, r, n_r) && !as_r) ||
+        (gate && overlaps(o.p, o.n, gate, n_g)))
+      return fail(CRVQ_ERR_INVALID, "%s: an output overlaps an input without being x or r", fn);
+    for (const void* w : {w_post, b_post, w_pre, b_pre})
+      if (w && overlaps(o.p, o.n, w, n_w)) return fail(CRVQ_ERR_INVALID, "%s: an output overlaps a weight", fn);
+    for (const Out& other : outs)
+      if (&other != &o && other.p && overlaps(o.p, o.n, other.p, other.n))
+        return fail(CRVQ_ERR_INVALID, "%s: outputs overlap", fn);
+  }
+  const NormDesc d = {N,      x,     r,      gate,  r_out, h,        ldx, ldr,
+                      ldg,    ldro,  ldh,    w_post, b_post, w_pre,  b_pre, h_scales,
+                      eps,    static_cast<float>(alpha), kind == CRVQ_NORM_LAYER, post ? 1 : 0, w_dtype == CRVQ_F32};
+  return hip_status(launch_norm(d, T, dtype, r_dtype, static_cast<hipStream_t>(stream)), fn);
 }

@@ -310,4 +310,29 @@ size_t w4_gemv_ws_bytes(int64_t M, int64_t N, int64_t T);
 hipError_t launch_w4_gemv(const W4& w, int64_t T, const void* x, int64_t ldx, int x_type, void* y, int64_t ldy, int y_type,
                           void* ws, hipStream_t stream);
 
+// ---- 8-bit matrices with a scale for each row, and their product (k_w8.hip) ------------------------
+struct W8 {
+  const int8_t* codes;
+  const float* scales;
+  int64_t rows, ld;
+};
+hipError_t launch_w8_quantize(const void* X, int64_t ldx, int type, int64_t rows, int64_t N, int8_t* codes, int64_t ld,
+                              float* scales, hipStream_t stream);
+size_t w8_gemm_ws_bytes(int64_t M, int64_t N, int64_t T);
+hipError_t launch_w8_gemm(const W8& w, const W8& x, int64_t N, void* y, int64_t ldy, int y_type, void* ws, hipStream_t stream);
+
+// ---- norms with gate and residual sum (k_norm.hip) -------------------------------------------------
+struct NormDesc {
+  int64_t N;
+  const void *x, *r, *gate;  // r, gate: may be NULL; ldg 0: one gate for all rows
+  void *r_out, *h;           // may be NULL
+  int64_t ldx, ldr, ldg, ldro, ldh;
+  const void *w_post, *b_post, *w_pre, *b_pre;
+  float* h_scale;  // h is in 8 bits where it is given
+  double eps;
+  float alpha;
+  int layer, post, w_f32;
+};
+hipError_t launch_norm(const NormDesc& d, int64_t T, int x_type, int r_type, hipStream_t stream);
+
 }  // namespace crvq
