@@ -508,6 +508,102 @@ crvq_status crvq_kv_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int
                               int32_t window, float* lse, void* workspace, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Drafted tokens over the cache.  A tree of drafted tokens is appended like any
+ * new tokens (crvq_kv_append with the places of crvq_tree_mask as positions), verified in
+ * one call, and the accepted ones are moved behind the context (crvq_kv_gather).
+ * ------------------------------------------------------------------------- */
+
+/* crvq_tree_mask -- what the drafted tokens of a tree see.  parents[row]
+ * (int32[n_tokens], device) is the index of the token's parent among its
+ * sequence's new tokens, below its own, or -1 for a token that follows the
+ * context itself; start, kv_len and max_new as in a batch.
+ *   mask (uint64 [n_tokens][ld_mask], 64 ld_mask >= max_new, or NULL): bit j of
+ *     row i is 1 for j = i and every ancestor j (of those the `window` nearest, i among
+ *     them, where window > 0)
+ *   places (int32[n_tokens], or NULL) = kv_len - n + depth - 1: a token's place
+ *     behind the context, n being the sequence's new tokens
+ * A token with a parent that is neither -1 nor below its child, its own or an
+ * ancestor's, gets a mask of zeros and the place -1 (which crvq_kv_append turns into NaN
+ * queries).  Rows of a sequence that is not within [0, n_tokens] or has more than max_new are left out. */
+crvq_status crvq_tree_mask(int32_t B, const int32_t* parents, const int32_t* start, const int32_t* kv_len, int32_t max_new,
+                           int64_t n_tokens, int32_t window, uint64_t* mask, int64_t ld_mask, int32_t* places, void* stream);
+
+/* crvq_kv_tree_attention -- crvq_kv_attention (its batch, arithmetic, lse, NaN and
+ * left-out rules) with a mask of its own among the new tokens: token i of a
+ * sequence's n sees the context, t < kv_len[b] - n, and new token j where bit
+ * j % 64 of word mask[row i][j / 64] is 1; bits from n on do not matter.  Any mask will
+ * do; a row that sees nothing is 0.  window > 0: of the context only t > P_i - window, P_i =
+ * places[row i] (int32, device), or kv_len[b] - n + i where places is NULL;
+ * new tokens are seen as the mask says.
+ * workspace: crvq_kv_tree_attention_workspace_size(...) bytes. */
+size_t crvq_kv_tree_attention_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new, int32_t max_kv);
+crvq_status crvq_kv_tree_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages,
+                                   const int8_t* k_cache, const int8_t* v_cache, const float* k_scale, const float* v_scale,
+                                   const int32_t* block_table, int64_t ld_table, const int32_t* start, const int32_t* kv_len,
+                                   int32_t max_new, int32_t max_kv, int64_t n_tokens, int dtype, const void* q, int64_t q_tok,
+                                   int64_t q_head, void* out, int64_t o_tok, int64_t o_head, float scale, const uint64_t* mask,
+                                   int64_t ld_mask, int32_t window, const int32_t* places, float* lse, void* workspace,
+                                   size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The cache within a budget: the attention weight every cached token receives is
+ * added up (crvq_kv_weights, after the attention of the same rows), the tokens with the most
+ * are kept (crvq_kv_select) and moved to other pages (crvq_kv_gather); the old
+ * pages are free then.  Weights: float [B][Hkv][ld], token t of sequence b's
+ * cache and key head h at (b * Hkv + h) * ld + t.
+ * ------------------------------------------------------------------------- */
+
+/* crvq_kv_weights -- for every sequence that brings rows, key head and token t < kv_len[b]:
+ *
+ *   after[t] = decay * before[t] + sum_{i, h: row i of head h sees t} exp(scale q_ih . K_t - lse_ih)
+ *
+ * over the query heads of the key head; the sequence's new tokens have no
+ * `before`, and before = NULL is 0 for all; after may be before.  q, lse (as
+ * crvq_kv_attention or crvq_kv_tree_attention returned it), scale, causal and
+ * window are those of the attention; mask != NULL: of a tree, with places (causal is not
+ * looked at).  Rows whose lse is infinite or NaN add nothing, nor do tokens whose page is
+ * outside [0, n_pages) or whose scale is negative or not finite.  Sequences
+ * that bring no rows, whose rows are not within [0, n_tokens] or more than
+ * max_new, or with kv_len[b] < 0, > max_kv or > ld_table * page, and tokens from kv_len[b] on, stay as they were in `after`.
+ * Products are exact (CRVQ_F32 queries as three bf16 terms), sums fp32 in a
+ * fixed order.  ld >= max_kv.
+ * workspace: crvq_kv_weights_workspace_size(...) bytes. */
+size_t crvq_kv_weights_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new, int32_t max_kv);
+crvq_status crvq_kv_weights(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages, const int8_t* k_cache,
+                            const float* k_scale, const int32_t* block_table, int64_t ld_table, const int32_t* start,
+                            const int32_t* kv_len, int32_t max_new, int32_t max_kv, int64_t n_tokens, int dtype, const void* q,
+                            int64_t q_tok, int64_t q_head, const float* lse, float scale, int causal, int32_t window,
+                            const uint64_t* mask, int64_t ld_mask, const int32_t* places, float decay, const float* before,
+                            float* after, int64_t ld, void* workspace, size_t ws_bytes, void* stream);
+
+/* crvq_kv_select -- the min(kv_len[b], budget) tokens of every key head that are
+ * kept: the first `sinks`, the last `recent` (sinks + recent <= budget), and of
+ * the others those with the largest weights, the lower index first where they are equal; NaN counts as
+ * less than everything.  keep (int32 [B][Hkv][ld_keep], ld_keep >= min(budget,
+ * ld)) gets them in order, kept_weights ([B][Hkv][ld_keep] or NULL) their weights, kept_len (int32[B]) their number,
+ * the same for all heads; 0 where kv_len[b] < 0 or > ld.  Entries from kept_len[b] on stay as they were. */
+crvq_status crvq_kv_select(int32_t B, int32_t Hkv, const int32_t* kv_len, const float* weights, int64_t ld, int32_t budget,
+                           int32_t sinks, int32_t recent, int32_t* keep, int64_t ld_keep, int32_t* kept_len, float* kept_weights,
+                           void* stream);
+
+/* crvq_kv_gather -- moves tokens to other pages: slot j % page of page
+ * to_table[b * ld_to + j / page] becomes token keep[b][h][j] (int32 [B][keep_heads][ld_keep],
+ * keep_heads = Hkv, or 1 for the same tokens of every head) of sequence b, for
+ * j < kept_len[b] <= max_keep (host).  A new page's scale is the largest of its tokens' old ones
+ * and a code becomes rint(c * (old / new)), in fp32: tokens that shared a page
+ * keep their codes, the others lose up to half a step.  Slots of the last page from
+ * kept_len[b] on become 0.  The new pages must be none that the call reads and in
+ * one place of to_table (otherwise their contents are undefined; nothing outside the cache is
+ * touched).  A token outside [0, kv_len[b]), or whose page is outside [0, n_pages)
+ * or has a scale that is negative or not finite, makes the new page's head NaN with codes 0.  A
+ * sequence with kept_len[b] above ld_keep or ld_to * page, and new pages outside [0, n_pages), are
+ * left out. */
+crvq_status crvq_kv_gather(int32_t B, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages, int8_t* k_cache, int8_t* v_cache,
+                           float* k_scale, float* v_scale, const int32_t* block_table, int64_t ld_table, const int32_t* kv_len,
+                           const int32_t* keep, int64_t ld_keep, int32_t keep_heads, const int32_t* kept_len, int32_t max_keep,
+                           const int32_t* to_table, int64_t ld_to, void* stream);
+
+/* ---------------------------------------------------------------------------
  * 4-bit matrices.  An M x N matrix as codes c in 0 .. 15 with a scale s and a
  * zero point z for every `group` (32, 64, 128 or 256) consecutive columns of a row:
  *   W[r][j] = s[r][j/group] * (c[r][j] - z[r][j/group]),   z = 8 when zeros is NULL.
@@ -620,6 +716,7 @@ crvq_status crvq_norm(int64_t T, int64_t N, int kind, const void* x, int64_t ldx
  *                       n_cols = max_kv              (crvq_kv_attention)
  *   CRVQ_OP_W4_GEMV     M, N, K = T                  (crvq_w4_gemv)
  *   CRVQ_OP_W8_GEMM     M, N, K = T                  (crvq_w8_gemm)
+ *   CRVQ_OP_KV_WEIGHTS  as CRVQ_OP_KV_ATTENTION      (crvq_kv_weights; crvq_kv_tree_attention's is CRVQ_OP_KV_ATTENTION)
  * Returns 0 for an unknown op or a shape the call rejects (and for calls that
  * need no workspace at that shape).  Ks is a host array of n_books entries.
  */
@@ -636,7 +733,8 @@ typedef enum {
   CRVQ_OP_HINV = 9,
   CRVQ_OP_KV_ATTENTION = 10,
   CRVQ_OP_W4_GEMV = 11,
-  CRVQ_OP_W8_GEMM = 12
+  CRVQ_OP_W8_GEMM = 12,
+  CRVQ_OP_KV_WEIGHTS = 13
 } crvq_op;
 size_t crvq_workspace_size(int op, int64_t n_vectors, int64_t K, int32_t beam, int32_t n_books, int32_t d,
                            const int64_t* Ks, int64_t M, int64_t N, int64_t n_cols);

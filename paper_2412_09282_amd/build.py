@@ -37,6 +37,7 @@ SOURCES = {
     "k_hinv.hip": [],
     "k_kv.hip": [],
     "k_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "k_evict.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "k_w4.hip": [],
     "k_w8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "k_norm.hip": [],

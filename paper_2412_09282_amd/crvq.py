@@ -97,6 +97,16 @@ def lib(build_if_missing: bool = True):
                 "crvq_kv_attention_workspace_size": ([I32] * 6, SZ),
                 "crvq_kv_attention": ([I32] * 5 + [I64] + [P] * 5 + [I64, P, P, I32, I32, I64, ctypes.c_int] +
                                       [P, I64, I64] * 2 + [ctypes.c_float, ctypes.c_int, I32, P, P, SZ, P], ctypes.c_int),
+                "crvq_tree_mask": ([I32, P, P, P, I32, I64, I32, P, I64, P, P], ctypes.c_int),
+                "crvq_kv_tree_attention_workspace_size": ([I32] * 6, SZ),
+                "crvq_kv_tree_attention": ([I32] * 5 + [I64] + [P] * 5 + [I64, P, P, I32, I32, I64, ctypes.c_int] +
+                                           [P, I64, I64] * 2 + [ctypes.c_float, P, I64, I32, P, P, P, SZ, P], ctypes.c_int),
+                "crvq_kv_weights_workspace_size": ([I32] * 6, SZ),
+                "crvq_kv_weights": ([I32] * 5 + [I64, P, P, P, I64, P, P, I32, I32, I64, ctypes.c_int, P, I64, I64, P,
+                                     ctypes.c_float, ctypes.c_int, I32, P, I64, P, ctypes.c_float, P, P, I64, P, SZ, P],
+                                    ctypes.c_int),
+                "crvq_kv_select": ([I32, I32, P, P, I64, I32, I32, I32, P, I64, P, P, P], ctypes.c_int),
+                "crvq_kv_gather": ([I32] * 4 + [I64] + [P] * 5 + [I64, P, P, I64, I32, P, I32, P, I64, P], ctypes.c_int),
                 "crvq_w4_quantize": ([I64, I64, I32, P, I64, ctypes.c_int, P, I64, P, ctypes.c_int, I64, P, I64, P],
                                      ctypes.c_int),
                 "crvq_w4_dequant": ([I64, I64, I32, P, I64, P, ctypes.c_int, I64, P, I64, P, I64, ctypes.c_int, P],
@@ -698,3 +708,117 @@ def crvq_norm(x: torch.Tensor, h: Optional[torch.Tensor] = None, residual: Optio
              dtype_code(x), int(post), _ptr(w_post), _ptr(b_post), _ptr(gate), ldg, alpha, _ptr(residual), ldr,
              _ptr(residual_out), ldro, r_dtype, _ptr(w_pre), _ptr(b_pre),
              CRVQ_F32 if w_dtype is None else _DTYPE_CODES[w_dtype], eps, _ptr(h), ldh, _ptr(h_scales))
+
+
+# ---- drafts over the cache, and the cache within a budget ------------------------------------------
+def _mask_args(mask: torch.Tensor, n_tokens: int, max_new: int):
+    assert mask.dtype == torch.int64 and mask.dim() == 2 and mask.shape[0] == n_tokens and mask.is_contiguous()
+    assert mask.shape[1] * 64 >= max_new
+    return mask.data_ptr(), mask.shape[1]
+
+
+def _places_ok(places: Optional[torch.Tensor], n_tokens: int) -> None:
+    assert places is None or (places.dtype == torch.int32 and places.is_contiguous() and places.numel() == n_tokens)
+
+
+def crvq_tree_mask(parents: torch.Tensor, start: torch.Tensor, kv_len: torch.Tensor, max_new: int,
+                   mask: Optional[torch.Tensor] = None, places: Optional[torch.Tensor] = None, window: int = 0,
+                   stream=None) -> None:
+    """What the drafted tokens of a tree see (mask: int64, tokens x words of 64 bits) and their places, from the index of
+    every token's parent among its sequence's new tokens (-1: it follows the context)."""
+    n, B = parents.numel(), kv_len.numel()
+    assert parents.dtype == start.dtype == kv_len.dtype == torch.int32 and start.numel() == B + 1
+    assert parents.is_contiguous() and start.is_contiguous() and kv_len.is_contiguous()
+    m = (None, 0) if mask is None else _mask_args(mask, n, max_new)
+    _places_ok(places, n)
+    _one_device(parents, start, kv_len, mask, places)
+    _enqueue("crvq_tree_mask", parents, stream, B, parents.data_ptr(), start.data_ptr(), kv_len.data_ptr(), max_new, n,
+             window, *m, _ptr(places))
+
+
+def crvq_kv_tree_attention(q: torch.Tensor, out: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                           k_scale: torch.Tensor, v_scale: torch.Tensor, block_table: torch.Tensor, start: torch.Tensor,
+                           kv_len: torch.Tensor, max_new: int, max_kv: int, mask: torch.Tensor,
+                           scale: Optional[float] = None, window: int = 0, places: Optional[torch.Tensor] = None,
+                           lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of the new tokens' queries q (tokens x Hq x D) over the paged 8-bit cache: of the new tokens every row
+    sees those whose bits its row of mask (crvq_tree_mask) has, and the context before them; scale: D ** -0.5."""
+    L = lib()
+    n, Hq = q.shape[0], q.shape[1]
+    assert lse is None or (lse.dtype == torch.float32 and lse.shape == (n, Hq) and lse.is_contiguous())
+    m = _mask_args(mask, n, max_new)
+    _places_ok(places, n)
+    B, Hkv, D, page, cache = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len)
+    rows = _row_args(q, n, Hq, D, q.dtype) + _row_args(out, n, Hq, D, q.dtype)
+    _one_device(q, out, k_cache, v_cache, k_scale, v_scale, block_table, start, kv_len, mask, places, lse)
+    nbytes = L.crvq_kv_tree_attention_workspace_size(B, Hq, Hkv, D, max_new, max_kv)
+    ws = _workspace_for(nbytes, q.device, stream) if nbytes else None
+    _enqueue("crvq_kv_tree_attention", q, stream, B, Hq, Hkv, D, page, *cache, max_new, max_kv, n, dtype_code(q), *rows,
+             D ** -0.5 if scale is None else scale, *m, window, _ptr(places), _ptr(lse), _ptr(ws), nbytes)
+
+
+def crvq_kv_weights(q: torch.Tensor, lse: torch.Tensor, before: Optional[torch.Tensor], after: torch.Tensor,
+                    k_cache: torch.Tensor, k_scale: torch.Tensor, block_table: torch.Tensor, start: torch.Tensor,
+                    kv_len: torch.Tensor, max_new: int, max_kv: int, scale: Optional[float] = None, causal: bool = True,
+                    window: int = 0, mask: Optional[torch.Tensor] = None, places: Optional[torch.Tensor] = None,
+                    decay: float = 1.0, stream=None) -> None:
+    """after (B x Hkv x tokens; may be before) = decay before + the attention weight that every cached token received from
+    the rows of q, whose attention returned lse; new tokens start from 0."""
+    n_pages, Hkv, page, D = k_cache.shape
+    (n, Hq), B = lse.shape, kv_len.numel()
+    assert k_cache.dtype == torch.int8 and k_cache.is_contiguous() and k_scale.is_contiguous()
+    assert k_scale.shape == (n_pages, Hkv) and k_scale.dtype == torch.float32
+    assert start.dtype == kv_len.dtype == block_table.dtype == torch.int32 and start.numel() == B + 1
+    assert start.is_contiguous() and kv_len.is_contiguous()
+    assert block_table.dim() == 2 and block_table.shape[0] == B and (B == 0 or block_table.is_contiguous())
+    assert lse.dtype == after.dtype == torch.float32 and lse.is_contiguous() and after.is_contiguous()
+    assert after.dim() == 3 and after.shape[:2] == (B, Hkv)
+    assert before is None or (before.shape == after.shape and before.dtype == torch.float32 and before.is_contiguous())
+    m = (None, 0) if mask is None else _mask_args(mask, n, max_new)
+    _places_ok(places, n)
+    rows = _row_args(q, n, Hq, D, q.dtype)
+    _one_device(q, lse, before, after, k_cache, k_scale, block_table, start, kv_len, mask, places)
+    nbytes = lib().crvq_kv_weights_workspace_size(B, Hq, Hkv, D, max_new, max_kv)
+    ws = _workspace_for(nbytes, q.device, stream) if nbytes else None
+    _enqueue("crvq_kv_weights", q, stream, B, Hq, Hkv, D, page, n_pages, k_cache.data_ptr(), k_scale.data_ptr(),
+             block_table.data_ptr(), block_table.shape[1], start.data_ptr(), kv_len.data_ptr(), max_new, max_kv, n,
+             dtype_code(q), *rows, lse.data_ptr(), D ** -0.5 if scale is None else scale, int(causal), window, *m,
+             _ptr(places), decay, _ptr(before), after.data_ptr(), after.shape[2], _ptr(ws), nbytes)
+
+
+def crvq_kv_select(weights: torch.Tensor, kv_len: torch.Tensor, budget: int, keep: torch.Tensor, kept_len: torch.Tensor,
+                   kept_weights: Optional[torch.Tensor] = None, sinks: int = 0, recent: int = 0, stream=None) -> None:
+    """The tokens of every key head that a budget keeps (keep: int32, B x Hkv x room, in order; kept_len: int32, B): the
+    first `sinks`, the last `recent`, and of the others those with the largest weights (B x Hkv x tokens)."""
+    B, Hkv, ld = weights.shape
+    assert weights.dtype == torch.float32 and weights.is_contiguous()
+    assert keep.dtype == kv_len.dtype == kept_len.dtype == torch.int32 and keep.dim() == 3 and keep.shape[:2] == (B, Hkv)
+    assert keep.is_contiguous() and kv_len.is_contiguous() and kept_len.is_contiguous()
+    assert kv_len.numel() == kept_len.numel() == B
+    assert kept_weights is None or (kept_weights.shape == keep.shape and kept_weights.dtype == torch.float32 and
+                                    kept_weights.is_contiguous())
+    _one_device(weights, kv_len, keep, kept_len, kept_weights)
+    _enqueue("crvq_kv_select", weights, stream, B, Hkv, kv_len.data_ptr(), weights.data_ptr(), ld, budget, sinks, recent,
+             keep.data_ptr(), keep.shape[2], kept_len.data_ptr(), _ptr(kept_weights))
+
+
+def crvq_kv_gather(k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                   block_table: torch.Tensor, kv_len: torch.Tensor, keep: torch.Tensor, kept_len: torch.Tensor,
+                   to_table: torch.Tensor, stream=None) -> None:
+    """Moves the tokens keep[b][h][:kept_len[b]] (B x Hkv x room, or B x 1 x room: the same ones of every head) of every
+    sequence to the pages of to_table (B x pages), none of which the call may read."""
+    n_pages, Hkv, page, D = k_cache.shape
+    B = kv_len.numel()
+    assert v_cache.shape == (n_pages, Hkv, D, page) and k_cache.dtype == v_cache.dtype == torch.int8
+    assert k_scale.shape == v_scale.shape == (n_pages, Hkv) and k_scale.dtype == v_scale.dtype == torch.float32
+    assert k_cache.is_contiguous() and v_cache.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()
+    assert kv_len.dtype == kept_len.dtype == keep.dtype == block_table.dtype == to_table.dtype == torch.int32
+    assert keep.dim() == 3 and keep.shape[0] == B and kept_len.numel() == B
+    assert block_table.dim() == to_table.dim() == 2 and block_table.shape[0] == to_table.shape[0] == B
+    assert B == 0 or (block_table.is_contiguous() and to_table.is_contiguous())
+    assert keep.is_contiguous() and kv_len.is_contiguous() and kept_len.is_contiguous()
+    _one_device(k_cache, v_cache, k_scale, v_scale, block_table, kv_len, keep, kept_len, to_table)
+    _enqueue("crvq_kv_gather", k_cache, stream, B, Hkv, D, page, n_pages, k_cache.data_ptr(), v_cache.data_ptr(),
+             k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(), block_table.shape[1], kv_len.data_ptr(),
+             keep.data_ptr(), keep.shape[2], keep.shape[1], kept_len.data_ptr(),
+             min(keep.shape[2], to_table.shape[1] * page), to_table.data_ptr(), to_table.shape[1])

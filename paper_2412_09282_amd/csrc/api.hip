@@ -755,6 +755,10 @@ size_t crvq_workspace_size(int op, int64_t n_vectors, int64_t K, int32_t beam, i
                                               static_cast<int32_t>(N), d, static_cast<int32_t>(K),
                                               static_cast<int32_t>(n_cols));
     case CRVQ_OP_W4_GEMV: return crvq_w4_gemv_workspace_size(M, N, K);
+    case CRVQ_OP_KV_WEIGHTS:
+      if (n_vectors > 0x7fffffffLL || M > 0x7fffffffLL || N > 0x7fffffffLL || K > 0x7fffffffLL || n_cols > 0x7fffffffLL) return 0;
+      return crvq_kv_weights_workspace_size(static_cast<int32_t>(n_vectors), static_cast<int32_t>(M), static_cast<int32_t>(N), d,
+                                            static_cast<int32_t>(K), static_cast<int32_t>(n_cols));
     case CRVQ_OP_W8_GEMM: return crvq_w8_gemm_workspace_size(M, N, K);
     default: return 0;
   }
@@ -974,8 +978,200 @@ crvq_status crvq_kv_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int
   }
   if ((s = check_ws(workspace, ws_bytes, crvq_kv_attention_workspace_size(B, Hq, Hkv, D, max_new, max_kv), fn))) return s;
   return hip_status(launch_kv_attention(c, bt, max_kv, dtype, Hq, {const_cast<void*>(q), q_tok, q_head},
-                                        {out, o_tok, o_head}, scale, causal ? 1 : 0, window, lse, workspace,
+                                        {out, o_tok, o_head}, scale, causal ? 1 : 0, window, {}, lse, workspace,
                                         static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+// ---- drafts over the cache, and the cache within a budget -------------------------------------------
+namespace {
+
+crvq_status check_tree(const uint64_t* mask, int64_t ld_mask, const int32_t* places, int32_t max_new, const char* fn) {
+  if (ld_mask < cdiv(max_new, 64))
+    return fail(CRVQ_ERR_INVALID, "%s: ld_mask = %lld words for max_new = %d tokens", fn, (long long)ld_mask, max_new);
+  if ((reinterpret_cast<uintptr_t>(mask) & 7) || (reinterpret_cast<uintptr_t>(places) & 3))
+    return fail(CRVQ_ERR_INVALID, "%s: mask or places is not aligned to its type", fn);
+  return CRVQ_OK;
+}
+
+size_t mask_bytes(int64_t n_tokens, int64_t ld_mask) { return static_cast<size_t>(n_tokens) * ld_mask * 8; }
+
+}  // namespace
+
+crvq_status crvq_tree_mask(int32_t B, const int32_t* parents, const int32_t* start, const int32_t* kv_len, int32_t max_new,
+                           int64_t n_tokens, int32_t window, uint64_t* mask, int64_t ld_mask, int32_t* places, void* stream) {
+  const ApiRange range("crvq_tree_mask");
+  static const char* fn = "crvq_tree_mask";
+  g_err.clear();
+  if (B < 0 || max_new < 0 || n_tokens < 0 || window < 0)
+    return fail(CRVQ_ERR_INVALID, "%s: negative B, max_new, n_tokens or window", fn);
+  if (B > 65535) return fail(CRVQ_ERR_UNSUPPORTED, "%s: B = %d exceeds 65535", fn, B);
+  if (n_tokens > 0x7fffffffLL) return fail(CRVQ_ERR_UNSUPPORTED, "%s: %lld rows exceed 2^31 - 1", fn, (long long)n_tokens);
+  if (B == 0 || max_new == 0 || n_tokens == 0 || (!mask && !places)) return CRVQ_OK;
+  if (!parents || !start || !kv_len) return fail(CRVQ_ERR_INVALID, "%s: parents, start and kv_len must not be NULL", fn);
+  crvq_status s;
+  if (mask && (s = check_tree(mask, ld_mask, places, max_new, fn))) return s;
+  const size_t p_n = static_cast<size_t>(n_tokens) * 4, m_n = mask ? mask_bytes(n_tokens, ld_mask) : 0;
+  if ((mask && overlaps(mask, m_n, parents, p_n)) || (places && overlaps(places, p_n, parents, p_n)) ||
+      (mask && places && overlaps(mask, m_n, places, p_n)))
+    return fail(CRVQ_ERR_INVALID, "%s: parents, mask and places must not overlap", fn);
+  return hip_status(launch_tree_mask(B, parents, start, kv_len, max_new, n_tokens, window, mask, ld_mask, places,
+                                     static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+size_t crvq_kv_tree_attention_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new, int32_t max_kv) {
+  return crvq_kv_attention_workspace_size(B, Hq, Hkv, D, max_new, max_kv);
+}
+
+crvq_status crvq_kv_tree_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages,
+                                   const int8_t* k_cache, const int8_t* v_cache, const float* k_scale, const float* v_scale,
+                                   const int32_t* block_table, int64_t ld_table, const int32_t* start, const int32_t* kv_len,
+                                   int32_t max_new, int32_t max_kv, int64_t n_tokens, int dtype, const void* q, int64_t q_tok,
+                                   int64_t q_head, void* out, int64_t o_tok, int64_t o_head, float scale, const uint64_t* mask,
+                                   int64_t ld_mask, int32_t window, const int32_t* places, float* lse, void* workspace,
+                                   size_t ws_bytes, void* stream) {
+  const ApiRange range("crvq_kv_tree_attention");
+  static const char* fn = "crvq_kv_tree_attention";
+  g_err.clear();
+  KvCache c;
+  KvBatch bt;
+  crvq_status s = check_cache(B, Hkv, D, page, n_pages, k_cache, v_cache, k_scale, v_scale, block_table, ld_table, start,
+                              kv_len, max_new, n_tokens, dtype, fn, &c, &bt);
+  if (s) return s;
+  if (Hq < 1 || Hq % Hkv) return fail(CRVQ_ERR_INVALID, "%s: Hq = %d is not a multiple of Hkv = %d", fn, Hq, Hkv);
+  if (max_kv < 0 || max_kv > CRVQ_KV_MAX_LEN)
+    return fail(CRVQ_ERR_INVALID, "%s: max_kv = %d outside [0, 2^30]", fn, max_kv);
+  if (!std::isfinite(scale)) return fail(CRVQ_ERR_INVALID, "%s: scale is not finite", fn);
+  if (window < 0) return fail(CRVQ_ERR_INVALID, "%s: window < 0", fn);
+  if (B == 0 || max_new == 0 || n_tokens == 0) return CRVQ_OK;
+  if (!mask) return fail(CRVQ_ERR_INVALID, "%s: mask must not be NULL", fn);
+  if ((s = check_tree(mask, ld_mask, places, max_new, fn))) return s;
+  if ((s = check_rows("q", q, q_tok, q_head, Hq, D, dtype, fn))) return s;
+  if ((s = check_out_rows("out", out, o_tok, o_head, n_tokens, Hq, D, dtype, fn))) return s;
+  const int es = esize(dtype);
+  const size_t q_n = extent(n_tokens, q_tok, Hq, q_head, D, es), o_n = extent(n_tokens, o_tok, Hq, o_head, D, es);
+  const size_t m_n = mask_bytes(n_tokens, ld_mask), p_n = places ? static_cast<size_t>(n_tokens) * 4 : 0;
+  if (overlaps(out, o_n, q, q_n) && !(out == q && o_tok == q_tok && o_head == q_head))
+    return fail(CRVQ_ERR_INVALID, "%s: out overlaps q without being q", fn);
+  const size_t l_n = lse ? static_cast<size_t>(n_tokens) * Hq * 4 : 0;
+  if (lse && (overlaps(lse, l_n, q, q_n) || overlaps(lse, l_n, out, o_n)))
+    return fail(CRVQ_ERR_INVALID, "%s: lse overlaps q or out", fn);
+  if (overlaps(out, o_n, mask, m_n) || (places && overlaps(out, o_n, places, p_n)) ||
+      (lse && (overlaps(lse, l_n, mask, m_n) || (places && overlaps(lse, l_n, places, p_n)))))
+    return fail(CRVQ_ERR_INVALID, "%s: out or lse overlaps mask or places", fn);
+  if ((s = check_ws(workspace, ws_bytes, crvq_kv_tree_attention_workspace_size(B, Hq, Hkv, D, max_new, max_kv), fn))) return s;
+  return hip_status(launch_kv_attention(c, bt, max_kv, dtype, Hq, {const_cast<void*>(q), q_tok, q_head},
+                                        {out, o_tok, o_head}, scale, 0, window, {mask, ld_mask, places}, lse, workspace,
+                                        static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+size_t crvq_kv_weights_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new, int32_t max_kv) {
+  if (B < 1 || Hkv < 1 || Hq < Hkv || Hq % Hkv || D < 16 || D > CRVQ_KV_MAX_D || D % 16 || max_new < 1 || max_kv < 1) return 0;
+  return kv_weights_ws_bytes(B, Hq, Hkv, D, max_new, max_kv);
+}
+
+crvq_status crvq_kv_weights(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages, const int8_t* k_cache,
+                            const float* k_scale, const int32_t* block_table, int64_t ld_table, const int32_t* start,
+                            const int32_t* kv_len, int32_t max_new, int32_t max_kv, int64_t n_tokens, int dtype, const void* q,
+                            int64_t q_tok, int64_t q_head, const float* lse, float scale, int causal, int32_t window,
+                            const uint64_t* mask, int64_t ld_mask, const int32_t* places, float decay, const float* before,
+                            float* after, int64_t ld, void* workspace, size_t ws_bytes, void* stream) {
+  const ApiRange range("crvq_kv_weights");
+  static const char* fn = "crvq_kv_weights";
+  g_err.clear();
+  KvCache c;
+  KvBatch bt;
+  // values are not read: the keys stand in their place
+  crvq_status s = check_cache(B, Hkv, D, page, n_pages, k_cache, k_cache, k_scale, k_scale, block_table, ld_table, start,
+                              kv_len, max_new, n_tokens, dtype, fn, &c, &bt);
+  if (s) return s;
+  if (Hq < 1 || Hq % Hkv) return fail(CRVQ_ERR_INVALID, "%s: Hq = %d is not a multiple of Hkv = %d", fn, Hq, Hkv);
+  if (max_kv < 0 || max_kv > CRVQ_KV_MAX_LEN)
+    return fail(CRVQ_ERR_INVALID, "%s: max_kv = %d outside [0, 2^30]", fn, max_kv);
+  if (!std::isfinite(scale) || !std::isfinite(decay)) return fail(CRVQ_ERR_INVALID, "%s: scale or decay is not finite", fn);
+  if (window < 0 || (window && !causal && !mask)) return fail(CRVQ_ERR_INVALID, "%s: window < 0, or a window without causal or mask", fn);
+  if (ld < max_kv) return fail(CRVQ_ERR_INVALID, "%s: ld = %lld below max_kv = %d", fn, (long long)ld, max_kv);
+  if (B == 0 || max_new == 0 || n_tokens == 0 || max_kv == 0) return CRVQ_OK;
+  if (static_cast<int64_t>(max_new) * (Hq / Hkv) > 0x7fffff00LL || static_cast<int64_t>(B) * Hkv > 65535)
+    return fail(CRVQ_ERR_UNSUPPORTED, "%s: more than 2^31 - 256 rows of a key head, or more than 65535 key heads of all sequences", fn);
+  if (mask && (s = check_tree(mask, ld_mask, places, max_new, fn))) return s;
+  if ((s = check_rows("q", q, q_tok, q_head, Hq, D, dtype, fn))) return s;
+  if (!lse || !after) return fail(CRVQ_ERR_INVALID, "%s: lse and after must not be NULL", fn);
+  if ((reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(before) | reinterpret_cast<uintptr_t>(after)) & 3)
+    return fail(CRVQ_ERR_INVALID, "%s: lse, before or after is not aligned to its type", fn);
+  const size_t w_n = static_cast<size_t>(B) * Hkv * ld * 4;
+  if ((before && before != after && overlaps(before, w_n, after, w_n)) ||
+      overlaps(after, w_n, q, extent(n_tokens, q_tok, Hq, q_head, D, esize(dtype))) ||
+      overlaps(after, w_n, lse, static_cast<size_t>(n_tokens) * Hq * 4) ||
+      (mask && overlaps(after, w_n, mask, mask_bytes(n_tokens, ld_mask))) ||
+      (mask && places && overlaps(after, w_n, places, static_cast<size_t>(n_tokens) * 4)))
+    return fail(CRVQ_ERR_INVALID, "%s: after overlaps an input without being before", fn);
+  if ((s = check_ws(workspace, ws_bytes, crvq_kv_weights_workspace_size(B, Hq, Hkv, D, max_new, max_kv), fn))) return s;
+  const KvWeights w = {lse, before, after, ld, scale, decay, mask ? 0 : causal ? 1 : 0, window, {mask, ld_mask, mask ? places : nullptr}};
+  return hip_status(launch_kv_weights(c, bt, max_kv, dtype, Hq, {const_cast<void*>(q), q_tok, q_head}, w, workspace,
+                                      static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+crvq_status crvq_kv_select(int32_t B, int32_t Hkv, const int32_t* kv_len, const float* weights, int64_t ld, int32_t budget,
+                           int32_t sinks, int32_t recent, int32_t* keep, int64_t ld_keep, int32_t* kept_len, float* kept_weights,
+                           void* stream) {
+  const ApiRange range("crvq_kv_select");
+  static const char* fn = "crvq_kv_select";
+  g_err.clear();
+  if (B < 0 || Hkv < 1) return fail(CRVQ_ERR_INVALID, "%s: B = %d, Hkv = %d", fn, B, Hkv);
+  if (budget < 0 || sinks < 0 || recent < 0 || static_cast<int64_t>(sinks) + recent > budget)
+    return fail(CRVQ_ERR_INVALID, "%s: sinks = %d and recent = %d do not fit a budget of %d", fn, sinks, recent, budget);
+  if (ld < 0 || ld > CRVQ_KV_MAX_LEN) return fail(CRVQ_ERR_INVALID, "%s: ld = %lld outside [0, 2^30]", fn, (long long)ld);
+  const int64_t most = budget < ld ? budget : ld;
+  if (ld_keep < most) return fail(CRVQ_ERR_INVALID, "%s: ld_keep = %lld below %lld tokens", fn, (long long)ld_keep, (long long)most);
+  if (static_cast<int64_t>(B) * Hkv > 0x7fffffffLL) return fail(CRVQ_ERR_UNSUPPORTED, "%s: B * Hkv exceeds 2^31 - 1", fn);
+  if (B == 0) return CRVQ_OK;
+  if (!kv_len || !kept_len || (ld > 0 && !weights) || (most > 0 && !keep))
+    return fail(CRVQ_ERR_INVALID, "%s: kv_len, weights, keep and kept_len must not be NULL", fn);
+  if ((reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(keep) |
+       reinterpret_cast<uintptr_t>(kept_len) | reinterpret_cast<uintptr_t>(kept_weights)) & 3)
+    return fail(CRVQ_ERR_INVALID, "%s: an array is not aligned to its type", fn);
+  const size_t heads = static_cast<size_t>(B) * Hkv, w_n = heads * ld * 4, k_n = heads * ld_keep * 4, l_n = static_cast<size_t>(B) * 4;
+  const struct {
+    const void* p;
+    size_t n;
+  } all[5] = {{keep, k_n}, {kept_len, l_n}, {kept_weights, kept_weights ? k_n : 0}, {weights, w_n}, {kv_len, l_n}};
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 5; ++j)
+      if (all[i].n && all[j].n && overlaps(all[i].p, all[i].n, all[j].p, all[j].n))
+        return fail(CRVQ_ERR_INVALID, "%s: an output overlaps another array", fn);
+  return hip_status(launch_kv_select(B, Hkv, kv_len, weights, ld, budget, sinks, recent, {keep, ld_keep, Hkv, kept_len},
+                                     kept_weights, static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+crvq_status crvq_kv_gather(int32_t B, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages, int8_t* k_cache, int8_t* v_cache,
+                           float* k_scale, float* v_scale, const int32_t* block_table, int64_t ld_table, const int32_t* kv_len,
+                           const int32_t* keep, int64_t ld_keep, int32_t keep_heads, const int32_t* kept_len, int32_t max_keep,
+                           const int32_t* to_table, int64_t ld_to, void* stream) {
+  const ApiRange range("crvq_kv_gather");
+  static const char* fn = "crvq_kv_gather";
+  g_err.clear();
+  KvCache c;
+  KvBatch bt;
+  crvq_status s = check_cache(B, Hkv, D, page, n_pages, k_cache, v_cache, k_scale, v_scale, block_table, ld_table, kv_len,
+                              kv_len, max_keep, 1, CRVQ_F32, fn, &c, &bt);
+  if (s) return s;
+  if (keep_heads != 1 && keep_heads != Hkv) return fail(CRVQ_ERR_INVALID, "%s: keep_heads = %d is neither 1 nor Hkv", fn, keep_heads);
+  if (ld_to < 0 || ld_keep < max_keep)
+    return fail(CRVQ_ERR_INVALID, "%s: ld_to < 0, or ld_keep = %lld below max_keep = %d", fn, (long long)ld_keep, max_keep);
+  if (B == 0 || max_keep == 0) return CRVQ_OK;
+  if (!keep || !kept_len || (ld_to > 0 && !to_table))
+    return fail(CRVQ_ERR_INVALID, "%s: keep, kept_len and to_table must not be NULL", fn);
+  const size_t page_bytes = static_cast<size_t>(n_pages) * Hkv * D * page, scales = static_cast<size_t>(n_pages) * Hkv * 4;
+  if (overlaps(k_cache, page_bytes, v_cache, page_bytes) || overlaps(k_scale, scales, v_scale, scales))
+    return fail(CRVQ_ERR_INVALID, "%s: the cache's arrays overlap", fn);
+  return hip_status(launch_kv_gather(c, B, block_table, ld_table, kv_len,
+                                     {const_cast<int32_t*>(keep), ld_keep, keep_heads, const_cast<int32_t*>(kept_len)}, max_keep,
+                                     to_table, ld_to, static_cast<hipStream_t>(stream)),
                     fn);
 }
 

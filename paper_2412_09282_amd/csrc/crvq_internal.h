@@ -282,10 +282,41 @@ hipError_t launch_kv_append(const KvCache& c, const KvBatch& bt, int type, const
                             const KvRows& q, const KvRows& q_out, const KvRotation& rt, hipStream_t stream);
 hipError_t launch_kv_read(const KvCache& c, const KvBatch& bt, int type, const KvRows& k_out, const KvRows& v_out,
                           hipStream_t stream);
+struct KvTree {  // which of its sequence's new tokens a row sees: bit j of its `ld` words is the j-th
+  const uint64_t* mask;  // NULL: none
+  int64_t ld;
+  const int32_t* places;  // of the rows, for the window; NULL: context + row
+};
 size_t kv_attention_ws_bytes(int B, int Hq, int Hkv, int D, int max_new, int max_kv);
 hipError_t launch_kv_attention(const KvCache& c, const KvBatch& bt, int max_kv, int type, int Hq, const KvRows& q,
-                               const KvRows& out, float scale, int causal, int window, float* lse, void* ws,
+                               const KvRows& out, float scale, int causal, int window, const KvTree& tree, float* lse, void* ws,
                                hipStream_t stream);
+
+// ---- drafts over the cache and the cache within a budget (k_evict.hip) ------------------------------
+hipError_t launch_tree_mask(int B, const int32_t* parents, const int32_t* start, const int32_t* kv_len, int max_new,
+                            int64_t n_tokens, int window, uint64_t* mask, int64_t ld, int32_t* places, hipStream_t stream);
+struct KvWeights {
+  const float* lse;     // [n_tokens][Hq]
+  const float* before;  // [B][Hkv][ld]; may be `after`, or NULL: nothing
+  float* after;
+  int64_t ld;
+  float scale, decay;
+  int causal, window;
+  KvTree tree;
+};
+size_t kv_weights_ws_bytes(int B, int Hq, int Hkv, int D, int max_new, int max_kv);
+hipError_t launch_kv_weights(const KvCache& c, const KvBatch& bt, int max_kv, int type, int Hq, const KvRows& q,
+                             const KvWeights& w, void* ws, hipStream_t stream);
+struct KvKeep {
+  int32_t* keep;  // [B][heads][ld]
+  int64_t ld;
+  int heads;      // Hkv, or 1: the same tokens for all
+  int32_t* len;   // [B]
+};
+hipError_t launch_kv_select(int B, int Hkv, const int32_t* kv_len, const float* weights, int64_t ld, int budget, int sinks,
+                            int recent, const KvKeep& k, float* kept_weights, hipStream_t stream);
+hipError_t launch_kv_gather(const KvCache& c, int B, const int32_t* table, int64_t ld_table, const int32_t* kv_len, const KvKeep& k,
+                            int max_keep, const int32_t* to, int64_t ld_to, hipStream_t stream);
 
 // ---- 4-bit matrices with group scales (k_w4.hip) --------------------------------------------------
 struct W4 {

@@ -52,6 +52,7 @@ struct AttnArgs {
   float *po, *pm, *pl;  // partial results [split][b][i][h][D], and their maxima and sums
   float scale;
   int Hq, G, causal, window, splits, tiles, o_vec;
+  KvTree tree;  // of the kernels with TREE
 };
 
 __device__ __forceinline__ float quarters_max(float x) {
@@ -153,8 +154,9 @@ __device__ __forceinline__ int ranked(const KvBatch& bt, int rank) {
 
 // The state of a wave's 16 QB columns; DT tiles of 16 elements hold a head.  HALF: keys come widened to fp16, and a
 // query row is fp16 relative to a power of two (a bf16 element keeps its 8 bits down to 2^-28 of the row's largest).
-// SMALL: the 16 tokens of a lane may have a page, and scales, of their own.
-template <typename T, int DT, int QB, bool HALF, bool SMALL>
+// SMALL: the 16 tokens of a lane may have a page, and scales, of their own.  TREE: of the sequence's new tokens a column
+// sees those whose bits its row of the mask has, before them what the window leaves of the context.
+template <typename T, int DT, int QB, bool HALF, bool SMALL, bool TREE>
 struct Columns {
   static constexpr int DC = HALF ? (DT + 1) / 2 : (DT + 3) / 4;      // chunks of a head: 32 (HALF) or 64 elements
   static constexpr int NT = HALF ? 1 : 3;                            // digits of a query element
@@ -163,6 +165,8 @@ struct Columns {
   float step[QB], m[QB], l[QB];
   int e[QB];                          // exponents that value scales are taken relative to
   int lo[QB], hi[QB];                 // the tokens a column sees
+  const uint64_t* bits[TREE ? QB : 1];  // rows of the mask
+  int context;                        // tokens before the new ones (TREE)
   float slack;                        // kSlack; once a maximum has passed kFar, so low that every step renews it
   int first, last, all_lo, all_hi;    // the tokens any of them sees, and those that all of them see
   at_f4 o[QB][DT];                    // in units of 2^(m + e - kLift)
@@ -215,7 +219,15 @@ struct Columns {
       }
       hi[n] = ok ? sq.len : 0;
       lo[n] = 0;
-      if (a.causal) {
+      if constexpr (TREE) {
+        context = sq.len - sq.n;
+        bits[n] = a.tree.mask + (sq.row0 + i) * a.tree.ld;
+        if (a.window) {
+          const int64_t place = a.tree.places ? a.tree.places[sq.row0 + i] : context + i;
+          const int64_t from = place + 1 - a.window;
+          lo[n] = static_cast<int>(from < 0 ? 0 : from < context ? from : max(context, 0));
+        }
+      } else if (a.causal) {
         const int place = sq.len - sq.n + i;
         hi[n] = min(hi[n], max(place + 1, 0));
         if (a.window) lo[n] = max(place + 1 - a.window, 0);
@@ -240,6 +252,18 @@ struct Columns {
     first = min(wave_min(first), last) & ~(kTokens - 1);
     all_lo = wave_max(all_lo);
     all_hi = wave_min(all_hi);
+    if constexpr (TREE) all_hi = min(all_hi, context);
+  }
+
+  // Which of the 16 tokens from `base` on the mask lets column n see: all of the context, of the new ones as their bits say.
+  __device__ __forceinline__ uint32_t drafted(const AttnArgs& a, int n, int base) const {
+    const int j = base - context;  // the first one's bit
+    if (j <= -16) return 0xffffu;
+    if (hi[n] <= base) return 0;  // and the mask's words end with the sequence's tokens
+    const int word = max(j, 0) >> 6, shift = max(j, 0) & 63;
+    uint64_t x = bits[n][word] >> shift;
+    if (shift > 48 && word + 1 < a.tree.ld) x |= bits[n][word + 1] << (64 - shift);
+    return static_cast<uint32_t>(j < 0 ? x << -j | ((1u << -j) - 1u) : x) & 0xffffu;
   }
 
   // The scores of 64 tokens, in query steps: key(u, ch) is the left operand of tile u and chunk ch.
@@ -285,7 +309,7 @@ struct Columns {
   }
 
   // Scores to weights; ks and vs are the scales of this lane's 16 tokens, `good` whether they can be used.
-  __device__ __forceinline__ void weigh(at_f4 (&s)[QB][4], int t0, float ks, float vs, bool good) {
+  __device__ __forceinline__ void weigh(const AttnArgs& a, at_f4 (&s)[QB][4], int t0, float ks, float vs, bool good) {
     const int c = (threadIdx.x >> 4) & 3;
     // the value scale as 2^ve times a number in [1/2, 1)
     const bool some = good && vs > 0.f;
@@ -303,6 +327,7 @@ struct Columns {
       for (int n = 0; n < QB; ++n) {
         const int x = min(max(lo[n] - base, 0), 16), y = min(max(hi[n] - base, 0), 16);
         seen[n] = ((1u << y) - 1u) & ~((1u << x) - 1u);
+        if constexpr (TREE) seen[n] &= drafted(a, n, base);
 #pragma unroll
         for (int j = 0; j < 16; ++j)
           if (!(seen[n] >> j & 1)) s[n][j >> 2][j & 3] = -kInf;  // stays below every score whatever its page's scale is
@@ -589,7 +614,7 @@ __device__ __forceinline__ void share_of(const AttnArgs& a, int split, int round
 // memory into the operands' registers, a step's keys while the step before is computed.  Reads bound it: 32 sequences
 // of 2048 to 4096 tokens (682 MB) take 133 us, 5.1 TB/s (a device copy, which writes as much as it reads, moves 4.9); one
 // sequence of 131001 tokens (268 MB) in 64 shares of 8 heads 62.5 us, 4.3 TB/s, 8 us of it the join.
-template <typename T, int DT, bool SMALL>
+template <typename T, int DT, bool SMALL, bool TREE>
 __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel(const AttnArgs a) {
   constexpr int kRow = DT * 16 + 4, kStride = 4 * kTokens;
   __shared__ __align__(16) float join[4 * 16 * kRow];
@@ -601,7 +626,7 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel
   const int cols = min(sq.n, a.bt.max_new) * a.G, col0 = pc.tile * 16;
   if (col0 >= cols) return;
   const bool ok = sq.ok && (sq.len == 0 || a.c.n_pages > 0);
-  Columns<T, DT, 1, false, SMALL> w;
+  Columns<T, DT, 1, false, SMALL, TREE> w;
   w.begin(a, sq, ok, pc.hk, col0, cols);
   int first = w.first, last = w.last;
   share_of(a, pc.split, kStride, first, last);
@@ -647,7 +672,7 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel
     if (t0 + kStride < last) load_keys(t0 + kStride, kp);
     vp = SMALL ? value_page(t0 + kStride) : kp;
     kp = key_page(t0 + 2 * kStride);
-    w.weigh(s, t0, ks, vs, good);
+    w.weigh(a, s, t0, ks, vs, good);
     w.template add<false>(s, [&](int d, int half) {
       asm volatile("" : "+v"(vreg[d]));  // widened where it is used, in every pass
       return widen<T>(vreg[d][2 * half], vreg[d][2 * half + 1]);
@@ -693,7 +718,7 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel
 // in one wave they come one after the other, as do scores, weights and values.  Two waves a SIMD hide a part of that (one: 1.95 for
 // 1.33 ms, when that was measured).  Smaller calls lose at their end, when the last workgroups run alone: two prompts of 2048 and
 // 393, 348 us (696 TFLOP/s; 360 to 382 with the calls in a graph, from one card to another).
-template <typename T, int DT, int QB, bool SMALL>
+template <typename T, int DT, int QB, bool SMALL, bool TREE>
 __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kernel(const AttnArgs a) {
   constexpr bool HALF = sizeof(T) == 2;
   constexpr int kKeyRow = DT * 16 * (HALF ? 2 : 1) + 16, kValueRow = kTokens * 2 + 16;
@@ -708,7 +733,7 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kern
   const int cols = min(sq.n, a.bt.max_new) * a.G, tile0 = pc.tile * (64 * QB), col0 = tile0 + wave * (16 * QB);
   if (tile0 >= cols) return;
   const bool ok = sq.ok && (sq.len == 0 || a.c.n_pages > 0), mine = col0 < cols;
-  Columns<T, DT, QB, HALF, SMALL> w;
+  Columns<T, DT, QB, HALF, SMALL, TREE> w;
   w.begin(a, sq, ok, pc.hk, min(col0, cols - 1), cols);
   // the workgroup's tokens
   int* shared = reinterpret_cast<int*>(lds);
@@ -818,7 +843,7 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_prompt_kern
       __builtin_amdgcn_s_setprio(1);
       w.template scores<true>(s, [&](int u, int ch) { return *reinterpret_cast<const at_i4*>(from + (u * 16 + r) * kKeyRow + ch * 64 + c * 16); });
       __builtin_amdgcn_s_setprio(0);
-      w.weigh(s, t0, ks, vs, good);
+      w.weigh(a, s, t0, ks, vs, good);
       __builtin_amdgcn_s_setprio(1);
       const uint8_t* v = from + kKeyBytes + r * kValueRow + c * 32;
       w.template add<true>(s, [&](int d, int half) { return *reinterpret_cast<const at_u4*>(v + d * 16 * kValueRow + half * 16); });
@@ -971,7 +996,7 @@ AttnWs carve_attention(WsCursor& c, const AttnPlan& p, int B, int Hq, int D, int
   return w;
 }
 
-template <typename T, int DT>
+template <typename T, int DT, bool TREE>
 hipError_t attend_as(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
   constexpr int QB = prompt_blocks(DT * 16);
   const int64_t blocks = static_cast<int64_t>(p.tiles) * p.splits * a.bt.B * a.c.Hkv;
@@ -980,20 +1005,20 @@ hipError_t attend_as(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
   const bool small = a.c.page_log2 < 6;
   const size_t lds = 2 * (kTokens * (DT * 16 * (sizeof(T) == 2 ? 2 : 1) + 16) + DT * 16 * (kTokens * 2 + 16));
   if (p.prompt) {
-    if (small) kv_attention_prompt_kernel<T, DT, QB, true><<<grid, 256, lds, stream>>>(a);
-    else kv_attention_prompt_kernel<T, DT, QB, false><<<grid, 256, lds, stream>>>(a);
+    if (small) kv_attention_prompt_kernel<T, DT, QB, true, TREE><<<grid, 256, lds, stream>>>(a);
+    else kv_attention_prompt_kernel<T, DT, QB, false, TREE><<<grid, 256, lds, stream>>>(a);
   } else {
-    if (small) kv_attention_step_kernel<T, DT, true><<<grid, 256, 0, stream>>>(a);
-    else kv_attention_step_kernel<T, DT, false><<<grid, 256, 0, stream>>>(a);
+    if (small) kv_attention_step_kernel<T, DT, true, TREE><<<grid, 256, 0, stream>>>(a);
+    else kv_attention_step_kernel<T, DT, false, TREE><<<grid, 256, 0, stream>>>(a);
   }
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, bool TREE>
 hipError_t attend(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
   const int D = a.c.D;
-  hipError_t e = D <= 64 ? attend_as<T, 4>(p, a, stream)
-                 : D <= 128 ? attend_as<T, 8>(p, a, stream) : attend_as<T, 16>(p, a, stream);
+  hipError_t e = D <= 64 ? attend_as<T, 4, TREE>(p, a, stream)
+                 : D <= 128 ? attend_as<T, 8, TREE>(p, a, stream) : attend_as<T, 16, TREE>(p, a, stream);
   if (e != hipSuccess || p.splits == 1) return e;
   const int64_t rows = static_cast<int64_t>(a.bt.B) * a.bt.max_new * a.Hq;
   if (rows > 0x7fffffffLL) return hipErrorInvalidConfiguration;
@@ -1015,15 +1040,16 @@ size_t kv_attention_ws_bytes(int B, int Hq, int Hkv, int D, int max_new, int max
 }
 
 hipError_t launch_kv_attention(const KvCache& c, const KvBatch& bt, int max_kv, int type, int Hq, const KvRows& q,
-                               const KvRows& out, float scale, int causal, int window, float* lse, void* ws,
+                               const KvRows& out, float scale, int causal, int window, const KvTree& tree, float* lse, void* ws,
                                hipStream_t stream) {
   const AttnPlan p = plan_attention(bt.B, Hq, c.Hkv, c.D, bt.max_new, max_kv);
   WsCursor cur(ws);
   const AttnWs w = carve_attention(cur, p, bt.B, Hq, c.D, bt.max_new);
-  AttnArgs a = {c, bt, q, out, lse, w.po, w.pm, w.pl, scale, Hq, Hq / c.Hkv, causal, window, p.splits, p.tiles, 0};
+  AttnArgs a = {c, bt, q, out, lse, w.po, w.pm, w.pl, scale, Hq, Hq / c.Hkv, causal, window, p.splits, p.tiles, 0, tree};
   const int es = type == ET_F32 ? 4 : 2;
   a.o_vec = (reinterpret_cast<uintptr_t>(out.p) % (4 * es)) == 0 && out.tok % 4 == 0 && out.head % 4 == 0;
-  return type == ET_F32 ? attend<uint32_t>(p, a, stream) : attend<uint16_t>(p, a, stream);
+  if (tree.mask) return type == ET_F32 ? attend<uint32_t, true>(p, a, stream) : attend<uint16_t, true>(p, a, stream);
+  return type == ET_F32 ? attend<uint32_t, false>(p, a, stream) : attend<uint16_t, false>(p, a, stream);
 }
 
 }  // namespace crvq
