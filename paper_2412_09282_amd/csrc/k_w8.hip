@@ -13,15 +13,16 @@ typedef int w8_i16 __attribute__((ext_vector_type(16)));
 template <typename X, typename Tile>
 __global__ __launch_bounds__(Tile::kBlock) void w8_quantize_kernel(const X* X_, int64_t ldx, int64_t rows, int N, int8_t* codes,
                                                                    int64_t ld, float* scales) {
-  __shared__ uint32_t red[16];
+  __shared__ uint32_t red[Tile::kRows][16];
   Tile tile;
   tile.N = N;
   tile.t = threadIdx.x % Tile::kThreads;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * Tile::kRows + threadIdx.x / Tile::kThreads;
-  if (row >= rows) return;  // whole waves
+  const int mine = threadIdx.x / Tile::kThreads;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * Tile::kRows + mine, row = at < rows ? at : rows - 1;
   float x[Tile::kVectors][8];
-  tile.load(X_ + row * ldx, x);
-  tile.quantize(x, codes + row * ld, scales + row, red);
+#pragma unroll
+  for (int v = 0; v < Tile::kVectors; ++v) tile.load(X_ + row * ldx, v, x[v]);
+  tile.quantize(x, codes + row * ld, scales + row, red[mine], at < rows);
 }
 
 constexpr int64_t kMostLd = int64_t{1} << 22;
@@ -314,23 +315,16 @@ hipError_t tile(const W8Args& a, hipStream_t stream) {
 
 hipError_t launch_w8_quantize(const void* X, int64_t ldx, int type, int64_t rows, int64_t N, int8_t* codes, int64_t ld,
                               float* scales, hipStream_t stream) {
-  const int es = type == ET_F32 ? 4 : 2;
-  auto as = [&](auto* p, auto vec) {
+  auto as = [&](auto* p) {
     using X_ = std::remove_const_t<std::remove_pointer_t<decltype(p)>>;
-    return with_row_tile<decltype(vec)::value>(N, [&](auto tile) {
+    return with_row_tile(N, [&](auto tile) {
       using Tile = decltype(tile);
       w8_quantize_kernel<X_, Tile><<<dim3(static_cast<uint32_t>(cdiv(rows, Tile::kRows))), Tile::kBlock, 0, stream>>>(
           p, ldx, rows, static_cast<int>(N), codes, ld, scales);
       return hipGetLastError();
     });
   };
-  const bool vec = N % 8 == 0 && reinterpret_cast<uintptr_t>(X) % 16 == 0 && ldx * es % 16 == 0;
-  if (type == ET_F32) {
-    const auto* p = static_cast<const uint32_t*>(X);
-    return vec ? as(p, std::true_type{}) : as(p, std::false_type{});
-  }
-  const auto* p = static_cast<const uint16_t*>(X);
-  return vec ? as(p, std::true_type{}) : as(p, std::false_type{});
+  return type == ET_F32 ? as(static_cast<const uint32_t*>(X)) : as(static_cast<const uint16_t*>(X));
 }
 
 namespace {
