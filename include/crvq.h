@@ -716,7 +716,8 @@ crvq_status crvq_norm(int64_t T, int64_t N, int kind, const void* x, int64_t ldx
  *                       n_cols = max_kv              (crvq_kv_attention)
  *   CRVQ_OP_W4_GEMV     M, N, K = T                  (crvq_w4_gemv)
  *   CRVQ_OP_W8_GEMM     M, N, K = T                  (crvq_w8_gemm)
- *   CRVQ_OP_KV_WEIGHTS  as CRVQ_OP_KV_ATTENTION      (crvq_kv_weights; crvq_kv_tree_attention's is CRVQ_OP_KV_ATTENTION)
+ *   CRVQ_OP_KV_WEIGHTS, CRVQ_OP_KV_TREE_ATTENTION  as CRVQ_OP_KV_ATTENTION
+ *                                                    (crvq_kv_weights, crvq_kv_tree_attention)
  * Returns 0 for an unknown op or a shape the call rejects (and for calls that
  * need no workspace at that shape).  Ks is a host array of n_books entries.
  */
@@ -734,7 +735,8 @@ typedef enum {
   CRVQ_OP_KV_ATTENTION = 10,
   CRVQ_OP_W4_GEMV = 11,
   CRVQ_OP_W8_GEMM = 12,
-  CRVQ_OP_KV_WEIGHTS = 13
+  CRVQ_OP_KV_WEIGHTS = 13,
+  CRVQ_OP_KV_TREE_ATTENTION = 14
 } crvq_op;
 size_t crvq_workspace_size(int op, int64_t n_vectors, int64_t K, int32_t beam, int32_t n_books, int32_t d,
                            const int64_t* Ks, int64_t M, int64_t N, int64_t n_cols);

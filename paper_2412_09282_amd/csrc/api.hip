@@ -755,6 +755,11 @@ size_t crvq_workspace_size(int op, int64_t n_vectors, int64_t K, int32_t beam, i
                                               static_cast<int32_t>(N), d, static_cast<int32_t>(K),
                                               static_cast<int32_t>(n_cols));
     case CRVQ_OP_W4_GEMV: return crvq_w4_gemv_workspace_size(M, N, K);
+    case CRVQ_OP_KV_TREE_ATTENTION:
+      if (n_vectors > 0x7fffffffLL || M > 0x7fffffffLL || N > 0x7fffffffLL || K > 0x7fffffffLL || n_cols > 0x7fffffffLL) return 0;
+      return crvq_kv_tree_attention_workspace_size(static_cast<int32_t>(n_vectors), static_cast<int32_t>(M),
+                                                   static_cast<int32_t>(N), d, static_cast<int32_t>(K),
+                                                   static_cast<int32_t>(n_cols));
     case CRVQ_OP_KV_WEIGHTS:
       if (n_vectors > 0x7fffffffLL || M > 0x7fffffffLL || N > 0x7fffffffLL || K > 0x7fffffffLL || n_cols > 0x7fffffffLL) return 0;
       return crvq_kv_weights_workspace_size(static_cast<int32_t>(n_vectors), static_cast<int32_t>(M), static_cast<int32_t>(N), d,
@@ -942,7 +947,7 @@ crvq_status crvq_kv_read(int32_t B, int32_t Hkv, int32_t D, int32_t page, int64_
 
 size_t crvq_kv_attention_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new, int32_t max_kv) {
   if (B < 1 || Hkv < 1 || Hq < Hkv || Hq % Hkv || D < 16 || D > CRVQ_KV_MAX_D || D % 16 || max_new < 1 || max_kv < 0) return 0;
-  return kv_attention_ws_bytes(B, Hq, Hkv, D, max_new, max_kv);
+  return kv_attention_ws_bytes(B, Hq, Hkv, D, max_new, max_kv, false);
 }
 
 crvq_status crvq_kv_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages,
@@ -1021,7 +1026,8 @@ crvq_status crvq_tree_mask(int32_t B, const int32_t* parents, const int32_t* sta
 }
 
 size_t crvq_kv_tree_attention_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new, int32_t max_kv) {
-  return crvq_kv_attention_workspace_size(B, Hq, Hkv, D, max_new, max_kv);
+  if (B < 1 || Hkv < 1 || Hq < Hkv || Hq % Hkv || D < 16 || D > CRVQ_KV_MAX_D || D % 16 || max_new < 1 || max_kv < 0) return 0;
+  return kv_attention_ws_bytes(B, Hq, Hkv, D, max_new, max_kv, true);
 }
 
 crvq_status crvq_kv_tree_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages,

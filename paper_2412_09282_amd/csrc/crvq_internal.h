@@ -287,7 +287,7 @@ struct KvTree {  // which of its sequence's new tokens a row sees: bit j of its 
   int64_t ld;
   const int32_t* places;  // of the rows, for the window; NULL: context + row
 };
-size_t kv_attention_ws_bytes(int B, int Hq, int Hkv, int D, int max_new, int max_kv);
+size_t kv_attention_ws_bytes(int B, int Hq, int Hkv, int D, int max_new, int max_kv, bool tree);
 hipError_t launch_kv_attention(const KvCache& c, const KvBatch& bt, int max_kv, int type, int Hq, const KvRows& q,
                                const KvRows& out, float scale, int causal, int window, const KvTree& tree, float* lse, void* ws,
                                hipStream_t stream);

@@ -155,8 +155,9 @@ __device__ __forceinline__ int ranked(const KvBatch& bt, int rank) {
 // The state of a wave's 16 QB columns; DT tiles of 16 elements hold a head.  HALF: keys come widened to fp16, and a
 // query row is fp16 relative to a power of two (a bf16 element keeps its 8 bits down to 2^-28 of the row's largest).
 // SMALL: the 16 tokens of a lane may have a page, and scales, of their own.  TREE: of the sequence's new tokens a column
-// sees those whose bits its row of the mask has, before them what the window leaves of the context.
-template <typename T, int DT, int QB, bool HALF, bool SMALL, bool TREE>
+// sees those whose bits its row of the mask has, before them what the window leaves of the context.  PAIRS: a lane's elements of two chunks
+// of 32 are 16 neighbours, the first eight and the others, as it has a key's codes in 16 bytes.
+template <typename T, int DT, int QB, bool HALF, bool SMALL, bool TREE, bool PAIRS = false>
 struct Columns {
   static constexpr int DC = HALF ? (DT + 1) / 2 : (DT + 3) / 4;      // chunks of a head: 32 (HALF) or 64 elements
   static constexpr int NT = HALF ? 1 : 3;                            // digits of a query element
@@ -180,11 +181,12 @@ struct Columns {
       const int i = col / a.G, h = hk * a.G + col - i * a.G;
       const T* row = static_cast<const T*>(a.q.p) + (sq.row0 + i) * a.q.tok + h * a.q.head;
       constexpr int E = HALF ? 8 : 16;
+      auto first_of = [c](int ch) { return PAIRS ? (ch >> 1) * 64 + c * 16 + (ch & 1) * 8 : (ch * 4 + c) * E; };
       uint32_t most = 0;
 #pragma unroll
       for (int ch = 0; ch < DC; ++ch)
-        if ((ch * 4 + c) * E < D)
-          for (int x = 0; x < E; ++x) most = max(most, __float_as_uint(elem(row, (ch * 4 + c) * E + x)) & 0x7fffffffu);
+        if (first_of(ch) < D)
+          for (int x = 0; x < E; ++x) most = max(most, __float_as_uint(elem(row, first_of(ch) + x)) & 0x7fffffffu);
       most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 16)));
       most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32)));
       const bool finite = most < 0x7f800000u;
@@ -194,7 +196,7 @@ struct Columns {
       step[n] = !finite ? __uint_as_float(0x7fc00000u) : static_cast<float>(HALF ? ldexp(slope, -up) : size / kSteps * slope);
 #pragma unroll
       for (int ch = 0; ch < DC; ++ch) {
-        const int at = (ch * 4 + c) * E;
+        const int at = first_of(ch);
         if constexpr (HALF) {
           at_h8 h = {};
           if (finite && at < D) {
@@ -709,6 +711,160 @@ __global__ __launch_bounds__(256, DT <= 8 ? 2 : 1) void kv_attention_step_kernel
   }
 }
 
+// A load from a place that is the same for the whole wave, on the scalar unit: its wait is not one for the vector loads on their way.
+template <typename V>
+__device__ __forceinline__ V scalar_load(const V* p) {
+  const uint64_t at = reinterpret_cast<uintptr_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
+  return *reinterpret_cast<const __attribute__((address_space(4))) V*>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// A tree's columns, 17 to 96 of them: the four waves of a workgroup share 16 QB columns and take turns at the tokens, so that the
+// cache is read once.  The registers hold the columns; a step's codes wait in LDS, where the loads themselves put them: a lane's 16
+// bytes of each load in its own place, so that nobody else waits for them.  A step's keys are asked for as soon as the scores
+// of the step before are done, its values as soon as theirs are added.  32 sequences of up to 4096 tokens with drafts of up to 24 by
+// 32 heads of 128 (746 MB): 169 us, 4.4 TB/s.
+template <typename T, int DT, int QB, bool SMALL>
+__global__ __launch_bounds__(256, 2) void kv_attention_draft_kernel(const AttnArgs a) {
+  constexpr int kRow = DT * 16 + 4, kStride = 4 * kTokens, kCols = 16 * QB, DK = (DT + 3) / 4;
+  constexpr int kKeys = 4 * DK, kPieces = kKeys + DT;  // loads of a step
+  extern __shared__ __align__(16) uint8_t lds[];       // [4 waves][kPieces][64 lanes][16]; at the end the waves' results
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, c = lane >> 4;
+  const int D = a.c.D, pl2 = a.c.page_log2, in_page = (1 << pl2) - 1;
+  const Place pc = place_of(a);
+  const KvSeq sq = kv_seq(a.bt, pc.b, pl2);
+  const int cols = min(sq.n, a.bt.max_new) * a.G, col0 = pc.tile * kCols;
+  if (col0 >= cols) return;
+  const bool ok = sq.ok && (sq.len == 0 || a.c.n_pages > 0);
+  Columns<T, DT, QB, true, SMALL, true, true> w;
+  w.begin(a, sq, ok, pc.hk, col0, cols);
+  int first = w.first, last = w.last;
+  share_of(a, pc.split, kStride, first, last);
+  const int from = first + wave * kTokens;
+
+  const Pages pages = {a.bt.table + static_cast<int64_t>(pc.b) * a.bt.ld_table, a.c.n_pages, sq.len, pl2};
+  const int group = r >> 2;  // the 16 tokens of a step that this lane's row of a key tile belongs to
+  auto page_at = [&](int t, int t0) -> int {
+    if (t0 >= last) return 0;
+    const int at = (t < sq.len ? t : t0) >> pl2;
+    if constexpr (SMALL) return pages.table[at];
+    else return scalar_load(pages.table + at);
+  };
+  auto head_of = [&](int p) { return static_cast<int64_t>(pages.there(p) ? p : 0) * a.c.Hkv + pc.hk; };
+  auto key_page = [&](int t0) { return page_at(SMALL ? t0 + 16 * group : t0, t0); };
+  auto value_page = [&](int t0) { return page_at(SMALL ? t0 + 16 * c : t0, t0); };
+  auto scale_at = [&](const float* p) -> float {
+    if constexpr (SMALL) return *p;
+    else return scalar_load(p);
+  };
+  const int64_t head_bytes = static_cast<int64_t>(D) << pl2;
+  uint32_t koff[DK];
+#pragma unroll
+  for (int ch = 0; ch < DK; ++ch)  // past D the queries are 0, and any codes will do
+    koff[ch] = ((SMALL ? 0 : 16 * group) + (r & 3)) * D + (ch * 64 + c * 16 < D ? ch * 64 + c * 16 : 0);
+  const uint32_t voff = (static_cast<uint32_t>(r) << pl2) + (SMALL ? 0 : 16 * c);
+  const int tiles = D >> 4;
+  uint8_t* store = lds + wave * (kPieces * 1024);
+  auto piece = [&](int i) { return *reinterpret_cast<const at_i4*>(store + i * 1024 + lane * 16); };
+  auto ask = [&](const int8_t* p, int i) {
+    __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uintptr_t>(p)),
+                                     reinterpret_cast<__attribute__((address_space(3))) void*>(
+                                         static_cast<uint32_t>(reinterpret_cast<uintptr_t>(store + i * 1024))), 16, 0, 0);
+  };
+  auto ask_keys = [&](int t0, int p) {
+    const int8_t* k = a.c.k + head_of(p) * head_bytes + ((SMALL ? t0 + 16 * group : t0) & in_page) * D;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int ch = 0; ch < DK; ++ch) ask(k + (koff[ch] + 4 * u * D), u * DK + ch);
+  };
+  auto ask_values = [&](int t0, int p) {
+    const int8_t* v = a.c.v + head_of(p) * head_bytes + ((SMALL ? t0 + 16 * c : t0) & in_page);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) ask(v + ((static_cast<int64_t>(min(d, tiles - 1) * 16) << pl2) + voff), kKeys + d);
+  };
+
+  // pages are looked up two steps ahead, scales read one step ahead
+  int kp = key_page(from), vp = SMALL ? value_page(from) : kp;
+  float ks_next = 0.f, vs_next = 0.f;
+  bool good_next = false;
+  auto ask_scales = [&](int p) {
+    const int64_t head = head_of(p);
+    ks_next = scale_at(a.c.k_scale + head);
+    vs_next = scale_at(a.c.v_scale + head);
+    good_next = pages.there(p);
+  };
+  if (from < last) {
+    ask_scales(vp);
+    ask_keys(from, kp);
+    ask_values(from, vp);
+  }
+  kp = key_page(from + kStride);
+  vp = SMALL ? value_page(from + kStride) : kp;
+  for (int t0 = from; t0 < last; t0 += kStride) {
+    const float ks = ks_next, vs = vs_next;
+    const bool good = good_next && usable(ks, vs);
+    // The step after the last one is asked for too, as its tokens' place in page 0, and never read: what is on its way is then always
+    // known.  At most what was asked for after the keys may be now: the values.
+    const int t1 = t0 + kStride;
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(DT) : "memory");
+    at_f4 s[QB][4];
+    w.template scores<false>(s, [&](int u, int ch) {
+      const at_i4 k = piece(u * DK + (ch >> 1));
+      return __builtin_bit_cast(at_i4, widen<T>(k[2 * (ch & 1)], k[2 * (ch & 1) + 1]));
+    });
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the keys have been read
+    ask_scales(vp);
+    ask_keys(t1, kp);
+    w.weigh(a, s, t0, ks, vs, good);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kKeys) : "memory");
+    w.template add<false>(s, [&](int d, int half) {
+      const at_i4 v = piece(kKeys + d);
+      return widen<T>(v[2 * half], v[2 * half + 1]);
+    });
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    ask_values(t1, vp);
+    kp = key_page(t1 + kStride);
+    vp = SMALL ? value_page(t1 + kStride) : kp;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing comes to LDS any more
+  w.end();
+
+  float* join = reinterpret_cast<float*>(lds);  // [4][kCols][kRow], then the maxima and sums
+  float *join_m = join + 4 * kCols * kRow, *join_l = join_m + 4 * kCols;
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < QB; ++n) {
+    const int at0 = wave * kCols + n * 16 + r;
+    if (c == 0) {
+      join_m[at0] = w.m[n];
+      join_l[at0] = w.l[n];
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<at_f4*>(join + at0 * kRow + d * 16 + 4 * c) = w.o[n][d];
+  }
+  __syncthreads();
+  const Results<T> out = {a, sq, pc, ok};
+  for (int x = threadIdx.x; x < kCols * DT * 4; x += 256) {
+    const int col = x / (DT * 4), d = (x - col * (DT * 4)) * 4;
+    if (col0 + col >= cols) break;
+    float mm = -kInf;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mm = fmaxf(mm, join_m[k * kCols + col]);
+    float ll = 0.f;
+    at_f4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int at = k * kCols + col;
+      const float f = join_m[at] == -kInf ? 0.f : __builtin_amdgcn_exp2f(join_m[at] - mm);
+      ll = fmaf(f, join_l[at], ll);
+      y += f * *reinterpret_cast<const at_f4*>(join + at * kRow + d);
+    }
+    if (d == 0) out.stats(col0 + col, mm, ll);
+    out.put(col0 + col, d, y, ll);
+  }
+}
+
 // Many columns: every wave has 16 QB of its own, and the four of a workgroup walk the same tokens.  A step's keys
 // and values pass through LDS, two steps of them, widened once for all four waves (keys of fp32 queries as they are).  Rows of
 // LDS are padded by 16 bytes, and a key's row is u * 16 + r for the token that is row r of tile u, so that the 16 rows
@@ -963,19 +1119,27 @@ __global__ __launch_bounds__(256) void kv_attention_join_rows_kernel(const AttnA
 // cost a long sequence 68 us instead of 64 and prompts with heads of 192 elements 437 instead of 318).  One tile of columns: its workgroups' four waves share the columns (16) and take turns at the
 // tokens; more: every wave has 16 prompt_blocks columns of its own.  Tokens are split over workgroups until
 // kWorkgroups are at work, a share being at least kShare tokens.
+// The drafts of a tree are few rows of their own, and tiles that share the columns do not leave most of the prompts' 128 empty: bf16 up to
+// 96 columns in tiles of 32 (us, 32 sequences of up to 4096 tokens, 32 heads: 24 columns 169 for 307, 40 203 for 347, 96 318 for 386;
+// 240 columns of 8 sequences of 8000 tokens 114 for 95; all of a wave's 64 columns at once 272 for the 40), fp32 up to 64 and
+// bf16 heads of more than 128 elements up to 48 in tiles of 16 (16 sequences of up to 4000 tokens, 16 heads: fp32 24 columns 67
+// for 156, 64 103 for 154; heads of 256 24 columns 124 for 175, 48 156 for 177, 64 of 4 sequences 59 for 46).
 struct AttnPlan {
   bool prompt;
-  int tiles, splits;
+  int tiles, splits, blocks;  // blocks: of 16 columns that each wave has where the four share them
 };
 constexpr int prompt_blocks(int D) { return D <= 128 ? 2 : 1; }  // what the registers hold
 constexpr int64_t kWorkgroups = 512;
 constexpr int kFewSplits = 8;
 constexpr int kShare = 512;
-AttnPlan plan_attention(int B, int Hq, int Hkv, int D, int max_new, int max_kv) {
+constexpr int kDraftColumns = 96;
+AttnPlan plan_attention(int B, int Hq, int Hkv, int D, int max_new, int max_kv, bool tree, bool wide) {
   AttnPlan p;
   const int64_t cols = static_cast<int64_t>(max_new) * (Hq / Hkv);
-  p.prompt = cols > 16;
-  p.tiles = static_cast<int>(cdiv(cols, p.prompt ? 64 * prompt_blocks(D) : 16));
+  const bool draft = tree && !wide && D <= 128;
+  p.blocks = draft && cols > 16 && cols <= kDraftColumns ? 2 : 1;
+  p.prompt = cols > (tree && !draft ? wide ? 64 : 48 : 16) && p.blocks == 1;
+  p.tiles = static_cast<int>(cdiv(cols, p.prompt ? 64 * prompt_blocks(D) : 16 * p.blocks));
   const int64_t groups = static_cast<int64_t>(B) * Hkv * p.tiles;
   const int64_t most = cdiv(max_kv, kShare), want = cdiv(kWorkgroups, groups);
   const int64_t n = want < most ? want : most;
@@ -996,6 +1160,15 @@ AttnWs carve_attention(WsCursor& c, const AttnPlan& p, int B, int Hq, int D, int
   return w;
 }
 
+template <typename T, int DT, int QB>
+hipError_t draft_as(bool small, const AttnArgs& a, dim3 grid, hipStream_t stream) {
+  constexpr size_t codes = 4 * (4 * ((DT + 3) / 4) + DT) * 1024, join = 4 * 16 * QB * (DT * 16 + 4 + 2) * sizeof(float);
+  const size_t lds = codes > join ? codes : join;
+  if (small) kv_attention_draft_kernel<T, DT, QB, true><<<grid, 256, lds, stream>>>(a);
+  else kv_attention_draft_kernel<T, DT, QB, false><<<grid, 256, lds, stream>>>(a);
+  return hipGetLastError();
+}
+
 template <typename T, int DT, bool TREE>
 hipError_t attend_as(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
   constexpr int QB = prompt_blocks(DT * 16);
@@ -1008,6 +1181,9 @@ hipError_t attend_as(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
     if (small) kv_attention_prompt_kernel<T, DT, QB, true, TREE><<<grid, 256, lds, stream>>>(a);
     else kv_attention_prompt_kernel<T, DT, QB, false, TREE><<<grid, 256, lds, stream>>>(a);
   } else {
+    if constexpr (TREE && sizeof(T) == 2 && DT <= 8) {
+      if (p.blocks == 2) return draft_as<T, DT, 2>(small, a, grid, stream);
+    }
     if (small) kv_attention_step_kernel<T, DT, true, TREE><<<grid, 256, 0, stream>>>(a);
     else kv_attention_step_kernel<T, DT, false, TREE><<<grid, 256, 0, stream>>>(a);
   }
@@ -1033,16 +1209,21 @@ hipError_t attend(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-size_t kv_attention_ws_bytes(int B, int Hq, int Hkv, int D, int max_new, int max_kv) {
-  WsCursor c(nullptr);
-  carve_attention(c, plan_attention(B, Hq, Hkv, D, max_new, max_kv), B, Hq, D, max_new);
-  return c.used;
+// What either type of queries needs.
+size_t kv_attention_ws_bytes(int B, int Hq, int Hkv, int D, int max_new, int max_kv, bool tree) {
+  size_t most = 0;
+  for (const bool wide : {false, true}) {
+    WsCursor c(nullptr);
+    carve_attention(c, plan_attention(B, Hq, Hkv, D, max_new, max_kv, tree, wide), B, Hq, D, max_new);
+    if (c.used > most) most = c.used;
+  }
+  return most;
 }
 
 hipError_t launch_kv_attention(const KvCache& c, const KvBatch& bt, int max_kv, int type, int Hq, const KvRows& q,
                                const KvRows& out, float scale, int causal, int window, const KvTree& tree, float* lse, void* ws,
                                hipStream_t stream) {
-  const AttnPlan p = plan_attention(bt.B, Hq, c.Hkv, c.D, bt.max_new, max_kv);
+  const AttnPlan p = plan_attention(bt.B, Hq, c.Hkv, c.D, bt.max_new, max_kv, tree.mask != nullptr, type == ET_F32);
   WsCursor cur(ws);
   const AttnWs w = carve_attention(cur, p, bt.B, Hq, c.D, bt.max_new);
   AttnArgs a = {c, bt, q, out, lse, w.po, w.pm, w.pl, scale, Hq, Hq / c.Hkv, causal, window, p.splits, p.tiles, 0, tree};
