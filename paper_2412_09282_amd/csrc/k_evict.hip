@@ -74,6 +74,26 @@ __device__ __forceinline__ ev_b8 widen8(int a, int b) {
   return __builtin_bit_cast(ev_b8, v);
 }
 
+// A load from a place that is the same for the whole wave, on the scalar unit.
+template <typename V>
+__device__ __forceinline__ V scalar_load(const V* p) {
+  const uint64_t at = reinterpret_cast<uintptr_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
+  return *reinterpret_cast<const __attribute__((address_space(4))) V*>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// 16 or 4 bytes of every lane to LDS, one lane's after the other's from `to` on, which is the same for the whole wave.
+typedef const __attribute__((address_space(1))) void* global_ptr;
+typedef __attribute__((address_space(3))) void* lds_ptr;
+__device__ __forceinline__ void load_lds16(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds(reinterpret_cast<global_ptr>(reinterpret_cast<uintptr_t>(from)),
+                                   reinterpret_cast<lds_ptr>(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(to))), 16, 0, 0);
+}
+__device__ __forceinline__ void load_lds4(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds(reinterpret_cast<global_ptr>(reinterpret_cast<uintptr_t>(from)),
+                                   reinterpret_cast<lds_ptr>(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(to))), 4, 0, 0);
+}
+
 // Sums over the 16 lanes of a row, in every one of them.
 __device__ __forceinline__ float row_sum(float x) {
   auto add = [&](auto ror) {
@@ -86,8 +106,40 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// 16 columns: their queries as right operands, what they see, and their log-sum-exps in powers of two.  DC chunks of 64 elements hold a head; a lane's 16
-// elements of a chunk lie as the 16 code bytes it has of a token, the first eight in one instruction, the others in the next.
+// What a lane reads of a column's query: 16 elements of a chunk of 64, as it has 16 code bytes of a token.
+template <typename T, int DC>
+struct RawQuery {
+  static constexpr int NV = sizeof(T) == 4 ? 4 : 2;
+  ev_u4 x[DC][NV];
+  float lse;
+
+  // query row i, head g of the key head; always one that there is
+  __device__ __forceinline__ void load(const WeightArgs& a, const KvSeq& sq, int hk, int i, int g) {
+    const int c = (threadIdx.x >> 4) & 3, h = hk * a.G + g;
+    const int64_t row = sq.row0 + i;
+    lse = a.w.lse[row * a.Hq + h];
+    const T* p = static_cast<const T*>(a.q.p) + row * a.q.tok + h * a.q.head;
+#pragma unroll
+    for (int ch = 0; ch < DC; ++ch) {
+      const T* e = p + (ch * 64 + c * 16 < a.c.D ? ch * 64 + c * 16 : 0);  // past D the codes are 0
+      if (a.q_vec) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) x[ch][v] = *reinterpret_cast<const ev_u4*>(e + v * (16 / NV));
+      } else {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if constexpr (NV == 4) x[ch][v][k] = e[v * 4 + k];
+            else x[ch][v][k] = e[v * 8 + 2 * k] | static_cast<uint32_t>(e[v * 8 + 2 * k + 1]) << 16;
+          }
+      }
+    }
+  }
+};
+
+// 16 columns: their queries as right operands, what they see, and their log-sum-exps in powers of two.  DC chunks of 64 elements hold a
+// head; the first eight of a lane's 16 elements of a chunk are of one instruction, the others of the next.
 template <typename T, int DC>
 struct Queries {
   static constexpr int NT = sizeof(T) == 4 ? 3 : 1;
@@ -96,46 +148,25 @@ struct Queries {
   int lo, hi;
   const uint64_t* bits;
 
-  __device__ __forceinline__ void load(const WeightArgs& a, const KvSeq& sq, int hk, int col, int cols) {
-    const int c = (threadIdx.x >> 4) & 3, i = col / a.G, h = hk * a.G + col - i * a.G;
-    const int64_t row = sq.row0 + i;
-    float lse = -kInf;
-    if (col < cols) lse = a.w.lse[row * a.Hq + h];
-    const bool ok = fabsf(lse) < kInf;  // neither a row that sees nothing nor one that is NaN has weights
-    lse2 = lse * kLog2e;
-    lo = hi = 0;
-    bits = nullptr;
-    const T* p = static_cast<const T*>(a.q.p) + row * a.q.tok + h * a.q.head + c * 16;
+  // The operands; `ok`: of a row that has weights.
+  __device__ __forceinline__ void operands(const RawQuery<T, DC>& raw, bool ok) {
+    lse2 = ok ? raw.lse * kLog2e : 0.f;
 #pragma unroll
     for (int ch = 0; ch < DC; ++ch) {
-      const bool there = ok && ch * 64 + c * 16 < a.c.D;
-      if constexpr (sizeof(T) == 2) {
-        ev_u4 x[2] = {};
-        if (there) {
-          if (a.q_vec) {
-            x[0] = *reinterpret_cast<const ev_u4*>(p + ch * 64);
-            x[1] = *reinterpret_cast<const ev_u4*>(p + ch * 64 + 8);
-          } else {
+      if constexpr (NT == 1) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e >> 3][(e >> 1) & 3] |= static_cast<uint32_t>(p[ch * 64 + e]) << (16 * (e & 1));
-          }
+        for (int half = 0; half < 2; ++half) {
+          ev_u4 v = raw.x[ch][half];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = ok ? v[k] : 0u;
+          q[ch][half][0] = __builtin_bit_cast(ev_b8, v);
         }
-        q[ch][0][0] = __builtin_bit_cast(ev_b8, x[0]);
-        q[ch][1][0] = __builtin_bit_cast(ev_b8, x[1]);
       } else {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          float x[8] = {};
-          if (there) {
-            const float* f = reinterpret_cast<const float*>(p) + ch * 64 + half * 8;
-            if (a.q_vec) {
-              const float4 u = *reinterpret_cast<const float4*>(f), v = *reinterpret_cast<const float4*>(f + 4);
-              x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
-            } else {
+          float x[8];
 #pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = f[e];
-            }
-          }
+          for (int e = 0; e < 8; ++e) x[e] = ok ? __uint_as_float(raw.x[ch][2 * half + (e >> 2)][e & 3]) : 0.f;
 #pragma unroll
           for (int t = 0; t < 3; ++t) {  // the upper halves, then what they leave
             ev_u4 v;
@@ -148,10 +179,18 @@ struct Queries {
         }
       }
     }
+  }
+  __device__ __forceinline__ void set_plain(const RawQuery<T, DC>& raw) { operands(raw, true); }
+  __device__ __forceinline__ void set(const WeightArgs& a, const KvSeq& sq, const RawQuery<T, DC>& raw, int i, bool there) {
+    const bool ok = there && fabsf(raw.lse) < kInf;  // neither a row that sees nothing nor one that is NaN has weights
+    operands(raw, ok);
+    lo = hi = 0;
+    bits = nullptr;
     if (!ok) return;
     const int context = sq.len - sq.n;
     hi = sq.len;
     if (a.w.tree.mask) {
+      const int64_t row = sq.row0 + i;
       bits = a.w.tree.mask + row * a.w.tree.ld;
       if (a.w.window) {
         const int64_t from = static_cast<int64_t>(a.w.tree.places ? a.w.tree.places[row] : context + i) + 1 - a.w.window;
@@ -163,71 +202,172 @@ struct Queries {
     }
   }
 
-  // whether this lane's column sees token t; context: tokens before the new ones
-  __device__ __forceinline__ bool sees(int t, int context) const {
-    if (t < lo || t >= hi) return false;
-    const int j = t - context;
-    return !bits || j < 0 || (bits[j >> 6] >> (j & 63) & 1);
+  // Which of the tokens t .. t + 3 this lane's column sees; context: tokens before the new ones.
+  __device__ __forceinline__ uint32_t sees(int t, int context) const {
+    const int x = min(max(lo - t, 0), 4), y = min(max(hi - t, 0), 4);
+    uint32_t m = ((1u << y) - 1u) & ~((1u << x) - 1u);
+    if (bits && t + 3 >= context && m) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int j = t + i - context;
+        if (j >= 0 && (m >> i & 1) && !(bits[j >> 6] >> (j & 63) & 1)) m &= ~(1u << i);
+      }
+    }
+    return m;
   }
 };
 
-// 64 tokens of a wave: their codes as left operands, their scales, and the sums so far.
+// 64 tokens of a wave, in four tiles of 16 that each lie in one page: their codes as they are in memory, and their scales.
 template <int DC>
-struct Tokens {
-  ev_b8 k[4][DC][2];
-  float ks[4];
-  bool good[4];
-  ev_f4 sum[4];
+struct RawTokens {
+  ev_i4 k[4][DC];
+  float ks[4];  // with the softmax's scale, in powers of two; 0 where `good` is not
+  uint32_t good;  // tiles whose page and scale can be used
 
   __device__ __forceinline__ void load(const WeightArgs& a, const KvSeq& sq, int b, int hk, int t0) {
     const int r = threadIdx.x & 15, c = (threadIdx.x >> 4) & 3, D = a.c.D, pl2 = a.c.page_log2;
+    const int32_t* table = a.bt.table + b * a.bt.ld_table;
+    int64_t head[4];
+    good = 0;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int t = t0 + 16 * u;  // the tile's tokens lie in one page
-      const int page = t < sq.len ? a.bt.table[b * a.bt.ld_table + (t >> pl2)] : -1;
-      good[u] = static_cast<uint32_t>(page) < static_cast<uint32_t>(a.c.n_pages);
-      const int64_t head = static_cast<int64_t>(good[u] ? page : 0) * a.c.Hkv + hk;
-      ks[u] = good[u] ? a.c.k_scale[head] : 0.f;
-      good[u] = good[u] && ks[u] >= 0.f && ks[u] < kInf;
-      const int8_t* p = a.c.k + ((head << pl2) + ((t & ((1 << pl2) - 1)) + r)) * D + c * 16;
-      sum[u] = ev_f4{0.f, 0.f, 0.f, 0.f};
+      const int t = t0 + 16 * u, page = t < sq.len ? scalar_load(table + (t >> pl2)) : -1;
+      const bool there = static_cast<uint32_t>(page) < static_cast<uint32_t>(a.c.n_pages);
+      good |= there ? 1u << u : 0u;
+      head[u] = static_cast<int64_t>(there ? page : 0) * a.c.Hkv + hk;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int t = t0 + 16 * u;
+      const int8_t* p = a.c.k + ((head[u] << pl2) + ((t & ((1 << pl2) - 1)) + r)) * D + c * 16;
 #pragma unroll
       for (int ch = 0; ch < DC; ++ch) {
-        ev_i4 x = {0, 0, 0, 0};
-        if (good[u] && ch * 64 + c * 16 < D) x = *reinterpret_cast<const ev_i4*>(p + ch * 64);
-        k[u][ch][0] = widen8(x[0], x[1]);
-        k[u][ch][1] = widen8(x[2], x[3]);
+        k[u][ch] = ev_i4{0, 0, 0, 0};
+        if ((good >> u & 1) && ch * 64 + c * 16 < D) k[u][ch] = *reinterpret_cast<const ev_i4*>(p + ch * 64);
       }
-      ks[u] = good[u] ? ks[u] * (a.w.scale * kLog2e) : 0.f;
+      ks[u] = 0.f;
+      if (good >> u & 1) ks[u] = scalar_load(a.c.k_scale + head[u]);
     }
-  }
-
-  // Adds the weights of 16 columns; whole: every column sees every token.
-  template <typename T>
-  __device__ __forceinline__ void add(const Queries<T, DC>& q, int t0, int context, bool whole) {
-    const int c = (threadIdx.x >> 4) & 3;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      ev_f4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int t = Queries<T, DC>::NT - 1; t >= 0; --t)
-#pragma unroll
-        for (int ch = 0; ch < DC; ++ch) {
-          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u][ch][0], q.q[ch][0][t], s, 0, 0, 0);
-          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u][ch][1], q.q[ch][1][t], s, 0, 0, 0);
-        }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[i], ks[u], -q.lse2));
-        sum[u][i] += (whole || (good[u] && q.sees(t0 + 16 * u + 4 * c + i, context))) ? p : 0.f;
-      }
+      if (!(ks[u] >= 0.f && ks[u] < kInf)) good &= ~(1u << u);
+      ks[u] = (good >> u & 1) ? ks[u] * (a.w.scale * kLog2e) : 0.f;
     }
   }
 };
 
+// Adds the weights of 16 columns to the sums of a tile of 16 tokens from t on: k are its left operands.
 template <typename T, int DC>
+__device__ __forceinline__ void add_weights(const ev_b8 (&k)[DC][2], float ks, bool good, const Queries<T, DC>& q, int t, int context,
+                                            bool whole, ev_f4& sum) {
+  ev_f4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int n = Queries<T, DC>::NT - 1; n >= 0; --n)
+#pragma unroll
+    for (int ch = 0; ch < DC; ++ch) {
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[ch][0], q.q[ch][0][n], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[ch][1], q.q[ch][1][n], s, 0, 0, 0);
+    }
+  if (whole) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(fmaf(s[i], ks, -q.lse2));
+  } else {
+    asm volatile("; a branch, not selections");
+    const uint32_t m = good ? q.sees(t + 4 * ((threadIdx.x >> 4) & 3), context) : 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(s[i], ks, -q.lse2));
+      sum[i] += m >> i & 1 ? p : 0.f;
+    }
+  }
+}
+
+// The sums of 64 tokens over the columns: lane (r, c) takes the token of tile r / 4 that is element r % 4 of its quarter.
+__device__ __forceinline__ float over_columns(const ev_f4 (&sum)[4]) {
+  const int r = threadIdx.x & 15;
+  float mine = 0.f;
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = row_sum(sum[u][i]);
+      mine = r == 4 * u + i ? x : mine;
+    }
+  return mine;
+}
+__device__ __forceinline__ int token_of(int t0) {
+  const int r = threadIdx.x & 15, c = (threadIdx.x >> 4) & 3;
+  return t0 + 16 * (r >> 2) + 4 * c + (r & 3);
+}
+
+// Up to 16 NB columns: their queries stay in registers and every wave walks 64 tokens at a time, the next ones' codes on their way.
+// Memory bounds it: a token of 32 sequences of up to 4096, 32 heads of 128 (384 MB), 94 us, 4.1 TB/s; with 24 tokens each
+// (two blocks of columns) 106 us.
+template <typename T, int DC, int NB>
+__global__ __launch_bounds__(256) void kv_weights_step_kernel(const WeightArgs a) {
+  const int lane = threadIdx.x & 63, r = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t item = blockIdx.x;
+  const int hk = static_cast<int>(item % a.c.Hkv);
+  item /= a.c.Hkv;
+  const int part = static_cast<int>(item % a.shares), b = static_cast<int>(item / a.shares);
+  const KvSeq sq = kv_seq(a.bt, b, a.c.page_log2);
+  if (!sq.ok || sq.n == 0 || sq.len > a.max_kv) return;
+  const int cols = sq.n * a.G, context = sq.len - sq.n, stride = a.shares * 256;
+  int t0 = (part * 4 + wave) * 64;
+  if (t0 >= sq.len) return;
+  RawTokens<DC> next;
+  next.load(a, sq, b, hk, t0);
+  Queries<T, DC> q[NB];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    const int col = min(n * 16 + r, cols - 1), i = col / a.G;
+    RawQuery<T, DC> raw;
+    raw.load(a, sq, hk, i, col - i * a.G);
+    q[n].set(a, sq, raw, i, n * 16 + r < cols);
+  }
+  const int64_t head = static_cast<int64_t>(b) * a.c.Hkv + hk;
+  for (; t0 < sq.len; t0 += stride) {
+    const RawTokens<DC> now = next;
+    const int t = token_of(t0);
+    const int64_t at = head * a.w.ld + t;
+    const float old = a.w.before && t < context ? a.w.before[at] : 0.f;
+    if (t0 + stride < sq.len) next.load(a, sq, b, hk, t0 + stride);
+    bool whole[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+      whole[n] = now.good == 15u && __all(n * 16 + r >= cols || (q[n].lo <= t0 && q[n].hi >= t0 + 64 && (!q[n].bits || t0 + 64 <= context)));
+    ev_f4 sum[4] = {};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      ev_b8 k[DC][2];
+#pragma unroll
+      for (int ch = 0; ch < DC; ++ch) {
+        k[ch][0] = widen8(now.k[u][ch][0], now.k[u][ch][1]);
+        k[ch][1] = widen8(now.k[u][ch][2], now.k[u][ch][3]);
+      }
+#pragma unroll
+      for (int n = NB - 1; n >= 0; --n) {
+        add_weights(k, now.ks[u], now.good >> u & 1, q[n], t0 + 16 * u, context, whole[n], sum[u]);
+        if (whole[n] && n * 16 + r >= cols) sum[u] = ev_f4{0.f, 0.f, 0.f, 0.f};  // columns past the last one
+      }
+    }
+    const float mine = over_columns(sum);
+    if (t < sq.len) a.w.after[at] = a.w.before && t < context ? fmaf(a.w.decay, old, mine) : mine;
+  }
+}
+
+// More columns: every wave keeps 64 tokens in registers, and the four of a workgroup walk the columns that see any of theirs, 32 at a
+// time, whose queries lie in LDS for all of them, two steps ahead, put there by the loads themselves (16 bytes of a lane
+// where it reads them).  The vector units bound it, with 16 exponentials, products and sums of a lane for a tile of 64 tokens by 16
+// columns (three quarters of the time; the matrix instructions a quarter beside them): two prompts of up to 2048 rows over
+// 4000 tokens, 64 heads over 8, take 361 us (514 TFLOP/s), with every wave reading the queries for itself 399.
+constexpr int weights_step_bytes(int dc, int nv) { return 2 * dc * nv * 1024 + 4 * 256; }
+template <typename T, int DC, bool VEC>
 __global__ __launch_bounds__(256) void kv_weights_kernel(const WeightArgs a) {
-  const int lane = threadIdx.x & 63, r = lane & 15, c = lane >> 4, wave = threadIdx.x >> 6;
+  constexpr int NV = RawQuery<T, DC>::NV, kPieces = DC * NV, kBlock = kPieces * 1024, kStage = weights_step_bytes(DC, NV);
+  constexpr int kLoads = 2 * kPieces / 4 + 1;  // of a wave in a step
+  extern __shared__ __align__(16) uint8_t lds[];  // [3 steps]([2 blocks of 16 columns][DC][NV][64 lanes][16], [4 waves][64 lanes] lse)
+  const int lane = threadIdx.x & 63, r = lane & 15, c = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t item = blockIdx.x;
   const int hk = static_cast<int>(item % a.c.Hkv);
   item /= a.c.Hkv;
@@ -235,49 +375,162 @@ __global__ __launch_bounds__(256) void kv_weights_kernel(const WeightArgs a) {
   item /= a.shares;
   const int tile = static_cast<int>(item % a.tiles), b = static_cast<int>(item / a.tiles);
   const KvSeq sq = kv_seq(a.bt, b, a.c.page_log2);
-  const int t0 = (tile * 4 + wave) * 64;
-  if (!sq.ok || sq.n == 0 || sq.len > a.max_kv || t0 >= sq.len) return;
+  const int tile0 = tile * 256, t0 = tile0 + wave * 64;
+  if (!sq.ok || sq.n == 0 || sq.len > a.max_kv || tile0 >= sq.len) return;
   const int cols = sq.n * a.G, context = sq.len - sq.n;
-  int first = 0, last = cols;  // the columns that see any of the tokens
-  if (a.w.causal) {
-    if (t0 > context) first = (t0 - context) * a.G;
-    if (a.w.window) last = static_cast<int>(min<int64_t>(last, (static_cast<int64_t>(t0) + 63 + a.w.window - context) * a.G));
+  // the columns that see any of the tokens from `from` to `to`
+  auto first_of = [&](int from) { return a.w.causal && from > context ? (from - context) * a.G : 0; };
+  auto last_of = [&](int to) {
+    if (!a.w.causal || !a.w.window) return cols;
+    return static_cast<int>(max<int64_t>(min<int64_t>(cols, (static_cast<int64_t>(to) + a.w.window - context) * a.G), 0));
+  };
+  int first = first_of(tile0) & ~31, last = last_of(tile0 + 255);
+  if (a.shares > 1) {  // an equal share of the steps
+    const int steps = (max(last - first, 0) + 31) >> 5, each = (steps + a.shares - 1) / a.shares;
+    first += share * each * 32;
+    last = min(last, first + each * 32);
   }
-  first &= ~15;
-  if (a.shares > 1) {  // an equal share of the column blocks
-    const int blocks = (max(last - first, 0) + 15) >> 4, each = (blocks + a.shares - 1) / a.shares;
-    first += share * each * 16;
-    last = min(last, first + each * 16);
+  const int my_first = first_of(t0), my_last = t0 < sq.len ? last_of(t0 + 63) : 0;
+  ev_b8 k[4][DC][2];
+  float ks[4];
+  uint32_t good;
+  {
+    RawTokens<DC> raw;
+    raw.load(a, sq, b, hk, t0);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int ch = 0; ch < DC; ++ch) {
+        k[u][ch][0] = widen8(raw.k[u][ch][0], raw.k[u][ch][1]);
+        k[u][ch][1] = widen8(raw.k[u][ch][2], raw.k[u][ch][3]);
+      }
+      ks[u] = raw.ks[u];
+    }
+    good = raw.good;
   }
-  Tokens<DC> k;
-  k.load(a, sq, b, hk, t0);
-  ev_f4 total[4] = {};
-  int n = 0;
-  for (int col = first; col < last; col += 16) {
-    Queries<T, DC> q;
-    q.load(a, sq, hk, col + r, cols);
-    const bool sees_all = q.lo <= t0 && q.hi >= t0 + 64 && (!q.bits || t0 + 64 <= context);
-    const bool whole = __all(sees_all && k.good[0] && k.good[1] && k.good[2] && k.good[3]);
-    k.add(q, t0, context, whole);
-    if (++n == 32) {  // sums of sums: the error of long ones grows with their root
+  // Columns between these two see every token of the wave: they need no masks, nor selections where no row is out.
+  int plain_from = 0, plain_to = cols & ~15;
+  if (a.w.tree.mask) {
+    if (t0 + 64 > context || a.w.window) plain_to = 0;
+  } else if (a.w.causal) {
+    plain_from = max(t0 + 63 - context, 0) * a.G;
+    if (a.w.window) plain_to = static_cast<int>(min<int64_t>(plain_to, (static_cast<int64_t>(t0) - context + a.w.window) * a.G) & ~int64_t{15});
+  }
+  if (good != 15u || t0 + 64 > sq.len) plain_to = 0;
+
+  // This lane's column of the next block to fetch: its row and head, where its query and log-sum-exp are, and how far these move
+  // in 16 columns (`up` rows and `over` heads, a row more and G heads less where the heads end).
+  const int up = 16 / a.G, over = 16 - up * a.G;
+  int i = (first + r) / a.G, g = first + r - i * a.G;
+  const T* q_at = static_cast<const T*>(a.q.p) + (sq.row0 + i) * a.q.tok + (hk * a.G + g) * a.q.head;
+  const float* lse_at = a.w.lse + static_cast<int64_t>(sq.row0 + i) * a.Hq + hk * a.G + g;
+  const int64_t q_on = up * a.q.tok + over * a.q.head, q_wrap = a.q.tok - a.G * a.q.head;
+  const int lse_on = up * a.Hq + over, lse_wrap = a.Hq - a.G;
+  // what is there past the last column: the key head's first query
+  const T* q_first = static_cast<const T*>(a.q.p) + sq.row0 * a.q.tok + hk * a.G * a.q.head;
+  const float* lse_first = a.w.lse + static_cast<int64_t>(sq.row0) * a.Hq + hk * a.G;
+  int element[DC];  // past D the codes are 0
+#pragma unroll
+  for (int ch = 0; ch < DC; ++ch) element[ch] = ch * 64 + c * 16 < a.c.D ? ch * 64 + c * 16 : 0;
+  // Queries of 32 columns to LDS, and their log-sum-exps; past the last column those of one that there is.  Every wave has as
+  // many loads as any other: its pieces of the queries, and the log-sum-exps of block wave % 2.
+  auto fetch = [&](uint8_t* to) {
+#pragma unroll
+    for (int blk = 0; blk < 2; ++blk) {
+      const T* p = i < sq.n ? q_at : q_first;
+      auto load = [&](int ch, int v, int piece) {
+        const T* e = p + element[ch] + v * (16 / NV);
+        uint8_t* at = to + piece * 1024;
+        if constexpr (VEC) {
+          load_lds16(e, at);
+        } else {
+          ev_u4 y;
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            if constexpr (NV == 4) y[n] = e[n];
+            else y[n] = e[2 * n] | static_cast<uint32_t>(e[2 * n + 1]) << 16;
+          }
+          *reinterpret_cast<ev_u4*>(at + lane * 16) = y;
+        }
+      };
+      // the waves share a block's pieces
+      if constexpr (NV == 4) {
+#pragma unroll
+        for (int ch = 0; ch < DC; ++ch) load(ch, wave, blk * kPieces + ch * 4 + wave);
+      } else if constexpr (DC >= 2) {
+#pragma unroll
+        for (int ch = 0; ch < DC; ch += 2) {
+          const bool second = wave >> 1;
+          const T* keep = p;
+          p += second ? element[ch + 1] - element[ch] : 0;
+          load(ch, wave & 1, blk * kPieces + ch * 2 + wave);
+          p = keep;
+        }
+      } else if (wave >> 1 == blk) {  // two pieces a block
+        load(0, wave & 1, wave);
+      }
+      if ((wave & 1) == blk) load_lds4(i < sq.n ? lse_at : lse_first, to + 2 * kBlock + wave * 256);
+      i += up;
+      g += over;
+      q_at += q_on;
+      lse_at += lse_on;
+      if (g >= a.G) {
+        g -= a.G;
+        ++i;
+        q_at += q_wrap;
+        lse_at += lse_wrap;
+      }
+    }
+  };
+  ev_f4 total[4] = {}, sum[4] = {};
+  int buffer = 0, n = 0;
+  if (first < last) {
+    fetch(lds);
+    fetch(lds + kStage);
+  }
+  for (; first < last; first += 32) {
+    // this step's loads have arrived (the next one's may be on their way), for every wave, and every wave has read
+    // what the step after the next one takes the place of
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(VEC ? kLoads : 0) : "memory");
+    fetch(lds + (buffer == 0 ? 2 : buffer - 1) * kStage);
+#pragma unroll
+    for (int blk = 0; blk < 2; ++blk) {
+      const int col0 = first + blk * 16;
+      if (col0 + 16 <= my_first || col0 >= min(last, my_last)) continue;
+      RawQuery<T, DC> raw;
+      const uint8_t* from = lds + buffer * kStage + blk * kBlock + lane * 16;
+#pragma unroll
+      for (int ch = 0; ch < DC; ++ch)
+#pragma unroll
+        for (int v = 0; v < NV; ++v) raw.x[ch][v] = *reinterpret_cast<const ev_u4*>(from + (ch * NV + v) * 1024);
+      raw.lse = *reinterpret_cast<const float*>(lds + buffer * kStage + 2 * kBlock + blk * 256 + lane * 4);
+      Queries<T, DC> q;
+      if (col0 >= plain_from && col0 < plain_to && __all(fabsf(raw.lse) < kInf)) {
+        q.set_plain(raw);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) add_weights(k[u], ks[u], true, q, t0 + 16 * u, context, true, sum[u]);
+      } else {
+        asm volatile("; a branch, not selections");
+        q.set(a, sq, raw, min((col0 + r) / a.G, sq.n - 1), col0 + r < cols);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) add_weights(k[u], ks[u], good >> u & 1, q, t0 + 16 * u, context, false, sum[u]);
+      }
+    }
+    if (++n == 16) {  // sums of sums: the error of long ones grows with their root
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        total[u] += k.sum[u];
-        k.sum[u] = ev_f4{0.f, 0.f, 0.f, 0.f};
+        total[u] += sum[u];
+        sum[u] = ev_f4{0.f, 0.f, 0.f, 0.f};
       }
       n = 0;
     }
+    buffer = buffer == 2 ? 0 : buffer + 1;
   }
-  // lane (r, c) takes the token of tile r / 4 that is element r % 4 of its quarter
-  float mine = 0.f;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing comes to LDS any more
 #pragma unroll
-  for (int u = 0; u < 4; ++u)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x = row_sum(total[u][i] + k.sum[u][i]);
-      mine = r == 4 * u + i ? x : mine;
-    }
-  const int t = t0 + 16 * (r >> 2) + 4 * c + (r & 3);
+  for (int u = 0; u < 4; ++u) sum[u] += total[u];
+  const float mine = over_columns(sum);
+  const int t = token_of(t0);
   if (t >= sq.len) return;
   const int64_t head = static_cast<int64_t>(b) * a.c.Hkv + hk;
   if (a.shares > 1) {
@@ -298,11 +551,20 @@ __global__ __launch_bounds__(256) void kv_weights_join_kernel(const WeightArgs a
   a.w.after[at] = a.w.before && t < sq.len - sq.n ? fmaf(a.w.decay, a.w.before[at], x) : x;
 }
 
-int weight_shares(int B, int Hq, int Hkv, int max_new, int max_kv) {
-  const int64_t groups = static_cast<int64_t>(B) * Hkv * cdiv(max_kv, 256), blocks = cdiv(static_cast<int64_t>(max_new) * (Hq / Hkv), 16);
-  const int64_t want = cdiv(2048, groups > 0 ? groups : 1), most = cdiv(blocks, 32);
-  const int64_t n = want < most ? want : most;
-  return static_cast<int>(n < 1 ? 1 : n > 16 ? 16 : n);
+// How a call is divided.  Columns that fit four blocks stay in registers (us, 32 sequences of up to 4096 tokens, 32 heads: 24 columns 106
+// for 179 when they are walked, 40 147 for 200), the tokens over 2048 workgroups.  More are walked, in shares of 512 columns and more
+// until 2048 workgroups are at work, which a second launch joins in order.
+struct WeightPlan {
+  int blocks;  // of 16 columns in a wave's registers; 0: the columns are walked
+  int shares, parts;  // parts: shares that are joined by a second launch
+};
+WeightPlan plan_weights(int B, int Hq, int Hkv, int max_new, int max_kv) {
+  const int64_t cols = static_cast<int64_t>(max_new) * (Hq / Hkv), heads = static_cast<int64_t>(B) * Hkv, tiles = cdiv(max_kv, 256);
+  auto shares = [](int64_t want, int64_t most) { return static_cast<int>(want < 1 || most < 1 ? 1 : want < most ? want : most); };
+  if (cols <= 64) return {cols <= 16 ? 1 : cols <= 32 ? 2 : 4, shares(cdiv(2048, heads), tiles), 1};
+  const int64_t want = cdiv(2048, heads * tiles);
+  const int n = shares(want < 16 ? want : 16, cdiv(cols, 512));
+  return {0, n, n};
 }
 
 // ---- the tokens that a budget keeps ---------------------------------------------------------------------
@@ -495,35 +757,41 @@ hipError_t launch_tree_mask(int B, const int32_t* parents, const int32_t* start,
 }
 
 size_t kv_weights_ws_bytes(int B, int Hq, int Hkv, int D, int max_new, int max_kv) {
-  const int shares = weight_shares(B, Hq, Hkv, max_new, max_kv);
+  const WeightPlan p = plan_weights(B, Hq, Hkv, max_new, max_kv);
   WsCursor c(nullptr);
-  if (shares > 1) c.take<float>(static_cast<size_t>(shares) * B * Hkv * max_kv);
+  if (p.parts > 1) c.take<float>(static_cast<size_t>(p.parts) * B * Hkv * max_kv);
   return c.used;
 }
 
 hipError_t launch_kv_weights(const KvCache& c, const KvBatch& bt, int max_kv, int type, int Hq, const KvRows& q,
                              const KvWeights& w, void* ws, hipStream_t stream) {
-  const int shares = weight_shares(bt.B, Hq, c.Hkv, bt.max_new, max_kv), es = type == ET_F32 ? 4 : 2;
+  const WeightPlan p = plan_weights(bt.B, Hq, c.Hkv, bt.max_new, max_kv);
+  const int es = type == ET_F32 ? 4 : 2, tiles = static_cast<int>(cdiv(max_kv, 256));
   WsCursor cur(ws);
-  float* part = shares > 1 ? cur.take<float>(static_cast<size_t>(shares) * bt.B * c.Hkv * max_kv) : nullptr;
-  const int tiles = static_cast<int>(cdiv(max_kv, 256));
-  WeightArgs a = {c, bt, q, w, part, Hq, Hq / c.Hkv, shares, tiles, max_kv, 0};
+  float* part = p.parts > 1 ? cur.take<float>(static_cast<size_t>(p.parts) * bt.B * c.Hkv * max_kv) : nullptr;
+  WeightArgs a = {c, bt, q, w, part, Hq, Hq / c.Hkv, p.shares, tiles, max_kv, 0};
   a.q_vec = reinterpret_cast<uintptr_t>(q.p) % 16 == 0 && q.tok * es % 16 == 0 && q.head * es % 16 == 0;
-  const int64_t blocks = static_cast<int64_t>(bt.B) * c.Hkv * tiles * shares;
+  const int64_t blocks = static_cast<int64_t>(bt.B) * c.Hkv * p.shares * (p.blocks ? 1 : tiles);
   if (blocks == 0) return hipSuccess;
   if (blocks > 0x7fffffffLL || static_cast<int64_t>(bt.B) * c.Hkv > 65535) return hipErrorInvalidConfiguration;
   const dim3 grid(static_cast<uint32_t>(blocks));
-  auto as = [&](auto t) {
+  auto as = [&](auto t, auto dc) {
     using T = decltype(t);
-    if (c.D <= 64) kv_weights_kernel<T, 1><<<grid, 256, 0, stream>>>(a);
-    else if (c.D <= 128) kv_weights_kernel<T, 2><<<grid, 256, 0, stream>>>(a);
-    else kv_weights_kernel<T, 4><<<grid, 256, 0, stream>>>(a);
+    constexpr size_t lds = 3 * weights_step_bytes(decltype(dc)::value, sizeof(T) == 4 ? 4 : 2);
+    if (p.blocks == 1) kv_weights_step_kernel<T, decltype(dc)::value, 1><<<grid, 256, 0, stream>>>(a);
+    else if (p.blocks == 2) kv_weights_step_kernel<T, decltype(dc)::value, 2><<<grid, 256, 0, stream>>>(a);
+    else if (p.blocks == 4) kv_weights_step_kernel<T, decltype(dc)::value, 4><<<grid, 256, 0, stream>>>(a);
+    else if (a.q_vec) kv_weights_kernel<T, decltype(dc)::value, true><<<grid, 256, lds, stream>>>(a);
+    else kv_weights_kernel<T, decltype(dc)::value, false><<<grid, 256, lds, stream>>>(a);
+    return hipGetLastError();
   };
-  if (type == ET_F32) as(uint32_t{});
-  else as(uint16_t{});
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || shares == 1) return e;
-  kv_weights_join_kernel<<<dim3(static_cast<uint32_t>(cdiv(max_kv, 256)), static_cast<uint32_t>(bt.B * c.Hkv)), 256, 0, stream>>>(a);
+  auto of = [&](auto t) {
+    return c.D <= 64 ? as(t, std::integral_constant<int, 1>{}) : c.D <= 128 ? as(t, std::integral_constant<int, 2>{})
+                                                                              : as(t, std::integral_constant<int, 4>{});
+  };
+  const hipError_t e = type == ET_F32 ? of(uint32_t{}) : of(uint16_t{});
+  if (e != hipSuccess || p.parts == 1) return e;
+  kv_weights_join_kernel<<<dim3(static_cast<uint32_t>(tiles), static_cast<uint32_t>(bt.B * c.Hkv)), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
