@@ -581,10 +581,12 @@ crvq_status crvq_kv_weights(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32
  * the others those with the largest weights, the lower index first where they are equal; NaN counts as
  * less than everything.  keep (int32 [B][Hkv][ld_keep], ld_keep >= min(budget,
  * ld)) gets them in order, kept_weights ([B][Hkv][ld_keep] or NULL) their weights, kept_len (int32[B]) their number,
- * the same for all heads; 0 where kv_len[b] < 0 or > ld.  Entries from kept_len[b] on stay as they were. */
+ * the same for all heads; 0 where kv_len[b] < 0 or > ld.  Entries from kept_len[b] on stay as they were.
+ * workspace: crvq_kv_select_workspace_size(B, Hkv, ld) bytes. */
+size_t crvq_kv_select_workspace_size(int32_t B, int32_t Hkv, int64_t ld);
 crvq_status crvq_kv_select(int32_t B, int32_t Hkv, const int32_t* kv_len, const float* weights, int64_t ld, int32_t budget,
                            int32_t sinks, int32_t recent, int32_t* keep, int64_t ld_keep, int32_t* kept_len, float* kept_weights,
-                           void* stream);
+                           void* workspace, size_t ws_bytes, void* stream);
 
 /* crvq_kv_gather -- moves tokens to other pages: slot j % page of page
  * to_table[b * ld_to + j / page] becomes token keep[b][h][j] (int32 [B][keep_heads][ld_keep],
@@ -718,6 +720,7 @@ crvq_status crvq_norm(int64_t T, int64_t N, int kind, const void* x, int64_t ldx
  *   CRVQ_OP_W8_GEMM     M, N, K = T                  (crvq_w8_gemm)
  *   CRVQ_OP_KV_WEIGHTS, CRVQ_OP_KV_TREE_ATTENTION  as CRVQ_OP_KV_ATTENTION
  *                                                    (crvq_kv_weights, crvq_kv_tree_attention)
+ *   CRVQ_OP_KV_SELECT   n_vectors = B, N = Hkv, n_cols = ld  (crvq_kv_select)
  * Returns 0 for an unknown op or a shape the call rejects (and for calls that
  * need no workspace at that shape).  Ks is a host array of n_books entries.
  */
@@ -736,7 +739,8 @@ typedef enum {
   CRVQ_OP_W4_GEMV = 11,
   CRVQ_OP_W8_GEMM = 12,
   CRVQ_OP_KV_WEIGHTS = 13,
-  CRVQ_OP_KV_TREE_ATTENTION = 14
+  CRVQ_OP_KV_TREE_ATTENTION = 14,
+  CRVQ_OP_KV_SELECT = 15
 } crvq_op;
 size_t crvq_workspace_size(int op, int64_t n_vectors, int64_t K, int32_t beam, int32_t n_books, int32_t d,
                            const int64_t* Ks, int64_t M, int64_t N, int64_t n_cols);

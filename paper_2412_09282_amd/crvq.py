@@ -105,7 +105,8 @@ def lib(build_if_missing: bool = True):
                 "crvq_kv_weights": ([I32] * 5 + [I64, P, P, P, I64, P, P, I32, I32, I64, ctypes.c_int, P, I64, I64, P,
                                      ctypes.c_float, ctypes.c_int, I32, P, I64, P, ctypes.c_float, P, P, I64, P, SZ, P],
                                     ctypes.c_int),
-                "crvq_kv_select": ([I32, I32, P, P, I64, I32, I32, I32, P, I64, P, P, P], ctypes.c_int),
+                "crvq_kv_select_workspace_size": ([I32, I32, I64], SZ),
+                "crvq_kv_select": ([I32, I32, P, P, I64, I32, I32, I32, P, I64, P, P, P, SZ, P], ctypes.c_int),
                 "crvq_kv_gather": ([I32] * 4 + [I64] + [P] * 5 + [I64, P, P, I64, I32, P, I32, P, I64, P], ctypes.c_int),
                 "crvq_w4_quantize": ([I64, I64, I32, P, I64, ctypes.c_int, P, I64, P, ctypes.c_int, I64, P, I64, P],
                                      ctypes.c_int),
@@ -603,23 +604,25 @@ def crvq_w4_gemv(codes: torch.Tensor, scales: torch.Tensor, group: int, x: torch
 def _one_device(first: torch.Tensor, *others) -> None:
     """The kernels follow these pointers on the device of the first tensor: the others are there too, or in pinned host
     memory."""
-    if not first.is_cuda and not first.is_pinned():
+    device = first.get_device()  # below 0: the host's memory
+    if device < 0 and not first.is_pinned():
         raise ValueError("a tensor in host memory that is not pinned")
-    device = first.device
     for t in others:
-        if t is not None and t.device != device:
-            if t.is_cuda:
-                raise ValueError(f"tensors on {device} and {t.device}")
-            if not t.is_pinned():
+        if t is not None and t.get_device() != device:
+            if t.is_cuda and device >= 0:
+                raise ValueError(f"tensors on {first.device} and {t.device}")
+            if not t.is_cuda and not t.is_pinned():
                 raise ValueError("a tensor in host memory that is not pinned")
 
 
 def _enqueue(fn: str, on: torch.Tensor, stream, *args) -> None:
     """The C call, on the device that its tensors are on."""
-    call = getattr(lib(), fn)
-    if on.is_cuda and on.device.index != torch.cuda.current_device():
-        with torch.cuda.device(on.device):
+    call, device = getattr(_lib, fn) if _lib is not None else getattr(lib(), fn), on.get_device()
+    if device >= 0 and device != torch._C._cuda_getDevice():
+        with torch.cuda.device(device):
             status = call(*args, _stream(stream))
+    elif stream is None and device >= 0:
+        status = call(*args, torch._C._cuda_getCurrentRawStream(device))
     else:
         status = call(*args, _stream(stream))
     if status != 0:
@@ -798,8 +801,10 @@ def crvq_kv_select(weights: torch.Tensor, kv_len: torch.Tensor, budget: int, kee
     assert kept_weights is None or (kept_weights.shape == keep.shape and kept_weights.dtype == torch.float32 and
                                     kept_weights.is_contiguous())
     _one_device(weights, kv_len, keep, kept_len, kept_weights)
+    nbytes = lib().crvq_kv_select_workspace_size(B, Hkv, ld)
+    ws = _workspace_for(nbytes, weights.device, stream) if nbytes else None
     _enqueue("crvq_kv_select", weights, stream, B, Hkv, kv_len.data_ptr(), weights.data_ptr(), ld, budget, sinks, recent,
-             keep.data_ptr(), keep.shape[2], kept_len.data_ptr(), _ptr(kept_weights))
+             keep.data_ptr(), keep.shape[2], kept_len.data_ptr(), _ptr(kept_weights), _ptr(ws), nbytes)
 
 
 def crvq_kv_gather(k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,

@@ -764,6 +764,9 @@ size_t crvq_workspace_size(int op, int64_t n_vectors, int64_t K, int32_t beam, i
       if (n_vectors > 0x7fffffffLL || M > 0x7fffffffLL || N > 0x7fffffffLL || K > 0x7fffffffLL || n_cols > 0x7fffffffLL) return 0;
       return crvq_kv_weights_workspace_size(static_cast<int32_t>(n_vectors), static_cast<int32_t>(M), static_cast<int32_t>(N), d,
                                             static_cast<int32_t>(K), static_cast<int32_t>(n_cols));
+    case CRVQ_OP_KV_SELECT:
+      if (n_vectors > 0x7fffffffLL || N > 0x7fffffffLL) return 0;
+      return crvq_kv_select_workspace_size(static_cast<int32_t>(n_vectors), static_cast<int32_t>(N), n_cols);
     case CRVQ_OP_W8_GEMM: return crvq_w8_gemm_workspace_size(M, N, K);
     default: return 0;
   }
@@ -1121,9 +1124,14 @@ crvq_status crvq_kv_weights(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32
                     fn);
 }
 
+size_t crvq_kv_select_workspace_size(int32_t B, int32_t Hkv, int64_t ld) {
+  if (B < 1 || Hkv < 1 || ld < 0 || ld > CRVQ_KV_MAX_LEN || static_cast<int64_t>(B) * Hkv > 0x7fffffffLL) return 0;
+  return kv_select_ws_bytes(B, Hkv, ld);
+}
+
 crvq_status crvq_kv_select(int32_t B, int32_t Hkv, const int32_t* kv_len, const float* weights, int64_t ld, int32_t budget,
                            int32_t sinks, int32_t recent, int32_t* keep, int64_t ld_keep, int32_t* kept_len, float* kept_weights,
-                           void* stream) {
+                           void* workspace, size_t ws_bytes, void* stream) {
   const ApiRange range("crvq_kv_select");
   static const char* fn = "crvq_kv_select";
   g_err.clear();
@@ -1149,8 +1157,10 @@ crvq_status crvq_kv_select(int32_t B, int32_t Hkv, const int32_t* kv_len, const 
     for (int j = i + 1; j < 5; ++j)
       if (all[i].n && all[j].n && overlaps(all[i].p, all[i].n, all[j].p, all[j].n))
         return fail(CRVQ_ERR_INVALID, "%s: an output overlaps another array", fn);
+  crvq_status s;
+  if ((s = check_ws(workspace, ws_bytes, crvq_kv_select_workspace_size(B, Hkv, ld), fn))) return s;
   return hip_status(launch_kv_select(B, Hkv, kv_len, weights, ld, budget, sinks, recent, {keep, ld_keep, Hkv, kept_len},
-                                     kept_weights, static_cast<hipStream_t>(stream)),
+                                     kept_weights, workspace, static_cast<hipStream_t>(stream)),
                     fn);
 }
 

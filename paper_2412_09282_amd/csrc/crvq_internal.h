@@ -313,8 +313,9 @@ struct KvKeep {
   int heads;      // Hkv, or 1: the same tokens for all
   int32_t* len;   // [B]
 };
+size_t kv_select_ws_bytes(int B, int Hkv, int64_t ld);
 hipError_t launch_kv_select(int B, int Hkv, const int32_t* kv_len, const float* weights, int64_t ld, int budget, int sinks,
-                            int recent, const KvKeep& k, float* kept_weights, hipStream_t stream);
+                            int recent, const KvKeep& k, float* kept_weights, void* ws, hipStream_t stream);
 hipError_t launch_kv_gather(const KvCache& c, int B, const int32_t* table, int64_t ld_table, const int32_t* kv_len, const KvKeep& k,
                             int max_keep, const int32_t* to, int64_t ld_to, hipStream_t stream);
 

@@ -569,8 +569,9 @@ WeightPlan plan_weights(int B, int Hq, int Hkv, int max_new, int max_kv) {
 
 // ---- the tokens that a budget keeps ---------------------------------------------------------------------
 //
-// One workgroup has a head's weights: four passes of a radix select find the smallest key that is kept and how many equal to
-// it are, a last one writes the kept tokens in order.
+// Keys of 32 bits order the weights; three passes of a radix select (11, 11 and 10 bits) find the smallest key that is kept and how many
+// equal to it are, then the kept tokens are written in order.  Up to kSelectMost tokens one workgroup has a head's keys in
+// its registers; beyond, a head's tokens are divided over workgroups, whose counts meet in the workspace between four launches.
 
 // Orders weights as numbers: NaN below all, then from -infinity to infinity; 0 and -0 are equal.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -586,66 +587,246 @@ struct SelectArgs {
   KvKeep k;
   float* kept;  // [B][Hkv][k.ld], or NULL
   int Hkv, budget, sinks, recent;
+  // of the divided form: `per` tokens a workgroup, `chunks` of them a head
+  int64_t per;
+  int chunks;
+  uint32_t *bins[3], *above, *found;  // [heads][chunks][2048 / 2048 / 1024], [heads][chunks][2], [heads][4]
 };
 
-__global__ __launch_bounds__(1024) void kv_select_kernel(const SelectArgs a) {
-  __shared__ uint32_t hist[256], pick[2];
-  __shared__ uint32_t scan[2][16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int hk = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
-  const int64_t row = static_cast<int64_t>(b) * a.Hkv + hk;
-  const int given = a.kv_len[b], len = given < 0 || given > a.ld ? 0 : given, n = min(len, a.budget);
-  if (hk == 0 && tid == 0) a.k.len[b] = n;
-  const float* w = a.weights + row * a.ld;
-  auto key = [&](int t) { return t < a.sinks || t >= len - a.recent ? 0xffffffffu : key_of(w[t]); };
-  // the n-th largest key, and how many of those equal to it are kept
-  uint32_t least = 0, equal = 0;
-  if (n < len) {
-    uint32_t left = n;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
+constexpr int kSelectThreads = 1024, kSelectMost = 16384;
+__device__ constexpr int select_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ constexpr uint32_t select_mask(int pass) { return pass == 2 ? 1023u : 2047u; }
+
+// What a head keeps.
+struct SelectHead {
+  int64_t row;
+  int len, n, left;  // tokens, kept ones, and those among them that are kept for their weight
+  const float* w;
+  __device__ __forceinline__ SelectHead(const SelectArgs& a, int head, bool first) {
+    const int b = head / a.Hkv, given = a.kv_len[b];
+    row = head;
+    len = given < 0 || given > a.ld ? 0 : given;
+    n = min(len, a.budget);
+    left = n < len ? n - a.sinks - a.recent : 0;  // where some are not kept, sinks and recent ones are so many
+    w = a.weights + row * a.ld;
+    if (first && head % a.Hkv == 0) a.k.len[b] = n;
+  }
+  __device__ __forceinline__ bool always(const SelectArgs& a, int t) const { return n == len || t < a.sinks || t >= len - a.recent; }
+};
+
+// Inclusive sums over the workgroup's threads, and the total; `waves`: 16 entries that nobody else uses until the next barrier.
+__device__ __forceinline__ uint64_t block_scan(uint64_t x, uint64_t* waves, uint64_t& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 63) waves[wave] = x;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int v = 0; v < kSelectThreads / 64; ++v) {
+    const uint64_t y = waves[v];
+    if (v < wave) x += y;
+    total += y;
+  }
+  return x;
+}
+
+// The bin that the left-th largest key lies in, counts x0 and x1 being those of bins 2 t and 2 t + 1 of thread t, and what is left
+// of `left` within it.
+__device__ __forceinline__ void find_bin(uint32_t x0, uint32_t x1, uint32_t& left, uint32_t& bin, uint64_t* waves, uint32_t* pick) {
+  uint64_t total;
+  const uint32_t up_to = static_cast<uint32_t>(block_scan(static_cast<uint64_t>(x0) + x1, waves, total));
+  const uint32_t above1 = static_cast<uint32_t>(total) - up_to, above0 = above1 + x1;  // keys in higher bins
+  if (above1 < left && left <= above1 + x1) pick[0] = 2 * threadIdx.x + 1, pick[1] = left - above1;
+  if (above0 < left && left <= above0 + x0) pick[0] = 2 * threadIdx.x, pick[1] = left - above0;
+  __syncthreads();
+  bin = pick[0];
+  left = pick[1];
+}
+
+// The weights of tokens t .. t + K - 1, 0 from `to` on.
+struct __attribute__((packed, aligned(4))) FourWeights {
+  float x[4];
+};
+template <int K>
+__device__ __forceinline__ void load_weights(const float* from, int t, int to, float (&w)[K]) {
+#pragma unroll
+  for (int k = 0; k < K; k += 4) {
+    if (t + k + 3 < to) {
+      const FourWeights f = *reinterpret_cast<const FourWeights*>(from + t + k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[k + e] = f.x[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[k + e] = t + k + e < to ? from[t + k + e] : 0.f;
+    }
+  }
+}
+
+// Writes those of a thread's K tokens from t on that are kept: with keys above `least`, and the first `equal` ones equal to it.
+// before: how many of either kind there are in the tokens before the workgroup's, (above << 32) + equal; counted on.
+template <int K>
+__device__ __forceinline__ void write_kept(const SelectArgs& a, const SelectHead& h, const float (&w)[K], int t, int to, uint32_t least,
+                                           uint32_t equal, uint64_t& before, uint64_t* waves) {
+  uint32_t gt = 0, eq = 0;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const bool there = t + k < to, always = there && h.always(a, t + k);
+    const uint32_t x = key_of(w[k]);
+    gt += always || (there && h.left > 0 && x > least);
+    eq += there && !always && h.left > 0 && x == least;
+  }
+  uint64_t total;
+  const uint64_t up_to = before + block_scan(static_cast<uint64_t>(gt) << 32 | eq, waves, total);
+  before += total;
+  uint32_t g = static_cast<uint32_t>(up_to >> 32) - gt, e = static_cast<uint32_t>(up_to) - eq;  // before this thread's tokens
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const bool there = t + k < to, always = there && h.always(a, t + k);
+    const uint32_t x = key_of(w[k]);
+    const bool more = always || (there && h.left > 0 && x > least), same = there && !always && h.left > 0 && x == least;
+    if (more || (same && e < equal)) {
+      const int64_t at = h.row * a.k.ld + g + min(e, equal);
+      a.k.keep[at] = t + k;
+      if (a.kept) a.kept[at] = w[k];
+    }
+    g += more;
+    e += same;
+  }
+}
+
+// A head in one workgroup: thread t has tokens t K .. t K + K - 1.
+template <int K>
+__global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(const SelectArgs a) {
+  __shared__ uint32_t hist[2048], pick[2];
+  __shared__ uint64_t waves[kSelectThreads / 64];
+  const int tid = threadIdx.x, at = tid * K;
+  const SelectHead h(a, blockIdx.x, tid == 0);
+  float w[K];
+  load_weights<K>(h.w, at, h.len, w);
+  uint32_t least = 0xffffffffu, equal = 0, left = h.left;
+  if (left > 0) {
+    least = 0;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = select_shift(pass);
+      for (int x = tid; x < 2048; x += kSelectThreads) hist[x] = 0;
       __syncthreads();
-      for (int t = tid; t < len; t += 1024) {
-        const uint32_t x = key(t);
-        if (shift == 24 || (x >> (shift + 8)) == (least >> (shift + 8))) atomicAdd(&hist[(x >> shift) & 255u], 1u);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const uint32_t x = key_of(w[k]);
+        const bool in = pass == 0 || x >> select_shift(pass == 0 ? 0 : pass - 1) == least >> select_shift(pass == 0 ? 0 : pass - 1);
+        if (in && at + k < h.len && !h.always(a, at + k)) atomicAdd(&hist[x >> shift & select_mask(pass)], 1u);
       }
       __syncthreads();
-      if (tid == 0) {
-        int d = 255;
-        while (d > 0 && hist[d] < left) left -= hist[d--];
-        pick[0] = static_cast<uint32_t>(d) << shift;
-        pick[1] = left;
-      }
-      __syncthreads();
-      least |= pick[0];
-      left = pick[1];
+      uint32_t bin;
+      find_bin(hist[2 * tid], hist[2 * tid + 1], left, bin, waves, pick);
+      least |= bin << shift;
     }
     equal = left;
   }
-  // in order: those above it, and the first `equal` ones equal to it
-  uint32_t above = 0, same = 0;  // of the tokens before this round
-  for (int t0 = 0; t0 < len; t0 += 1024) {
-    const int t = t0 + tid;
-    const uint32_t x = t < len ? key(t) : 0;
-    const bool gt = t < len && (n == len || x > least), eq = n < len && t < len && x == least;
-    const unsigned long long bg = __ballot(gt), be = __ballot(eq), before = (1ull << lane) - 1;
-    __syncthreads();
-    if (lane == 0) {
-      scan[0][wave] = __popcll(bg);
-      scan[1][wave] = __popcll(be);
+  uint64_t before = 0;
+  write_kept<K>(a, h, w, at, h.len, least, equal, before, waves);
+}
+
+// Always kept tokens before token t.
+__device__ __forceinline__ int n_always_before(const SelectArgs& a, const SelectHead& h, int t) {
+  if (h.n == h.len) return t;
+  return min(a.sinks, t) + max(t - (h.len - a.recent), 0);
+}
+
+// A head's chunk in one workgroup, launch PASS of four: counts of the chunk's keys by 11, 11 and 10 bits, each of those that share the
+// higher bits of the smallest kept key, which the chunks' counts of the launch before give; then the kept tokens.
+template <int PASS>
+__global__ __launch_bounds__(kSelectThreads) void kv_select_chunk_kernel(const SelectArgs a) {
+  __shared__ uint32_t hist[2048], pick[2];
+  __shared__ uint64_t waves[kSelectThreads / 64];
+  const int tid = threadIdx.x;
+  const int head = blockIdx.x / a.chunks, chunk = blockIdx.x - head * a.chunks;
+  const SelectHead h(a, head, PASS == 0 && chunk == 0 && tid == 0);
+  const int64_t from = chunk * a.per;
+  const int to = static_cast<int>(from + a.per < h.len ? from + a.per : h.len), chunks = static_cast<int>((h.len + a.per - 1) / a.per);
+  if (from >= h.len || (PASS < 3 && h.left <= 0)) return;
+  const int64_t mine = static_cast<int64_t>(head) * a.chunks + chunk;
+  constexpr int kBins[3] = {2048, 2048, 1024};
+  uint32_t* found = a.found + static_cast<int64_t>(head) * 4;  // the first two bins, and what is left within the second
+  uint32_t least = 0xffffffffu, left = h.left, bin = 0;
+  if (PASS > 0 && h.left > 0) {
+    if (PASS > 1) {
+      least = found[0] << 21;
+      left = found[1];
+    } else {
+      least = 0;
     }
+    if (PASS > 2) {
+      least |= found[2] << 10;
+      left = found[3];
+    }
+    // all chunks' counts of the launch before; this chunk's keys above the bin that they give are kept
+    constexpr int kOf = PASS > 0 ? PASS - 1 : 0, kCount = kBins[kOf];
+    uint32_t x[2] = {0, 0}, own[2] = {0, 0};
+    if (2 * tid < kCount)
+      for (int c = 0; c < chunks; ++c) {
+        const uint2 y = *reinterpret_cast<const uint2*>(a.bins[kOf] + (static_cast<int64_t>(head) * a.chunks + c) * kCount + 2 * tid);
+        x[0] += y.x, x[1] += y.y;
+        if (c == chunk) own[0] = y.x, own[1] = y.y;
+      }
+    find_bin(x[0], x[1], left, bin, waves, pick);
+    least |= bin << select_shift(kOf);
+    if (PASS < 3) {
+      uint64_t total;
+      block_scan((2 * tid > static_cast<int>(bin) ? own[0] : 0u) + (2 * tid + 1 > static_cast<int>(bin) ? own[1] : 0u), waves, total);
+      if (tid == 0) {
+        a.above[mine * 2 + kOf] = static_cast<uint32_t>(total);
+        if (chunk == 0) {
+          found[2 * kOf] = bin;
+          found[2 * kOf + 1] = left;
+        }
+      }
+    }
+  }
+  // rounds of 8 neighbouring tokens a thread
+  constexpr int K = 8, kRound = K * kSelectThreads;
+  if constexpr (PASS < 3) {
+    constexpr int kHigher = PASS > 0 ? select_shift(PASS - 1) : 0;
+    for (int x = tid; x < kBins[PASS]; x += kSelectThreads) hist[x] = 0;
     __syncthreads();
-    uint32_t g = above + __popcll(bg & before), e = same + __popcll(be & before);
+    for (int64_t t0 = from; t0 < to; t0 += kRound) {
+      const int t = static_cast<int>(t0) + tid * K;
+      float w[K];
+      load_weights<K>(h.w, t, to, w);
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const uint32_t p = scan[0][v], q = scan[1][v];
-      if (v < wave) g += p, e += q;
-      above += p, same += q;
+      for (int k = 0; k < K; ++k) {
+        const uint32_t x = key_of(w[k]);
+        if ((PASS == 0 || x >> kHigher == least >> kHigher) && t + k < to && !h.always(a, t + k))
+          atomicAdd(&hist[x >> select_shift(PASS) & select_mask(PASS)], 1u);
+      }
     }
-    if (gt || (eq && e < equal)) {
-      const int64_t at = row * a.k.ld + g + min(e, equal);
-      a.k.keep[at] = t;
-      if (a.kept) a.kept[at] = w[t];
+    __syncthreads();
+    for (int x = tid; x < kBins[PASS]; x += kSelectThreads) a.bins[PASS][mine * kBins[PASS] + x] = hist[x];
+  } else {
+    const uint32_t equal = h.left > 0 ? left : 0;
+    // kept tokens of the chunks before: those above the bins, those above the key in the last bins, and the always kept ones
+    uint64_t count = 0;
+    for (int c = 0; c < chunk && h.left > 0; ++c) {
+      const int64_t other = static_cast<int64_t>(head) * a.chunks + c;
+      const uint32_t y = a.bins[2][other * 1024 + tid];
+      if (static_cast<uint32_t>(tid) > bin) count += static_cast<uint64_t>(y) << 32;
+      if (static_cast<uint32_t>(tid) == bin) count += y;
+      if (tid < 2) count += static_cast<uint64_t>(a.above[other * 2 + tid]) << 32;
+    }
+    uint64_t total;
+    block_scan(count, waves, total);
+    uint64_t before = total + (static_cast<uint64_t>(n_always_before(a, h, static_cast<int>(from))) << 32);
+    for (int64_t t0 = from; t0 < to; t0 += kRound) {
+      const int t = static_cast<int>(t0) + tid * K;
+      float w[K];
+      load_weights<K>(h.w, t, to, w);
+      write_kept<K>(a, h, w, t, to, least, equal, before, waves);
     }
   }
 }
@@ -660,11 +841,28 @@ struct GatherArgs {
   int B, pages;  // pages: grid's bound of a sequence's new ones
 };
 
-// A new page's scale is the largest of its tokens' old ones; a code becomes rint(c (old / new)).
+// Four codes times a factor each, rounded to the nearest integer: the product's last places under 1.5 * 2^23.
+__device__ __forceinline__ uint32_t moved4(uint32_t codes, const float (&f)[4]) {
+  uint32_t z[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float y = static_cast<float>(static_cast<int8_t>(codes >> (8 * i))) * f[i];
+    z[i] = __float_as_uint(y + 12582912.f);
+  }
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(z[3], z[2], 0x0c0c0400u), __builtin_amdgcn_perm(z[1], z[0], 0x0c0c0400u), 0x05040100u);
+}
+
+// A new page's scale is the largest of its tokens' old ones; a code becomes rint(c (old / new)).  Keys move 16 bytes at a time.  Values
+// lie transposed, so that a kept one is a byte among others that are not kept: neighbouring tokens of one old page are a run,
+// and the runs' rows pass through LDS whole, some elements at a time, where they are few enough; otherwise byte by byte (GATHER_FIGURES).
+constexpr int kGatherLds = 16384;
 __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
   __shared__ int64_t from[256];     // the token's head and slot: (page * Hkv + hk) * page size + slot
   __shared__ float by[2][256];      // old scale over new
   __shared__ float red[2][4];
+  __shared__ int64_t run_head[256];  // the old page's head of a run
+  __shared__ int runs_of[4];
+  extern __shared__ __align__(16) uint8_t rows[];  // kGatherLds bytes where pages are of 64 tokens or more: [run][element][slot]
   const int tid = threadIdx.x, D = a.c.D, pl2 = a.c.page_log2, P = 1 << pl2;
   uint32_t item = blockIdx.x;
   const int hk = static_cast<int>(item % a.c.Hkv);
@@ -709,7 +907,18 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
     by[1][tid] = vs == v_new ? 1.f : vs / v_new;
   }
   const bool k_ok = k_new == k_new, v_ok = v_new == v_new;
+  // runs, and which one each token is of
+  const bool begins = tid < n && (tid == 0 || from[tid] >> pl2 != from[tid - 1] >> pl2);
+  const unsigned long long begun = __ballot(begins);
+  if ((tid & 63) == 0) runs_of[tid >> 6] = __popcll(begun);
   __syncthreads();
+  int run = __popcll(begun & ((2ull << (tid & 63)) - 1)) - 1, runs = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i < tid >> 6) run += runs_of[i];
+    runs += runs_of[i];
+  }
+  if (begins) run_head[run] = from[tid] >> pl2;
   const int64_t head = static_cast<int64_t>(dest) * a.c.Hkv + hk;
   if (tid == 0) {
     a.c.k_scale[head] = k_new;
@@ -726,23 +935,52 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
       const float f = by[0][j];
       if (f != 1.f) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int v = moved(static_cast<int8_t>(y[i >> 2] >> (8 * (i & 3))), f);
-          y[i >> 2] = (y[i >> 2] & ~(255 << (8 * (i & 3)))) | ((v & 255) << (8 * (i & 3)));
-        }
+        for (int i = 0; i < 4; ++i) y[i] = static_cast<int>(moved4(static_cast<uint32_t>(y[i]), {f, f, f, f}));
       }
     }
     *reinterpret_cast<ev_i4*>(k_to + j * D + e) = y;
   }
   int8_t* v_to = a.c.v + (head << pl2) * D;
-  for (int x = tid; x < P * D; x += 256) {
-    const int e = x >> pl2, j = x & (P - 1);
-    int8_t y = 0;
-    if (j < n && v_ok) {
-      const int64_t head_from = from[j] >> pl2;
-      y = moved(a.c.v[((head_from * D + e) << pl2) + (from[j] & (P - 1))], by[1][j]);
+  if (!v_ok || P < 64 || runs << pl2 > kGatherLds / 4) {
+    for (int x = tid; x < P * D; x += 256) {
+      const int e = x >> pl2, j = x & (P - 1);
+      int8_t y = 0;
+      if (j < n && v_ok) {
+        const int64_t head_from = from[j] >> pl2;
+        y = moved(a.c.v[((head_from * D + e) << pl2) + (from[j] & (P - 1))], by[1][j]);
+      }
+      v_to[x] = y;
     }
-    v_to[x] = y;
+    return;
+  }
+  // this thread's four tokens of an element: where they are in their run's row, and their factors
+  __shared__ int place[256];
+  const int lanes = P >> 2, j0 = (tid & (lanes - 1)) * 4, each = min(D, kGatherLds / (runs << pl2));  // elements at a time
+  if (tid < n) place[tid] = ((run * each) << pl2) + static_cast<int>(from[tid] & (P - 1));
+  __syncthreads();
+  int at[4];
+  float f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    at[i] = j0 + i < n ? place[j0 + i] : 0;
+    f[i] = j0 + i < n ? by[1][j0 + i] : 0.f;
+  }
+  for (int e0 = 0; e0 < D; e0 += each) {
+    const int count = min(each, D - e0), row_pieces = count << pl2 >> 4;  // 16-byte pieces of a run
+    __syncthreads();
+    for (int x = tid; x < runs * row_pieces; x += 256) {
+      const int u = x / row_pieces, y = x - u * row_pieces;
+      *reinterpret_cast<ev_i4*>(rows + ((u * each) << pl2) + y * 16) =
+          *reinterpret_cast<const ev_i4*>(a.c.v + ((run_head[u] * D + e0) << pl2) + y * 16);
+    }
+    __syncthreads();
+    for (int x = tid; x < count * lanes; x += 256) {
+      const int e = x / lanes;
+      const uint8_t* row = rows + (e << pl2);
+      const uint32_t word = row[at[0]] | static_cast<uint32_t>(row[at[1]]) << 8 | static_cast<uint32_t>(row[at[2]]) << 16 |
+                            static_cast<uint32_t>(row[at[3]]) << 24;
+      *reinterpret_cast<uint32_t*>(v_to + (static_cast<int64_t>(e0 + e) << pl2) + j0) = moved4(word, f);
+    }
   }
 }
 
@@ -795,12 +1033,52 @@ hipError_t launch_kv_weights(const KvCache& c, const KvBatch& bt, int max_kv, in
   return hipGetLastError();
 }
 
+namespace {
+// Chunks of the divided form: of 8192 tokens, or what leaves about 1024 of them for all heads.
+int select_chunks(int64_t heads, int64_t ld) {
+  if (ld <= kSelectMost) return 0;
+  const int64_t most = cdiv(ld, 8192), want = cdiv(1024, heads);
+  return static_cast<int>(want < most ? want : most);
+}
+void carve_select(WsCursor& c, int64_t heads, int chunks, SelectArgs& a) {
+  if (!chunks) return;
+  const size_t n = static_cast<size_t>(heads) * chunks;
+  a.bins[0] = c.take<uint32_t>(n * 2048);
+  a.bins[1] = c.take<uint32_t>(n * 2048);
+  a.bins[2] = c.take<uint32_t>(n * 1024);
+  a.above = c.take<uint32_t>(n * 2);
+  a.found = c.take<uint32_t>(static_cast<size_t>(heads) * 4);
+}
+}  // namespace
+
+size_t kv_select_ws_bytes(int B, int Hkv, int64_t ld) {
+  const int64_t heads = static_cast<int64_t>(B) * Hkv;
+  SelectArgs a = {};
+  WsCursor c(nullptr);
+  carve_select(c, heads, select_chunks(heads, ld), a);
+  return c.used;
+}
+
 hipError_t launch_kv_select(int B, int Hkv, const int32_t* kv_len, const float* weights, int64_t ld, int budget, int sinks,
-                            int recent, const KvKeep& k, float* kept_weights, hipStream_t stream) {
-  const int64_t blocks = static_cast<int64_t>(B) * Hkv;
-  if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-  const SelectArgs a = {kv_len, weights, ld, k, kept_weights, Hkv, budget, sinks, recent};
-  kv_select_kernel<<<dim3(static_cast<uint32_t>(blocks)), 1024, 0, stream>>>(a);
+                            int recent, const KvKeep& k, float* kept_weights, void* ws, hipStream_t stream) {
+  const int64_t heads = static_cast<int64_t>(B) * Hkv;
+  const int chunks = select_chunks(heads, ld);
+  if (heads * (chunks > 0 ? chunks : 1) > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  SelectArgs a = {kv_len, weights, ld, k, kept_weights, Hkv, budget, sinks, recent, 0, chunks, {}, nullptr, nullptr};
+  const dim3 grid(static_cast<uint32_t>(heads * (chunks > 0 ? chunks : 1)));
+  if (!chunks) {
+    if (ld <= 4096) kv_select_kernel<4><<<grid, kSelectThreads, 0, stream>>>(a);
+    else if (ld <= 8192) kv_select_kernel<8><<<grid, kSelectThreads, 0, stream>>>(a);
+    else kv_select_kernel<16><<<grid, kSelectThreads, 0, stream>>>(a);
+    return hipGetLastError();
+  }
+  a.per = cdiv(cdiv(ld, chunks), kSelectThreads) * kSelectThreads;
+  WsCursor cur(ws);
+  carve_select(cur, heads, chunks, a);
+  kv_select_chunk_kernel<0><<<grid, kSelectThreads, 0, stream>>>(a);
+  kv_select_chunk_kernel<1><<<grid, kSelectThreads, 0, stream>>>(a);
+  kv_select_chunk_kernel<2><<<grid, kSelectThreads, 0, stream>>>(a);
+  kv_select_chunk_kernel<3><<<grid, kSelectThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -810,7 +1088,7 @@ hipError_t launch_kv_gather(const KvCache& c, int B, const int32_t* table, int64
   if (blocks == 0) return hipSuccess;
   if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
   const GatherArgs a = {c, table, to, kv_len, ld_table, ld_to, k, B, static_cast<int>(pages)};
-  kv_gather_kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, stream>>>(a);
+  kv_gather_kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, c.page_log2 >= 6 ? kGatherLds : 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -48,7 +48,7 @@ def weights(L, **kw):
 
 
 def select(L, **kw):
-    a = dict(B=2, Hkv=4, kv_len=P(1), w=P(2), ld=1000, budget=100, sinks=4, recent=20, keep=P(3), ld_keep=100, n=P(4), kept=P(5))
+    a = dict(B=2, Hkv=4, kv_len=P(1), w=P(2), ld=1000, budget=100, sinks=4, recent=20, keep=P(3), ld_keep=100, n=P(4), kept=P(5), ws=P(20), wsb=1 << 40)
     a.update(kw)
     return L.crvq_kv_select(*a.values(), None)
 
@@ -124,6 +124,10 @@ def test_select_arguments(L):
                         (dict(B=1 << 30, Hkv=4), 2)]:
         assert select(L, **bad) == status and "crvq_kv_select" in err(L), (bad, err(L))
     assert select(L, B=0, kv_len=None) == 0
+    need = L.crvq_kv_select_workspace_size(2, 4, 200000)
+    assert need and need % 256 == 0 and need == L.crvq_workspace_size(15, 2, 0, 0, 0, 0, None, 0, 4, 200000)
+    assert select(L, ld=200000, ws=None) == 3 and select(L, ld=200000, wsb=need - 1) == 3 and select(L, ld=200000, ws=P(20, 8)) == 3
+    assert L.crvq_kv_select_workspace_size(2, 4, 1000) == 0 and L.crvq_kv_select_workspace_size(2, 4, -1) == 0
 
 
 def test_gather_arguments(L):
