@@ -1,18 +1,23 @@
 """The attention block of a decoder on quantized data, as a sequence of libcrvq calls.
 
     python -m paper_2412_09282_amd.decode [--channels 4096 --heads 32 --kv-heads 32 --seqs 4 --prompt 300 --steps 32]
+                                          [--bits 8 --layers 4 --draft 8 --budget 256]
 
-A block holds its projections in 4 bits with group scales (crvq_w4_quantize) and its keys and values in a paged
-cache of 8 bits with a scale for each page and head.  One call of the block takes the activations of every
-sequence's new tokens (prompts, single tokens, or both in one batch) through
+A block holds its projections in 4 bits with group scales (crvq_w4_quantize) or in 8 bits with a scale for each
+channel (crvq_w8_quantize), and its keys and values in a paged cache of 8 bits with a scale for each page and head.
+One call of the block takes the activations of every sequence's new tokens (prompts, single tokens, drafts, or all in
+one batch) through
 
-    crvq_w4_gemv       queries, keys and values, one stacked matrix
-    crvq_kv_append     rotation by the tokens' places, quantization and storage of keys and values
-    crvq_kv_attention  attention of the new tokens over the cache
-    crvq_w4_gemv       the output projection
+    crvq_w4_gemv, crvq_w8_gemm     queries, keys and values, one stacked matrix
+    crvq_kv_append                 rotation by the tokens' places, quantization and storage of keys and values
+    crvq_kv_attention, crvq_kv_tree_attention   attention of the new tokens over the cache
+    crvq_kv_weights                what the cached tokens were attended to, where the cache tracks it
+    crvq_w4_gemv, crvq_w8_gemm     the output projection
 
-Every arithmetic step runs in the library's kernels; this module allocates device tensors, hands out pages and
-sequences the calls.  The program decodes with random weights and activations and prints the time of a step.
+A stack of blocks has the norms, gates and residual sums between them (crvq_norm).  PagedCache.accept keeps the accepted
+ones of a tree's drafted tokens, PagedCache.evict brings sequences to a budget of tokens (crvq_kv_select,
+crvq_kv_gather).  Every arithmetic step runs in the library's kernels; this module allocates device tensors, hands out
+pages and sequences the calls.  The program decodes with random weights and activations and prints the time of a step.
 """
 from __future__ import annotations
 
@@ -45,11 +50,43 @@ class W4Matrix:
         return y
 
 
-class PagedCache:
-    """Pages of keys and values in 8 bits and the sequences that own them."""
+class W8Matrix:
+    """An M x N matrix in 8 bits with a scale for each row."""
 
-    def __init__(self, n_pages: int, kv_heads: int, head_dim: int, page: int = 64, device="cuda"):
-        self.page = page
+    def __init__(self, W: torch.Tensor):
+        M, N = W.shape
+        self.codes = torch.empty(M, -(-N // 16) * 16, dtype=torch.int8, device=W.device)
+        self.scales = torch.empty(M, device=W.device)
+        C.crvq_w8_quantize(W, self.codes, self.scales)
+
+    def product(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                dtype=torch.bfloat16) -> torch.Tensor:
+        """x (T x N) times the matrix transposed, x brought to 8 bits token by token; with scales x is codes already.
+        y: T x M of x's type (of dtype for codes) unless given."""
+        T = x.shape[0]
+        if y is None:
+            y = torch.empty(T, self.codes.shape[0], dtype=dtype if scales is not None else x.dtype, device=x.device)
+        if scales is None:
+            codes = torch.empty(T, self.codes.shape[1], dtype=torch.int8, device=x.device)
+            scales = torch.empty(T, device=x.device)
+            C.crvq_w8_quantize(x, codes, scales)
+            x = codes
+        C.crvq_w8_gemm(self.codes, self.scales, x, scales, y)
+        return y
+
+
+class PagedCache:
+    """Pages of keys and values in 8 bits and the sequences that own them.
+
+    lengths: tokens of a sequence in the cache; places: where its next token stands, which is more once tokens were
+    evicted.  track: room for so many tokens of every sequence's accumulated attention weights, which `evict` goes by."""
+
+    def __init__(self, n_pages: int, kv_heads: int, head_dim: int, page: int = 64, device="cuda", track: int = 0):
+        self.page, self.track = page, track
+        self.weights: Optional[torch.Tensor] = None  # sequences x kv_heads x track
+        self.places: List[int] = []
+        self.drafts: Optional[List[int]] = None  # of the batch that waits for `accept`
+        self.evicted = False
         self.k = torch.zeros(n_pages, kv_heads, page, head_dim, dtype=torch.int8, device=device)
         self.v = torch.zeros(n_pages, kv_heads, head_dim, page, dtype=torch.int8, device=device)
         self.k_scale = torch.zeros(n_pages, kv_heads, device=device)
@@ -61,33 +98,138 @@ class PagedCache:
     def add_sequence(self) -> int:
         self.pages.append([])
         self.lengths.append(0)
+        self.places.append(0)
+        if self.track:
+            more = torch.zeros(1, self.k.shape[1], self.track, device=self.k.device)
+            self.weights = more if self.weights is None else torch.cat((self.weights, more))
         return len(self.lengths) - 1
 
     def drop_sequence(self, b: int) -> None:
         """The sequence's pages are free again; it stays in the batch with nothing in it."""
         self.free.extend(reversed(self.pages[b]))
-        self.pages[b], self.lengths[b] = [], 0
+        self.pages[b], self.lengths[b], self.places[b] = [], 0, 0
+        if self.drafts is not None:
+            self.drafts[b] = 0
 
-    def grow(self, counts: Sequence[int]) -> "Batch":
-        """Room for counts[b] more tokens of every sequence, and the batch arrays of the call that brings them."""
+    def _ints(self, v) -> torch.Tensor:
+        return torch.tensor(v, dtype=torch.int32, device=self.k.device)
+
+    def _table(self, pages: Sequence[Sequence[int]]) -> torch.Tensor:
+        width = max(1, max((len(p) for p in pages), default=1))
+        return self._ints([list(p) + [0] * (width - len(p)) for p in pages]).view(len(pages), width)
+
+    def grow(self, counts: Sequence[int], parents: Optional[Sequence[Sequence[int]]] = None) -> "Batch":
+        """Room for counts[b] more tokens of every sequence, and the batch arrays of the call that brings them.  parents:
+        the new tokens are drafts, parents[b][i] being the index of token i's parent among them, below i, or -1; `accept`
+        says which of them stay."""
+        if self.drafts is not None:
+            raise RuntimeError("drafted tokens wait to be accepted")
         if len(counts) != len(self.lengths):
             raise ValueError(f"{len(counts)} counts for {len(self.lengths)} sequences")
         if min(counts, default=0) < 0:
             raise ValueError("a sequence cannot bring a negative number of tokens")
+        if parents is not None and [len(p) for p in parents] != list(counts):
+            raise ValueError("every drafted token has a parent, or -1")
+        if self.track and max((n + k for n, k in zip(counts, self.lengths)), default=0) > self.track:
+            raise RuntimeError(f"more tokens than the {self.track} whose weights are tracked")
         need = [max(0, -(-(n + k) // self.page) - len(p)) for n, k, p in zip(counts, self.lengths, self.pages)]
         if sum(need) > len(self.free):
             raise RuntimeError(f"the cache is full: {sum(need)} pages needed, {len(self.free)} free")
         for b, n in enumerate(need):
             self.pages[b].extend(self.free.pop() for _ in range(n))
             self.lengths[b] += counts[b]
-        dev, width = self.k.device, max(1, max((len(p) for p in self.pages), default=1))
         starts = [0]
         for n in counts:
             starts.append(starts[-1] + n)
-        ints = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)  # noqa: E731
-        table = ints([p + [0] * (width - len(p)) for p in self.pages]).view(len(self.pages), width)
-        return Batch(table, ints(starts), ints(self.lengths), max(counts, default=0), max(self.lengths, default=0),
-                     starts[-1])
+        batch = Batch(self._table(self.pages), self._ints(starts), self._ints(self.lengths), max(counts, default=0),
+                      max(self.lengths, default=0), starts[-1])
+        if parents is not None:
+            self.drafts = list(counts)
+            batch.mask = torch.zeros(starts[-1], -(-max(batch.max_new, 1) // 64), dtype=torch.int64, device=self.k.device)
+            batch.places = torch.zeros(starts[-1], dtype=torch.int32, device=self.k.device)
+            C.crvq_tree_mask(self._ints([p for tree in parents for p in tree]), batch.start,
+                             self._ints([p + n for p, n in zip(self.places, counts)]), batch.max_new, batch.mask, batch.places)
+            return batch
+        if self.places != [k - n for n, k in zip(counts, self.lengths)]:
+            batch.places = self._ints([p + i for p, n in zip(self.places, counts) for i in range(n)])
+        self.places = [p + n for p, n in zip(self.places, counts)]
+        return batch
+
+    def _move(self, what, tables, lengths, keep, counts, kept_len) -> List[List[int]]:
+        """New pages of the sequences `what` that hold their tokens `keep` (sequences x heads x room) of `tables`; counts:
+        how many (kept_len on the device)."""
+        room = [-(-n // self.page) if b in what else 0 for b, n in enumerate(counts)]
+        new = [[self.free.pop() for _ in range(n)] for n in room]
+        C.crvq_kv_gather(*self.tensors, self._table(tables), lengths, keep, kept_len, self._table(new))
+        return new
+
+    def accept(self, tokens: Sequence[Sequence[int]]) -> None:
+        """Of the last batch's drafted tokens those at tokens[b] (in order, a path of the tree) become sequence b's next
+        ones; the others are gone."""
+        if self.drafts is None:
+            raise RuntimeError("no drafted tokens wait to be accepted")
+        if len(tokens) != len(self.drafts):
+            raise ValueError(f"{len(tokens)} lists for {len(self.drafts)} sequences")
+        tokens = [list(t) for t in tokens]
+        for t, n in zip(tokens, self.drafts):
+            if any(not 0 <= i < n for i in t) or any(i >= j for i, j in zip(t, t[1:])):
+                raise ValueError(f"{t} are not drafted tokens in order: there are {n}")
+        B, P = len(tokens), self.page
+        context = [k - n for k, n in zip(self.lengths, self.drafts)]
+        first = [c // P for c in context]  # the page that the drafts begin in
+        what = {b for b, t in enumerate(tokens) if t != list(range(len(t)))}
+        if what:
+            rows = [list(range(c - f * P)) + [c - f * P + i for i in t] if b in what else []
+                    for b, (c, f, t) in enumerate(zip(context, first, tokens))]
+            need = sum(-(-len(r) // P) for r in rows)
+            if need > len(self.free):
+                raise RuntimeError(f"the cache is full: {need} pages needed, {len(self.free)} free")
+            width = max(len(r) for r in rows)
+            keep = self._ints([r + [-1] * (width - len(r)) for r in rows]).view(B, 1, width)
+            lengths = self._ints([k - f * P for k, f in zip(self.lengths, first)])
+            counts = [len(r) for r in rows]
+            new = self._move(what, [p[f:] for p, f in zip(self.pages, first)], lengths, keep, counts, self._ints(counts))
+        for b, t in enumerate(tokens):
+            if b in what:
+                self.free.extend(reversed(self.pages[b][first[b]:]))
+                self.pages[b] = self.pages[b][:first[b]] + new[b]
+                if self.weights is not None:
+                    at = torch.tensor([context[b] + i for i in t], device=self.k.device)
+                    self.weights[b, :, context[b]:context[b] + len(t)] = self.weights[b].index_select(1, at)
+            self.lengths[b] = context[b] + len(t)
+            self.places[b] += len(t)
+            left = -(-self.lengths[b] // P)
+            self.free.extend(reversed(self.pages[b][left:]))
+            self.pages[b] = self.pages[b][:left]
+        self.drafts = None
+
+    def evict(self, budget: int, sinks: int = 4, recent: int = 0) -> None:
+        """Brings every sequence that has more than `budget` tokens down to as many: its first `sinks`, its last `recent`, and
+        of each head the others that were attended to most."""
+        if self.weights is None:
+            raise RuntimeError("the cache does not track attention weights")
+        if self.drafts is not None:
+            raise RuntimeError("drafted tokens wait to be accepted")
+        if budget < 1 or min(sinks, recent) < 0 or sinks + recent > budget:
+            raise ValueError(f"{sinks} first and {recent} last tokens in a budget of {budget}")
+        P, B = self.page, len(self.lengths)
+        waiting = [b for b, n in enumerate(self.lengths) if n > budget]
+        while waiting:
+            fit = len(self.free) // -(-budget // P)  # sequences that there are pages for
+            if not fit:
+                raise RuntimeError(f"the cache is full: {-(-budget // P)} pages needed, {len(self.free)} free")
+            what, waiting = set(waiting[:fit]), waiting[fit:]
+            lengths = self._ints([n if b in what else 0 for b, n in enumerate(self.lengths)])
+            keep = torch.empty(B, self.k.shape[1], budget, dtype=torch.int32, device=self.k.device)
+            kept = torch.empty(B, self.k.shape[1], budget, device=self.k.device)
+            kept_len = torch.empty(B, dtype=torch.int32, device=self.k.device)
+            C.crvq_kv_select(self.weights, lengths, budget, keep, kept_len, kept_weights=kept, sinks=sinks, recent=recent)
+            new = self._move(what, self.pages, lengths, keep, [budget] * B, kept_len)
+            for b in what:
+                self.free.extend(reversed(self.pages[b]))
+                self.pages[b], self.lengths[b] = new[b], budget
+                self.weights[b, :, :budget] = kept[b]
+            self.evicted = True
 
     @property
     def tensors(self):
@@ -103,6 +245,8 @@ class Batch:
     max_new: int
     max_kv: int
     tokens: Optional[int] = None  # new tokens of all sequences
+    places: Optional[torch.Tensor] = None  # of the new tokens, where they are not those behind the cached ones
+    mask: Optional[torch.Tensor] = None  # of drafted tokens: which of them each one sees
 
 
 def rotary_angles(n: int, rot: int, base: float = 10000.0, device="cuda"):
@@ -113,28 +257,109 @@ def rotary_angles(n: int, rot: int, base: float = 10000.0, device="cuda"):
 
 
 class AttentionBlock:
-    """Stacked query / key / value projection, cache and output projection of one decoder layer."""
+    """Stacked query / key / value projection, cache and output projection of one decoder layer; bits: of the projections'
+    weights, 4 or 8 (with 8 the activations have 8 bits too)."""
 
     def __init__(self, W_qkv: torch.Tensor, W_out: torch.Tensor, heads: int, kv_heads: int, cache: PagedCache, cos, sin,
-                 group: int = 128, zeros: bool = False, window: int = 0):
+                 group: int = 128, zeros: bool = False, window: int = 0, bits: int = 4):
         D = cache.k.shape[3]
         if W_qkv.shape[0] != (heads + 2 * kv_heads) * D or W_out.shape[1] != heads * D:
             raise ValueError("the projections do not fit the heads")
-        self.heads, self.kv_heads, self.D, self.window = heads, kv_heads, D, window
-        self.qkv, self.out = W4Matrix(W_qkv, group, zeros), W4Matrix(W_out, group, zeros)
+        if bits not in (4, 8):
+            raise ValueError(f"{bits} bits: 4 or 8")
+        self.heads, self.kv_heads, self.D, self.window, self.bits = heads, kv_heads, D, window, bits
+        matrix = (lambda W: W4Matrix(W, group, zeros)) if bits == 4 else W8Matrix
+        self.qkv, self.out = matrix(W_qkv), matrix(W_out)
         self.cache, self.cos, self.sin = cache, cos, sin
 
-    def __call__(self, x: torch.Tensor, batch: Batch) -> torch.Tensor:
-        """x: the new tokens' activations, T x channels, sequence after sequence."""
+    def __call__(self, x: torch.Tensor, batch: Batch, scales: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x: the new tokens' activations, T x channels, sequence after sequence; with scales in 8 bits already (blocks of
+        8 bits; the result is bf16 then)."""
         if batch.tokens is not None and x.shape[0] != batch.tokens:
             raise ValueError(f"{x.shape[0]} rows for a batch of {batch.tokens} new tokens")
+        if scales is not None and self.bits != 8:
+            raise ValueError("8-bit activations for a block of 4 bits")
+        if self.window and self.cache.evicted:
+            raise ValueError("a window counts tokens, and some were evicted")
         H, K, D = self.heads, self.kv_heads, self.D
-        q, k, v = (t.unflatten(1, (-1, D)) for t in self.qkv.product(x).split([H * D, K * D, K * D], 1))
+        qkv = self.qkv.product(x) if scales is None else self.qkv.product(x, scales=scales)
+        q, k, v = (t.unflatten(1, (-1, D)) for t in qkv.split([H * D, K * D, K * D], 1))
         where = (*self.cache.tensors, batch.table, batch.start, batch.kv_len)
-        C.crvq_kv_append(k, v, *where, batch.max_new, cos=self.cos, sin=self.sin, q=q, q_out=q)
-        o = torch.empty(x.shape[0], H, D, dtype=x.dtype, device=x.device)
-        C.crvq_kv_attention(q, o, *where, batch.max_new, batch.max_kv, window=self.window)
+        C.crvq_kv_append(k, v, *where, batch.max_new, cos=self.cos, sin=self.sin, positions=batch.places, q=q, q_out=q)
+        o = torch.empty(q.shape[0], H, D, dtype=q.dtype, device=q.device)
+        track = self.cache.weights is not None
+        lse = torch.empty(q.shape[0], H, device=q.device) if track else None
+        if batch.mask is not None:
+            C.crvq_kv_tree_attention(q, o, *where, batch.max_new, batch.max_kv, batch.mask, window=self.window,
+                                     places=batch.places, lse=lse)
+        else:
+            C.crvq_kv_attention(q, o, *where, batch.max_new, batch.max_kv, window=self.window, lse=lse)
+        if track:
+            w = self.cache.weights
+            C.crvq_kv_weights(q, lse, w, w, self.cache.k, self.cache.k_scale, batch.table, batch.start, batch.kv_len,
+                              batch.max_new, batch.max_kv, window=self.window, mask=batch.mask,
+                              places=batch.places if batch.mask is not None else None)
         return self.out.product(o.flatten(1))
+
+
+class Stack:
+    """Blocks with a norm before each (pre[i]), and after each where post is given, around a residual stream in fp32:
+    r = r + alpha norm(block(norm(r) pre[i])) post[i].  A block of 8 bits takes the norm's result in 8 bits."""
+
+    def __init__(self, blocks: Sequence[AttentionBlock], pre: Sequence[torch.Tensor],
+                 post: Optional[Sequence[torch.Tensor]] = None, alpha: float = 1.0, eps: float = 1e-5, dtype=torch.bfloat16):
+        if len(pre) != len(blocks) or (post is not None and len(post) != len(blocks)):
+            raise ValueError("every block has its norms")
+        self.blocks, self.pre, self.post = list(blocks), list(pre), list(post) if post is not None else [None] * len(blocks)
+        self.alpha, self.eps, self.dtype = alpha, eps, dtype
+
+    def __call__(self, r: torch.Tensor, batches: Sequence[Batch]) -> torch.Tensor:
+        """r: T x channels, fp32, which the result takes the place of; batches: of every block's cache."""
+        if len(batches) != len(self.blocks):
+            raise ValueError(f"{len(batches)} batches for {len(self.blocks)} blocks")
+        T, N = r.shape
+        out, w_post, given = torch.zeros(T, N, dtype=self.dtype, device=r.device), None, None
+        for block, pre, post, batch in zip(self.blocks, self.pre, self.post, batches):
+            scales = torch.empty(T, device=r.device) if block.bits == 8 else None
+            h = torch.empty(T, N, dtype=self.dtype, device=r.device) if scales is None else \
+                torch.empty(T, -(-N // 16) * 16, dtype=torch.int8, device=r.device)
+            # the sum of the block before and this one's norm; the first block has nothing before it
+            C.crvq_norm(out, h, residual=r, residual_out=given, w_pre=pre, w_post=w_post, alpha=self.alpha, eps=self.eps,
+                        h_scales=scales)
+            out, w_post, given = block(h, batch, scales), post, r
+        if given is not None:
+            C.crvq_norm(out, None, residual=r, residual_out=r, w_post=w_post, alpha=self.alpha, eps=self.eps)
+        return r
+
+
+def _decode(args, stack: Stack, caches: Sequence[PagedCache], rand) -> None:
+    """Steps of a stack with drafts and a budget of tokens, timed."""
+    def forward(counts, parents=None):
+        return stack(rand(sum(counts), args.channels), [c.grow(counts, parents) for c in caches])
+
+    forward([args.prompt] * args.seqs)
+    n = max(1, args.draft)
+    tree = [-1 if i == 0 else (i - 1) // 2 for i in range(n)]  # two continuations of every token
+    path = [n - 1]
+    while tree[path[0]] >= 0:
+        path.insert(0, tree[path[0]])
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    for i in range(args.steps):
+        if i == min(4, args.steps - 1):
+            start.record()
+        if args.budget and max(caches[0].lengths) + n > args.budget + args.budget // 4:
+            for c in caches:
+                c.evict(args.budget, recent=args.budget // 4)
+        r = forward([n] * args.seqs, [tree] * args.seqs if args.draft else None)
+        if args.draft:
+            for c in caches:
+                c.accept([path] * args.seqs)
+    end.record()
+    torch.cuda.synchronize()
+    n = args.steps - min(4, args.steps - 1)
+    print(f"{args.layers} layers of {args.bits} bits, {args.seqs} sequences, {args.draft} drafts of which {len(path)} stay, "
+          f"{max(caches[0].lengths)} tokens at the end: {start.elapsed_time(end) / n * 1e3:.1f} us a step; output finite: "
+          f"{bool(torch.isfinite(r).all())}", flush=True)
 
 
 def main(argv=None):
@@ -145,16 +370,32 @@ def main(argv=None):
     ap.add_argument("--seqs", type=int, default=4)
     ap.add_argument("--prompt", type=int, default=300)
     ap.add_argument("--steps", type=int, default=32)
+    ap.add_argument("--bits", type=int, default=4, choices=(4, 8), help="of the projections")
+    ap.add_argument("--layers", type=int, default=0, help="attention blocks with the norms and residual sums between them")
+    ap.add_argument("--draft", type=int, default=0, help="drafted tokens of a step, a path of which is accepted (with --layers)")
+    ap.add_argument("--budget", type=int, default=0, help="tokens that sequences are brought down to (with --layers)")
     args = ap.parse_args(argv)
-    D, total = args.channels // args.heads, args.prompt + args.steps
+    if (args.draft or args.budget) and not args.layers:
+        ap.error("--draft and --budget need --layers")
+    D, total = args.channels // args.heads, args.prompt + args.steps * max(1, args.draft)
     g = torch.Generator(device="cuda").manual_seed(0)
     rand = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
-    cache = PagedCache(args.seqs * (-(-total // 64)), args.kv_heads, D)
-    W = rand((args.heads + 2 * args.kv_heads) * D, args.channels).mul_(0.02).bfloat16()
-    Wo = rand(args.channels, args.heads * D).mul_(0.02).bfloat16()
-    block = AttentionBlock(W, Wo, args.heads, args.kv_heads, cache, *rotary_angles(total, D))
-    for _ in range(args.seqs):
-        cache.add_sequence()
+    pages = args.seqs * (-(-total // 64))
+    if args.layers:
+        pages += args.seqs * (-(-args.budget // 64) + 2)  # for what is moved
+    caches = [PagedCache(pages, args.kv_heads, D, track=total if args.budget else 0) for _ in range(max(1, args.layers))]
+    angles = rotary_angles(total, D)
+    blocks = []
+    for cache in caches:
+        W = rand((args.heads + 2 * args.kv_heads) * D, args.channels).mul_(0.02).bfloat16()
+        Wo = rand(args.channels, args.heads * D).mul_(0.02).bfloat16()
+        blocks.append(AttentionBlock(W, Wo, args.heads, args.kv_heads, cache, *angles, bits=args.bits))
+        for _ in range(args.seqs):
+            cache.add_sequence()
+    if args.layers:
+        ones = [torch.ones(args.channels, device="cuda") for _ in blocks]
+        return _decode(args, Stack(blocks, ones, ones), caches, rand)
+    cache, block = caches[0], blocks[0]
     y = block(rand(args.seqs * args.prompt, args.channels).bfloat16(), cache.grow([args.prompt] * args.seqs))
     start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     for i in range(args.steps):
