@@ -534,7 +534,7 @@ crvq_status crvq_tree_mask(int32_t B, const int32_t* parents, const int32_t* sta
  * j % 64 of word mask[row i][j / 64] is 1; bits from n on do not matter.  Any mask will
  * do; a row that sees nothing is 0.  window > 0: of the context only t > P_i - window, P_i =
  * places[row i] (int32, device), or kv_len[b] - n + i where places is NULL;
- * new tokens are seen as the mask says.
+ * new tokens are seen as the mask says.  At most 2^16 query heads a key head, and 2^30 rows of them.
  * workspace: crvq_kv_tree_attention_workspace_size(...) bytes. */
 size_t crvq_kv_tree_attention_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new, int32_t max_kv);
 crvq_status crvq_kv_tree_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages,
@@ -566,7 +566,7 @@ crvq_status crvq_kv_tree_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D
  * that bring no rows, whose rows are not within [0, n_tokens] or more than
  * max_new, or with kv_len[b] < 0, > max_kv or > ld_table * page, and tokens from kv_len[b] on, stay as they were in `after`.
  * Products are exact (CRVQ_F32 queries as three bf16 terms), sums fp32 in a
- * fixed order.  ld >= max_kv.
+ * fixed order.  ld >= max_kv; B * Hkv is at most 65535, and rows as in crvq_kv_tree_attention.
  * workspace: crvq_kv_weights_workspace_size(...) bytes. */
 size_t crvq_kv_weights_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new, int32_t max_kv);
 crvq_status crvq_kv_weights(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int64_t n_pages, const int8_t* k_cache,

@@ -629,12 +629,16 @@ def _enqueue(fn: str, on: torch.Tensor, stream, *args) -> None:
         _check(fn, status)
 
 
+def _ld(t: torch.Tensor, to: int = 1) -> int:
+    """The row stride; of one row or none whatever fits, since torch may give any."""
+    rows, N = t.shape
+    return t.stride(0) if rows > 1 else -(-N // to) * to
+
+
 def _w8_args(codes: torch.Tensor, scales: torch.Tensor):
     assert codes.dim() == 2 and codes.dtype == torch.int8 and codes.shape[0] == scales.numel()
-    assert scales.dtype == torch.float32 and scales.is_contiguous()
-    ld, one = codes.stride()
-    assert one == 1
-    return codes.data_ptr(), ld, scales.data_ptr()
+    assert scales.dtype == torch.float32 and scales.is_contiguous() and codes.stride(1) == 1
+    return codes.data_ptr(), _ld(codes, 16), scales.data_ptr()
 
 
 def crvq_w8_quantize(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
@@ -643,7 +647,7 @@ def crvq_w8_quantize(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
     assert X.stride(1) == 1 and codes.shape[0] == rows and codes.shape[1] >= -(-N // 16) * 16
     c, ld, s = _w8_args(codes, scales)
     _one_device(X, codes, scales)
-    _enqueue("crvq_w8_quantize", X, stream, rows, N, X.data_ptr(), X.stride(0), dtype_code(X), c, ld, s)
+    _enqueue("crvq_w8_quantize", X, stream, rows, N, X.data_ptr(), _ld(X), dtype_code(X), c, ld, s)
 
 
 def crvq_w8_gemm(codes: torch.Tensor, scales: torch.Tensor, x_codes: torch.Tensor, x_scales: torch.Tensor,
@@ -659,7 +663,7 @@ def crvq_w8_gemm(codes: torch.Tensor, scales: torch.Tensor, x_codes: torch.Tenso
     _one_device(y, codes, scales, x_codes, x_scales)
     nbytes = lib().crvq_w8_gemm_workspace_size(M, N, T)
     ws = _workspace_for(nbytes, y.device, stream) if nbytes else None
-    _enqueue("crvq_w8_gemm", y, stream, M, N, T, c, ld, s, xc, ldx, xs, y.data_ptr(), y.stride(0), dtype_code(y),
+    _enqueue("crvq_w8_gemm", y, stream, M, N, T, c, ld, s, xc, ldx, xs, y.data_ptr(), _ld(y), dtype_code(y),
              _ptr(ws), nbytes)
 
 
@@ -688,13 +692,13 @@ def crvq_norm(x: torch.Tensor, h: Optional[torch.Tensor] = None, residual: Optio
             r_dtype = dtype_code(t)
     if residual is not None:
         assert residual_out is None or residual_out.dtype == residual.dtype
-        ldr = residual.stride(0)
+        ldr = _ld(residual)
     if residual_out is not None:
-        ldro = residual_out.stride(0)
+        ldro = _ld(residual_out)
     assert x.stride(1) == 1
     ldh = 0
     if h is not None:
-        ldh = h.stride(0)
+        ldh = _ld(h, 1 if h_scales is None else 16)
         assert h.dim() == 2 and h.shape[0] == T and h.stride(1) == 1
         if h_scales is None:
             assert h.shape[1] == N and h.dtype == x.dtype
@@ -707,7 +711,7 @@ def crvq_norm(x: torch.Tensor, h: Optional[torch.Tensor] = None, residual: Optio
             assert w.shape == (N,) and w.is_contiguous() and w_dtype in (None, w.dtype)
             w_dtype = w.dtype
     _one_device(x, h, residual, residual_out, w_pre, b_pre, w_post, b_post, gate, h_scales)
-    _enqueue("crvq_norm", x, stream, T, N, CRVQ_NORM_LAYER if kind == "layer" else CRVQ_NORM_RMS, x.data_ptr(), x.stride(0),
+    _enqueue("crvq_norm", x, stream, T, N, CRVQ_NORM_LAYER if kind == "layer" else CRVQ_NORM_RMS, x.data_ptr(), _ld(x),
              dtype_code(x), int(post), _ptr(w_post), _ptr(b_post), _ptr(gate), ldg, alpha, _ptr(residual), ldr,
              _ptr(residual_out), ldro, r_dtype, _ptr(w_pre), _ptr(b_pre),
              CRVQ_F32 if w_dtype is None else _DTYPE_CODES[w_dtype], eps, _ptr(h), ldh, _ptr(h_scales))

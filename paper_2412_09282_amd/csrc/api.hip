@@ -1002,6 +1002,13 @@ crvq_status check_tree(const uint64_t* mask, int64_t ld_mask, const int32_t* pla
   return CRVQ_OK;
 }
 
+// The kernels count a key head's columns (new tokens times query heads) in 32 bits, with room for some tiles past the last one.
+crvq_status check_columns(int32_t max_new, int32_t G, const char* fn) {
+  if (G > 1 << 16 || static_cast<int64_t>(max_new) * G > 1 << 30)
+    return fail(CRVQ_ERR_UNSUPPORTED, "%s: %d rows of %d query heads a key head exceed 2^30, or the heads 2^16", fn, max_new, G);
+  return CRVQ_OK;
+}
+
 size_t mask_bytes(int64_t n_tokens, int64_t ld_mask) { return static_cast<size_t>(n_tokens) * ld_mask * 8; }
 
 }  // namespace
@@ -1055,7 +1062,7 @@ crvq_status crvq_kv_tree_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D
   if (window < 0) return fail(CRVQ_ERR_INVALID, "%s: window < 0", fn);
   if (B == 0 || max_new == 0 || n_tokens == 0) return CRVQ_OK;
   if (!mask) return fail(CRVQ_ERR_INVALID, "%s: mask must not be NULL", fn);
-  if ((s = check_tree(mask, ld_mask, places, max_new, fn))) return s;
+  if ((s = check_tree(mask, ld_mask, places, max_new, fn)) || (s = check_columns(max_new, Hq / Hkv, fn))) return s;
   if ((s = check_rows("q", q, q_tok, q_head, Hq, D, dtype, fn))) return s;
   if ((s = check_out_rows("out", out, o_tok, o_head, n_tokens, Hq, D, dtype, fn))) return s;
   const int es = esize(dtype);
@@ -1103,8 +1110,9 @@ crvq_status crvq_kv_weights(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32
   if (window < 0 || (window && !causal && !mask)) return fail(CRVQ_ERR_INVALID, "%s: window < 0, or a window without causal or mask", fn);
   if (ld < max_kv) return fail(CRVQ_ERR_INVALID, "%s: ld = %lld below max_kv = %d", fn, (long long)ld, max_kv);
   if (B == 0 || max_new == 0 || n_tokens == 0 || max_kv == 0) return CRVQ_OK;
-  if (static_cast<int64_t>(max_new) * (Hq / Hkv) > 0x7fffff00LL || static_cast<int64_t>(B) * Hkv > 65535)
-    return fail(CRVQ_ERR_UNSUPPORTED, "%s: more than 2^31 - 256 rows of a key head, or more than 65535 key heads of all sequences", fn);
+  if (static_cast<int64_t>(B) * Hkv > 65535)
+    return fail(CRVQ_ERR_UNSUPPORTED, "%s: %lld key heads of all sequences exceed 65535", fn, static_cast<long long>(B) * Hkv);
+  if ((s = check_columns(max_new, Hq / Hkv, fn))) return s;
   if (mask && (s = check_tree(mask, ld_mask, places, max_new, fn))) return s;
   if ((s = check_rows("q", q, q_tok, q_head, Hq, D, dtype, fn))) return s;
   if (!lse || !after) return fail(CRVQ_ERR_INVALID, "%s: lse and after must not be NULL", fn);

@@ -93,6 +93,7 @@ def test_tree_attention_arguments(L):
     for bad in (dict(mask=None), dict(out=None), dict(o_tok=500), dict(out=P(8, 64)), dict(lse=P(8)), dict(lse=P(9)), dict(out=P(10)),
                 dict(out=P(11)), dict(lse=P(10)), dict(lse=P(11)), dict(v=None), dict(vs=None), dict(v=P(2, 4))):
         assert attend(L, **bad) == 1, bad
+    assert attend(L, Hq=4 << 17, max_new=1) == 2 and attend(L, Hq=4 << 16, max_new=1 << 15, ld_mask=1 << 9) == 2
     need = L.crvq_kv_tree_attention_workspace_size(2, 8, 4, 64, 9, 100000)
     assert need and attend(L, max_kv=100000, wsb=need - 1) == 3 and attend(L, max_kv=100000, ws=None) == 3
     for none in [(0, 8, 4, 64, 9, 99), (2, 6, 4, 64, 9, 99), (2, 8, 4, 63, 9, 99), (2, 8, 4, 64, 0, 99), (2, 8, 4, 64, 9, -1)]:
@@ -103,7 +104,8 @@ def test_weights_arguments(L):
     for bad, status in [(dict(causal=0, window=5), 1), (dict(decay=float("nan")), 1), (dict(ld_w=159), 1), (dict(lse=None), 1), (dict(after=None), 1),
                         (dict(lse=P(12, 2)), 1), (dict(before=P(13, 1)), 1), (dict(after=P(14, 2)), 1), (dict(after=P(13, 64)), 1),
                         (dict(after=P(8)), 1), (dict(after=P(12)), 1), (dict(mask=P(14, 8), ld_mask=1), 1),
-                        (dict(mask=P(10), ld_mask=1, places=P(14)), 1), (dict(B=20000), 2), (dict(Hq=4 << 28, max_new=9), 2)]:
+                        (dict(mask=P(10), ld_mask=1, places=P(14)), 1), (dict(B=20000), 2), (dict(Hq=4 << 28, max_new=9), 2), (dict(Hq=4 << 16, max_new=1 << 15), 2),
+                        (dict(Hq=4 << 17, max_new=1), 2)]:
         assert weights(L, **bad) == status, (bad, err(L))
     for fine in (dict(max_kv=0), dict(max_kv=0, after=None)):
         assert weights(L, **fine) == 0

@@ -139,3 +139,20 @@ def test_captured_and_replayed(T):
         C.crvq_w8_gemm(c, sw, xe, se, ye, n_cols=1000)
         torch.cuda.synchronize()
         assert torch.equal(got, ye)
+
+
+def test_one_row_of_any_stride():
+    """A tensor of one row may have any stride between rows, 1 for instance."""
+    row = torch.randn(40, device="cuda")
+    one = torch.as_strided(row, (1, 40), (1, 1))
+    store, s = torch.zeros(48, dtype=torch.int8, device="cuda"), torch.zeros(1, device="cuda")
+    codes = torch.as_strided(store, (1, 48), (1, 1))
+    C.crvq_w8_quantize(one, codes, s)
+    c, sx = block.w8_quantize(host(one))
+    same_bits(host(codes), c, "codes")
+    y = torch.as_strided(torch.zeros(1, device="cuda"), (1, 1), (1, 1))
+    C.crvq_w8_gemm(codes, s, codes, s, y)
+    same_bits(host(y), block.w8_product(c, sx, c, sx, 40, False), "y")
+    h, r = torch.as_strided(torch.zeros(40, device="cuda"), (1, 40), (1, 1)), torch.as_strided(row.clone(), (1, 40), (1, 1))
+    C.crvq_norm(one, h, residual=r, residual_out=r)
+    assert torch.equal(r, (one + one).clone()) and torch.isfinite(h).all()
