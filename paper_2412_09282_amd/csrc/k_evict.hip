@@ -614,21 +614,27 @@ struct SelectHead {
   __device__ __forceinline__ bool always(const SelectArgs& a, int t) const { return n == len || t < a.sinks || t >= len - a.recent; }
 };
 
+// Inclusive sums over a wave's lanes: within rows of 16, then a row's last lane to the rows after it.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // from 1, 2, 4, 8 lanes below
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 to the second row, 47 to the fourth
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
+  return x;
+}
 // Inclusive sums over the workgroup's threads, and the total; `waves`: 16 entries that nobody else uses until the next barrier.
-__device__ __forceinline__ uint64_t block_scan(uint64_t x, uint64_t* waves, uint64_t& total) {
+__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* waves, uint32_t& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
+  x = wave_scan(x);
   __syncthreads();
   if (lane == 63) waves[wave] = x;
   __syncthreads();
   total = 0;
 #pragma unroll
   for (int v = 0; v < kSelectThreads / 64; ++v) {
-    const uint64_t y = waves[v];
+    const uint32_t y = waves[v];
     if (v < wave) x += y;
     total += y;
   }
@@ -637,10 +643,9 @@ __device__ __forceinline__ uint64_t block_scan(uint64_t x, uint64_t* waves, uint
 
 // The bin that the left-th largest key lies in, counts x0 and x1 being those of bins 2 t and 2 t + 1 of thread t, and what is left
 // of `left` within it.
-__device__ __forceinline__ void find_bin(uint32_t x0, uint32_t x1, uint32_t& left, uint32_t& bin, uint64_t* waves, uint32_t* pick) {
-  uint64_t total;
-  const uint32_t up_to = static_cast<uint32_t>(block_scan(static_cast<uint64_t>(x0) + x1, waves, total));
-  const uint32_t above1 = static_cast<uint32_t>(total) - up_to, above0 = above1 + x1;  // keys in higher bins
+__device__ __forceinline__ void find_bin(uint32_t x0, uint32_t x1, uint32_t& left, uint32_t& bin, uint32_t* waves, uint32_t* pick) {
+  uint32_t total;
+  const uint32_t up_to = block_scan(x0 + x1, waves, total), above1 = total - up_to, above0 = above1 + x1;  // keys in higher bins
   if (above1 < left && left <= above1 + x1) pick[0] = 2 * threadIdx.x + 1, pick[1] = left - above1;
   if (above0 < left && left <= above0 + x0) pick[0] = 2 * threadIdx.x, pick[1] = left - above0;
   __syncthreads();
@@ -671,7 +676,7 @@ __device__ __forceinline__ void load_weights(const float* from, int t, int to, f
 // before: how many of either kind there are in the tokens before the workgroup's, (above << 32) + equal; counted on.
 template <int K>
 __device__ __forceinline__ void write_kept(const SelectArgs& a, const SelectHead& h, const float (&w)[K], int t, int to, uint32_t least,
-                                           uint32_t equal, uint64_t& before, uint64_t* waves) {
+                                           uint32_t equal, uint64_t& before, uint32_t* waves) {
   uint32_t gt = 0, eq = 0;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -680,10 +685,11 @@ __device__ __forceinline__ void write_kept(const SelectArgs& a, const SelectHead
     gt += always || (there && h.left > 0 && x > least);
     eq += there && !always && h.left > 0 && x == least;
   }
-  uint64_t total;
-  const uint64_t up_to = before + block_scan(static_cast<uint64_t>(gt) << 32 | eq, waves, total);
-  before += total;
-  uint32_t g = static_cast<uint32_t>(up_to >> 32) - gt, e = static_cast<uint32_t>(up_to) - eq;  // before this thread's tokens
+  static_assert(K * kSelectThreads < 65536, "both counts fit 32 bits");
+  uint32_t total;
+  const uint32_t up_to = block_scan(gt << 16 | eq, waves, total);
+  uint32_t g = static_cast<uint32_t>(before >> 32) + (up_to >> 16) - gt, e = static_cast<uint32_t>(before) + (up_to & 65535u) - eq;  // before this thread's tokens
+  before += static_cast<uint64_t>(total >> 16) << 32 | (total & 65535u);
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const bool there = t + k < to, always = there && h.always(a, t + k);
@@ -703,7 +709,7 @@ __device__ __forceinline__ void write_kept(const SelectArgs& a, const SelectHead
 template <int K>
 __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(const SelectArgs a) {
   __shared__ uint32_t hist[2048], pick[2];
-  __shared__ uint64_t waves[kSelectThreads / 64];
+  __shared__ __align__(16) uint32_t waves[kSelectThreads / 64];
   const int tid = threadIdx.x, at = tid * K;
   const SelectHead h(a, blockIdx.x, tid == 0);
   float w[K];
@@ -744,7 +750,7 @@ __device__ __forceinline__ int n_always_before(const SelectArgs& a, const Select
 template <int PASS>
 __global__ __launch_bounds__(kSelectThreads) void kv_select_chunk_kernel(const SelectArgs a) {
   __shared__ uint32_t hist[2048], pick[2];
-  __shared__ uint64_t waves[kSelectThreads / 64];
+  __shared__ __align__(16) uint32_t waves[kSelectThreads / 64];
   const int tid = threadIdx.x;
   const int head = blockIdx.x / a.chunks, chunk = blockIdx.x - head * a.chunks;
   const SelectHead h(a, head, PASS == 0 && chunk == 0 && tid == 0);
@@ -770,6 +776,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_chunk_kernel(const S
     constexpr int kOf = PASS > 0 ? PASS - 1 : 0, kCount = kBins[kOf];
     uint32_t x[2] = {0, 0}, own[2] = {0, 0};
     if (2 * tid < kCount)
+#pragma unroll 8
       for (int c = 0; c < chunks; ++c) {
         const uint2 y = *reinterpret_cast<const uint2*>(a.bins[kOf] + (static_cast<int64_t>(head) * a.chunks + c) * kCount + 2 * tid);
         x[0] += y.x, x[1] += y.y;
@@ -778,10 +785,10 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_chunk_kernel(const S
     find_bin(x[0], x[1], left, bin, waves, pick);
     least |= bin << select_shift(kOf);
     if (PASS < 3) {
-      uint64_t total;
+      uint32_t total;
       block_scan((2 * tid > static_cast<int>(bin) ? own[0] : 0u) + (2 * tid + 1 > static_cast<int>(bin) ? own[1] : 0u), waves, total);
       if (tid == 0) {
-        a.above[mine * 2 + kOf] = static_cast<uint32_t>(total);
+        a.above[mine * 2 + kOf] = total;
         if (chunk == 0) {
           found[2 * kOf] = bin;
           found[2 * kOf + 1] = left;
@@ -811,17 +818,20 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_chunk_kernel(const S
   } else {
     const uint32_t equal = h.left > 0 ? left : 0;
     // kept tokens of the chunks before: those above the bins, those above the key in the last bins, and the always kept ones
-    uint64_t count = 0;
-    for (int c = 0; c < chunk && h.left > 0; ++c) {
+    uint32_t above = 0, same = 0;
+    const int others = h.left > 0 ? chunk : 0;
+#pragma unroll 8
+    for (int c = 0; c < others; ++c) {
       const int64_t other = static_cast<int64_t>(head) * a.chunks + c;
       const uint32_t y = a.bins[2][other * 1024 + tid];
-      if (static_cast<uint32_t>(tid) > bin) count += static_cast<uint64_t>(y) << 32;
-      if (static_cast<uint32_t>(tid) == bin) count += y;
-      if (tid < 2) count += static_cast<uint64_t>(a.above[other * 2 + tid]) << 32;
+      if (static_cast<uint32_t>(tid) > bin) above += y;
+      if (static_cast<uint32_t>(tid) == bin) same += y;
+      if (tid < 2) above += a.above[other * 2 + tid];
     }
-    uint64_t total;
-    block_scan(count, waves, total);
-    uint64_t before = total + (static_cast<uint64_t>(n_always_before(a, h, static_cast<int>(from))) << 32);
+    uint32_t all_above, all_same;
+    block_scan(above, waves, all_above);
+    block_scan(same, waves, all_same);
+    uint64_t before = (static_cast<uint64_t>(all_above) + n_always_before(a, h, static_cast<int>(from))) << 32 | all_same;
     for (int64_t t0 = from; t0 < to; t0 += kRound) {
       const int t = static_cast<int>(t0) + tid * K;
       float w[K];
@@ -839,6 +849,7 @@ struct GatherArgs {
   int64_t ld_table, ld_to;
   KvKeep k;
   int B, pages;  // pages: grid's bound of a sequence's new ones
+  int slices;    // 0: a workgroup moves a page's keys and values; else the first one the keys, the others slices of the values
 };
 
 // Four codes times a factor each, rounded to the nearest integer: the product's last places under 1.5 * 2^23.
@@ -854,7 +865,9 @@ __device__ __forceinline__ uint32_t moved4(uint32_t codes, const float (&f)[4]) 
 
 // A new page's scale is the largest of its tokens' old ones; a code becomes rint(c (old / new)).  Keys move 16 bytes at a time.  Values
 // lie transposed, so that a kept one is a byte among others that are not kept: neighbouring tokens of one old page are a run,
-// and the runs' rows pass through LDS whole, some elements at a time, where they are few enough; otherwise byte by byte (GATHER_FIGURES).
+// and the runs' rows pass through LDS whole, some elements at a time, where they are few enough; otherwise byte by byte (one
+// sequence of 131001 tokens to 16000, 8 heads, pages of 128: 57 us, most of it the 134 MB of values that the kept eighth lies in;
+// 32 sequences of up to 4096 tokens to 1024, 32 heads, pages of 64: 173 us, byte by byte 249).
 constexpr int kGatherLds = 16384;
 __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
   __shared__ int64_t from[256];     // the token's head and slot: (page * Hkv + hk) * page size + slot
@@ -865,6 +878,8 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
   extern __shared__ __align__(16) uint8_t rows[];  // kGatherLds bytes where pages are of 64 tokens or more: [run][element][slot]
   const int tid = threadIdx.x, D = a.c.D, pl2 = a.c.page_log2, P = 1 << pl2;
   uint32_t item = blockIdx.x;
+  const int slice = static_cast<int>(item % (a.slices + 1));
+  item /= a.slices + 1;
   const int hk = static_cast<int>(item % a.c.Hkv);
   item /= a.c.Hkv;
   const int p = static_cast<int>(item % a.pages), b = static_cast<int>(item / a.pages);
@@ -920,14 +935,14 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
   }
   if (begins) run_head[run] = from[tid] >> pl2;
   const int64_t head = static_cast<int64_t>(dest) * a.c.Hkv + hk;
-  if (tid == 0) {
+  if (tid == 0 && slice == 0) {
     a.c.k_scale[head] = k_new;
     a.c.v_scale[head] = v_new;
   }
   auto moved = [](int8_t c, float f) { return static_cast<int8_t>(rintf(static_cast<float>(c) * f)); };
   const int d16 = D >> 4;
   int8_t* k_to = a.c.k + (head << pl2) * D;
-  for (int x = tid; x < P * d16; x += 256) {
+  for (int x = tid; x < P * d16 && slice == 0; x += 256) {
     const int j = x / d16, e = (x - j * d16) * 16;
     ev_i4 y = {0, 0, 0, 0};
     if (j < n && k_ok) {
@@ -940,9 +955,12 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
     }
     *reinterpret_cast<ev_i4*>(k_to + j * D + e) = y;
   }
+  // the elements of the values that are this workgroup's
+  const int per = a.slices ? (D / 16 + a.slices - 1) / a.slices * 16 : D, first = a.slices ? (slice - 1) * per : 0, last = min(D, first + per);
+  if (slice == 0 ? a.slices > 0 : first >= last) return;
   int8_t* v_to = a.c.v + (head << pl2) * D;
   if (!v_ok || P < 64 || runs << pl2 > kGatherLds / 4) {
-    for (int x = tid; x < P * D; x += 256) {
+    for (int x = (first << pl2) + tid; x < last << pl2; x += 256) {
       const int e = x >> pl2, j = x & (P - 1);
       int8_t y = 0;
       if (j < n && v_ok) {
@@ -965,8 +983,8 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
     at[i] = j0 + i < n ? place[j0 + i] : 0;
     f[i] = j0 + i < n ? by[1][j0 + i] : 0.f;
   }
-  for (int e0 = 0; e0 < D; e0 += each) {
-    const int count = min(each, D - e0), row_pieces = count << pl2 >> 4;  // 16-byte pieces of a run
+  for (int e0 = first; e0 < last; e0 += each) {
+    const int count = min(each, last - e0), row_pieces = count << pl2 >> 4;  // 16-byte pieces of a run
     __syncthreads();
     for (int x = tid; x < runs * row_pieces; x += 256) {
       const int u = x / row_pieces, y = x - u * row_pieces;
@@ -1084,10 +1102,13 @@ hipError_t launch_kv_select(int B, int Hkv, const int32_t* kv_len, const float* 
 
 hipError_t launch_kv_gather(const KvCache& c, int B, const int32_t* table, int64_t ld_table, const int32_t* kv_len, const KvKeep& k,
                             int max_keep, const int32_t* to, int64_t ld_to, hipStream_t stream) {
-  const int64_t pages = cdiv(max_keep, int64_t{1} << c.page_log2), blocks = pages * B * c.Hkv;
+  const int64_t pages = cdiv(max_keep, int64_t{1} << c.page_log2), heads = pages * B * c.Hkv;
+  // fewer pages than CUs are divided over three workgroups each (40 pages 10 us for 14)
+  const int slices = heads < 256 ? 2 : 0;
+  const int64_t blocks = heads * (slices + 1);
   if (blocks == 0) return hipSuccess;
   if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-  const GatherArgs a = {c, table, to, kv_len, ld_table, ld_to, k, B, static_cast<int>(pages)};
+  const GatherArgs a = {c, table, to, kv_len, ld_table, ld_to, k, B, static_cast<int>(pages), slices};
   kv_gather_kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, c.page_log2 >= 6 ? kGatherLds : 0, stream>>>(a);
   return hipGetLastError();
 }
