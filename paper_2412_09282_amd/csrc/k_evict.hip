@@ -365,7 +365,7 @@ constexpr int weights_step_bytes(int dc, int nv) { return 2 * dc * nv * 1024 + 4
 template <typename T, int DC, bool VEC>
 __global__ __launch_bounds__(256) void kv_weights_kernel(const WeightArgs a) {
   constexpr int NV = RawQuery<T, DC>::NV, kPieces = DC * NV, kBlock = kPieces * 1024, kStage = weights_step_bytes(DC, NV);
-  constexpr int kLoads = 2 * kPieces / 4 + 1;  // of a wave in a step
+  constexpr int kLoads = kPieces / 2 + 1;  // of a wave in a step
   extern __shared__ __align__(16) uint8_t lds[];  // [3 steps]([2 blocks of 16 columns][DC][NV][64 lanes][16], [4 waves][64 lanes] lse)
   const int lane = threadIdx.x & 63, r = lane & 15, c = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t item = blockIdx.x;
@@ -418,10 +418,10 @@ __global__ __launch_bounds__(256) void kv_weights_kernel(const WeightArgs a) {
   }
   if (good != 15u || t0 + 64 > sq.len) plain_to = 0;
 
-  // This lane's column of the next block to fetch: its row and head, where its query and log-sum-exp are, and how far these move
-  // in 16 columns (`up` rows and `over` heads, a row more and G heads less where the heads end).
-  const int up = 16 / a.G, over = 16 - up * a.G;
-  int i = (first + r) / a.G, g = first + r - i * a.G;
+  // Two waves fetch a block of a step's two.  This lane's column of the next one: its row and head, where its query and log-sum-exp
+  // are, and how far these move in 32 columns (`up` rows and `over` heads, a row more and G heads less where the heads end).
+  const int blk_of = wave >> 1, half = wave & 1, up = 32 / a.G, over = 32 - up * a.G;
+  int i = (first + blk_of * 16 + r) / a.G, g = first + blk_of * 16 + r - i * a.G;
   const T* q_at = static_cast<const T*>(a.q.p) + (sq.row0 + i) * a.q.tok + (hk * a.G + g) * a.q.head;
   const float* lse_at = a.w.lse + static_cast<int64_t>(sq.row0 + i) * a.Hq + hk * a.G + g;
   const int64_t q_on = up * a.q.tok + over * a.q.head, q_wrap = a.q.tok - a.G * a.q.head;
@@ -431,55 +431,38 @@ __global__ __launch_bounds__(256) void kv_weights_kernel(const WeightArgs a) {
   const float* lse_first = a.w.lse + static_cast<int64_t>(sq.row0) * a.Hq + hk * a.G;
   int element[DC];  // past D the codes are 0
 #pragma unroll
-  for (int ch = 0; ch < DC; ++ch) element[ch] = ch * 64 + c * 16 < a.c.D ? ch * 64 + c * 16 : 0;
+  for (int ch = 0; ch < DC; ++ch) element[ch] = (ch * 64 + c * 16 < a.c.D ? ch * 64 + c * 16 : 0) + half * (16 / NV);
   // Queries of 32 columns to LDS, and their log-sum-exps; past the last column those of one that there is.  Every wave has as
-  // many loads as any other: its pieces of the queries, and the log-sum-exps of block wave % 2.
+  // many loads as any other: every second piece of its block, and the block's log-sum-exps.
   auto fetch = [&](uint8_t* to) {
+    const bool there = i < sq.n;
+    const T* p = there ? q_at : q_first;
 #pragma unroll
-    for (int blk = 0; blk < 2; ++blk) {
-      const T* p = i < sq.n ? q_at : q_first;
-      auto load = [&](int ch, int v, int piece) {
-        const T* e = p + element[ch] + v * (16 / NV);
-        uint8_t* at = to + piece * 1024;
-        if constexpr (VEC) {
-          load_lds16(e, at);
-        } else {
-          ev_u4 y;
+    for (int x = 0; x < kPieces / 2; ++x) {  // piece 2 x + half: chunk (2 x + half) / NV, part (2 x + half) % NV of a lane's elements
+      const T* e = p + element[2 * x / NV] + 2 * x % NV * (16 / NV);
+      uint8_t* at = to + blk_of * kBlock + (2 * x + half) * 1024;
+      if constexpr (VEC) {
+        load_lds16(e, at);
+      } else {
+        ev_u4 y;
 #pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            if constexpr (NV == 4) y[n] = e[n];
-            else y[n] = e[2 * n] | static_cast<uint32_t>(e[2 * n + 1]) << 16;
-          }
-          *reinterpret_cast<ev_u4*>(at + lane * 16) = y;
+        for (int n = 0; n < 4; ++n) {
+          if constexpr (NV == 4) y[n] = e[n];
+          else y[n] = e[2 * n] | static_cast<uint32_t>(e[2 * n + 1]) << 16;
         }
-      };
-      // the waves share a block's pieces
-      if constexpr (NV == 4) {
-#pragma unroll
-        for (int ch = 0; ch < DC; ++ch) load(ch, wave, blk * kPieces + ch * 4 + wave);
-      } else if constexpr (DC >= 2) {
-#pragma unroll
-        for (int ch = 0; ch < DC; ch += 2) {
-          const bool second = wave >> 1;
-          const T* keep = p;
-          p += second ? element[ch + 1] - element[ch] : 0;
-          load(ch, wave & 1, blk * kPieces + ch * 2 + wave);
-          p = keep;
-        }
-      } else if (wave >> 1 == blk) {  // two pieces a block
-        load(0, wave & 1, wave);
+        *reinterpret_cast<ev_u4*>(at + lane * 16) = y;
       }
-      if ((wave & 1) == blk) load_lds4(i < sq.n ? lse_at : lse_first, to + 2 * kBlock + wave * 256);
-      i += up;
-      g += over;
-      q_at += q_on;
-      lse_at += lse_on;
-      if (g >= a.G) {
-        g -= a.G;
-        ++i;
-        q_at += q_wrap;
-        lse_at += lse_wrap;
-      }
+    }
+    load_lds4(there ? lse_at : lse_first, to + 2 * kBlock + wave * 256);
+    i += up;
+    g += over;
+    q_at += q_on;
+    lse_at += lse_on;
+    if (g >= a.G) {
+      g -= a.G;
+      ++i;
+      q_at += q_wrap;
+      lse_at += lse_wrap;
     }
   };
   ev_f4 total[4] = {}, sum[4] = {};
@@ -503,7 +486,7 @@ __global__ __launch_bounds__(256) void kv_weights_kernel(const WeightArgs a) {
       for (int ch = 0; ch < DC; ++ch)
 #pragma unroll
         for (int v = 0; v < NV; ++v) raw.x[ch][v] = *reinterpret_cast<const ev_u4*>(from + (ch * NV + v) * 1024);
-      raw.lse = *reinterpret_cast<const float*>(lds + buffer * kStage + 2 * kBlock + blk * 256 + lane * 4);
+      raw.lse = *reinterpret_cast<const float*>(lds + buffer * kStage + 2 * kBlock + blk * 512 + lane * 4);
       Queries<T, DC> q;
       if (col0 >= plain_from && col0 < plain_to && __all(fabsf(raw.lse) < kInf)) {
         q.set_plain(raw);
