@@ -500,6 +500,7 @@ __global__ __launch_bounds__(256) void kv_weights_kernel(const WeightArgs a) {
       }
     }
     if (++n == 16) {  // sums of sums: the error of long ones grows with their root
+      asm volatile("; a branch, not selections");
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         total[u] += sum[u];
