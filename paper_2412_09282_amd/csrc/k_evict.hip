@@ -409,12 +409,12 @@ __global__ __launch_bounds__(256) void kv_weights_kernel(const WeightArgs a) {
     good = raw.good;
   }
   // Columns between these two see every token of the wave: they need no masks, nor selections where no row is out.
-  int plain_from = 0, plain_to = cols & ~15;
+  int plain_from = 0, plain_to = cols & ~31;
   if (a.w.tree.mask) {
     if (t0 + 64 > context || a.w.window) plain_to = 0;
   } else if (a.w.causal) {
     plain_from = max(t0 + 63 - context, 0) * a.G;
-    if (a.w.window) plain_to = static_cast<int>(min<int64_t>(plain_to, (static_cast<int64_t>(t0) - context + a.w.window) * a.G) & ~int64_t{15});
+    if (a.w.window) plain_to = static_cast<int>(min<int64_t>(plain_to, (static_cast<int64_t>(t0) - context + a.w.window) * a.G) & ~int64_t{31});
   }
   if (good != 15u || t0 + 64 > sq.len) plain_to = 0;
 
@@ -476,25 +476,35 @@ __global__ __launch_bounds__(256) void kv_weights_kernel(const WeightArgs a) {
     // what the step after the next one takes the place of
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(VEC ? kLoads : 0) : "memory");
     fetch(lds + (buffer == 0 ? 2 : buffer - 1) * kStage);
-#pragma unroll
-    for (int blk = 0; blk < 2; ++blk) {
-      const int col0 = first + blk * 16;
-      if (col0 + 16 <= my_first || col0 >= min(last, my_last)) continue;
-      RawQuery<T, DC> raw;
-      const uint8_t* from = lds + buffer * kStage + blk * kBlock + lane * 16;
+    const uint8_t* step = lds + buffer * kStage + lane * 16;
+    auto read = [&](int blk, RawQuery<T, DC>& raw) {
 #pragma unroll
       for (int ch = 0; ch < DC; ++ch)
 #pragma unroll
-        for (int v = 0; v < NV; ++v) raw.x[ch][v] = *reinterpret_cast<const ev_u4*>(from + (ch * NV + v) * 1024);
+        for (int v = 0; v < NV; ++v) raw.x[ch][v] = *reinterpret_cast<const ev_u4*>(step + blk * kBlock + (ch * NV + v) * 1024);
       raw.lse = *reinterpret_cast<const float*>(lds + buffer * kStage + 2 * kBlock + blk * 512 + lane * 4);
-      Queries<T, DC> q;
-      if (col0 >= plain_from && col0 < plain_to && __all(fabsf(raw.lse) < kInf)) {
-        q.set_plain(raw);
+    };
+    RawQuery<T, DC> raw[2];
+    read(0, raw[0]);
+    read(1, raw[1]);
+    if (first >= plain_from && first + 32 <= plain_to && __all(fabsf(raw[0].lse) < kInf && fabsf(raw[1].lse) < kInf)) {
+      Queries<T, DC> q[2];
+      q[0].set_plain(raw[0]);
+      q[1].set_plain(raw[1]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) add_weights(k[u], ks[u], true, q, t0 + 16 * u, context, true, sum[u]);
-      } else {
-        asm volatile("; a branch, not selections");
-        q.set(a, sq, raw, min((col0 + r) / a.G, sq.n - 1), col0 + r < cols);
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) add_weights(k[u], ks[u], true, q[blk], t0 + 16 * u, context, true, sum[u]);
+    } else {
+      asm volatile("; a branch, not selections");
+#pragma unroll 1
+      for (int blk = 0; blk < 2; ++blk) {
+        const int col0 = first + blk * 16;
+        if (col0 + 16 <= my_first || col0 >= min(last, my_last)) continue;
+        RawQuery<T, DC> one;
+        read(blk, one);
+        Queries<T, DC> q;
+        q.set(a, sq, one, min((col0 + r) / a.G, sq.n - 1), col0 + r < cols);
 #pragma unroll
         for (int u = 0; u < 4; ++u) add_weights(k[u], ks[u], good >> u & 1, q, t0 + 16 * u, context, false, sum[u]);
       }
