@@ -359,8 +359,9 @@ __global__ __launch_bounds__(256) void kv_weights_step_kernel(const WeightArgs a
 // More columns: every wave keeps 64 tokens in registers, and the four of a workgroup walk the columns that see any of theirs, 32 at a
 // time, whose queries lie in LDS for all of them, two steps ahead, put there by the loads themselves (16 bytes of a lane
 // where it reads them).  The vector units bound it, with 16 exponentials, products and sums of a lane for a tile of 64 tokens by 16
-// columns (three quarters of the time; the matrix instructions a quarter beside them): two prompts of up to 2048 rows over
-// 4000 tokens, 64 heads over 8, take 361 us (514 TFLOP/s), with every wave reading the queries for itself 399.
+// columns (over half of the cycles; the matrix instructions a quarter beside them): two prompts of up to 2048 rows over
+// 4000 tokens, 64 heads over 8, take 320 us (580 TFLOP/s; with every wave reading the queries for itself 399); one of 2048 over
+// 8192, 32 heads with keys of their own, 179 us (673 TFLOP/s).
 constexpr int weights_step_bytes(int dc, int nv) { return 2 * dc * nv * 1024 + 4 * 256; }
 template <typename T, int DC, bool VEC>
 __global__ __launch_bounds__(256) void kv_weights_kernel(const WeightArgs a) {
@@ -547,7 +548,8 @@ __global__ __launch_bounds__(256) void kv_weights_join_kernel(const WeightArgs a
 
 // How a call is divided.  Columns that fit four blocks stay in registers (us, 32 sequences of up to 4096 tokens, 32 heads: 24 columns 106
 // for 179 when they are walked, 40 147 for 200), the tokens over 2048 workgroups.  More are walked, in shares of 512 columns and more
-// until 2048 workgroups are at work, which a second launch joins in order.
+// until 2048 workgroups are at work, of 128 until each CU has one, which a second launch joins in order (us, 300 rows over 1500 tokens, 12
+// heads over 4: 24 in shares of 128 columns, 48 of 512; four sequences of 512 rows, heads of 256: 77 and 48).
 struct WeightPlan {
   int blocks;  // of 16 columns in a wave's registers; 0: the columns are walked
   int shares, parts;  // parts: shares that are joined by a second launch
@@ -556,9 +558,12 @@ WeightPlan plan_weights(int B, int Hq, int Hkv, int max_new, int max_kv) {
   const int64_t cols = static_cast<int64_t>(max_new) * (Hq / Hkv), heads = static_cast<int64_t>(B) * Hkv, tiles = cdiv(max_kv, 256);
   auto shares = [](int64_t want, int64_t most) { return static_cast<int>(want < 1 || most < 1 ? 1 : want < most ? want : most); };
   if (cols <= 64) return {cols <= 16 ? 1 : cols <= 32 ? 2 : 4, shares(cdiv(2048, heads), tiles), 1};
-  const int64_t want = cdiv(2048, heads * tiles);
-  const int n = shares(want < 16 ? want : 16, cdiv(cols, 512));
-  return {0, n, n};
+  auto of = [&](int64_t workgroups, int64_t columns) {
+    const int64_t want = cdiv(workgroups, heads * tiles);
+    return shares(want < 16 ? want : 16, cdiv(cols, columns));
+  };
+  const int n = of(2048, 512), few = of(256, 128);
+  return {0, n > few ? n : few, n > few ? n : few};
 }
 
 // ---- the tokens that a budget keeps ---------------------------------------------------------------------
