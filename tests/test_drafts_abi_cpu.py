@@ -195,3 +195,26 @@ def test_binding_refusals():
                  lambda: C.crvq_kv_gather(kc, vc, sc, sc.clone(), table, n, keep.long(), n, table)):
         with pytest.raises(AssertionError):
             call()
+
+
+class Somewhere:
+    """What the binding asks a tensor about where it is."""
+
+    def __init__(self, device, pinned=False):
+        self.device, self.pinned = device, pinned
+
+    is_cuda = property(lambda self: self.device >= 0)
+
+    def get_device(self):
+        return self.device
+
+    def is_pinned(self):
+        return self.pinned
+
+
+def test_tensors_of_one_call_are_on_one_device():
+    C._one_device(Somewhere(1), Somewhere(1), None, Somewhere(-1, True))
+    C._one_device(Somewhere(-1, True), Somewhere(-1, True), Somewhere(0))
+    for first, other, text in [(Somewhere(0), Somewhere(1), "tensors on"), (Somewhere(0), Somewhere(-1), "host memory"), (Somewhere(-1), Somewhere(0), "host memory")]:
+        with pytest.raises(ValueError, match=text):
+            C._one_device(first, Somewhere(first.device, True), other)
