@@ -866,7 +866,7 @@ __device__ __forceinline__ uint32_t moved4(uint32_t codes, const float (&f)[4]) 
 // lie transposed, so that a kept one is a byte among others that are not kept: neighbouring tokens of one old page are a run,
 // and the runs' rows pass through LDS whole, some elements at a time, where they are few enough; otherwise byte by byte (one
 // sequence of 131001 tokens to 16000, 8 heads, pages of 128: 57 us, most of it the 134 MB of values that the kept eighth lies in;
-// 32 sequences of up to 4096 tokens to 1024, 32 heads, pages of 64: 173 us, byte by byte 249).
+// 32 sequences of up to 4096 tokens to 1024, 32 heads, pages of 64: 166 us, byte by byte 249).
 constexpr int kGatherLds = 16384;
 __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
   __shared__ int64_t from[256];     // the token's head and slot: (page * Hkv + hk) * page size + slot
@@ -982,15 +982,31 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
     at[i] = j0 + i < n ? place[j0 + i] : 0;
     f[i] = j0 + i < n ? by[1][j0 + i] : 0.f;
   }
-  for (int e0 = first; e0 < last; e0 += each) {
-    const int count = min(each, last - e0), row_pieces = count << pl2 >> 4;  // 16-byte pieces of a run
-    __syncthreads();
-    for (int x = tid; x < runs * row_pieces; x += 256) {
-      const int u = x / row_pieces, y = x - u * row_pieces;
-      *reinterpret_cast<ev_i4*>(rows + ((u * each) << pl2) + y * 16) =
-          *reinterpret_cast<const ev_i4*>(a.c.v + ((run_head[u] * D + e0) << pl2) + y * 16);
+  // the rows of the next elements are on their way while these are written (the 32 sequences 174 us without)
+  constexpr int kHeld = kGatherLds / 16 / 256;
+  ev_i4 held[kHeld];
+  auto rows_of = [&](int e0, auto&& use) {  // this thread's 16-byte pieces: of run u, y pieces into its elements from e0 on
+    const int row_pieces = min(each, last - e0) << pl2 >> 4;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int x = tid + i * 256, u = x / row_pieces;
+      if (u < runs) use(i, u, x - u * row_pieces);
     }
-    __syncthreads();
+  };
+  auto fetch = [&](int e0) {
+    rows_of(e0, [&](int i, int u, int y) {
+      held[i] = *reinterpret_cast<const ev_i4*>(a.c.v + ((run_head[u] * D + e0) << pl2) + y * 16);
+    });
+  };
+  // all waves' LDS accesses are over; loads and stores to memory go on
+  auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  fetch(first);
+  for (int e0 = first; e0 < last; e0 += each) {
+    const int count = min(each, last - e0);
+    barrier();
+    rows_of(e0, [&](int i, int u, int y) { *reinterpret_cast<ev_i4*>(rows + ((u * each) << pl2) + y * 16) = held[i]; });
+    barrier();
+    if (e0 + each < last) fetch(e0 + each);
     for (int x = tid; x < count * lanes; x += 256) {
       const int e = x / lanes;
       const uint8_t* row = rows + (e << pl2);
