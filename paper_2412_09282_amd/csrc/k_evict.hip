@@ -302,9 +302,10 @@ __device__ __forceinline__ int token_of(int t0) {
 
 // Up to 16 NB columns: their queries stay in registers and every wave walks 64 tokens at a time, the next ones' codes on their way.
 // Memory bounds it: a token of 32 sequences of up to 4096, 32 heads of 128 (384 MB), 94 us, 4.1 TB/s; with 24 tokens each
-// (two blocks of columns) 106 us.
+// (two blocks of columns) 106 us, with 40 136.  Two waves a SIMD where the registers do: products then end in
+// registers that the vector unit reads (40 tokens 136 us for 146).
 template <typename T, int DC, int NB>
-__global__ __launch_bounds__(256) void kv_weights_step_kernel(const WeightArgs a) {
+__global__ __launch_bounds__(256, DC * sizeof(T) <= 4 || (DC * NB <= 4 && DC * sizeof(T) <= 8) ? 2 : 1) void kv_weights_step_kernel(const WeightArgs a) {
   const int lane = threadIdx.x & 63, r = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t item = blockIdx.x;
   const int hk = static_cast<int>(item % a.c.Hkv);
@@ -359,12 +360,12 @@ __global__ __launch_bounds__(256) void kv_weights_step_kernel(const WeightArgs a
 // More columns: every wave keeps 64 tokens in registers, and the four of a workgroup walk the columns that see any of theirs, 32 at a
 // time, whose queries lie in LDS for all of them, two steps ahead, put there by the loads themselves (16 bytes of a lane
 // where it reads them).  The vector units bound it, with 16 exponentials, products and sums of a lane for a tile of 64 tokens by 16
-// columns (over half of the cycles; the matrix instructions a quarter beside them): two prompts of up to 2048 rows over
-// 4000 tokens, 64 heads over 8, take 320 us (580 TFLOP/s; with every wave reading the queries for itself 399); one of 2048 over
-// 8192, 32 heads with keys of their own, 179 us (673 TFLOP/s).
+// columns (half of the cycles; the matrix instructions a quarter beside them): two prompts of up to 2048 rows over
+// 4000 tokens, 64 heads over 8, take 295 us (630 TFLOP/s); one of 2048 over 8192, 32 heads with keys of their own, 172 us
+// (700 TFLOP/s).
 constexpr int weights_step_bytes(int dc, int nv) { return 2 * dc * nv * 1024 + 4 * 256; }
 template <typename T, int DC, bool VEC>
-__global__ __launch_bounds__(256) void kv_weights_kernel(const WeightArgs a) {
+__global__ __launch_bounds__(256, DC * sizeof(T) <= 4 ? 2 : 1) void kv_weights_kernel(const WeightArgs a) {
   constexpr int NV = RawQuery<T, DC>::NV, kPieces = DC * NV, kBlock = kPieces * 1024, kStage = weights_step_bytes(DC, NV);
   constexpr int kLoads = kPieces / 2 + 1;  // of a wave in a step
   extern __shared__ __align__(16) uint8_t lds[];  // [3 steps]([2 blocks of 16 columns][DC][NV][64 lanes][16], [4 waves][64 lanes] lse)
