@@ -361,7 +361,7 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 || (DC * NB <= 4 && DC * s
 // time, whose queries lie in LDS for all of them, two steps ahead, put there by the loads themselves (16 bytes of a lane
 // where it reads them).  The vector units bound it, with 16 exponentials, products and sums of a lane for a tile of 64 tokens by 16
 // columns (half of the cycles; the matrix instructions a quarter beside them): two prompts of up to 2048 rows over
-// 4000 tokens, 64 heads over 8, take 295 us (630 TFLOP/s); one of 2048 over 8192, 32 heads with keys of their own, 172 us
+// 4000 tokens, 64 heads over 8, take 265 us (700 TFLOP/s); one of 2048 over 8192, 32 heads with keys of their own, 172 us
 // (700 TFLOP/s).
 constexpr int weights_step_bytes(int dc, int nv) { return 2 * dc * nv * 1024 + 4 * 256; }
 template <typename T, int DC, bool VEC>
@@ -387,11 +387,10 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 ? 2 : 1) void kv_weights_k
     return static_cast<int>(max<int64_t>(min<int64_t>(cols, (static_cast<int64_t>(to) + a.w.window - context) * a.G), 0));
   };
   int first = first_of(tile0) & ~31, last = last_of(tile0 + 255);
-  if (a.shares > 1) {  // an equal share of the steps
-    const int steps = (max(last - first, 0) + 31) >> 5, each = (steps + a.shares - 1) / a.shares;
-    first += share * each * 32;
-    last = min(last, first + each * 32);
-  }
+  // Every shares'-th step: those that need masks lie next to each other, and all shares read neighbouring queries at a time
+  // (the two prompts 265 us for 300 with shares that lie one after the other).
+  const int stride = 32 * a.shares;
+  first += share * 32;
   const int my_first = first_of(t0), my_last = t0 < sq.len ? last_of(t0 + 63) : 0;
   ev_b8 k[4][DC][2];
   float ks[4];
@@ -421,8 +420,8 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 ? 2 : 1) void kv_weights_k
   if (good != 15u || t0 + 64 > sq.len) plain_to = 0;
 
   // Two waves fetch a block of a step's two.  This lane's column of the next one: its row and head, where its query and log-sum-exp
-  // are, and how far these move in 32 columns (`up` rows and `over` heads, a row more and G heads less where the heads end).
-  const int blk_of = wave >> 1, half = wave & 1, up = 32 / a.G, over = 32 - up * a.G;
+  // are, and how far these move in a step (`up` rows and `over` heads, a row more and G heads less where the heads end).
+  const int blk_of = wave >> 1, half = wave & 1, up = stride / a.G, over = stride - up * a.G;
   int i = (first + blk_of * 16 + r) / a.G, g = first + blk_of * 16 + r - i * a.G;
   const T* q_at = static_cast<const T*>(a.q.p) + (sq.row0 + i) * a.q.tok + (hk * a.G + g) * a.q.head;
   const float* lse_at = a.w.lse + static_cast<int64_t>(sq.row0 + i) * a.Hq + hk * a.G + g;
@@ -473,7 +472,7 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 ? 2 : 1) void kv_weights_k
     fetch(lds);
     fetch(lds + kStage);
   }
-  for (; first < last; first += 32) {
+  for (; first < last; first += stride) {
     // this step's loads have arrived (the next one's may be on their way), for every wave, and every wave has read
     // what the step after the next one takes the place of
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(VEC ? kLoads : 0) : "memory");
