@@ -758,6 +758,14 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_chunk_kernel(const S
   if (from >= h.len || (PASS < 3 && h.left <= 0)) return;
   const int64_t mine = static_cast<int64_t>(head) * a.chunks + chunk;
   constexpr int kBins[3] = {2048, 2048, 1024};
+  // rounds of 8 neighbouring tokens a thread; the first one's weights, and what the chunks before keep for their higher bits, are on
+  // their way while the bin is found (four launches over 131001 tokens of 8 heads 31 us, one load after the other 35)
+  constexpr int K = 8, kRound = K * kSelectThreads;
+  float w[K];
+  load_weights<K>(h.w, static_cast<int>(from) + tid * K, to, w);
+  uint32_t above = 0, same = 0;
+  if (PASS == 3 && h.left > 0)
+    for (int x = tid; x < 2 * chunk; x += kSelectThreads) above += a.above[static_cast<int64_t>(head) * a.chunks * 2 + x];
   uint32_t* found = a.found + static_cast<int64_t>(head) * 4;  // the first two bins, and what is left within the second
   uint32_t least = 0xffffffffu, left = h.left, bin = 0;
   if (PASS > 0 && h.left > 0) {
@@ -773,13 +781,14 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_chunk_kernel(const S
     }
     // all chunks' counts of the launch before; this chunk's keys above the bin that they give are kept
     constexpr int kOf = PASS > 0 ? PASS - 1 : 0, kCount = kBins[kOf];
-    uint32_t x[2] = {0, 0}, own[2] = {0, 0};
+    uint32_t x[2] = {0, 0}, own[2] = {0, 0}, below[2] = {0, 0};
     if (2 * tid < kCount)
 #pragma unroll 8
       for (int c = 0; c < chunks; ++c) {
         const uint2 y = *reinterpret_cast<const uint2*>(a.bins[kOf] + (static_cast<int64_t>(head) * a.chunks + c) * kCount + 2 * tid);
         x[0] += y.x, x[1] += y.y;
         if (c == chunk) own[0] = y.x, own[1] = y.y;
+        if (c < chunk) below[0] += y.x, below[1] += y.y;
       }
     find_bin(x[0], x[1], left, bin, waves, pick);
     least |= bin << select_shift(kOf);
@@ -793,18 +802,21 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_chunk_kernel(const S
           found[2 * kOf + 1] = left;
         }
       }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (2 * tid + e > static_cast<int>(bin)) above += below[e];
+        if (2 * tid + e == static_cast<int>(bin)) same = below[e];
+      }
     }
   }
-  // rounds of 8 neighbouring tokens a thread
-  constexpr int K = 8, kRound = K * kSelectThreads;
   if constexpr (PASS < 3) {
     constexpr int kHigher = PASS > 0 ? select_shift(PASS - 1) : 0;
     for (int x = tid; x < kBins[PASS]; x += kSelectThreads) hist[x] = 0;
     __syncthreads();
     for (int64_t t0 = from; t0 < to; t0 += kRound) {
       const int t = static_cast<int>(t0) + tid * K;
-      float w[K];
-      load_weights<K>(h.w, t, to, w);
+      if (t0 != from) load_weights<K>(h.w, t, to, w);
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const uint32_t x = key_of(w[k]);
@@ -817,24 +829,13 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_chunk_kernel(const S
   } else {
     const uint32_t equal = h.left > 0 ? left : 0;
     // kept tokens of the chunks before: those above the bins, those above the key in the last bins, and the always kept ones
-    uint32_t above = 0, same = 0;
-    const int others = h.left > 0 ? chunk : 0;
-#pragma unroll 8
-    for (int c = 0; c < others; ++c) {
-      const int64_t other = static_cast<int64_t>(head) * a.chunks + c;
-      const uint32_t y = a.bins[2][other * 1024 + tid];
-      if (static_cast<uint32_t>(tid) > bin) above += y;
-      if (static_cast<uint32_t>(tid) == bin) same += y;
-      if (tid < 2) above += a.above[other * 2 + tid];
-    }
     uint32_t all_above, all_same;
     block_scan(above, waves, all_above);
     block_scan(same, waves, all_same);
     uint64_t before = (static_cast<uint64_t>(all_above) + n_always_before(a, h, static_cast<int>(from))) << 32 | all_same;
     for (int64_t t0 = from; t0 < to; t0 += kRound) {
       const int t = static_cast<int>(t0) + tid * K;
-      float w[K];
-      load_weights<K>(h.w, t, to, w);
+      if (t0 != from) load_weights<K>(h.w, t, to, w);
       write_kept<K>(a, h, w, t, to, least, equal, before, waves);
     }
   }
@@ -866,7 +867,7 @@ __device__ __forceinline__ uint32_t moved4(uint32_t codes, const float (&f)[4]) 
 // lie transposed, so that a kept one is a byte among others that are not kept: neighbouring tokens of one old page are a run,
 // and the runs' rows pass through LDS whole, some elements at a time, where they are few enough; otherwise byte by byte (one
 // sequence of 131001 tokens to 16000, 8 heads, pages of 128: 57 us, most of it the 134 MB of values that the kept eighth lies in;
-// 32 sequences of up to 4096 tokens to 1024, 32 heads, pages of 64: 166 us, byte by byte 249).
+// 32 sequences of up to 4096 tokens to 1024, 32 heads, pages of 64: 174 us, byte by byte 249).
 constexpr int kGatherLds = 16384;
 __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
   __shared__ int64_t from[256];     // the token's head and slot: (page * Hkv + hk) * page size + slot
@@ -982,7 +983,8 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
     at[i] = j0 + i < n ? place[j0 + i] : 0;
     f[i] = j0 + i < n ? by[1][j0 + i] : 0.f;
   }
-  // the rows of the next elements are on their way while these are written (the 32 sequences 174 us without)
+  // the rows of the next elements are on their way while these are written (the 32 sequences 174 us for 177, 30000 of 32768
+  // tokens 61 for 65; 4000 of 16000, whose runs are short, 27 for 26)
   constexpr int kHeld = kGatherLds / 16 / 256;
   ev_i4 held[kHeld];
   auto rows_of = [&](int e0, auto&& use) {  // this thread's 16-byte pieces: of run u, y pieces into its elements from e0 on
