@@ -476,7 +476,6 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 ? 2 : 1) void kv_weights_k
     // this step's loads have arrived (the next one's may be on their way), for every wave, and every wave has read
     // what the step after the next one takes the place of
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(VEC ? kLoads : 0) : "memory");
-    fetch(lds + (buffer == 0 ? 2 : buffer - 1) * kStage);
     const uint8_t* step = lds + buffer * kStage + lane * 16;
     auto read = [&](int blk, RawQuery<T, DC>& raw) {
 #pragma unroll
@@ -488,6 +487,7 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 ? 2 : 1) void kv_weights_k
     RawQuery<T, DC> raw[2];
     read(0, raw[0]);
     read(1, raw[1]);
+    fetch(lds + (buffer == 0 ? 2 : buffer - 1) * kStage);  // while these are read (264 us after it, 252 now)
     if (first >= plain_from && first + 32 <= plain_to && __all(fabsf(raw[0].lse) < kInf && fabsf(raw[1].lse) < kInf)) {
       Queries<T, DC> q[2];
       q[0].set_plain(raw[0]);
