@@ -361,8 +361,8 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 || (DC * NB <= 4 && DC * s
 // time, whose queries lie in LDS for all of them, two steps ahead, put there by the loads themselves (16 bytes of a lane
 // where it reads them).  The vector units bound it, with 16 exponentials, products and sums of a lane for a tile of 64 tokens by 16
 // columns (half of the cycles; the matrix instructions a quarter beside them): two prompts of up to 2048 rows over
-// 4000 tokens, 64 heads over 8, take 265 us (700 TFLOP/s); one of 2048 over 8192, 32 heads with keys of their own, 172 us
-// (700 TFLOP/s).
+// 4000 tokens, 64 heads over 8, take 244 us (760 TFLOP/s); one of 2048 over 8192, 32 heads with keys of their own, 155 us
+// (775 TFLOP/s).
 constexpr int weights_step_bytes(int dc, int nv) { return 2 * dc * nv * 1024 + 4 * 256; }
 template <typename T, int DC, bool VEC>
 __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 ? 2 : 1) void kv_weights_kernel(const WeightArgs a) {
@@ -425,11 +425,14 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 ? 2 : 1) void kv_weights_k
   int i = (first + blk_of * 16 + r) / a.G, g = first + blk_of * 16 + r - i * a.G;
   const T* q_at = static_cast<const T*>(a.q.p) + (sq.row0 + i) * a.q.tok + (hk * a.G + g) * a.q.head;
   const float* lse_at = a.w.lse + static_cast<int64_t>(sq.row0 + i) * a.Hq + hk * a.G + g;
-  const int64_t q_on = up * a.q.tok + over * a.q.head, q_wrap = a.q.tok - a.G * a.q.head;
-  const int lse_on = up * a.Hq + over, lse_wrap = a.Hq - a.G;
+  int64_t q_on = up * a.q.tok + over * a.q.head, q_wrap = a.q.tok - a.G * a.q.head;
+  int64_t lse_on = up * a.Hq + over, lse_wrap = a.Hq - a.G;
   // what is there past the last column: the key head's first query
   const T* q_first = static_cast<const T*>(a.q.p) + sq.row0 * a.q.tok + hk * a.G * a.q.head;
   const float* lse_first = a.w.lse + static_cast<int64_t>(sq.row0) * a.Hq + hk * a.G;
+  // In vector registers, as they are added to lanes' places: there are too few scalar ones
+  // (252 us with them there, 244 now).
+  asm("" : "+v"(q_on), "+v"(q_wrap), "+v"(lse_on), "+v"(lse_wrap), "+v"(q_first), "+v"(lse_first));
   int element[DC];  // past D the codes are 0
 #pragma unroll
   for (int ch = 0; ch < DC; ++ch) element[ch] = (ch * 64 + c * 16 < a.c.D ? ch * 64 + c * 16 : 0) + half * (16 / NV);
