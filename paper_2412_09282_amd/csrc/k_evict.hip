@@ -361,8 +361,8 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 || (DC * NB <= 4 && DC * s
 // time, whose queries lie in LDS for all of them, two steps ahead, put there by the loads themselves (16 bytes of a lane
 // where it reads them).  The vector units bound it, with 16 exponentials, products and sums of a lane for a tile of 64 tokens by 16
 // columns (over half of the cycles; the matrix instructions a third beside them): two prompts of up to 2048 rows over
-// 4000 tokens, 64 heads over 8, take 221 us (841 TFLOP/s; 244 in a short run of a graph, as the figures below); one of 2048 over 8192, 32 heads with keys of their own, 155 us
-// (775 TFLOP/s).
+// 4000 tokens, 64 heads over 8, take 221 us (841 TFLOP/s; 244 in a short run of a graph, as the figures below); one of 2048
+// over 8192, 32 heads with keys of their own, 155 us (775 TFLOP/s).
 constexpr int weights_step_bytes(int dc, int nv) { return 2 * dc * nv * 1024 + 4 * 256; }
 template <typename T, int DC, bool VEC>
 __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 ? 2 : 1) void kv_weights_kernel(const WeightArgs a) {
