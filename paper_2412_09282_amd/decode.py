@@ -79,10 +79,11 @@ class PagedCache:
     """Pages of keys and values in 8 bits and the sequences that own them.
 
     lengths: tokens of a sequence in the cache; places: where its next token stands, which is more once tokens were
-    evicted.  track: room for so many tokens of every sequence's accumulated attention weights, which `evict` goes by."""
+    evicted.  window: of the block whose keys and values these are (0: none), by which drafts are masked.  track: room
+    for so many tokens of every sequence's accumulated attention weights, which `evict` goes by."""
 
     def __init__(self, n_pages: int, kv_heads: int, head_dim: int, page: int = 64, device="cuda", track: int = 0):
-        self.page, self.track = page, track
+        self.page, self.track, self.window = page, track, 0
         self.weights: Optional[torch.Tensor] = None  # sequences x kv_heads x track
         self.places: List[int] = []
         self.drafts: Optional[List[int]] = None  # of the batch that waits for `accept`
@@ -148,7 +149,9 @@ class PagedCache:
             batch.mask = torch.zeros(starts[-1], -(-max(batch.max_new, 1) // 64), dtype=torch.int64, device=self.k.device)
             batch.places = torch.zeros(starts[-1], dtype=torch.int32, device=self.k.device)
             C.crvq_tree_mask(self._ints([p for tree in parents for p in tree]), batch.start,
-                             self._ints([p + n for p, n in zip(self.places, counts)]), batch.max_new, batch.mask, batch.places)
+                             self._ints([p + n for p, n in zip(self.places, counts)]), batch.max_new, batch.mask, batch.places,
+                             window=self.window)
+            batch.window = self.window
             return batch
         if self.places != [k - n for n, k in zip(counts, self.lengths)]:
             batch.places = self._ints([p + i for p, n in zip(self.places, counts) for i in range(n)])
@@ -247,6 +250,7 @@ class Batch:
     tokens: Optional[int] = None  # new tokens of all sequences
     places: Optional[torch.Tensor] = None  # of the new tokens, where they are not those behind the cached ones
     mask: Optional[torch.Tensor] = None  # of drafted tokens: which of them each one sees
+    window: Optional[int] = None  # that the mask was made with
 
 
 def rotary_angles(n: int, rot: int, base: float = 10000.0, device="cuda"):
@@ -271,6 +275,7 @@ class AttentionBlock:
         matrix = (lambda W: W4Matrix(W, group, zeros)) if bits == 4 else W8Matrix
         self.qkv, self.out = matrix(W_qkv), matrix(W_out)
         self.cache, self.cos, self.sin = cache, cos, sin
+        cache.window = window
 
     def __call__(self, x: torch.Tensor, batch: Batch, scales: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x: the new tokens' activations, T x channels, sequence after sequence; with scales in 8 bits already (blocks of
@@ -281,6 +286,8 @@ class AttentionBlock:
             raise ValueError("8-bit activations for a block of 4 bits")
         if self.window and self.cache.evicted:
             raise ValueError("a window counts tokens, and some were evicted")
+        if batch.mask is not None and batch.window not in (None, self.window):
+            raise ValueError(f"drafts masked for a window of {batch.window} in a block with one of {self.window}")
         H, K, D = self.heads, self.kv_heads, self.D
         qkv = self.qkv.product(x) if scales is None else self.qkv.product(x, scales=scales)
         q, k, v = (t.unflatten(1, (-1, D)) for t in qkv.split([H * D, K * D, K * D], 1))

@@ -1,0 +1,66 @@
+"""CPU-only: drafted tokens in decode.py, with the library's calls replaced by their definitions in oracle/drafts.py or noted
+down."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import drafts
+from paper_2412_09282_amd import crvq as C
+from paper_2412_09282_amd import decode
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Masks as oracle/drafts.py has them; what other calls got."""
+    noted = []
+
+    def tree_mask(parents, start, kv_len, max_new, mask=None, places=None, window=0, stream=None):
+        for b in range(kv_len.numel()):
+            r0, r1 = int(start[b]), int(start[b + 1])
+            m, p = drafts.tree(parents[r0:r1].numpy(), int(kv_len[b]), mask.shape[1], window)
+            mask[r0:r1] = torch.from_numpy(m.view(np.int64))
+            places[r0:r1] = torch.from_numpy(p)
+
+    monkeypatch.setattr(C, "crvq_tree_mask", tree_mask)
+    for name in ("crvq_w8_quantize", "crvq_w8_gemm", "crvq_kv_append", "crvq_kv_attention", "crvq_kv_tree_attention", "crvq_kv_weights",
+                 "crvq_kv_gather"):
+        monkeypatch.setattr(C, name, lambda *a, _name=name, **k: noted.append((_name, a, k)))
+    return noted
+
+
+def block_of(cache, window=0, N=32):
+    heads, D = cache.k.shape[1], cache.k.shape[3]
+    return decode.AttentionBlock(torch.zeros(3 * heads * D, N), torch.zeros(N, heads * D), heads, heads, cache, torch.ones(99, D // 2),
+                                 torch.zeros(99, D // 2), window=window, bits=8)
+
+
+def cache_of(lengths, **kw):
+    c = decode.PagedCache(24, 2, 16, page=16, device="cpu", **kw)
+    for _ in lengths:
+        c.add_sequence()
+    c.grow(lengths)
+    return c
+
+
+@pytest.mark.parametrize("window", [1, 8, 20, 100])
+def test_drafts_see_no_further_than_the_window(calls, window):
+    """A chain of drafts sees what the same tokens see as plain rows."""
+    c = cache_of([30, 3])
+    block = block_of(c, window)
+    batch = c.grow([20, 7], [[i - 1 for i in range(20)], [i - 1 for i in range(7)]])
+    masks, places = batch.mask.numpy().view(np.uint64), batch.places.numpy()
+    for rows, n, k in ((slice(0, 20), 20, 50), (slice(20, 27), 7, 10)):
+        assert (drafts.sees_mask(masks[rows], n, k, places[rows], window) == drafts.sees_causal(n, k, True, window)).all()
+    block(torch.zeros(27, 32), batch)
+    assert [k["window"] for name, _, k in calls if name == "crvq_kv_tree_attention"] == [window]
+
+
+def test_masks_of_another_window_are_refused(calls):
+    c = cache_of([30])
+    block = block_of(c, 8)
+    batch = c.grow([4], [[-1, 0, 1, 2]])
+    block.window = 3
+    with pytest.raises(ValueError, match="window"):
+        block(torch.zeros(4, 32), batch)
+    batch.window = None  # a mask of the program's own
+    block(torch.zeros(4, 32), batch)
