@@ -80,11 +80,13 @@ class PagedCache:
 
     lengths: tokens of a sequence in the cache; places: where its next token stands, which is more once tokens were
     evicted.  window: of the block whose keys and values these are (0: none), by which drafts are masked.  track: room
-    for so many tokens of every sequence's accumulated attention weights, which `evict` goes by."""
+    for so many tokens of every sequence's accumulated attention weights, which `evict` goes by (drafts count once they
+    are accepted)."""
 
     def __init__(self, n_pages: int, kv_heads: int, head_dim: int, page: int = 64, device="cuda", track: int = 0):
         self.page, self.track, self.window = page, track, 0
-        self.weights: Optional[torch.Tensor] = None  # sequences x kv_heads x track
+        self._weights: Optional[torch.Tensor] = None
+        self._attended: Optional[tuple] = None  # what the drafts that wait attended to: see `attended`
         self.places: List[int] = []
         self.drafts: Optional[List[int]] = None  # of the batch that waits for `accept`
         self.evicted = False
@@ -102,7 +104,7 @@ class PagedCache:
         self.places.append(0)
         if self.track:
             more = torch.zeros(1, self.k.shape[1], self.track, device=self.k.device)
-            self.weights = more if self.weights is None else torch.cat((self.weights, more))
+            self._weights = more if self._weights is None else torch.cat((self._weights, more))
         return len(self.lengths) - 1
 
     def drop_sequence(self, b: int) -> None:
@@ -111,6 +113,58 @@ class PagedCache:
         self.pages[b], self.lengths[b], self.places[b] = [], 0, 0
         if self.drafts is not None:
             self.drafts[b] = 0
+
+    @property
+    def tracks(self) -> bool:
+        return self._weights is not None
+
+    @property
+    def weights(self) -> Optional[torch.Tensor]:
+        """Accumulated attention weights, sequences x kv_heads x track.  While drafts wait, a copy that holds what it would
+        if all of them stayed."""
+        if self._attended is None:
+            return self._weights
+        q, lse, batch, window = self._attended
+        w = self._weights.clone()
+        self._add(w, q, lse, batch, window)
+        return w
+
+    @weights.setter
+    def weights(self, w: torch.Tensor) -> None:
+        self._weights = w
+
+    def attended(self, q: torch.Tensor, lse: torch.Tensor, batch: "Batch", window: int) -> None:
+        """Adds what the rows q attended to (lse as their attention returned it) to the tokens' weights; of drafts, `accept`
+        adds it for those that stay, so that refused ones never count."""
+        if batch.counts is None:
+            self._add(self._weights, q, lse, batch, window)
+        elif q.is_cuda and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("what drafts attended to is known when some are accepted: not in a graph")
+        else:
+            self._attended = q, lse, batch, window
+
+    def _add(self, w: torch.Tensor, q: torch.Tensor, lse: torch.Tensor, batch: "Batch", window: int) -> None:
+        w = w[:batch.kv_len.numel()]  # sequences that came after the batch are not in it
+        C.crvq_kv_weights(q, lse, w, w, self.k, self.k_scale, batch.table, batch.start, batch.kv_len, batch.max_new, batch.max_kv,
+                          window=window, mask=batch.mask, places=batch.places if batch.mask is not None else None)
+
+    def _add_accepted(self, tokens: Sequence[Sequence[int]]) -> None:
+        """Adds what the accepted drafts attended to; rows without a finite log-sum-exp add nothing."""
+        if self._attended is None:
+            return
+        (q, lse, batch, window), self._attended = self._attended, None
+        first, rows = 0, []
+        for n, t in zip(batch.counts, tokens):
+            rows += [first + i for i in t]
+            first += n
+        if not rows:
+            return
+        at, stay = torch.tensor(rows, device=lse.device), torch.full_like(lse, float("inf"))
+        stay[at] = lse[at]
+        self._add(self._weights, q, stay, batch, window)
+        if q.is_cuda:  # they may be of another stream
+            for t in (q, lse, batch.table, batch.start, batch.kv_len, batch.mask, batch.places):
+                t.record_stream(torch.cuda.current_stream(q.device))
 
     def _ints(self, v) -> torch.Tensor:
         return torch.tensor(v, dtype=torch.int32, device=self.k.device)
@@ -145,7 +199,7 @@ class PagedCache:
         batch = Batch(self._table(self.pages), self._ints(starts), self._ints(self.lengths), max(counts, default=0),
                       max(self.lengths, default=0), starts[-1])
         if parents is not None:
-            self.drafts = list(counts)
+            self.drafts, batch.counts = list(counts), list(counts)
             batch.mask = torch.zeros(starts[-1], -(-max(batch.max_new, 1) // 64), dtype=torch.int64, device=self.k.device)
             batch.places = torch.zeros(starts[-1], dtype=torch.int32, device=self.k.device)
             C.crvq_tree_mask(self._ints([p for tree in parents for p in tree]), batch.start,
@@ -187,6 +241,8 @@ class PagedCache:
             need = sum(-(-len(r) // P) for r in rows)
             if need > len(self.free):
                 raise RuntimeError(f"the cache is full: {need} pages needed, {len(self.free)} free")
+        self._add_accepted(tokens)
+        if what:
             width = max(len(r) for r in rows)
             keep = self._ints([r + [-1] * (width - len(r)) for r in rows]).view(B, 1, width)
             lengths = self._ints([k - f * P for k, f in zip(self.lengths, first)])
@@ -196,9 +252,9 @@ class PagedCache:
             if b in what:
                 self.free.extend(reversed(self.pages[b][first[b]:]))
                 self.pages[b] = self.pages[b][:first[b]] + new[b]
-                if self.weights is not None:
+                if self._weights is not None:
                     at = torch.tensor([context[b] + i for i in t], device=self.k.device)
-                    self.weights[b, :, context[b]:context[b] + len(t)] = self.weights[b].index_select(1, at)
+                    self._weights[b, :, context[b]:context[b] + len(t)] = self._weights[b].index_select(1, at)
             self.lengths[b] = context[b] + len(t)
             self.places[b] += len(t)
             left = -(-self.lengths[b] // P)
@@ -209,7 +265,7 @@ class PagedCache:
     def evict(self, budget: int, sinks: int = 4, recent: int = 0) -> None:
         """Brings every sequence that has more than `budget` tokens down to as many: its first `sinks`, its last `recent`, and
         of each head the others that were attended to most."""
-        if self.weights is None:
+        if self._weights is None:
             raise RuntimeError("the cache does not track attention weights")
         if self.drafts is not None:
             raise RuntimeError("drafted tokens wait to be accepted")
@@ -226,12 +282,12 @@ class PagedCache:
             keep = torch.empty(B, self.k.shape[1], budget, dtype=torch.int32, device=self.k.device)
             kept = torch.empty(B, self.k.shape[1], budget, device=self.k.device)
             kept_len = torch.empty(B, dtype=torch.int32, device=self.k.device)
-            C.crvq_kv_select(self.weights, lengths, budget, keep, kept_len, kept_weights=kept, sinks=sinks, recent=recent)
+            C.crvq_kv_select(self._weights, lengths, budget, keep, kept_len, kept_weights=kept, sinks=sinks, recent=recent)
             new = self._move(what, self.pages, lengths, keep, [budget] * B, kept_len)
             for b in what:
                 self.free.extend(reversed(self.pages[b]))
                 self.pages[b], self.lengths[b] = new[b], budget
-                self.weights[b, :, :budget] = kept[b]
+                self._weights[b, :, :budget] = kept[b]
             self.evicted = True
 
     @property
@@ -251,6 +307,7 @@ class Batch:
     places: Optional[torch.Tensor] = None  # of the new tokens, where they are not those behind the cached ones
     mask: Optional[torch.Tensor] = None  # of drafted tokens: which of them each one sees
     window: Optional[int] = None  # that the mask was made with
+    counts: Optional[List[int]] = None  # of drafts that wait to be accepted: how many each sequence brought
 
 
 def rotary_angles(n: int, rot: int, base: float = 10000.0, device="cuda"):
@@ -294,7 +351,7 @@ class AttentionBlock:
         where = (*self.cache.tensors, batch.table, batch.start, batch.kv_len)
         C.crvq_kv_append(k, v, *where, batch.max_new, cos=self.cos, sin=self.sin, positions=batch.places, q=q, q_out=q)
         o = torch.empty(q.shape[0], H, D, dtype=q.dtype, device=q.device)
-        track = self.cache.weights is not None
+        track = self.cache.tracks
         lse = torch.empty(q.shape[0], H, device=q.device) if track else None
         if batch.mask is not None:
             C.crvq_kv_tree_attention(q, o, *where, batch.max_new, batch.max_kv, batch.mask, window=self.window,
@@ -302,10 +359,7 @@ class AttentionBlock:
         else:
             C.crvq_kv_attention(q, o, *where, batch.max_new, batch.max_kv, window=self.window, lse=lse)
         if track:
-            w = self.cache.weights
-            C.crvq_kv_weights(q, lse, w, w, self.cache.k, self.cache.k_scale, batch.table, batch.start, batch.kv_len,
-                              batch.max_new, batch.max_kv, window=self.window, mask=batch.mask,
-                              places=batch.places if batch.mask is not None else None)
+            self.cache.attended(q, lse, batch, self.window)
         return self.out.product(o.flatten(1))
 
 

@@ -64,3 +64,49 @@ def test_masks_of_another_window_are_refused(calls):
         block(torch.zeros(4, 32), batch)
     batch.window = None  # a mask of the program's own
     block(torch.zeros(4, 32), batch)
+
+
+def test_weights_are_of_the_accepted_drafts(calls):
+    """Nothing is added before it is known which drafts stay; then the others' rows add nothing, and all of it before tokens
+    move."""
+    c = cache_of([30, 3, 9], track=90)
+    block = block_of(c)
+    trees = [[-1, 0, 0, 2, 1], [-1, -1, 1], [-1, 0]]
+    for name in ("accept", "refuse"):
+        lengths = list(c.lengths)
+        batch = c.grow([5, 3, 2], trees)
+        del calls[:]
+        block(torch.zeros(10, 32), batch)
+        assert not [x for x in calls if x[0] == "crvq_kv_weights"]
+        lse = next(k["lse"] for n, _, k in calls if n == "crvq_kv_tree_attention")
+        lse.copy_(torch.arange(20).view(10, 2))
+        c.accept([[0, 2, 3], [], [0, 1]] if name == "accept" else [[], [], []])
+        made = [n for n, _, _ in calls if n in ("crvq_kv_weights", "crvq_kv_gather")]
+        if name == "refuse":
+            assert made == [] and c.lengths == lengths
+            continue
+        assert made == ["crvq_kv_weights", "crvq_kv_gather"]
+        _, (q, got, before, after, *where), k = next(x for x in calls if x[0] == "crvq_kv_weights")
+        stay = [0, 2, 3, 8, 9]
+        assert (got[stay] == lse[stay]).all() and torch.isinf(got).all(1).nonzero().flatten().tolist() == [1, 4, 5, 6, 7]
+        assert after.data_ptr() == before.data_ptr() == c.weights.data_ptr() and k["mask"] is batch.mask and k["places"] is batch.places
+        assert where[4] is batch.kv_len and where[2] is batch.table and c.lengths == [33, 3, 11]
+
+
+def test_weights_while_drafts_wait_and_of_other_masks(calls):
+    c = cache_of([30, 3], track=90)
+    block = block_of(c)
+    batch = c.grow([2, 1], [[-1, 0], [-1]])
+    block(torch.zeros(3, 32), batch)
+    del calls[:]
+    held = c.weights  # as if all stayed: a copy
+    assert [x[0] for x in calls] == ["crvq_kv_weights"] and calls[0][1][3].data_ptr() == held.data_ptr()
+    c.add_sequence()  # not in the batch
+    c.accept([[0, 1], []])
+    assert c.weights.shape == (3, 2, 90) and calls[-1][1][3].shape == (2, 2, 90) and c.weights.data_ptr() != held.data_ptr()
+    # a mask of the program's own: its rows are no drafts, and count at once
+    plain = c.grow([1, 1, 0])
+    plain.mask = torch.ones(2, 1, dtype=torch.int64)
+    del calls[:]
+    block(torch.zeros(2, 32), plain)
+    assert [x[0] for x in calls].count("crvq_kv_weights") == 1

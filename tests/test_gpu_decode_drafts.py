@@ -61,3 +61,50 @@ def test_a_chain_of_drafts_in_a_window(window):
     y = t.block(x, batch)
     places = [c + i for c, n in zip(context, counts) for i in range(n)]
     t.check(y, batch, t.queries(x, places), [drafts.sees_causal(n, c + n, True, window) for c, n in zip(context, counts)])
+
+
+def parents_of(g, n):
+    return [-1 if i == 0 else int(g.integers(max(-1, i - 4), i)) for i in range(n)]
+
+
+@pytest.mark.parametrize("heads,kv_heads,D,page,window", [(4, 2, 32, 16, 0), (3, 3, 16, 32, 6)])
+def test_refused_drafts_do_not_count(heads, kv_heads, D, page, window):
+    """Of the accepted drafts alone a cache's weights are what 64 bits make of them, token by token; the log-sum-exps that they are
+    relative to are the kernel's, which move a weight by less than 1e-4 of itself."""
+    say(f"weights of accepted drafts, {heads}/{kv_heads} x {D}, pages of {page}, window {window}")
+    t = Block([30, 7, 60], heads, kv_heads, D, page=page, window=window, track=150, seed=D)
+    for counts in ([9, 20, 1], [6, 0, 33]):
+        trees = [parents_of(t.g, n) for n in counts]
+        context = list(t.cache.lengths)
+        x, base = t.rand(sum(counts), t.N), host(t.cache.weights).copy()
+        batch = t.cache.grow(counts, trees)
+        y = t.block(x, batch)
+        q = t.queries(x, host(batch.places))
+        words = batch.mask.shape[1]
+        masks = [drafts.tree(p, c + n, words, window) for p, c, n in zip(trees, context, counts)]
+        sees = [drafts.sees_mask(m, n, c + n, p, window) for (m, p), c, n in zip(masks, context, counts)]
+        lse = t.check(y, batch, q, sees)
+        accepted, start = [], host(batch.start)
+        for b, p in enumerate(trees):
+            path, i = [], len(p) // 2
+            while p and i >= 0:
+                path.insert(0, i)
+                i = p[i]
+            accepted.append(path)
+            refused = np.setdiff1d(np.arange(len(p)), path)
+            lse[start[b] + refused] = np.inf
+        assert np.isinf(lse).any()
+        held, table, lens = [host(a) for a in t.cache.tensors], host(batch.table), host(batch.kv_len)
+        exp, tol = drafts.weights(held, table, start, lens, q, D ** -0.5, lse, sees, base, base, 1.0)
+        if counts[0] == 9:  # while they wait: all of them
+            every = host(t.cache.weights)[0].astype(np.float64)
+            every[:, :30] -= base[0, :, :30]
+            assert np.allclose(every[:, :39].sum(1), 9 * heads / kv_heads, rtol=1e-4, atol=1e-4)
+        t.cache.accept(accepted)
+        got = host(t.cache.weights)
+        for b, (c, a) in enumerate(zip(context, accepted)):
+            now = list(range(c)) + [c + i for i in a]
+            e, old = exp[b][:, now], np.concatenate([base[b, :, :c], np.zeros((kv_heads, len(a)))], 1)
+            assert (np.abs(got[b, :, :len(now)] - e) <= tol[b][:, now] + 1e-4 * np.abs(e - old)).all()
+            # a row's weights add up to 1
+            assert np.allclose((e - old).sum(1), len(a) * heads / kv_heads, rtol=1e-6)
