@@ -89,6 +89,7 @@ class PagedCache:
         self._attended: Optional[tuple] = None  # what the drafts that wait attended to: see `attended`
         self.places: List[int] = []
         self.drafts: Optional[List[int]] = None  # of the batch that waits for `accept`
+        self.parents: Optional[List[List[int]]] = None  # of those drafts
         self.evicted = False
         self.k = torch.zeros(n_pages, kv_heads, page, head_dim, dtype=torch.int8, device=device)
         self.v = torch.zeros(n_pages, kv_heads, head_dim, page, dtype=torch.int8, device=device)
@@ -200,6 +201,7 @@ class PagedCache:
                       max(self.lengths, default=0), starts[-1])
         if parents is not None:
             self.drafts, batch.counts = list(counts), list(counts)
+            self.parents = [list(p) for p in parents]
             batch.mask = torch.zeros(starts[-1], -(-max(batch.max_new, 1) // 64), dtype=torch.int64, device=self.k.device)
             batch.places = torch.zeros(starts[-1], dtype=torch.int32, device=self.k.device)
             C.crvq_tree_mask(self._ints([p for tree in parents for p in tree]), batch.start,
@@ -221,8 +223,8 @@ class PagedCache:
         return new
 
     def accept(self, tokens: Sequence[Sequence[int]]) -> None:
-        """Of the last batch's drafted tokens those at tokens[b] (in order, a path of the tree) become sequence b's next
-        ones; the others are gone."""
+        """Of the last batch's drafted tokens those at tokens[b] become sequence b's next ones: a path of the tree from a
+        token without a parent on, or none.  The others are gone."""
         if self.drafts is None:
             raise RuntimeError("no drafted tokens wait to be accepted")
         if len(tokens) != len(self.drafts):
@@ -231,6 +233,9 @@ class PagedCache:
         for t, n in zip(tokens, self.drafts):
             if any(not 0 <= i < n for i in t) or any(i >= j for i, j in zip(t, t[1:])):
                 raise ValueError(f"{t} are not drafted tokens in order: there are {n}")
+        for t, p in zip(tokens, self.parents or []):
+            if any(p[j] != i for i, j in zip([-1] + t, t)):
+                raise ValueError(f"{t} are no path of a tree with parents {p}")
         B, P = len(tokens), self.page
         context = [k - n for k, n in zip(self.lengths, self.drafts)]
         first = [c // P for c in context]  # the page that the drafts begin in
@@ -260,7 +265,7 @@ class PagedCache:
             left = -(-self.lengths[b] // P)
             self.free.extend(reversed(self.pages[b][left:]))
             self.pages[b] = self.pages[b][:left]
-        self.drafts = None
+        self.drafts = self.parents = None
 
     def evict(self, budget: int, sinks: int = 4, recent: int = 0) -> None:
         """Brings every sequence that has more than `budget` tokens down to as many: its first `sinks`, its last `recent`, and

@@ -110,3 +110,24 @@ def test_weights_while_drafts_wait_and_of_other_masks(calls):
     del calls[:]
     block(torch.zeros(2, 32), plain)
     assert [x[0] for x in calls].count("crvq_kv_weights") == 1
+
+
+@pytest.mark.parametrize("bad", [[1], [3], [0, 3], [0, 2, 4], [0, 1, 2], [0, 5], [5, 6], [0, 1, 3, 6]])
+def test_only_paths_of_the_tree_are_accepted(calls, bad):
+    c = cache_of([10, 4])
+    trees = [[-1, 0, 0, 1, 3, -1, 2], [-1, 0]]
+    c.grow([7, 2], trees)
+    before = [list(p) for p in c.pages], list(c.lengths), list(c.free), list(c.places)
+    with pytest.raises(ValueError, match="path"):
+        c.accept([bad, [0]])
+    with pytest.raises(ValueError, match="path"):
+        c.accept([[0], [1]])
+    assert before == (c.pages, c.lengths, c.free, c.places) and c.drafts == [7, 2] and not calls
+    c.accept([[0, 1, 3, 4], []])
+    assert c.lengths == [14, 4] and c.drafts is None
+    c.grow([1, 2], [[-1], [-1, -1]])  # two that follow the context themselves
+    c.drop_sequence(0)
+    with pytest.raises(ValueError, match="path"):
+        c.accept([[], [0, 1]])
+    c.accept([[], [1]])
+    assert c.lengths == [0, 5]
