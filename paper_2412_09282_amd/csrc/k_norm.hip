@@ -29,7 +29,7 @@ template <typename Tile, int V>
 __device__ __forceinline__ void normed(const Tile& tile, float (&x)[V][8], bool layer, const void* w, const void* b, bool w_f32,
                                        double eps, double* red) {
   const double n = static_cast<double>(tile.N);
-  double s = 0.0;
+  double s = 0.0, by = 1.0;
   if (layer) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -37,14 +37,18 @@ __device__ __forceinline__ void normed(const Tile& tile, float (&x)[V][8], bool 
 #pragma unroll
       for (int e = 0; e < 8; ++e) s += static_cast<double>(x[v][e]);  // past N they are 0
     }
+    // x - mean leaves fp32's range only where the mean is near it, and is then held by halves; a mean that large leaves no
+    // difference so small that half of it is not fp32's
     const double mean = tile.sum(s, red) / n;
+    by = fabs(mean) >= 0x1p100 ? 0.5 : 1.0;
+    const double from = -mean * by;
     s = 0.0;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       one_by_one<V>(x[v]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const double y = tile.has(v, e) ? static_cast<double>(x[v][e]) - mean : 0.0;
+        const double y = tile.has(v, e) ? fma(static_cast<double>(x[v][e]), by, from) : 0.0;
         s = fma(y, y, s);
         x[v][e] = static_cast<float>(y);
       }
@@ -57,7 +61,7 @@ __device__ __forceinline__ void normed(const Tile& tile, float (&x)[V][8], bool 
       for (int e = 0; e < 8; ++e) s = fma(static_cast<double>(x[v][e]), static_cast<double>(x[v][e]), s);
     }
   }
-  const double inv = 1.0 / sqrt(tile.sum(s, red + 16) / n + eps);
+  const double inv = 1.0 / (sqrt(tile.sum(s, red + 16) / (n * by * by) + eps) * by);
   // |x| inv is at most sqrt(N) whatever the row's size, but inv itself may leave fp32's range where eps is 0
   const float f = static_cast<float>(inv);
   if (f < __builtin_inff() && f >= 0x1p-126f) {
@@ -66,12 +70,12 @@ __device__ __forceinline__ void normed(const Tile& tile, float (&x)[V][8], bool 
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[v][e] *= f;
   } else {
-    int up;
-    const float m = static_cast<float>(frexp(inv, &up));
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+    for (int v = 0; v < V; ++v) {
+      one_by_one<V>(x[v]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[v][e] = ldexpf(x[v][e] * m, up);
+      for (int e = 0; e < 8; ++e) x[v][e] = static_cast<float>(static_cast<double>(x[v][e]) * inv);
+    }
   }
 #pragma unroll
   for (int v = 0; v < V; ++v) {
