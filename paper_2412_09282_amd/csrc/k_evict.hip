@@ -903,8 +903,9 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
     from[tid] = (head << pl2) + (t & (P - 1));
     ks = good ? a.c.k_scale[head] : nan;
     vs = good ? a.c.v_scale[head] : nan;
-    if (!(ks >= 0.f && ks < kInf)) ks = nan;
-    if (!(vs >= 0.f && vs < kInf)) vs = nan;
+    // -0 is 0, whose bits lie below all others
+    ks = ks > 0.f && ks < kInf ? ks : ks == 0.f ? 0.f : nan;
+    vs = vs > 0.f && vs < kInf ? vs : vs == 0.f ? 0.f : nan;
   }
   // the largest as bits: NaN lies above all
   uint32_t mk = __float_as_uint(ks), mv = __float_as_uint(vs);
