@@ -339,9 +339,10 @@ class AttentionBlock:
         self.cache, self.cos, self.sin = cache, cos, sin
         cache.window = window
 
-    def __call__(self, x: torch.Tensor, batch: Batch, scales: Optional[torch.Tensor] = None) -> torch.Tensor:
+    def __call__(self, x: torch.Tensor, batch: Batch, scales: Optional[torch.Tensor] = None,
+                 dtype=torch.bfloat16) -> torch.Tensor:
         """x: the new tokens' activations, T x channels, sequence after sequence; with scales in 8 bits already (blocks of
-        8 bits; the result is bf16 then)."""
+        8 bits), and the block's own activations and result of dtype then, otherwise of x's type."""
         if batch.tokens is not None and x.shape[0] != batch.tokens:
             raise ValueError(f"{x.shape[0]} rows for a batch of {batch.tokens} new tokens")
         if scales is not None and self.bits != 8:
@@ -351,7 +352,7 @@ class AttentionBlock:
         if batch.mask is not None and batch.window not in (None, self.window):
             raise ValueError(f"drafts masked for a window of {batch.window} in a block with one of {self.window}")
         H, K, D = self.heads, self.kv_heads, self.D
-        qkv = self.qkv.product(x) if scales is None else self.qkv.product(x, scales=scales)
+        qkv = self.qkv.product(x) if scales is None else self.qkv.product(x, scales=scales, dtype=dtype)
         q, k, v = (t.unflatten(1, (-1, D)) for t in qkv.split([H * D, K * D, K * D], 1))
         where = (*self.cache.tensors, batch.table, batch.start, batch.kv_len)
         C.crvq_kv_append(k, v, *where, batch.max_new, cos=self.cos, sin=self.sin, positions=batch.places, q=q, q_out=q)
@@ -370,7 +371,8 @@ class AttentionBlock:
 
 class Stack:
     """Blocks with a norm before each (pre[i]), and after each where post is given, around a residual stream in fp32:
-    r = r + alpha norm(block(norm(r) pre[i])) post[i].  A block of 8 bits takes the norm's result in 8 bits."""
+    r = r + alpha norm(block(norm(r) pre[i])) post[i].  A block of 8 bits takes the norm's result in 8 bits; dtype: of all
+    other activations within and between the blocks."""
 
     def __init__(self, blocks: Sequence[AttentionBlock], pre: Sequence[torch.Tensor],
                  post: Optional[Sequence[torch.Tensor]] = None, alpha: float = 1.0, eps: float = 1e-5, dtype=torch.bfloat16):
@@ -392,7 +394,7 @@ class Stack:
             # the sum of the block before and this one's norm; the first block has nothing before it
             C.crvq_norm(out, h, residual=r, residual_out=given, w_pre=pre, w_post=w_post, alpha=self.alpha, eps=self.eps,
                         h_scales=scales)
-            out, w_post, given = block(h, batch, scales), post, r
+            out, w_post, given = block(h, batch, scales, self.dtype), post, r
         if given is not None:
             C.crvq_norm(out, None, residual=r, residual_out=r, w_post=w_post, alpha=self.alpha, eps=self.eps)
         return r

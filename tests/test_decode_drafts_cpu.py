@@ -1,4 +1,4 @@
-"""CPU-only: drafted tokens in decode.py, with the library's calls replaced by their definitions in oracle/drafts.py or noted
+"""CPU-only: drafted tokens and stacks in decode.py, with the library's calls replaced by their definitions in oracle/drafts.py or noted
 down."""
 import numpy as np
 import pytest
@@ -23,15 +23,15 @@ def calls(monkeypatch):
 
     monkeypatch.setattr(C, "crvq_tree_mask", tree_mask)
     for name in ("crvq_w8_quantize", "crvq_w8_gemm", "crvq_kv_append", "crvq_kv_attention", "crvq_kv_tree_attention", "crvq_kv_weights",
-                 "crvq_kv_gather"):
+                 "crvq_kv_gather", "crvq_norm", "crvq_w4_quantize", "crvq_w4_gemv"):
         monkeypatch.setattr(C, name, lambda *a, _name=name, **k: noted.append((_name, a, k)))
     return noted
 
 
-def block_of(cache, window=0, N=32):
+def block_of(cache, window=0, N=32, bits=8):
     heads, D = cache.k.shape[1], cache.k.shape[3]
     return decode.AttentionBlock(torch.zeros(3 * heads * D, N), torch.zeros(N, heads * D), heads, heads, cache, torch.ones(99, D // 2),
-                                 torch.zeros(99, D // 2), window=window, bits=8)
+                                 torch.zeros(99, D // 2), window=window, bits=bits)
 
 
 def cache_of(lengths, **kw):
@@ -131,3 +131,20 @@ def test_only_paths_of_the_tree_are_accepted(calls, bad):
         c.accept([[], [0, 1]])
     c.accept([[], [1]])
     assert c.lengths == [0, 5]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bits", [(8,), (8, 8), (4, 8, 4), (8, 4, 8)])
+def test_a_stack_keeps_its_type(calls, dtype, bits):
+    caches = [cache_of([0]) for _ in bits]
+    stack = decode.Stack([block_of(c, bits=b) for c, b in zip(caches, bits)], [torch.ones(32) for _ in bits], dtype=dtype)
+    del calls[:]
+    stack(torch.zeros(3, 32), [c.grow([3]) for c in caches])
+    for name, a, k in calls:
+        if name in ("crvq_w8_gemm", "crvq_w4_gemv"):  # queries, keys and values, and the block's result
+            assert a[4].dtype == dtype, name
+        elif name == "crvq_norm":
+            assert a[0].dtype == dtype and (a[1] is None or k.get("h_scales") is not None or a[1].dtype == dtype)
+        elif name == "crvq_kv_attention":
+            assert a[0].dtype == a[1].dtype == dtype
+    assert sum(n == "crvq_kv_attention" for n, _, _ in calls) == len(bits)
