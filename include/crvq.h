@@ -565,7 +565,7 @@ crvq_status crvq_kv_tree_attention(int32_t B, int32_t Hq, int32_t Hkv, int32_t D
  * outside [0, n_pages) or whose scale is negative or not finite.  Sequences
  * that bring no rows, whose rows are not within [0, n_tokens] or more than
  * max_new, or with kv_len[b] < 0, > max_kv or > ld_table * page, and tokens from kv_len[b] on, stay as they were in `after`.
- * Products are exact (CRVQ_F32 queries as three bf16 terms), sums fp32 in a
+ * Products are exact (CRVQ_F32 queries as three bf16 terms; down to 2^-110), sums fp32 in a
  * fixed order.  ld >= max_kv; B * Hkv is at most 65535, and rows as in crvq_kv_tree_attention.
  * workspace: crvq_kv_weights_workspace_size(...) bytes. */
 size_t crvq_kv_weights_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new, int32_t max_kv);

@@ -8,9 +8,11 @@ namespace {
 typedef int ev_i4 __attribute__((ext_vector_type(4)));
 typedef float ev_f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t ev_u4 __attribute__((ext_vector_type(4)));
+typedef uint16_t ev_s2 __attribute__((ext_vector_type(2)));
 typedef __bf16 ev_b8 __attribute__((ext_vector_type(8)));
 
 constexpr float kInf = __builtin_inff();
+constexpr float kMost = 0x1.fffffep127f;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // ---- masks of a tree of drafted tokens --------------------------------------------------------------
@@ -61,14 +63,14 @@ struct WeightArgs {
   int Hq, G, shares, tiles, max_kv, q_vec;
 };
 
-// Eight codes as bf16: integers of eight bits are the upper halves of their fp32.
-__device__ __forceinline__ ev_b8 widen8(int a, int b) {
+// Eight codes as bf16, `by` (a power of two) times: integers of eight bits are the upper halves of their fp32.
+__device__ __forceinline__ ev_b8 widen8(int a, int b, float by = 1.f) {
   ev_u4 v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t w = i < 2 ? a : b;
-    const float x = static_cast<float>(static_cast<int8_t>(w >> (16 * (i & 1))));
-    const float y = static_cast<float>(static_cast<int8_t>(w >> (16 * (i & 1) + 8)));
+    const float x = static_cast<float>(static_cast<int8_t>(w >> (16 * (i & 1)))) * by;
+    const float y = static_cast<float>(static_cast<int8_t>(w >> (16 * (i & 1) + 8))) * by;
     v[i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
   }
   return __builtin_bit_cast(ev_b8, v);
@@ -136,6 +138,29 @@ struct RawQuery {
       }
     }
   }
+
+  // Whether any of this lane's elements is 2^100 or more.
+  __device__ __forceinline__ bool far() const {
+    if constexpr (NV == 4) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int ch = 0; ch < DC; ++ch)
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) most = max(most, x[ch][v][k] & 0x7fffffffu);
+      return most >= 0x71800000u;
+    } else {
+      ev_s2 most = {0, 0};
+#pragma unroll
+      for (int ch = 0; ch < DC; ++ch)
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) most = __builtin_elementwise_max(most, __builtin_bit_cast(ev_s2, x[ch][v][k] & 0x7fff7fffu));
+      return max(most[0], most[1]) >= 0x7180;
+    }
+  }
 };
 
 // 16 columns: their queries as right operands, what they see, and their log-sum-exps in powers of two.  DC chunks of 64 elements hold a
@@ -180,6 +205,22 @@ struct Queries {
       }
     }
   }
+  // 2^-16 of them.
+  __device__ __forceinline__ void bring_down() {
+#pragma unroll
+    for (int ch = 0; ch < DC; ++ch)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          ev_u4 v = __builtin_bit_cast(ev_u4, q[ch][half][t]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[e] = __builtin_amdgcn_perm(__float_as_uint(__uint_as_float(v[e] & 0xffff0000u) * 0x1p-16f),
+                                         __float_as_uint(__uint_as_float(v[e] << 16) * 0x1p-16f), 0x07060302u);
+          q[ch][half][t] = __builtin_bit_cast(ev_b8, v);
+        }
+  }
   __device__ __forceinline__ void set_plain(const RawQuery<T, DC>& raw) { operands(raw, true); }
   __device__ __forceinline__ void set(const WeightArgs& a, const KvSeq& sq, const RawQuery<T, DC>& raw, int i, bool there) {
     const bool ok = there && fabsf(raw.lse) < kInf;  // neither a row that sees nothing nor one that is NaN has weights
@@ -221,10 +262,10 @@ struct Queries {
 template <int DC>
 struct RawTokens {
   ev_i4 k[4][DC];
-  float ks[4];  // with the softmax's scale, in powers of two; 0 where `good` is not
+  float ks[4];  // times `slope`; 0 where `good` is not
   uint32_t good;  // tiles whose page and scale can be used
 
-  __device__ __forceinline__ void load(const WeightArgs& a, const KvSeq& sq, int b, int hk, int t0) {
+  __device__ __forceinline__ void load(const WeightArgs& a, const KvSeq& sq, int b, int hk, int t0, float slope) {
     const int r = threadIdx.x & 15, c = (threadIdx.x >> 4) & 3, D = a.c.D, pl2 = a.c.page_log2;
     const int32_t* table = a.bt.table + b * a.bt.ld_table;
     int64_t head[4];
@@ -251,7 +292,7 @@ struct RawTokens {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (!(ks[u] >= 0.f && ks[u] < kInf)) good &= ~(1u << u);
-      ks[u] = (good >> u & 1) ? ks[u] * (a.w.scale * kLog2e) : 0.f;
+      ks[u] = (good >> u & 1) ? __builtin_amdgcn_fmed3f(ks[u] * slope, -kMost, kMost) : 0.f;  // a number, for sums of 0
     }
   }
 };
@@ -317,14 +358,25 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 || (DC * NB <= 4 && DC * s
   int t0 = (part * 4 + wave) * 64;
   if (t0 >= sq.len) return;
   RawTokens<DC> next;
-  next.load(a, sq, b, hk, t0);
+  float slope = a.w.scale * kLog2e;  // scores in powers of two
+  next.load(a, sq, b, hk, t0, slope);
   Queries<T, DC> q[NB];
+  bool far = false;
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     const int col = min(n * 16 + r, cols - 1), i = col / a.G;
     RawQuery<T, DC> raw;
     raw.load(a, sq, hk, i, col - i * a.G);
+    far = far || raw.far();
     q[n].set(a, sq, raw, i, n * 16 + r < cols);
+  }
+  // 2^-16 times, no sum of codes times queries leaves fp32; what products below 2^-126 lose by it is nothing beside them.
+  if (__any(far)) {
+    slope *= 0x1p16f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) next.ks[u] = __builtin_amdgcn_fmed3f(next.ks[u] * 0x1p16f, -kMost, kMost);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) q[n].bring_down();
   }
   const int64_t head = static_cast<int64_t>(b) * a.c.Hkv + hk;
   for (; t0 < sq.len; t0 += stride) {
@@ -332,7 +384,7 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 || (DC * NB <= 4 && DC * s
     const int t = token_of(t0);
     const int64_t at = head * a.w.ld + t;
     const float old = a.w.before && t < context ? a.w.before[at] : 0.f;
-    if (t0 + stride < sq.len) next.load(a, sq, b, hk, t0 + stride);
+    if (t0 + stride < sq.len) next.load(a, sq, b, hk, t0 + stride, slope);
     bool whole[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n)
@@ -397,15 +449,19 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 ? 2 : 1) void kv_weights_k
   uint32_t good;
   {
     RawTokens<DC> raw;
-    raw.load(a, sq, b, hk, t0);
+    raw.load(a, sq, b, hk, t0, a.w.scale * kLog2e);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
+      // 2^-16 times, no sum of codes times queries leaves fp32.  What products below 2^-126 lose by it is below 2^-42 of a score
+      // with scales below 2^60; with larger ones a score is out of fp32 before its sum is.
+      const bool near = fabsf(raw.ks[u]) < 0x1p60f;
+      const float by = near ? 0x1p-16f : 1.f;
 #pragma unroll
       for (int ch = 0; ch < DC; ++ch) {
-        k[u][ch][0] = widen8(raw.k[u][ch][0], raw.k[u][ch][1]);
-        k[u][ch][1] = widen8(raw.k[u][ch][2], raw.k[u][ch][3]);
+        k[u][ch][0] = widen8(raw.k[u][ch][0], raw.k[u][ch][1], by);
+        k[u][ch][1] = widen8(raw.k[u][ch][2], raw.k[u][ch][3], by);
       }
-      ks[u] = raw.ks[u];
+      ks[u] = raw.ks[u] * (near ? 0x1p16f : 1.f);
     }
     good = raw.good;
   }
