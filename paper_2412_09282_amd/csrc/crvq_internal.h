@@ -350,6 +350,10 @@ struct W8 {
 };
 hipError_t launch_w8_quantize(const void* X, int64_t ldx, int type, int64_t rows, int64_t N, int8_t* codes, int64_t ld,
                               float* scales, hipStream_t stream);
+struct W8Plan {
+  int form, splits;  // form: kFew1 .. kTile256; splits: of the columns
+};
+W8Plan plan_w8(int64_t M, int64_t N, int64_t T, bool far);  // far: rows lie 2^22 bytes and more apart
 size_t w8_gemm_ws_bytes(int64_t M, int64_t N, int64_t T);
 hipError_t launch_w8_gemm(const W8& w, const W8& x, int64_t N, void* y, int64_t ldy, int y_type, void* ws, hipStream_t stream);
 

@@ -327,8 +327,6 @@ hipError_t launch_w8_quantize(const void* X, int64_t ldx, int type, int64_t rows
   return type == ET_F32 ? as(static_cast<const uint32_t*>(X)) : as(static_cast<const uint16_t*>(X));
 }
 
-namespace {
-
 // How a product is divided.  Up to 64 tokens: 16 or 32 rows a workgroup, the columns over its waves; where there are rows for
 // tiles of 64 or 128 on most CUs, these, which read x less often (us, 28672 x 8192 by 16 tokens: 48 with tiles of 64, 58 with 32 rows
 // a workgroup; by 32 tokens 48, 69; 8192 x 8192 by 32: 24, 21, and with 16 rows 25; 4096 x 4096 by 32: 12, 11, 8; by
@@ -336,9 +334,6 @@ namespace {
 // More tokens: the tiles whose rounds on 256 CUs cost least, with the time of a step of 128 columns that each was
 // measured to take on a full chip; few of the smallest ones are split along the columns, eight steps at least, and
 // joined by a second launch (1000 x 14336 by 100: 14.7 us, unsplit 32).
-struct W8Plan {
-  int form, splits;
-};
 enum { kFew1, kFew2, kFew12, kFew22, kTile64x32, kTile128x64, kTile64, kTile128, kTile256x128, kTile256 };
 constexpr int64_t kRows32 = 6144, kRows64 = 12288, kRows128 = 20480;  // from these on: 32, 64, 128 rows
 W8Plan plan_w8(int64_t M, int64_t N, int64_t T, bool far) {
@@ -362,8 +357,6 @@ W8Plan plan_w8(int64_t M, int64_t N, int64_t T, bool far) {
   const int64_t room = 256 / n64, long_enough = cdiv(N, 128) / 8, n = room < long_enough ? room : long_enough;
   return {form, form == kTile64 && n > 1 ? static_cast<int>(n) : 1};
 }
-
-}  // namespace
 
 size_t w8_gemm_ws_bytes(int64_t M, int64_t N, int64_t T) {
   const W8Plan p = plan_w8(M, N, T, false);
