@@ -723,7 +723,7 @@ __device__ __forceinline__ V scalar_load(const V* p) {
 // cache is read once.  The registers hold the columns; a step's codes wait in LDS, where the loads themselves put them: a lane's 16
 // bytes of each load in its own place, so that nobody else waits for them.  A step's keys are asked for as soon as the scores
 // of the step before are done, its values as soon as theirs are added.  32 sequences of up to 4096 tokens with drafts of up to 24 by
-// 32 heads of 128 (746 MB): 169 us, 4.4 TB/s.
+// 32 heads of 128 (746 MB): 156 us, 4.8 TB/s (169 in a short run of a graph, as the figures at the plan).
 template <typename T, int DT, int QB, bool SMALL>
 __global__ __launch_bounds__(256, 2) void kv_attention_draft_kernel(const AttnArgs a) {
   constexpr int kRow = DT * 16 + 4, kStride = 4 * kTokens, kCols = 16 * QB, DK = (DT + 3) / 4;

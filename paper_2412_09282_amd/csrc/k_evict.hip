@@ -342,8 +342,8 @@ __device__ __forceinline__ int token_of(int t0) {
 }
 
 // Up to 16 NB columns: their queries stay in registers and every wave walks 64 tokens at a time, the next ones' codes on their way.
-// Memory bounds it: a token of 32 sequences of up to 4096, 32 heads of 128 (384 MB), 94 us, 4.1 TB/s; with 24 tokens each
-// (two blocks of columns) 106 us, with 40 136.  Two waves a SIMD where the registers do: products then end in
+// Memory bounds it: a token of 32 sequences of up to 4096, 32 heads of 128 (384 MB), 88 us, 4.3 TB/s, of fp32 queries 96;
+// with 24 tokens each (two blocks of columns) 101 us, with 40 135.  Two waves a SIMD where the registers do: products then end in
 // registers that the vector unit reads (40 tokens 136 us for 146).
 template <typename T, int DC, int NB>
 __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 || (DC * NB <= 4 && DC * sizeof(T) <= 8) ? 2 : 1) void kv_weights_step_kernel(const WeightArgs a) {
@@ -414,7 +414,8 @@ __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 || (DC * NB <= 4 && DC * s
 // where it reads them).  The vector units bound it, with 16 exponentials, products and sums of a lane for a tile of 64 tokens by 16
 // columns (over half of the cycles; the matrix instructions a third beside them): two prompts of up to 2048 rows over
 // 4000 tokens, 64 heads over 8, take 221 us (841 TFLOP/s; 244 in a short run of a graph, as the figures below); one of 2048
-// over 8192, 32 heads with keys of their own, 155 us (775 TFLOP/s).
+// over 8192, 32 heads with keys of their own, 153 us (788 TFLOP/s); the two prompts in fp32, with three times the matrix
+// instructions and one wave a SIMD, 785.
 constexpr int weights_step_bytes(int dc, int nv) { return 2 * dc * nv * 1024 + 4 * 256; }
 template <typename T, int DC, bool VEC>
 __global__ __launch_bounds__(256, DC * sizeof(T) <= 4 ? 2 : 1) void kv_weights_kernel(const WeightArgs a) {
@@ -926,7 +927,8 @@ __device__ __forceinline__ uint32_t moved4(uint32_t codes, const float (&f)[4]) 
 // lie transposed, so that a kept one is a byte among others that are not kept: neighbouring tokens of one old page are a run,
 // and the runs' rows pass through LDS whole, some elements at a time, where they are few enough; otherwise byte by byte (one
 // sequence of 131001 tokens to 16000, 8 heads, pages of 128: 57 us, most of it the 134 MB of values that the kept eighth lies in;
-// 32 sequences of up to 4096 tokens to 1024, 32 heads, pages of 64: 174 us, byte by byte 249).
+// 32 sequences of up to 4096 tokens to 1024, 32 heads, pages of 64: 174 us, byte by byte 249; with pages of 32, which go byte by
+// byte, 265, of 16 318).
 constexpr int kGatherLds = 16384;
 __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs a) {
   __shared__ int64_t from[256];     // the token's head and slot: (page * Hkv + hk) * page size + slot

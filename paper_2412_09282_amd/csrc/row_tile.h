@@ -144,7 +144,8 @@ struct RowTile {
 };
 
 // Calls f with the tile that a row of N elements takes: 8 elements a thread up to 2048, 16 up to 16384 (32 of them cost
-// registers that other rows' loads need: 8192 rows of 8192 in the norm 258 us, with 16 196), more only where a workgroup ends.
+// registers that other rows' loads need: 8192 rows of 8192 in the norm 258 us, with 16 196 when that was measured and 178
+// now), more only where a workgroup ends.
 template <class F>
 hipError_t with_row_tile(int64_t N, F&& f) {
   auto as = [&](auto threads, auto v) {

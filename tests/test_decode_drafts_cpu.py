@@ -148,3 +148,17 @@ def test_a_stack_keeps_its_type(calls, dtype, bits):
         elif name == "crvq_kv_attention":
             assert a[0].dtype == a[1].dtype == dtype
     assert sum(n == "crvq_kv_attention" for n, _, _ in calls) == len(bits)
+
+
+def test_drafts_of_a_tracking_cache_are_not_captured(monkeypatch, calls):
+    """Which of them count is known at accept, outside of any graph."""
+    class OnTheGpu:
+        is_cuda = True
+
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    c = cache_of([10], track=60)
+    with pytest.raises(RuntimeError, match="graph"):
+        c.attended(OnTheGpu(), None, c.grow([2], [[-1, 0]]), 0)
+    c.accept([[0]])
+    c.attended(OnTheGpu(), None, c.grow([2]), 0)  # tokens that stay whatever comes
+    assert calls[-1][0] == "crvq_kv_weights"
